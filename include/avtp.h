@@ -382,6 +382,127 @@ AVTP_API avtp_status_t avtp_layer_attention(const avtp_layout_t* layout, const i
 AVTP_API avtp_status_t avtp_layer_select(const int64_t* A, int32_t n_samples, int32_t n_layers, int32_t k,
                                          int64_t* rank_sum, int32_t* top_layers, avtp_stream_t stream);
 
+/* A paged cache of one layer's keys and values, where the kept rows of a pruned prefill go and
+ * later tokens attend to them. Slot s (0 <= s < n_pages * page_size) is row s % page_size of page
+ * s / page_size. A request's cached tokens, in their order, fill the pages of its row of a block
+ * table one after the other. Device bf16 [n_pages, page_size, n_kv_heads, head_dim], the last
+ * dimension contiguous, 16-byte aligned; strides in elements, multiples of 8, at least head_dim,
+ * the page stride no smaller than the others (so token-major and head-major pages are both fine,
+ * and K and V may share one allocation). head_dim 64 or 128. n_pages * page_size < 2^31.
+ * avtp_cache_attention wants a page_size that is a multiple of 16. */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int64_t k_page_stride;
+  int64_t k_token_stride;
+  int64_t k_head_stride;
+  int64_t v_page_stride;
+  int64_t v_token_stride;
+  int64_t v_head_stride;
+} avtp_cache_t;
+
+/* Block tables and slot maps of a step's new tokens, on the device. Request r has past_len[r]
+ * cached tokens, in the pages block_table[r][0 .. ceil(past_len[r] / page_size)), and brings
+ * cu_new[r+1] - cu_new[r] new ones; the pages they need beyond those are taken from free_pages,
+ * from entry *free_head on, request by request. cu_new may be out_cu_seqlens of avtp_prune: the
+ * pruned lengths are used where they were made, with no host round trip. */
+typedef struct {
+  int32_t n_requests;          /* R >= 1                                                     */
+  int64_t n_tokens;            /* length of slot_map, >= cu_new[R] (host); < 2^31            */
+  int32_t page_size;           /* >= 1                                                       */
+  int64_t n_pages;             /* of the pool; n_pages * page_size < 2^31                    */
+  int32_t max_pages;           /* columns of block_table                                     */
+  int64_t table_stride;        /* elements from row to row of block_table, >= max_pages      */
+  const int32_t* cu_new;       /* device [R+1], cu_new[0] = 0, non-decreasing                */
+  const int32_t* past_len;     /* device [R]; NULL: nothing cached                           */
+  const int32_t* free_pages;   /* device [n_free]: pages no request holds, each once         */
+  int64_t n_free;
+  const int32_t* free_head;    /* device [1]: the first free entry; NULL: 0                  */
+  int32_t* block_table;        /* device [R, max_pages]: entries of the new pages written    */
+  int32_t* seq_len;            /* device [R]: past_len + new, written; may be past_len       */
+  int32_t* slot_map;           /* device [n_tokens]: slot of every new token, -1 behind the last */
+  int32_t* free_head_out;      /* device [1] or NULL: the first entry left; may be free_head */
+} avtp_cache_slots_args_t;
+
+AVTP_API avtp_status_t avtp_cache_slots_workspace_size(const avtp_cache_slots_args_t* args, size_t* bytes);
+
+/* Writes block_table's new entries (the others stay as they are), seq_len, slot_map and
+ * free_head_out. Offsets that decrease or pass n_tokens, negative lengths, a request longer than
+ * max_pages pages, a free list that runs out, or a page to be used outside [0, n_pages) are
+ * recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. With past_len and free_head
+ * given as seq_len and free_head_out, replays of a captured call append step after step.
+ * Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_slots(const avtp_cache_slots_args_t* args, void* workspace, size_t workspace_bytes,
+                                        avtp_stream_t stream);
+
+/* Keys and values of new tokens to their slots: for j < n with slot_map[j] >= 0, row
+ * kept_idx[j] (or j) of k and v goes to slot slot_map[j]. With avtp_prune's kept_idx the gather of
+ * the kept rows and the write into the cache are one pass. */
+typedef struct {
+  const void* k;               /* device bf16 [n_rows, n_kv_heads, head_dim], contiguous heads;       */
+  const void* v;               /* token strides in elements, multiples of 8; 16-byte aligned          */
+  int64_t k_stride;
+  int64_t v_stride;
+  int64_t n_rows;
+  const int32_t* kept_idx;     /* device [n] or NULL: 0 .. n-1                                        */
+  const int32_t* slot_map;     /* device [n]; -1: the row is not written. A slot given twice holds
+                                * pieces of either row                                                */
+  int64_t n;
+} avtp_cache_write_args_t;
+
+/* A slot outside [-1, n_pages * page_size) or a row outside [0, n_rows) is skipped and recorded
+ * as AVTP_ERR_DEVICE_INPUT. workspace: 256-byte aligned, at least 16 bytes. Asynchronous on
+ * `stream`. */
+AVTP_API avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_cache_write_args_t* args, void* workspace,
+                                        size_t workspace_bytes, avtp_stream_t stream);
+
+/* Causal attention of a step's new tokens over the cache, which holds their own keys and values
+ * already: for the i-th of request r's n_r = cu_new[r+1] - cu_new[r] new tokens, its packed row
+ * t = cu_new[r] + i, and every query head h,
+ *   O[t, h]   = sum_u softmax_u(softmax_scale * q[t, h] . k[u, g(h)]) v[u, g(h)]
+ *   lse[h, t] = ln sum_u exp(softmax_scale * q[t, h] . k[u, g(h)])
+ * over the cached tokens u < seq_len[r] - n_r + i + 1 of the request, g(h) = h / (n_q_heads /
+ * n_kv_heads). A token that sees none (seq_len[r] < n_r - i) gets O = 0 and lse = -inf. One
+ * request may bring a chunk of thousands of tokens, another one token, another none. */
+typedef struct {
+  int32_t n_requests;          /* R >= 1                                                     */
+  int64_t n_tokens;            /* rows of q and o, >= cu_new[R] (host); < 2^31. Rows behind
+                                * cu_new[R] are neither read nor written                     */
+  int32_t max_new;             /* n_r is at most this (host)                                 */
+  int32_t n_q_heads;           /* a multiple of n_kv_heads, at most 128 times as many        */
+  const void* q;               /* device bf16 [n_tokens, n_q_heads, head_dim], contiguous heads;
+                                * 16-byte aligned, token stride a multiple of 8 elements     */
+  int64_t q_stride;
+  const int32_t* cu_new;       /* device [R+1]                                               */
+  const int32_t* seq_len;      /* device [R]: cached tokens, the new ones among them         */
+  const int32_t* block_table;  /* device [R, max_pages]; entries behind a request's last page
+                                * are not read                                               */
+  int32_t max_pages;
+  int64_t table_stride;        /* elements, >= max_pages                                     */
+  float softmax_scale;         /* > 0                                                        */
+  void* o;                     /* device bf16 [n_tokens, n_q_heads, head_dim], as q: written */
+  int64_t o_stride;
+  float* lse;                  /* device fp32 [n_q_heads, n_tokens] or NULL: written         */
+  int64_t lse_stride;          /* >= n_tokens                                                */
+} avtp_cache_attn_args_t;
+
+AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* cache,
+                                                           const avtp_cache_attn_args_t* args, size_t* bytes);
+
+/* Products on bf16 operands with fp32 accumulation, softmax in fp32, P rounded to bf16 before
+ * P V as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run.
+ * Offsets that decrease or pass n_tokens, a length that is negative or longer than max_pages
+ * pages, or more than max_new new tokens are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing
+ * is written; a page outside [0, n_pages) is recorded too, is not read, and leaves its request's rows
+ * unspecified. Slots behind a request's last token may hold anything; a value of a later new token
+ * that is not finite may reach the earlier tokens of its chunk (0 * inf). Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
+                                            void* workspace, size_t workspace_bytes, avtp_stream_t stream);
+
 /* Check of the failure path every pipeline kernel takes when a wait on an mbarrier (a
  * TMA copy, a tensor-core commit, a hand-off between warps) does not complete: one CTA
  * of 64 threads waits on a fresh count-1 mbarrier with the library's bounded waits,

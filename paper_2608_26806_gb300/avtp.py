@@ -75,6 +75,33 @@ class _Rows(ctypes.Structure):
                 ("out_stride", c_int64)]
 
 
+class _Cache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("n_pages", c_int64), ("page_size", c_int32),
+                ("n_kv_heads", c_int32), ("head_dim", c_int32), ("k_page_stride", c_int64),
+                ("k_token_stride", c_int64), ("k_head_stride", c_int64), ("v_page_stride", c_int64),
+                ("v_token_stride", c_int64), ("v_head_stride", c_int64)]
+
+
+class _CacheSlotsArgs(ctypes.Structure):
+    _fields_ = [("n_requests", c_int32), ("n_tokens", c_int64), ("page_size", c_int32), ("n_pages", c_int64),
+                ("max_pages", c_int32), ("table_stride", c_int64), ("cu_new", c_void_p), ("past_len", c_void_p),
+                ("free_pages", c_void_p), ("n_free", c_int64), ("free_head", c_void_p), ("block_table", c_void_p),
+                ("seq_len", c_void_p), ("slot_map", c_void_p), ("free_head_out", c_void_p)]
+
+
+class _CacheWriteArgs(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_stride", c_int64), ("v_stride", c_int64), ("n_rows", c_int64),
+                ("kept_idx", c_void_p), ("slot_map", c_void_p), ("n", c_int64)]
+
+
+class _CacheAttnArgs(ctypes.Structure):
+    _fields_ = [("n_requests", c_int32), ("n_tokens", c_int64), ("max_new", c_int32), ("n_q_heads", c_int32),
+                ("q", c_void_p), ("q_stride", c_int64), ("cu_new", c_void_p), ("seq_len", c_void_p),
+                ("block_table", c_void_p), ("max_pages", c_int32), ("table_stride", c_int64),
+                ("softmax_scale", c_float), ("o", c_void_p), ("o_stride", c_int64), ("lse", c_void_p),
+                ("lse_stride", c_int64)]
+
+
 class _ForwardArgs(ctypes.Structure):
     _fields_ = [("v", c_void_p), ("v_stride", c_int64), ("o", c_void_p), ("o_stride", c_int64), ("lse", c_void_p),
                 ("lse_stride", c_int64)]
@@ -106,6 +133,11 @@ SIGNATURES = {
     "avtp_kept_count_host": (c_int64, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32]),
     "avtp_pruned_layout": (c_int, [POINTER(_Layout), c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "avtp_kept_count_vis_host": (c_int64, [c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]),
+    "avtp_cache_slots_workspace_size": (c_int, [POINTER(_CacheSlotsArgs), POINTER(c_size_t)]),
+    "avtp_cache_slots": (c_int, [POINTER(_CacheSlotsArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_write": (c_int, [POINTER(_Cache), POINTER(_CacheWriteArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_attention_workspace_size": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), POINTER(c_size_t)]),
+    "avtp_cache_attention": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), c_void_p, c_size_t, c_void_p]),
     "avtp_wait_selftest": (c_int, [c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
     "avtp_layer_attention": (c_int, [POINTER(_Layout), c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_size_t,
                                      c_void_p]),
@@ -666,3 +698,228 @@ def prune(layout: Layout, criterion, *, keep_ratio: torch.Tensor, keep_ratio_hos
     call = PruneCall(layout, criterion, keep_ratio=keep_ratio, keep_ratio_host=keep_ratio_host, alpha=alpha,
                      r_min=r_min, r_max=r_max, relative=relative, rows=rows, planes=planes, **score_tensors)
     return call.run(stream)
+
+
+# ---------------------------------------------------------------- the paged cache
+def _on_one_device(where: str, *tensors: Optional[torch.Tensor]) -> torch.device:
+    """The tensors' device, which has to be the current one: the library launches there."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or (dev is not None and t.device != dev):
+            raise ValueError(f"{where}: every tensor must be on one CUDA device")
+        dev = t.device
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors are on {dev}, the current device is another")
+    return dev
+
+
+def _int32(where: str, name: str, t: Optional[torch.Tensor], shape: Tuple[int, ...]) -> None:
+    if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != shape or (t.numel() > 1 and not t.is_contiguous())):
+        raise ValueError(f"{where}: {name} must be a contiguous int32 tensor of shape {list(shape)}")
+
+
+def _int32_list(where: str, name: str, t: Optional[torch.Tensor]) -> None:
+    if t is None or t.dim() != 1:
+        raise ValueError(f"{where}: {name} must be a contiguous int32 tensor with one dimension")
+    _int32(where, name, t, tuple(t.shape))
+
+
+def _block_table(where: str, t: torch.Tensor, n_requests: int) -> Tuple[int, int]:
+    """(max_pages, row stride) of a block table."""
+    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != n_requests or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{where}: block_table must be int32 [R, max_pages] with a contiguous last dim")
+    return t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+@dataclass
+class PagedCache:
+    """One layer's keys and values in pages: bf16 [n_pages, page_size, Hkv, head_dim], the last
+    dimension contiguous. Pages of another order are passed as views: a head-major pool
+    [n_pages, Hkv, page_size, head_dim] as ``pool.transpose(1, 2)``."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    def __post_init__(self):
+        k, v = self.k, self.v
+        for t in (k, v):
+            if t.dtype != torch.bfloat16 or t.dim() != 4 or t.stride(3) != 1 or t.shape != k.shape:
+                raise ValueError("k and v must be bf16 [n_pages, page_size, Hkv, head_dim] with a contiguous last dim")
+        _on_one_device("PagedCache", k, v)
+
+    @staticmethod
+    def new(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, device="cuda") -> "PagedCache":
+        """A pool of ``n_pages`` pages, not initialised."""
+        shape = (int(n_pages), int(page_size), int(n_kv_heads), int(head_dim))
+        return PagedCache(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
+
+    @property
+    def n_pages(self) -> int:
+        return self.k.shape[0]
+
+    @property
+    def page_size(self) -> int:
+        return self.k.shape[1]
+
+    def c(self) -> _Cache:
+        """The avtp_cache_t the C calls take."""
+        n, p, h, d = self.k.shape
+
+        def strides(t):  # a dimension of one entry may carry any stride: one that the others allow
+            head = t.stride(2) if h > 1 else d
+            token = t.stride(1) if p > 1 else (h * d if h > 1 and head == d else max(head, d))
+            return (t.stride(0) if n > 1 else max(head * h, token * p), token, head)
+
+        return _Cache(_ptr(self.k), _ptr(self.v), n, p, h, d, *strides(self.k), *strides(self.v))
+
+
+class CacheSlotsCall:
+    """A prepared avtp_cache_slots call: block-table entries, slots and lengths of a step's new
+    tokens from ``cu_new`` (int32 [R+1], for example ``out_cu_seqlens`` of a prune) and the cached
+    tokens ``past_len`` (int32 [R], default none). New pages come from ``free_pages`` (int32), from
+    entry ``free_head`` (int32 [1], default 0) on. ``n_tokens``: at least ``cu_new[-1]``, the length
+    of ``slot_map``. ``seq_len=past_len`` and ``free_head_out=free_head`` advance them in place, so
+    that replays of a captured call append step after step."""
+
+    def __init__(self, cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages: int, block_table: torch.Tensor,
+                 free_pages: torch.Tensor, free_head=None, past_len=None, seq_len=None, slot_map=None,
+                 free_head_out=None, workspace=None):
+        name = "cache_slots"
+        _int32_list(name, "cu_new", cu_new)
+        _int32_list(name, "free_pages", free_pages)
+        R = cu_new.shape[0] - 1
+        max_pages, stride = _block_table(name, block_table, R)
+        dev = _on_one_device(name, cu_new, block_table, free_pages, free_head, past_len, seq_len, slot_map,
+                             free_head_out, workspace)
+        self.block_table = block_table
+        self.seq_len = seq_len if seq_len is not None else torch.empty(R, dtype=torch.int32, device=dev)
+        self.slot_map = slot_map if slot_map is not None else torch.empty(int(n_tokens), dtype=torch.int32, device=dev)
+        self.free_head_out = (free_head_out if free_head_out is not None
+                              else torch.empty(1, dtype=torch.int32, device=dev))
+        for what, t, shape in (("past_len", past_len, (R,)), ("seq_len", self.seq_len, (R,)),
+                               ("slot_map", self.slot_map, (int(n_tokens),)), ("free_head", free_head, (1,)),
+                               ("free_head_out", self.free_head_out, (1,))):
+            _int32(name, what, t, shape)
+        self._keep = (cu_new, free_pages, free_head, past_len)
+        self._a = _CacheSlotsArgs(R, int(n_tokens), int(page_size), int(n_pages), max_pages, stride, _ptr(cu_new),
+                                  _ptr(past_len), _ptr(free_pages), free_pages.shape[0], _ptr(free_head),
+                                  _ptr(block_table), _ptr(self.seq_len), _ptr(self.slot_map), _ptr(self.free_head_out))
+        if workspace is None:
+            n = c_size_t()
+            _check(load().avtp_cache_slots_workspace_size(ctypes.byref(self._a), ctypes.byref(n)),
+                   "avtp_cache_slots_workspace_size")
+            workspace = new_workspace(int(n.value), dev)
+        self.workspace = workspace
+
+    def run(self, stream=None) -> "CacheSlotsCall":
+        _check(load().avtp_cache_slots(ctypes.byref(self._a), _ptr(self.workspace), self.workspace.numel(),
+                                       _stream(stream)), "avtp_cache_slots")
+        return self
+
+
+def cache_slots(cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages: int, block_table: torch.Tensor,
+                free_pages: torch.Tensor, free_head=None, past_len=None, stream=None, **buffers):
+    """avtp_cache_slots: (slot_map int32 [n_tokens], seq_len int32 [R], free_head int32 [1]); the new
+    pages' entries go into ``block_table``. See :class:`CacheSlotsCall`."""
+    c = CacheSlotsCall(cu_new, n_tokens, page_size=page_size, n_pages=n_pages, block_table=block_table,
+                       free_pages=free_pages, free_head=free_head, past_len=past_len, **buffers).run(stream)
+    return c.slot_map, c.seq_len, c.free_head_out
+
+
+class CacheWriteCall:
+    """A prepared avtp_cache_write call: row ``kept_idx[j]`` (default j) of ``k`` and ``v`` (bf16
+    [n_rows, Hkv, head_dim]) to slot ``slot_map[j]`` of the cache, -1 for none."""
+
+    def __init__(self, cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, kept_idx=None,
+                 workspace=None):
+        name = "cache_write"
+        _int32_list(name, "slot_map", slot_map)
+        n = slot_map.shape[0]
+        if kept_idx is not None:
+            _int32(name, "kept_idx", kept_idx, (n,))
+        h, d = cache.k.shape[2:]
+        for t in (k, v):
+            if (t.dtype != torch.bfloat16 or t.dim() != 3 or tuple(t.shape[1:]) != (h, d) or t.stride(2) != 1
+                    or (h > 1 and t.stride(1) != d) or t.shape[0] != k.shape[0]):
+                raise ValueError(f"{name}: k / v must be bf16 [n_rows, Hkv, head_dim] with contiguous heads")
+        if kept_idx is None and k.shape[0] < n:
+            raise ValueError(f"{name}: fewer rows than slots")
+        dev = _on_one_device(name, cache.k, slot_map, k, v, kept_idx, workspace)
+        self.cache = cache
+        self._keep = (slot_map, k, v, kept_idx)
+        self._c = cache.c()
+        self._a = _CacheWriteArgs(_ptr(k), _ptr(v), k.stride(0) if k.shape[0] > 1 else h * d,
+                                  v.stride(0) if v.shape[0] > 1 else h * d, k.shape[0], _ptr(kept_idx), _ptr(slot_map), n)
+        self.workspace = workspace if workspace is not None else new_workspace(256, dev)
+
+    def run(self, stream=None) -> "CacheWriteCall":
+        _check(load().avtp_cache_write(ctypes.byref(self._c), ctypes.byref(self._a), _ptr(self.workspace),
+                                       self.workspace.numel(), _stream(stream)), "avtp_cache_write")
+        return self
+
+
+def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, kept_idx=None,
+                workspace=None, stream=None) -> None:
+    """avtp_cache_write: K and V rows to their slots; with a prune's ``kept_idx`` only the kept ones."""
+    CacheWriteCall(cache, slot_map, k, v, kept_idx=kept_idx, workspace=workspace).run(stream)
+
+
+class CacheAttentionCall:
+    """A prepared avtp_cache_attention call: causal attention of a step's new tokens ``q`` (bf16 [T,
+    Hq, head_dim], request r's rows ``cu_new[r] .. cu_new[r+1]``, at most ``max_new`` of them) over
+    the cache, where each request has ``seq_len[r]`` tokens, the new ones among them. ``o`` (bf16, as
+    q) and ``lse`` (fp32 [Hq, T]; False for none) are written for those rows alone."""
+
+    def __init__(self, cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,
+                 block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, workspace=None):
+        name = "cache_attention"
+        _int32_list(name, "cu_new", cu_new)
+        R = cu_new.shape[0] - 1
+        _int32(name, "seq_len", seq_len, (R,))
+        max_pages, stride = _block_table(name, block_table, R)
+        d = cache.k.shape[3]
+        if q.dim() != 3:
+            raise ValueError(f"{name}: q must be bf16 [T, Hq, head_dim] with contiguous heads")
+        T, Hq = q.shape[:2]
+        dev = _on_one_device(name, cache.k, q, cu_new, seq_len, block_table, o, lse if lse is not False else None,
+                             workspace)
+        self.o = o if o is not None else torch.empty(T, Hq, d, dtype=torch.bfloat16, device=dev)
+        for what, t in (("q", q), ("o", self.o)):
+            if (t.dtype != torch.bfloat16 or tuple(t.shape) != (T, Hq, d) or t.stride(2) != 1
+                    or (Hq > 1 and t.stride(1) != d)):
+                raise ValueError(f"{name}: {what} must be bf16 [T, Hq, head_dim] with contiguous heads")
+        self.lse = None if lse is False else (lse if lse is not None
+                                              else torch.empty(Hq, T, dtype=torch.float32, device=dev))
+        if self.lse is not None and (self.lse.dtype != torch.float32 or tuple(self.lse.shape) != (Hq, T)
+                                     or (T > 1 and self.lse.stride(1) != 1)):
+            raise ValueError(f"{name}: lse must be fp32 [Hq, T] with a contiguous last dim")
+        self.cache = cache
+        self._keep = (q, cu_new, seq_len, block_table)
+        self._c = cache.c()
+        self._a = _CacheAttnArgs(
+            R, T, int(max_new), Hq, _ptr(q), q.stride(0) if T > 1 else Hq * d, _ptr(cu_new), _ptr(seq_len),
+            _ptr(block_table), max_pages, stride, float(softmax_scale if softmax_scale is not None else d ** -0.5),
+            _ptr(self.o), self.o.stride(0) if T > 1 else Hq * d, _ptr(self.lse),
+            self.lse.stride(0) if self.lse is not None and Hq > 1 else max(T, 1))
+        if workspace is None:
+            n = c_size_t()
+            _check(load().avtp_cache_attention_workspace_size(ctypes.byref(self._c), ctypes.byref(self._a),
+                                                              ctypes.byref(n)), "avtp_cache_attention_workspace_size")
+            workspace = new_workspace(int(n.value), dev)
+        self.workspace = workspace
+
+    def run(self, stream=None) -> "CacheAttentionCall":
+        _check(load().avtp_cache_attention(ctypes.byref(self._c), ctypes.byref(self._a), _ptr(self.workspace),
+                                           self.workspace.numel(), _stream(stream)), "avtp_cache_attention")
+        return self
+
+
+def cache_attention(cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,
+                    block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, workspace=None,
+                    stream=None):
+    """avtp_cache_attention: (o, lse) of a chunk of new tokens, or a single one, a request over the
+    paged cache. See :class:`CacheAttentionCall`."""
+    c = CacheAttentionCall(cache, q, cu_new, seq_len, block_table, max_new=max_new, softmax_scale=softmax_scale, o=o,
+                           lse=lse, workspace=workspace).run(stream)
+    return c.o, c.lse
