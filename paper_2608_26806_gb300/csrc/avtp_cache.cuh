@@ -1,6 +1,8 @@
 // Host-side declarations of the paged cache's kernels (k_cache_*.cu).
 #pragma once
 
+#include <cuda.h>
+
 #include "avtp_internal.cuh"
 
 namespace avtp {
@@ -19,17 +21,37 @@ cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_arg
 
 // ---------------------------------------------------------------- attention
 // Rows of a (request, KV head) are its (new token, head of the group) pairs, token by token.
-constexpr int kCacheTile = 64;        // keys of a tile
-constexpr int kCacheMaxPieces = 32;   // pieces a row block's keys are split into, at most
+constexpr int kCacheTile = 64;        // keys of a tile of k_cache_attn
+constexpr int kCacheMaxPieces = 32;   // pieces that a row block's keys are split into, at most
+constexpr int kChunkRows = 256;       // rows of a unit of k_cache_chunk, two slots of 128
+// Requests of at most this many rows a KV head are k_cache_attn's, when no request of the call has
+// more; beside larger ones (max_new is the call's bound) those of at most kCacheFewMixed.
+constexpr int kCacheFewRows = 64;
+constexpr int kCacheFewMixed = 16;
+
+// A unit of k_cache_chunk in several pieces, for the kernel that joins them; c1 < c0: none.
+struct CacheChunkSplit {
+  int32_t row0, n, head, unit;  // request's first packed row and new tokens, KV head, unit of the request
+  int32_t c0, c1, slot0, pad;   // CTAs of the first and the last piece, place of the first piece
+};
+
 struct CacheAttnWs {
-  size_t status;   // DevStatus
-  size_t count;    // int32 [grid]: pieces done of the row block whose first piece is the CTA's last
-  size_t part_o;   // float [2 * grid][rows][d]: a piece's O, not yet divided by its sum
-  size_t part_ml;  // float2 [2 * grid][rows]: a piece's reference and sum (log2 units)
+  size_t status;    // DevStatus
+  size_t count;     // int32 [grid]: pieces done of the row block whose first piece is the CTA's last
+  size_t part_o;    // float [2 * grid][rows][d]: a piece's O, not yet divided by its sum
+  size_t part_ml;   // float2 [2 * grid][rows]: a piece's reference and sum (log2 units)
+  // of k_cache_chunk, when max_new allows a request for it
+  size_t chunk_o;   // float4 [2 * grid][2 slots][d / 4][128 rows]
+  size_t chunk_ml;  // float2 [2 * grid][2 slots][128 rows]
+  size_t split;     // CacheChunkSplit [grid]
   size_t total;
 };
 CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a);
 cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, void* ws,
                                    const CacheAttnWs& p, cudaStream_t s);
+
+struct CacheAttnDev;
+cudaError_t launch_cache_chunk(int head_dim, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
+                               const CUtensorMap& mv, const CacheAttnDev& a, cudaStream_t s);
 
 }  // namespace avtp

@@ -126,19 +126,6 @@ struct FwdArgs {
   DevStatus* st;
 };
 
-// 32 consecutive fp32 columns of this thread's TMEM lane, stored; complete after
-// tmem_wait_st().
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Diagnostic timeline build (-DAVTP_TIMELINE): clock stamps of slot 0 of the grid's first CTA
 // (the last request's last tile), per key block j. Stamps: 0-4 from softmax warp 0
 // (loop top, S ready, P of the first half computed, of the second half, P handed over); 5-9
@@ -158,16 +145,6 @@ __device__ __forceinline__ void fwd_stamp(int j, int slot) {
 #endif
 }
 
-__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
-  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&b);
-}
-// The larger of three (PTX max with three sources, sm_100 and later); NaN only if all are.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
 // 16 fp32 columns x 32 rows of shared memory (64-byte swizzle) to the output tensor.
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, const void* src, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
@@ -181,7 +158,6 @@ template <int N>
 __device__ __forceinline__ void bulk_wait_read() {
   asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // A unit of a CTA's work, seen by every role: two slots of 128 query rows on one key stream.
 template <bool kHeads>
@@ -532,7 +508,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             const int ac = e / (dead * 8), w = e - ac * dead * 8;
             *reinterpret_cast<uint4*>(v + ac * kPanel + valid * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
-          fence_proxy_async();
+          tc::fence_proxy_async();
         }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
@@ -558,8 +534,8 @@ k_attn_fwd(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
               const float p0 = tc::ex2(z01.x), p1 = tc::ex2(z01.y), p2 = tc::ex2(z23.x), p3 = tc::ex2(z23.y);
               acc0 = tc::add2(acc0, make_float2(p0, p1));
               acc1 = tc::add2(acc1, make_float2(p2, p3));
-              pk[c / 2] = pack_bf16x2(p0, p1);
-              pk[c / 2 + 1] = pack_bf16x2(p2, p3);
+              pk[c / 2] = tc::pack_bf16x2(p0, p1);
+              pk[c / 2 + 1] = tc::pack_bf16x2(p2, p3);
             }
             return (acc0.x + acc0.y) + (acc1.x + acc1.y);
           };
@@ -576,10 +552,10 @@ k_attn_fwd(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
               for (int c = 0; c < 64; c += 8) {
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
-                  t[w] = max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
+                  t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
               }
             }
-            const float mb = fmaxf(max3(t[0], t[1], t[2]), t[3]) * c2;  // -inf when nothing is visible
+            const float mb = fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2;  // -inf when nothing is visible
             float factor = 1.f;
             if (mb > m + kRescaleTau) {
               if (m != -INFINITY) factor = tc::ex2(m - mb);
@@ -598,16 +574,16 @@ k_attn_fwd(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
                 tc::tmem_wait(ov);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
-                tmem_st32(tO + oc, ov);
+                tc::tmem_st32(tO + oc, ov);
               }
-              tmem_wait_st();
+              tc::tmem_wait_st();
             }
             sum = exps();
           }
           l += sum;
           if (stamp) fwd_stamp(j, 2 + hf);
-          tmem_st32(tS + hf * 32, pk);
-          tmem_wait_st();
+          tc::tmem_st32(tS + hf * 32, pk);
+          tc::tmem_wait_st();
           tc::fence_before_sync();
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&sy.p_full[slot][hf]);
@@ -654,7 +630,7 @@ k_attn_fwd(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUt
             else if (live) *reinterpret_cast<float4*>(orow + oc + c) = o4;
           }
           if (whole) {
-            fence_proxy_async();
+            tc::fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
               tma_store_3d(&mapO, stage + b * kOutStage, oc + 16 * b, h, q0 + quad * 32);

@@ -25,8 +25,7 @@
 // values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 #include <cudaTypedefs.h>
 
-#include "avtp_cache.cuh"
-#include "avtp_tc.cuh"
+#include "avtp_cache_attn.cuh"
 
 namespace avtp {
 namespace {
@@ -38,34 +37,12 @@ constexpr int kPrepThreads = 256;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
-struct AttnDev {
-  const __nv_bfloat16* q;
-  int64_t q_stride;
-  const int32_t* cu;
-  const int32_t* seq;
-  const int32_t* table;
-  int64_t table_stride;
-  int64_t n_tokens, n_pages;
-  int R, max_new, max_pages, Hq, Hkv, G, page_size;
-  int box;        // rows of a TMA box: a power of two that divides the page size, at most a tile
-  int k_tok, v_tok;  // the map's second dimension is the row of the page, its third the head (else the reverse)
-  float c2;
-  __nv_bfloat16* o;
-  int64_t o_stride;
-  float* lse;
-  int64_t lse_stride;
-  DevStatus* st;
-  int32_t* count;
-  float* part_o;
-  float2* part_ml;
-};
-
 // A run's part of one row block.
 struct Segment {
   int32_t row0;        // the request's first packed row
   int32_t n, seq;      // its new tokens and cached tokens
-  int32_t head, block; // KV head (-1: no more), row block
-  int32_t tile0, tile1, tiles;
+  int32_t head;        // KV head (-1: no more)
+  int32_t tile0, tile1;
   int32_t c0, c1;      // CTAs of the block's first and last piece
   int32_t slot, slot0; // where this piece goes, when there are several, and the block's first
   int32_t req;
@@ -86,34 +63,16 @@ struct Shared {
   uint64_t kv_full[stages(D)], kv_empty[stages(D)];
   uint64_t seg_full[2], seg_empty[2];
   Segment seg[2];
-  int64_t pre[kThreads + 1];  // tiles before each thread's share of the requests
+  CachePlan<kThreads> plan;
   float m[4][16], l[4][16];
-  int32_t most;               // tiles of the longest row block
   int32_t last;
   int abort, bad_page;
-};
-
-// ---------------------------------------------------------------- what a request asks
-struct Request {
-  int32_t row0, n, seq;
-  __device__ __forceinline__ bool load(const AttnDev& a, int r) {
-    const int64_t lo = a.cu[r], hi = a.cu[r + 1];
-    row0 = static_cast<int32_t>(lo);
-    n = static_cast<int32_t>(hi - lo);
-    seq = a.seq[r];
-    return lo >= 0 && hi >= lo && hi <= a.n_tokens && hi - lo <= a.max_new && seq >= 0 &&
-           seq <= static_cast<int64_t>(a.max_pages) * a.page_size && (r > 0 || lo == 0);
-  }
-  __device__ __forceinline__ int tiles() const { return n == 0 ? 0 : max(1, (seq + kCacheTile - 1) / kCacheTile); }
-  __device__ __forceinline__ int blocks(const AttnDev& a, int rows) const {
-    return static_cast<int>((static_cast<int64_t>(n) * a.G + rows - 1) / rows);
-  }
 };
 
 // ---------------------------------------------------------------- validation
 // The first kernel of a call: the status word, the counters, and what the lengths have wrong. The
 // attention runs beside it and waits for it before its first use of either.
-__global__ void __launch_bounds__(kPrepThreads) k_cache_prep(AttnDev a, int counters) {
+__global__ void __launch_bounds__(kPrepThreads) k_cache_prep(CacheAttnDev a, int counters) {
   __shared__ int s_bad;
   pdl_wait();
   pdl_trigger();
@@ -121,7 +80,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_cache_prep(AttnDev a, int coun
   __syncthreads();
   for (int i = threadIdx.x; i < counters; i += kPrepThreads) a.count[i] = 0;
   for (int r = threadIdx.x; r < a.R; r += kPrepThreads) {
-    Request q;
+    CacheRequest q;
     if (!q.load(a, r)) atomicMin(&s_bad, r);
   }
   __syncthreads();
@@ -133,13 +92,6 @@ __global__ void __launch_bounds__(kPrepThreads) k_cache_prep(AttnDev a, int coun
 
 // ---------------------------------------------------------------- building blocks
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::
-          "r"(tc::smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(tc::smem_u32(bar))
-      : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -159,10 +111,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4],
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-  const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&b);
-}
 // Over the four lanes of a row. (The maximum passes a NaN over; its exponential is NaN all the
 // same and takes the row's sum with it.)
 __device__ __forceinline__ float quad_max(float x) {
@@ -176,24 +124,30 @@ __device__ __forceinline__ float quad_sum(float x) {
 
 // A row's result, four columns a lane: O divided by its sum and rounded, and the LSE.
 template <int D>
-__device__ __forceinline__ void store_row(const AttnDev& a, const Segment& g, int row, int col, float4 v, float m, float l) {
+__device__ __forceinline__ void store_row(const CacheAttnDev& a, const Segment& g, int row, int col, float4 v, float m, float l) {
   const int tok = row / a.G, head = g.head * a.G + (row - tok * a.G);
   const int64_t t = static_cast<int64_t>(g.row0) + tok;
   const float inv = l == 0.f ? 0.f : 1.f / l;  // no key visible: zeros
   uint2 w;
-  w.x = pack(v.x * inv, v.y * inv);
-  w.y = pack(v.z * inv, v.w * inv);
+  w.x = tc::pack_bf16x2(v.x * inv, v.y * inv);
+  w.y = tc::pack_bf16x2(v.z * inv, v.w * inv);
   *reinterpret_cast<uint2*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D + col) = w;
   if (col == 0 && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (m + log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------- attention
+// Tiles of a row block: one for an empty cache, whose rows are zeros; none for requests without new
+// tokens, or with more rows than this kernel takes.
+__device__ __forceinline__ int tiles_of(const CacheAttnDev& a, const CacheRequest& q) {
+  return q.n == 0 || q.rows(a) > a.few_rows ? 0 : max(1, (q.seq - 1) / kCacheTile + 1);
+}
+
 // mapK, mapV: the cache as {d, head, row of the page, page} (or {d, row, head, page}), box of 64
 // elements, one head, `box` rows, one page. kWM warps share the keys of a slice of the tile, 16
 // rows each.
 template <int D, int kWM>
 __global__ void __launch_bounds__(kThreads, 1)
-k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, AttnDev a) {
+k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, CacheAttnDev a) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ Shared<D> sh;
   constexpr int kStages = stages(D);
@@ -217,7 +171,6 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     }
     sh.abort = 0;
     sh.bad_page = -1;
-    sh.most = 1;
     tc::fence_mbar_init();
     tc::tma_prefetch_map(&mapK);
     tc::tma_prefetch_map(&mapV);
@@ -225,58 +178,19 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   pdl_trigger();
   __syncthreads();
 
-  // ---- the plan, by every CTA for itself: tiles before each thread's share of the requests
-  const int share = (a.R + kThreads - 1) / kThreads;
-  bool ok = true;
-  {
-    int64_t sum = 0;
-    int most = 1;
-    for (int r = tid * share; r < min(a.R, (tid + 1) * share); ++r) {
-      Request q;
-      ok = q.load(a, r) && ok;
-      sum += static_cast<int64_t>(q.tiles()) * q.blocks(a, kRows) * a.Hkv;
-      most = max(most, q.tiles());
-    }
-    atomicMax(&sh.most, most);
-    sh.pre[tid + 1] = sum;
-    if (tid == 0) sh.pre[0] = 0;
-    ok = __syncthreads_and(ok);
-    if (warp == 0) {
-      int64_t carry = 0;
-      for (int b = 0; b < kThreads; b += 32) {
-        int64_t x = sh.pre[b + lane + 1];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-          if (lane >= o) x += y;
-        }
-        x += carry;
-        sh.pre[b + lane + 1] = x;
-        carry = __shfl_sync(0xffffffffu, x, 31);
-      }
-    }
-    __syncthreads();
-  }
-  const int64_t total = ok ? sh.pre[kThreads] : 0;  // lengths that validation refuses: nothing
-  // CTAs at work: runs long enough that no row block has more than kCacheMaxPieces pieces
-  const int64_t least = (sh.most + kCacheMaxPieces - 3) / (kCacheMaxPieces - 2);
-  const int64_t N = max(int64_t(1), min(static_cast<int64_t>(gridDim.x), total / least));
-  const int64_t t0 = blockIdx.x < N ? blockIdx.x * total / N : 0, t1 = blockIdx.x < N ? (blockIdx.x + 1) * total / N : 0;
+  sh.plan.form(a, [&](const CacheRequest& q, int& most) {
+    const int t = tiles_of(a, q);
+    most = max(most, t);
+    return static_cast<int64_t>(t) * a.Hkv;
+  });
+  const CacheRuns runs(sh.plan.pre[kThreads], sh.plan.most, 1);
+  const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
   volatile int* abort_flag = &sh.abort;
 
   if (warp == kLoadWarp) {
     // ------------------------------------------------------------ segments and loads
-    int r = 0;
     int64_t pre = 0;  // tiles before request r
-    if (t0 < t1) {
-      int lo = 0, hi = kThreads;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (sh.pre[mid] <= t0) lo = mid; else hi = mid;
-      }
-      r = lo * share;
-      pre = sh.pre[lo];
-    }
+    int r = t0 < t1 ? sh.plan.find(a, t0, &pre) : 0;
     int n = 0, sc = 0;
     bool fine = true;
     for (int64_t t = t0; fine; ++sc) {
@@ -284,30 +198,28 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       g.head = -1;
       int64_t end = t;
       if (t < t1) {
-        Request q;
-        int64_t len;
+        CacheRequest q;
+        int tiles;
         for (;; ++r) {
           q.load(a, r);
-          len = static_cast<int64_t>(q.tiles()) * q.blocks(a, kRows) * a.Hkv;
+          tiles = tiles_of(a, q);
+          const int64_t len = static_cast<int64_t>(tiles) * a.Hkv;
           if (t < pre + len) break;
           pre += len;
         }
-        const int tiles = q.tiles(), nb = q.blocks(a, kRows);
-        const int64_t b = (t - pre) / tiles, s = pre + b * tiles;
+        g.head = static_cast<int>((t - pre) / tiles);
+        const int64_t s = pre + static_cast<int64_t>(g.head) * tiles;  // the block's first step
         end = min(t1, s + tiles);
         g.row0 = q.row0;
         g.n = q.n;
         g.seq = q.seq;
-        g.head = static_cast<int>(b / nb);
-        g.block = static_cast<int>(b - static_cast<int64_t>(g.head) * nb);
         g.tile0 = static_cast<int>(t - s);
         g.tile1 = static_cast<int>(end - s);
-        g.tiles = tiles;
-        g.c0 = static_cast<int>(((s + 1) * N - 1) / total);
-        g.c1 = static_cast<int>(((s + tiles) * N - 1) / total);
+        g.c0 = runs.cta(s);
+        g.c1 = runs.cta(s + tiles - 1);
         // a CTA's first segment goes to its even slot, its last (the only other that can be a piece) to its odd one
         g.slot = 2 * blockIdx.x + (t == t0 ? 0 : 1);
-        g.slot0 = 2 * g.c0 + (g.c0 * total / N == s ? 0 : 1);
+        g.slot0 = 2 * g.c0 + (runs.begin(g.c0) == s ? 0 : 1);
         g.req = r;
       }
       if (sc >= 2) fine = tc::mbar_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
@@ -378,15 +290,14 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sh.seg_empty[sc & 1]);
       if (g.head < 0) break;
-      const int rows = min(kRows, g.n * a.G - g.block * kRows);  // of the block
-      const int first = g.block * kRows;
+      const int rows = g.n * a.G;
       // Q as the A operand; keys visible to this lane's two rows
       uint32_t qa[D / 16][4];
       int limit[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = wm * 16 + gr + 8 * i;
-        const int at = first + min(row, rows - 1);
+        const int at = min(row, rows - 1);
         const int tok = at / a.G, head = g.head * a.G + (at - tok * a.G);
         limit[i] = min(g.seq, g.seq - g.n + tok + 1);
         const uint32_t* src = reinterpret_cast<const uint32_t*>(a.q + (static_cast<int64_t>(g.row0) + tok) * a.q_stride +
@@ -398,7 +309,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         }
         if (row >= rows) limit[i] = 0;
       }
-      const int all_see = g.seq - g.n + first / a.G + 1;  // keys that every row of the block sees
+      const int all_see = g.seq - g.n + 1;  // keys that every row sees
 
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
       float o[D / 8][4];
@@ -471,8 +382,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
             const float p2 = tc::ex2(fmaf(s[i][2], c2, -m1)), p3 = tc::ex2(fmaf(s[i][3], c2, -m1));
             l[0] += p0 + p1;
             l[1] += p2 + p3;
-            p[i >> 1][(i & 1) * 2] = pack(p0, p1);
-            p[i >> 1][(i & 1) * 2 + 1] = pack(p2, p3);
+            p[i >> 1][(i & 1) * 2] = tc::pack_bf16x2(p0, p1);
+            p[i >> 1][(i & 1) * 2 + 1] = tc::pack_bf16x2(p2, p3);
           }
           const bool tail = key0 + kKeys > g.seq;
 #pragma unroll
@@ -542,7 +453,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           v.w = fmaf(f, x.w, v.w);
         }
         if (pieces == 1) {
-          store_row<D>(a, g, first + row, col, v, M, L);
+          store_row<D>(a, g, row, col, v, M, L);
         } else {
           __stcg(reinterpret_cast<float4*>(a.part_o + (static_cast<int64_t>(g.slot) * kRows + row) * D + col), v);
           if (sub == 0) __stcg(a.part_ml + static_cast<int64_t>(g.slot) * kRows + row, make_float2(M, L));
@@ -579,7 +490,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           v.z = fmaf(f, x.z, v.z);
           v.w = fmaf(f, x.w, v.w);
         }
-        store_row<D>(a, g, first + row, col, v, M, L);
+        store_row<D>(a, g, row, col, v, M, L);
       }
     }
   }
@@ -624,7 +535,7 @@ bool cache_map(CUtensorMap* m, const void* base, const avtp_cache_t& c, int64_t 
 }
 
 template <int D, int kWM>
-cudaError_t launch_attn(int grid, const CUtensorMap& mk, const CUtensorMap& mv, const AttnDev& a, cudaStream_t s) {
+cudaError_t launch_attn(int grid, const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnDev& a, cudaStream_t s) {
   static PerDevice attrs;
   const cudaError_t e = once_per_device(attrs, [](int, int*) {
     return cudaFuncSetAttribute(k_cache_attn<D, kWM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -634,17 +545,44 @@ cudaError_t launch_attn(int grid, const CUtensorMap& mk, const CUtensorMap& mv, 
   return launch_kernel(k_cache_attn<D, kWM>, dim3(grid), dim3(kThreads), smem_bytes(D), s, /*pdl=*/true, mk, mv, a);
 }
 
-// Warps that share a slice of keys: 16 rows each, as many as a request can have, at most four.
-int row_warps(const avtp_cache_t& c, const avtp_cache_attn_args_t& a) {
-  const int64_t rows = static_cast<int64_t>(a.max_new) * (a.n_q_heads / c.n_kv_heads);
-  return rows <= 16 ? 1 : (rows <= 32 ? 2 : 4);
+// q as {d, head, token}, box of 64 elements, a group's heads, as many tokens as fit into 128 rows.
+bool query_map(CUtensorMap* m, const avtp_cache_attn_args_t& a, int d, int G) {
+  auto fn = encode_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(a.n_q_heads),
+                              static_cast<cuuint64_t>(a.n_tokens)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(a.q_stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(kChunkRows / 2 / G)};
+  const cuuint32_t es[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// What the call's bounds leave to each kernel.
+struct Shape {
+  int64_t rows;      // of a request's KV head, at most
+  bool few, chunks;  // k_cache_attn, k_cache_chunk
+  int64_t few_rows;
+  int row_warps;     // of k_cache_attn: 16 rows each
+};
+Shape shape_of(const avtp_cache_t& c, const avtp_cache_attn_args_t& a) {
+  Shape s{};
+  s.rows = static_cast<int64_t>(a.max_new) * (a.n_q_heads / c.n_kv_heads);
+  s.chunks = s.rows > kCacheFewRows;
+  s.few = !s.chunks || a.n_requests > 1;
+  s.few_rows = !s.few ? 0 : (s.chunks ? kCacheFewMixed : kCacheFewRows);
+  const int64_t most = s.rows < s.few_rows ? s.rows : s.few_rows;
+  s.row_warps = most <= 16 ? 1 : (most <= 32 ? 2 : 4);
+  return s;
 }
 
 }  // namespace
 
 CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a) {
   CacheAttnWs p{};
-  const size_t grid = static_cast<size_t>(device_sm_count()), rows = 16 * static_cast<size_t>(row_warps(c, a));
+  const Shape sh = shape_of(c, a);
+  const size_t grid = static_cast<size_t>(device_sm_count()), d = static_cast<size_t>(c.head_dim);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
@@ -653,15 +591,24 @@ CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_ar
   };
   p.status = take(sizeof(DevStatus));
   p.count = take(grid * 4);
-  p.part_o = take(2 * grid * rows * static_cast<size_t>(c.head_dim) * 4);
-  p.part_ml = take(2 * grid * rows * 8);
+  if (sh.few) {
+    const size_t rows = 16 * static_cast<size_t>(sh.row_warps);
+    p.part_o = take(2 * grid * rows * d * 4);
+    p.part_ml = take(2 * grid * rows * 8);
+  }
+  if (sh.chunks) {
+    p.chunk_o = take(2 * grid * kChunkRows * d * 4);
+    p.chunk_ml = take(2 * grid * kChunkRows * 8);
+    p.split = take(grid * sizeof(CacheChunkSplit));
+  }
   p.total = off;
   return p;
 }
 
 cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, void* ws,
                                    const CacheAttnWs& p, cudaStream_t s) {
-  AttnDev d{};
+  const Shape sh = shape_of(c, a);
+  CacheAttnDev d{};
   d.q = static_cast<const __nv_bfloat16*>(a.q);
   d.q_stride = a.q_stride;
   d.cu = a.cu_new;
@@ -677,10 +624,9 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.Hkv = c.n_kv_heads;
   d.G = a.n_q_heads / c.n_kv_heads;
   d.page_size = c.page_size;
-  d.box = 16;
-  while (d.box < kCacheTile && c.page_size % (2 * d.box) == 0) d.box *= 2;
   d.k_tok = c.k_token_stride < c.k_head_stride ? 1 : 0;
   d.v_tok = c.v_token_stride < c.v_head_stride ? 1 : 0;
+  d.few_rows = sh.few_rows;
   d.c2 = a.softmax_scale * kLog2e;
   d.o = static_cast<__nv_bfloat16*>(a.o);
   d.o_stride = a.o_stride;
@@ -690,17 +636,31 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.count = ws_at<int32_t>(ws, p.count);
   d.part_o = ws_at<float>(ws, p.part_o);
   d.part_ml = ws_at<float2>(ws, p.part_ml);
+  d.chunk_o = ws_at<float>(ws, p.chunk_o);
+  d.chunk_ml = ws_at<float2>(ws, p.chunk_ml);
+  d.split = ws_at<CacheChunkSplit>(ws, p.split);
   const int grid = device_sm_count();
   cudaError_t e = launch_kernel(k_cache_prep, dim3(1), dim3(kPrepThreads), 0, s, /*pdl=*/true, d, grid);
   if (e != cudaSuccess || a.n_tokens == 0) return e;
-  CUtensorMap mk, mv;
-  if (!cache_map(&mk, c.k, c, c.k_page_stride, c.k_token_stride, c.k_head_stride, d.box, d.k_tok != 0) ||
-      !cache_map(&mv, c.v, c, c.v_page_stride, c.v_token_stride, c.v_head_stride, d.box, d.v_tok != 0))
-    return cudaErrorInvalidValue;
-  const int wm = row_warps(c, a);
-  auto launch = c.head_dim == 128 ? (wm == 1 ? launch_attn<128, 1> : wm == 2 ? launch_attn<128, 2> : launch_attn<128, 4>)
-                                  : (wm == 1 ? launch_attn<64, 1> : wm == 2 ? launch_attn<64, 2> : launch_attn<64, 4>);
-  return launch(grid, mk, mv, d, s);
+  // boxes no longer than a kernel's tile, and whole in a page
+  auto maps = [&](int tile, CUtensorMap* mk, CUtensorMap* mv) {
+    d.box = 16;
+    while (d.box < tile && c.page_size % (2 * d.box) == 0) d.box *= 2;
+    return cache_map(mk, c.k, c, c.k_page_stride, c.k_token_stride, c.k_head_stride, d.box, d.k_tok != 0) &&
+           cache_map(mv, c.v, c, c.v_page_stride, c.v_token_stride, c.v_head_stride, d.box, d.v_tok != 0);
+  };
+  CUtensorMap mk, mv, mq;
+  if (sh.few) {
+    if (!maps(kCacheTile, &mk, &mv)) return cudaErrorInvalidValue;
+    const int wm = sh.row_warps;
+    auto launch = c.head_dim == 128
+                      ? (wm == 1 ? launch_attn<128, 1> : wm == 2 ? launch_attn<128, 2> : launch_attn<128, 4>)
+                      : (wm == 1 ? launch_attn<64, 1> : wm == 2 ? launch_attn<64, 2> : launch_attn<64, 4>);
+    if ((e = launch(grid, mk, mv, d, s)) != cudaSuccess) return e;
+  }
+  if (!sh.chunks) return cudaSuccess;
+  if (!maps(2 * kCacheTile, &mk, &mv) || !query_map(&mq, a, c.head_dim, d.G)) return cudaErrorInvalidValue;
+  return launch_cache_chunk(c.head_dim, grid, mq, mk, mv, d, s);
 }
 
 }  // namespace avtp
