@@ -18,7 +18,6 @@ struct CacheAttnDev {
   int64_t n_tokens, n_pages;
   int R, max_new, max_pages, Hq, Hkv, G, page_size;
   int box;           // rows of a TMA box: a power of two that divides the page size, at most a tile
-  int k_tok, v_tok;  // the map's second dimension is the row of the page, its third the head (else the reverse)
   int64_t few_rows;  // requests of at most this many rows a KV head are k_cache_attn's, the others k_cache_chunk's
   float c2;
   __nv_bfloat16* o;

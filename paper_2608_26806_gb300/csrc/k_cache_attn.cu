@@ -34,6 +34,10 @@ constexpr int kThreads = 160;
 constexpr int kConsumers = 128;
 constexpr int kLoadWarp = 4;
 constexpr int kPrepThreads = 256;
+// A tile's share of a row's sum above kRescaleSum moves the row's reference, if its maximum exceeds
+// the reference by more than kRescaleTau (log2 units).
+constexpr float kRescaleSum = 16384.f;
+constexpr float kRescaleTau = 8.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -92,6 +96,13 @@ __global__ void __launch_bounds__(kPrepThreads) k_cache_prep(CacheAttnDev a, int
 
 // ---------------------------------------------------------------- building blocks
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int row, int head, int page, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::
+          "r"(tc::smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(head), "r"(page), "r"(tc::smem_u32(bar))
+      : "memory");
+}
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -105,8 +116,7 @@ __device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t (&r)[4]) {
                : "memory");
 }
 __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -142,8 +152,9 @@ __device__ __forceinline__ int tiles_of(const CacheAttnDev& a, const CacheReques
   return q.n == 0 || q.rows(a) > a.few_rows ? 0 : max(1, (q.seq - 1) / kCacheTile + 1);
 }
 
-// mapK, mapV: the cache as {d, head, row of the page, page} (or {d, row, head, page}), box of 64
-// elements, one head, `box` rows, one page. kWM warps share the keys of a slice of the tile, 16
+// mapK, mapV: the cache as {64 elements, row of the page, panel of 64, head, page}, box of `box` rows
+// and all panels of one head and page: one TMA instruction a page piece. (One a panel, at pages of 16
+// rows 16 of them a tile, issued too slowly: 4.4 TB/s.) kWM warps share the keys of a slice of the tile, 16
 // rows each.
 template <int D, int kWM>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -154,7 +165,6 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   constexpr int kRows = 16 * kWM;
   constexpr int kSlices = 4 / kWM;            // slices of a tile's keys
   constexpr int kKeys = kCacheTile / kSlices; // keys of a slice
-  constexpr uint32_t kPanel = kCacheTile * 128;
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   float* s_out = reinterpret_cast<float*>(smem + kStages * stage_bytes(D));
@@ -250,16 +260,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
             sh.bad_page = g.req;
             page = 0;
           }
-          unsigned char* dst = smem + sb * stage_bytes(D) + lane * a.box * 128;
+          unsigned char* dst = smem + sb * stage_bytes(D) + lane * a.box * D * 2;
           const int in_page = (tile * kCacheTile + lane * a.box) % a.page_size;
-#pragma unroll
-          for (int p = 0; p < D / 64; ++p)
-            tma_load_4d(dst + p * kPanel, &mapK, p * 64, a.k_tok ? in_page : g.head, a.k_tok ? g.head : in_page, page,
-                        &sh.kv_full[sb]);
-#pragma unroll
-          for (int p = 0; p < D / 64; ++p)
-            tma_load_4d(dst + (D / 64 + p) * kPanel, &mapV, p * 64, a.v_tok ? in_page : g.head,
-                        a.v_tok ? g.head : in_page, page, &sh.kv_full[sb]);
+          tma_load_5d(dst, &mapK, in_page, g.head, page, &sh.kv_full[sb]);
+          tma_load_5d(dst + stage_bytes(D) / 2, &mapV, in_page, g.head, page, &sh.kv_full[sb]);
         }
         __syncwarp();
         page = next;
@@ -307,7 +311,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           qa[ks][i] = row < rows ? src[ks * 8 + tq] : 0u;
           qa[ks][i + 2] = row < rows ? src[ks * 8 + tq + 4] : 0u;
         }
-        if (row >= rows) limit[i] = 0;
+        if (row >= rows) limit[i] = 0x7fffffff;  // a row that is not stored: q = 0, and no mask
       }
       const int all_see = g.seq - g.n + 1;  // keys that every row sees
 
@@ -324,22 +328,47 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         }
         const int key0 = tile * kCacheTile + slice * kKeys;
         if (key0 < g.seq) {
-          const uint32_t kb = base + sb * stage_bytes(D), vb = kb + (D / 64) * kPanel;
+          // a box is its D / 64 panels of 128-byte rows one behind the other
+          const uint32_t kb = base + sb * stage_bytes(D), vb = kb + stage_bytes(D) / 2, panel = a.box * 128;
+          auto sixteen = [&](int kk) {  // 16 keys of the slice
+            const int key = slice * kKeys + kk * 16;
+            return static_cast<uint32_t>(key & ~(a.box - 1)) * (D * 2) + static_cast<uint32_t>(key & (a.box - 1)) * 128;
+          };
+          // S: two chains of products a tile of 8 keys, so that no product waits long for another
           float s[kKeys / 8][4];
+          uint32_t f[D / 16][4];  // K, then V fragments of 16 keys
 #pragma unroll
-          for (int i = 0; i < kKeys / 8; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+          for (int kk = 0; kk < kKeys / 16; ++kk) {
+            const int key = ((lane >> 4) << 3) + (lane & 7);
+            const uint32_t at = kb + sixteen(kk) + key * 128;
 #pragma unroll
-          for (int ks = 0; ks < D / 16; ++ks) {
-#pragma unroll
-            for (int kk = 0; kk < kKeys / 16; ++kk) {
-              const int key = slice * kKeys + kk * 16 + ((lane >> 4) << 3) + (lane & 7);
-              const int chunk = ks * 2 + ((lane >> 3) & 1);
-              uint32_t b[4];
-              ldsm4(kb + (chunk >> 3) * kPanel + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), b);
-              mma_16816(s[2 * kk], qa[ks], b[0], b[1]);
-              mma_16816(s[2 * kk + 1], qa[ks], b[2], b[3]);
+            for (int ks = 0; ks < D / 16; ++ks) {
+              const int chunk = (ks & 3) * 2 + ((lane >> 3) & 1);
+              ldsm4(at + (ks >> 2) * panel + ((chunk ^ (key & 7)) << 4), f[ks]);
             }
+            float e[2][4] = {}, o2[2][4] = {};
+#pragma unroll
+            for (int ks = 0; ks < D / 16; ks += 2) {
+              mma_16816(e[0], qa[ks], f[ks][0], f[ks][1]);
+              mma_16816(e[1], qa[ks], f[ks][2], f[ks][3]);
+              mma_16816(o2[0], qa[ks + 1], f[ks + 1][0], f[ks + 1][1]);
+              mma_16816(o2[1], qa[ks + 1], f[ks + 1][2], f[ks + 1][3]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) s[2 * kk + i][x] = e[i][x] + o2[i][x];
           }
+          auto load_v = [&](int kk) {
+            const int key = lane & 15;
+            const uint32_t at = vb + sixteen(kk) + key * 128;
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              const int chunk = (c & 3) * 2 + (lane >> 4);
+              ldsm4_t(at + (c >> 2) * panel + ((chunk ^ (key & 7)) << 4), f[c]);
+            }
+          };
+          load_v(0);
           if (key0 + kKeys > all_see) {
 #pragma unroll
             for (int i = 0; i < kKeys / 8; ++i) {
@@ -348,64 +377,73 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
                 if (key0 + i * 8 + 2 * tq + (e & 1) >= limit[e >> 1]) s[i][e] = -INFINITY;
             }
           }
-          // the running maximum; O and l follow it
-          float mx[2] = {-INFINITY, -INFINITY};
+          // P against the rows' references, and its sums. Only a sum above kRescaleSum, a row
+          // without a reference, or a NaN makes the warp take the maximum, move the references
+          // and compute P again.
+          uint32_t p[kKeys / 16][4];
+          float sum[2];
+          auto exps = [&]() {
+            const float m0 = m[0] == -INFINITY ? 0.f : m[0], m1 = m[1] == -INFINITY ? 0.f : m[1];
+            sum[0] = sum[1] = 0.f;
 #pragma unroll
-          for (int i = 0; i < kKeys / 8; ++i) {
-            mx[0] = fmaxf(mx[0], fmaxf(s[i][0], s[i][1]));
-            mx[1] = fmaxf(mx[1], fmaxf(s[i][2], s[i][3]));
-          }
-          float f[2];
-          bool moved = false;
+            for (int i = 0; i < kKeys / 8; ++i) {
+              const float p0 = tc::ex2(fmaf(s[i][0], c2, -m0)), p1 = tc::ex2(fmaf(s[i][1], c2, -m0));
+              const float p2 = tc::ex2(fmaf(s[i][2], c2, -m1)), p3 = tc::ex2(fmaf(s[i][3], c2, -m1));
+              sum[0] += p0 + p1;
+              sum[1] += p2 + p3;
+              p[i >> 1][(i & 1) * 2] = tc::pack_bf16x2(p0, p1);
+              p[i >> 1][(i & 1) * 2 + 1] = tc::pack_bf16x2(p2, p3);
+            }
+          };
+          exps();
+          if (__any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY || !(sum[0] <= kRescaleSum) ||
+                                          !(sum[1] <= kRescaleSum))) {
+            float f2[2];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float mn = fmaxf(m[i], quad_max(mx[i]) * c2);
-            f[i] = mn == m[i] ? 1.f : (m[i] == -INFINITY ? 0.f : tc::ex2(m[i] - mn));
-            moved = moved || mn != m[i];
-            m[i] = mn;
-            l[i] *= f[i];
-          }
-          if (__any_sync(0xffffffffu, moved)) {
+            for (int i = 0; i < 2; ++i) {
+              float mx = -INFINITY;
+#pragma unroll
+              for (int k = 0; k < kKeys / 8; ++k) mx = fmaxf(mx, fmaxf(s[k][2 * i], s[k][2 * i + 1]));
+              const float mb = quad_max(mx) * c2;  // -inf when nothing is visible
+              f2[i] = 1.f;
+              if (mb > m[i] + kRescaleTau) {
+                f2[i] = m[i] == -INFINITY ? 0.f : tc::ex2(m[i] - mb);
+                m[i] = mb;
+              }
+              l[i] *= f2[i];
+            }
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
-              o[i][0] *= f[0];
-              o[i][1] *= f[0];
-              o[i][2] *= f[1];
-              o[i][3] *= f[1];
+              o[i][0] *= f2[0];
+              o[i][1] *= f2[0];
+              o[i][2] *= f2[1];
+              o[i][3] *= f2[1];
             }
+            exps();
           }
-          const float m0 = m[0] == -INFINITY ? 0.f : m[0], m1 = m[1] == -INFINITY ? 0.f : m[1];
-          uint32_t p[kKeys / 16][4];
-#pragma unroll
-          for (int i = 0; i < kKeys / 8; ++i) {
-            const float p0 = tc::ex2(fmaf(s[i][0], c2, -m0)), p1 = tc::ex2(fmaf(s[i][1], c2, -m0));
-            const float p2 = tc::ex2(fmaf(s[i][2], c2, -m1)), p3 = tc::ex2(fmaf(s[i][3], c2, -m1));
-            l[0] += p0 + p1;
-            l[1] += p2 + p3;
-            p[i >> 1][(i & 1) * 2] = tc::pack_bf16x2(p0, p1);
-            p[i >> 1][(i & 1) * 2 + 1] = tc::pack_bf16x2(p2, p3);
-          }
+          l[0] += sum[0];
+          l[1] += sum[1];
           const bool tail = key0 + kKeys > g.seq;
 #pragma unroll
           for (int kk = 0; kk < kKeys / 16; ++kk) {
-            // values behind the request's last key: cleared, so that P = 0 meets no infinity
-            const int left = g.seq - (key0 + kk * 16 + 2 * tq);
-            const uint32_t k0 = left > 1 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
-            const uint32_t k1 = left > 9 ? 0xffffffffu : (left == 9 ? 0xffffu : 0u);
+            if (kk > 0) load_v(kk);
+            if (tail) {
+              // values behind the request's last key: cleared, so that P = 0 meets no infinity
+              const int left = g.seq - (key0 + kk * 16 + 2 * tq);
+              const uint32_t k0 = left > 1 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
+              const uint32_t k1 = left > 9 ? 0xffffffffu : (left == 9 ? 0xffffu : 0u);
+#pragma unroll
+              for (int c = 0; c < D / 16; ++c) {
+                f[c][0] &= k0;
+                f[c][1] &= k1;
+                f[c][2] &= k0;
+                f[c][3] &= k1;
+              }
+            }
 #pragma unroll
             for (int c = 0; c < D / 16; ++c) {
-              const int key = slice * kKeys + kk * 16 + (lane & 15);
-              const int chunk = c * 2 + (lane >> 4);
-              uint32_t b[4];
-              ldsm4_t(vb + (chunk >> 3) * kPanel + key * 128 + (((chunk & 7) ^ (key & 7)) << 4), b);
-              if (tail) {
-                b[0] &= k0;
-                b[1] &= k1;
-                b[2] &= k0;
-                b[3] &= k1;
-              }
-              mma_16816(o[2 * c], p[kk], b[0], b[1]);
-              mma_16816(o[2 * c + 1], p[kk], b[2], b[3]);
+              mma_16816(o[2 * c], p[kk], f[c][0], f[c][1]);
+              mma_16816(o[2 * c + 1], p[kk], f[c][2], f[c][3]);
             }
           }
         }
@@ -474,21 +512,38 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       __threadfence();
       for (int row = tid / kLanes; row < rows; row += kAtOnce) {
         auto slot = [&](int k) { return (k == 0 ? g.slot0 : 2 * (g.c0 + k)) * static_cast<int64_t>(kRows) + row; };
-        float M = -INFINITY;
-#pragma unroll 8
-        for (int k = 0; k < pieces; ++k) M = fmaxf(M, __ldcg(a.part_ml + slot(k)).x);
-        float L = 0.f;
+        // eight pieces' loads at a time, one trip to L2 each; the reference moves between them
+        float M = -INFINITY, L = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int k = 0; k < pieces; ++k) {
-          const float2 ml = __ldcg(a.part_ml + slot(k));
-          const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part_o + slot(k) * D + col));
-          const float f = ml.x == -INFINITY ? 0.f : tc::ex2(ml.x - M);
-          L = fmaf(f, ml.y, L);
-          v.x = fmaf(f, x.x, v.x);
-          v.y = fmaf(f, x.y, v.y);
-          v.z = fmaf(f, x.z, v.z);
-          v.w = fmaf(f, x.w, v.w);
+        for (int k0 = 0; k0 < pieces; k0 += 8) {
+          float2 ml[8];
+          float4 x[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            if (k0 + k < pieces) {
+              ml[k] = __ldcg(a.part_ml + slot(k0 + k));
+              x[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + slot(k0 + k) * D + col));
+            } else {
+              ml[k] = make_float2(-INFINITY, 0.f);
+              x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+          }
+          float mn = M;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
+          const float old = M == -INFINITY ? 0.f : tc::ex2(M - mn);
+          M = mn;
+          L *= old;
+          v = make_float4(v.x * old, v.y * old, v.z * old, v.w * old);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float f = ml[k].x == -INFINITY ? 0.f : tc::ex2(ml[k].x - M);
+            L = fmaf(f, ml[k].y, L);
+            v.x = fmaf(f, x[k].x, v.x);
+            v.y = fmaf(f, x[k].y, v.y);
+            v.z = fmaf(f, x[k].z, v.z);
+            v.w = fmaf(f, x[k].w, v.w);
+          }
         }
         store_row<D>(a, g, row, col, v, M, L);
       }
@@ -515,23 +570,44 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// The pool of one tensor, 64 elements x 1 head x `box` rows of a page in the 128-byte swizzle. A
-// map's strides ascend, so head and row come in the order of theirs.
-bool cache_map(CUtensorMap* m, const void* base, const avtp_cache_t& c, int64_t page, int64_t token, int64_t head,
-               int box, bool tok_inner) {
+bool encode(CUtensorMap* m, int rank, const void* base, const cuuint64_t* dims, const cuuint64_t* strides,
+            const cuuint32_t* box) {
   auto fn = encode_fn();
-  if (fn == nullptr) return false;
-  const cuuint64_t H = static_cast<cuuint64_t>(c.n_kv_heads), P = static_cast<cuuint64_t>(c.page_size);
-  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), tok_inner ? P : H, tok_inner ? H : P,
+  const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+  return fn != nullptr && fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, es,
+                             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Pool {  // one tensor of the cache; strides in bytes
+  const void* base;
+  cuuint64_t page, token, head;
+};
+
+// Whole rows, for k_cache_attn.
+bool rows_map(CUtensorMap* m, const Pool& t, const avtp_cache_t& c, int box) {
+  const cuuint64_t panels = static_cast<cuuint64_t>(c.head_dim) / 64;
+  const cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(c.page_size), panels, static_cast<cuuint64_t>(c.n_kv_heads),
                               static_cast<cuuint64_t>(c.n_pages)};
-  const cuuint64_t strides[3] = {static_cast<cuuint64_t>(tok_inner ? token : head) * 2,
-                                 static_cast<cuuint64_t>(tok_inner ? head : token) * 2, static_cast<cuuint64_t>(page) * 2};
-  const cuuint32_t b = static_cast<cuuint32_t>(box);
-  const cuuint32_t boxes[4] = {64, tok_inner ? b : 1, tok_inner ? 1 : b, 1};
-  const cuuint32_t es[4] = {1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t strides[4] = {t.token, 128, t.head, t.page};
+  const cuuint32_t boxes[5] = {64, static_cast<cuuint32_t>(box), static_cast<cuuint32_t>(panels), 1, 1};
+  return encode(m, 5, t.base, dims, strides, boxes);
+}
+// A panel of 64 elements, for k_cache_chunk, whose operands want a tile's panels whole.
+bool panel_map(CUtensorMap* m, const Pool& t, const avtp_cache_t& c, int box) {
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page_size),
+                              static_cast<cuuint64_t>(c.n_kv_heads), static_cast<cuuint64_t>(c.n_pages)};
+  const cuuint64_t strides[3] = {t.token, t.head, t.page};
+  const cuuint32_t boxes[4] = {64, static_cast<cuuint32_t>(box), 1, 1};
+  return encode(m, 4, t.base, dims, strides, boxes);
+}
+// q as {d, head, token}, box of 64 elements, a group's heads, as many tokens as fit into 128 rows.
+bool query_map(CUtensorMap* m, const avtp_cache_attn_args_t& a, int d, int G) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(a.n_q_heads),
+                              static_cast<cuuint64_t>(a.n_tokens)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(a.q_stride) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(kChunkRows / 2 / G)};
+  return encode(m, 3, a.q, dims, strides, box);
 }
 
 template <int D, int kWM>
@@ -543,20 +619,6 @@ cudaError_t launch_attn(int grid, const CUtensorMap& mk, const CUtensorMap& mv, 
   });
   if (e != cudaSuccess) return e;
   return launch_kernel(k_cache_attn<D, kWM>, dim3(grid), dim3(kThreads), smem_bytes(D), s, /*pdl=*/true, mk, mv, a);
-}
-
-// q as {d, head, token}, box of 64 elements, a group's heads, as many tokens as fit into 128 rows.
-bool query_map(CUtensorMap* m, const avtp_cache_attn_args_t& a, int d, int G) {
-  auto fn = encode_fn();
-  if (fn == nullptr) return false;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(a.n_q_heads),
-                              static_cast<cuuint64_t>(a.n_tokens)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(d) * 2, static_cast<cuuint64_t>(a.q_stride) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(G), static_cast<cuuint32_t>(kChunkRows / 2 / G)};
-  const cuuint32_t es[3] = {1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box, es,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // What the call's bounds leave to each kernel.
@@ -624,8 +686,6 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.Hkv = c.n_kv_heads;
   d.G = a.n_q_heads / c.n_kv_heads;
   d.page_size = c.page_size;
-  d.k_tok = c.k_token_stride < c.k_head_stride ? 1 : 0;
-  d.v_tok = c.v_token_stride < c.v_head_stride ? 1 : 0;
   d.few_rows = sh.few_rows;
   d.c2 = a.softmax_scale * kLog2e;
   d.o = static_cast<__nv_bfloat16*>(a.o);
@@ -642,16 +702,20 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   const int grid = device_sm_count();
   cudaError_t e = launch_kernel(k_cache_prep, dim3(1), dim3(kPrepThreads), 0, s, /*pdl=*/true, d, grid);
   if (e != cudaSuccess || a.n_tokens == 0) return e;
+  const Pool pk{c.k, static_cast<cuuint64_t>(c.k_page_stride) * 2, static_cast<cuuint64_t>(c.k_token_stride) * 2,
+                static_cast<cuuint64_t>(c.k_head_stride) * 2};
+  const Pool pv{c.v, static_cast<cuuint64_t>(c.v_page_stride) * 2, static_cast<cuuint64_t>(c.v_token_stride) * 2,
+                static_cast<cuuint64_t>(c.v_head_stride) * 2};
   // boxes no longer than a kernel's tile, and whole in a page
-  auto maps = [&](int tile, CUtensorMap* mk, CUtensorMap* mv) {
-    d.box = 16;
-    while (d.box < tile && c.page_size % (2 * d.box) == 0) d.box *= 2;
-    return cache_map(mk, c.k, c, c.k_page_stride, c.k_token_stride, c.k_head_stride, d.box, d.k_tok != 0) &&
-           cache_map(mv, c.v, c, c.v_page_stride, c.v_token_stride, c.v_head_stride, d.box, d.v_tok != 0);
+  auto box = [&](int tile) {
+    int b = 16;
+    while (b < tile && c.page_size % (2 * b) == 0) b *= 2;
+    return b;
   };
   CUtensorMap mk, mv, mq;
   if (sh.few) {
-    if (!maps(kCacheTile, &mk, &mv)) return cudaErrorInvalidValue;
+    d.box = box(kCacheTile);
+    if (!rows_map(&mk, pk, c, d.box) || !rows_map(&mv, pv, c, d.box)) return cudaErrorInvalidValue;
     const int wm = sh.row_warps;
     auto launch = c.head_dim == 128
                       ? (wm == 1 ? launch_attn<128, 1> : wm == 2 ? launch_attn<128, 2> : launch_attn<128, 4>)
@@ -659,7 +723,9 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
     if ((e = launch(grid, mk, mv, d, s)) != cudaSuccess) return e;
   }
   if (!sh.chunks) return cudaSuccess;
-  if (!maps(2 * kCacheTile, &mk, &mv) || !query_map(&mq, a, c.head_dim, d.G)) return cudaErrorInvalidValue;
+  d.box = box(2 * kCacheTile);
+  if (!panel_map(&mk, pk, c, d.box) || !panel_map(&mv, pv, c, d.box) || !query_map(&mq, a, c.head_dim, d.G))
+    return cudaErrorInvalidValue;
   return launch_cache_chunk(c.head_dim, grid, mq, mk, mv, d, s);
 }
 

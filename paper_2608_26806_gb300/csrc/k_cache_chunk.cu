@@ -107,7 +107,8 @@ __device__ __forceinline__ int units_of(const CacheAttnDev& a, const CacheReques
 }
 
 // ---------------------------------------------------------------- attention
-// mapQ: q {d, Hq, T}, box 64 x G x floor(128 / G); mapK, mapV as in k_cache_attn.cu.
+// mapQ: q {d, Hq, T}, box 64 x G x floor(128 / G); mapK, mapV: the cache as
+// {d, row of the page, head, page}, box of 64 elements and `box` rows.
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
@@ -256,11 +257,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           if (lane == 0) tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
           __syncwarp();
           if (lane < boxes) {
-            const int tok = kv ? a.v_tok : a.k_tok;
 #pragma unroll
             for (int p = 0; p < D / 64; ++p)
               tma_load_4d(sKV + sb * kTile + p * kPanel + lane * a.box * 128, kv ? &mapV : &mapK, p * 64,
-                          tok ? in_page : g.head, tok ? g.head : in_page, page, &sy.kv_full[sb]);
+                          in_page, g.head, page, &sy.kv_full[sb]);
           }
           __syncwarp();
         }
