@@ -32,7 +32,7 @@ constexpr int kCacheFewMixed = 16;
 // A unit of k_cache_chunk in several pieces, for the kernel that joins them; c1 < c0: none.
 struct CacheChunkSplit {
   int32_t row0, n, head, unit;  // request's first packed row and new tokens, KV head, unit of the request
-  int32_t c0, c1, slot0, pad;   // CTAs of the first and the last piece, place of the first piece
+  int32_t c0, c1;               // runs of the first and the last piece
 };
 
 struct CacheAttnWs {

@@ -47,31 +47,38 @@ struct CacheRequest {
   __device__ __forceinline__ int64_t rows(const CacheAttnDev& a) const { return static_cast<int64_t>(n) * a.G; }
 };
 
+// a / b of non-negative numbers, b > 0: in 32 bits where they fit, as they nearly always do. One copy
+// of it in a kernel, whose first pass over its code waits for instructions.
+static __device__ __noinline__ int64_t cache_div(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
+
 // A call's work as one line of steps, request by request, cut into equal runs. Every CTA forms the
-// cut for itself: NT threads take equal shares of the requests, pre[i] is the steps before thread
-// i's share and pre[NT] all of them (0 if validation refuses a length).
+// cut for itself, its loading warp alone for up to 32 requests (a lane each), else all its threads
+// (NT of them, equal shares of the requests; pre[i] is the steps before thread i's share).
+constexpr int kNearRequests = 32;
 template <int NT>
 struct CachePlan {
   int64_t pre[NT + 1];
-  int32_t most;  // steps of the longest row block (a row block's steps are one after the other on the line)
-  int32_t ok;
+  int64_t total;
+  int32_t most, ok;
 
-  // steps(request, most): its steps, with the longest block's in `most`. All NT threads; ends with
-  // a barrier. NT is a multiple of 32.
+  __device__ __forceinline__ static int share(const CacheAttnDev& a) { return (a.R + NT - 1) / NT; }
+  // For more than kNearRequests requests, all threads: steps(request, most) gives a request's steps,
+  // with those of its longest row block in `most`. NT is a multiple of 32.
   template <class F>
   __device__ void form(const CacheAttnDev& a, F steps) {
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, each = share(a);
     if (tid == 0) {
       most = 1;
       ok = 1;
-      pre[0] = 0;
     }
     __syncthreads();
-    const int share = (a.R + NT - 1) / NT;
     int64_t sum = 0;
     int longest = 1;
     bool fine = true;
-    for (int r = tid * share; r < min(a.R, (tid + 1) * share); ++r) {
+    for (int r = tid * each; r < min(a.R, (tid + 1) * each); ++r) {
       CacheRequest q;
       fine = q.load(a, r) && fine;
       if (fine) sum += steps(q, longest);
@@ -83,44 +90,111 @@ struct CachePlan {
     __syncthreads();
     if (tid < 32) {
       int64_t carry = 0;
-      for (int b = 0; b < NT; b += 32) {
-        int64_t x = pre[b + lane + 1];
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-          if (lane >= o) x += y;
-        }
-        x += carry;
-        pre[b + lane + 1] = ok ? x : 0;
+      const int used = min(NT, a.R);  // threads with a share
+      for (int b = 0; b < used; b += 32) {
+        const int64_t x = scan(pre[b + lane + 1]) + carry;
+        pre[b + lane + 1] = x;
         carry = __shfl_sync(0xffffffffu, x, 31);
+      }
+      if (lane == 0) {
+        pre[0] = 0;
+        total = carry;
       }
     }
     __syncthreads();
   }
-  // The first request of the share that step t lies in, and the steps before it.
-  __device__ __forceinline__ int find(const CacheAttnDev& a, int64_t t, int64_t* before) const {
-    int lo = 0, hi = NT;
+  // Inclusive sums over a warp.
+  __device__ __forceinline__ static int64_t scan(int64_t x) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    return x;
+  }
+};
+// The loading warp's view of the line.
+struct CacheLine {
+  int64_t total;  // 0 if validation refuses a length
+  int32_t most;   // steps of the longest row block (a row block's steps are one after the other on the line)
+  int64_t incl;   // up to kNearRequests requests: steps up to this lane's, its own included
+
+  template <int NT, class F>
+  __device__ __forceinline__ CacheLine(const CacheAttnDev& a, const CachePlan<NT>& plan, const CacheRequest& mine,
+                                       bool mine_ok, F steps) {
+    if (a.R > kNearRequests) {
+      total = plan.ok ? plan.total : 0;
+      most = plan.most;
+      incl = 0;
+    } else {
+      const int lane = threadIdx.x & 31;
+      int longest = 1;
+      incl = CachePlan<NT>::scan(lane < a.R && mine_ok ? steps(mine, longest) : 0);
+      most = __reduce_max_sync(0xffffffffu, longest);
+      total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
+    }
+  }
+  // A request at or before that of step t, t < total, and the steps before it.
+  template <int NT>
+  __device__ __forceinline__ int find(const CacheAttnDev& a, const CachePlan<NT>& plan, int64_t t, int64_t* before) const {
+    if (a.R <= kNearRequests) {
+      const int r = __popc(__ballot_sync(0xffffffffu, incl <= t));
+      const int64_t x = __shfl_sync(0xffffffffu, incl, r > 0 ? r - 1 : 0);
+      *before = r > 0 ? x : 0;
+      return r;
+    }
+    int lo = 0, hi = min(NT, a.R);
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (pre[mid] <= t) lo = mid; else hi = mid;
+      if (plan.pre[mid] <= t) lo = mid; else hi = mid;
     }
-    *before = pre[lo];
-    return lo * ((a.R + NT - 1) / NT);
+    *before = plan.pre[lo];
+    return lo * CachePlan<NT>::share(a);
   }
 };
 
-// The runs: CTA c of N takes steps [c total / N, (c + 1) total / N). N is as many CTAs as there are,
-// fewer where a run would be shorter than `least` steps or a block would have more than
+// The runs: N of them, the first total % N a step longer than the others. N is as many as there are
+// CTAs, fewer where a run would be shorter than `least` steps or a block would be in more than
 // kCacheMaxPieces pieces.
 struct CacheRuns {
-  int64_t total, N;
-  __device__ __forceinline__ CacheRuns(int64_t total_, int most, int least) : total(total_) {
+  int64_t total, each, longer;  // steps of a run, runs of one step more
+  int64_t N;
+  __device__ __forceinline__ CacheRuns(int64_t total_, int most, int least, int ctas) : total(total_) {
     const int64_t run = max((most + kCacheMaxPieces - 3) / (kCacheMaxPieces - 2), least);
-    N = max(int64_t(1), min(static_cast<int64_t>(gridDim.x), total / run));
+    N = total >= run * ctas ? ctas : max(int64_t(1), cache_div(total, run));
+    each = cache_div(total, N);
+    longer = total - each * N;
   }
-  __device__ __forceinline__ int64_t begin(int64_t c) const { return c < N ? c * total / N : total; }
-  // the CTA of step t: the last whose run begins at or before it
-  __device__ __forceinline__ int cta(int64_t t) const { return static_cast<int>(((t + 1) * N - 1) / total); }
+  __device__ __forceinline__ int64_t begin(int64_t c) const { return c < N ? c * each + min(c, longer) : total; }
+  // the run of step t
+  __device__ __forceinline__ int run(int64_t t) const {
+    const int64_t edge = longer * (each + 1);
+    return static_cast<int>(t < edge ? cache_div(t, each + 1) : longer + cache_div(t - edge, each));
+  }
+};
+// Where a run leaves a piece of a block: a block that began in an earlier run in its even place, one
+// that goes on in the next run in its odd one. A run has at most one of either kind.
+__device__ __forceinline__ int piece_place(int run, bool begins) { return 2 * run + (begins ? 1 : 0); }
+
+// Where a request's boxes of keys lie, 32 of them at a time: a warp looks them up in the block table, a
+// lane a box, and one thread issues their copies. Box i holds keys i * box ..
+struct CacheWindow {
+  int2 at[32];  // page, row of the page
+  // Boxes i0 .. i0 + 31 (i0 a multiple of 32) of a request of `seq` tokens; true if a page lies outside
+  // the pool: page 0 then stands in its place.
+  __device__ __forceinline__ bool load(const CacheAttnDev& a, const int32_t* row, int seq, int i0) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t i = static_cast<uint32_t>(i0 + lane), in_page = static_cast<uint32_t>(a.page_size / a.box);
+    const uint32_t p = i / in_page;
+    int page = 0;
+    if (static_cast<int64_t>(i) * a.box < seq) page = row[p];
+    const bool bad = page < 0 || page >= a.n_pages;
+    __syncwarp();  // the window before has been used
+    at[lane] = make_int2(bad ? 0 : page, static_cast<int>(i - p * in_page) * a.box);
+    __syncwarp();
+    return __any_sync(0xffffffffu, bad);
+  }
 };
 
 __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int z, int w, uint64_t* bar) {

@@ -25,6 +25,8 @@
 // values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 #include <cudaTypedefs.h>
 
+#include <type_traits>
+
 #include "avtp_cache_attn.cuh"
 
 namespace avtp {
@@ -48,7 +50,6 @@ struct Segment {
   int32_t head;        // KV head (-1: no more)
   int32_t tile0, tile1;
   int32_t c0, c1;      // CTAs of the block's first and last piece
-  int32_t slot, slot0; // where this piece goes, when there are several, and the block's first
   int32_t req;
 };
 
@@ -68,6 +69,7 @@ struct Shared {
   uint64_t seg_full[2], seg_empty[2];
   Segment seg[2];
   CachePlan<kThreads> plan;
+  CacheWindow window;
   float m[4][16], l[4][16];
   int32_t last;
   int abort, bad_page;
@@ -185,22 +187,27 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     tc::tma_prefetch_map(&mapK);
     tc::tma_prefetch_map(&mapV);
   }
+  CacheRequest mine;  // a lane's request of a call of few: on its way while the barriers are made
+  bool mine_ok = true;
+  if (warp == kLoadWarp && lane < a.R) mine_ok = mine.load(a, lane);
   pdl_trigger();
   __syncthreads();
-
-  sh.plan.form(a, [&](const CacheRequest& q, int& most) {
+  auto steps = [&](const CacheRequest& q, int& most) {
     const int t = tiles_of(a, q);
     most = max(most, t);
     return static_cast<int64_t>(t) * a.Hkv;
-  });
-  const CacheRuns runs(sh.plan.pre[kThreads], sh.plan.most, 1);
-  const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
+  };
+  if (a.R > kNearRequests) sh.plan.form(a, steps);
   volatile int* abort_flag = &sh.abort;
 
   if (warp == kLoadWarp) {
     // ------------------------------------------------------------ segments and loads
+    const CacheLine line(a, sh.plan, mine, mine_ok, steps);
+    const CacheRuns runs(line.total, line.most, 1, gridDim.x);
+    const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
+    const int per_tile = kCacheTile / a.box;
     int64_t pre = 0;  // tiles before request r
-    int r = t0 < t1 ? sh.plan.find(a, t0, &pre) : 0;
+    int r = t0 < t1 ? line.find(a, sh.plan, t0, &pre) : 0;
     int n = 0, sc = 0;
     bool fine = true;
     for (int64_t t = t0; fine; ++sc) {
@@ -217,7 +224,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           if (t < pre + len) break;
           pre += len;
         }
-        g.head = static_cast<int>((t - pre) / tiles);
+        g.head = static_cast<int>(cache_div(t - pre, tiles));
         const int64_t s = pre + static_cast<int64_t>(g.head) * tiles;  // the block's first step
         end = min(t1, s + tiles);
         g.row0 = q.row0;
@@ -225,11 +232,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         g.seq = q.seq;
         g.tile0 = static_cast<int>(t - s);
         g.tile1 = static_cast<int>(end - s);
-        g.c0 = runs.cta(s);
-        g.c1 = runs.cta(s + tiles - 1);
-        // a CTA's first segment goes to its even slot, its last (the only other that can be a piece) to its odd one
-        g.slot = 2 * blockIdx.x + (t == t0 ? 0 : 1);
-        g.slot0 = 2 * g.c0 + (runs.begin(g.c0) == s ? 0 : 1);
+        g.c0 = t == s ? static_cast<int>(blockIdx.x) : runs.run(s);
+        g.c1 = end == s + tiles ? static_cast<int>(blockIdx.x) : runs.run(s + tiles - 1);
         g.req = r;
       }
       if (sc >= 2) fine = tc::mbar_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
@@ -241,32 +245,26 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       __syncwarp();
       if (g.head < 0) break;
       const int32_t* row = a.table + g.req * a.table_stride;
-      auto page_of = [&](int tile) {
-        const int64_t key = static_cast<int64_t>(tile) * kCacheTile + lane * a.box;
-        return (lane * a.box < kCacheTile && key < g.seq) ? row[key / a.page_size] : 0;
-      };
-      int page = page_of(g.tile0);
-      for (int tile = g.tile0; tile < g.tile1; ++tile, ++n) {
-        const int next = tile + 1 < g.tile1 ? page_of(tile + 1) : 0;
-        const int sb = n % kStages;
-        if (n >= kStages) fine = tc::mbar_wait_warp(&sh.kv_empty[sb], (n / kStages - 1) & 1);
-        if (!fine || *abort_flag) break;
+      for (int tile = g.tile0; tile < g.tile1 && !*abort_flag; ++tile, ++n) {
+        const int i0 = tile * per_tile, sb = n % kStages;
+        if (tile == g.tile0 || (i0 & 31) == 0)
+          if (sh.window.load(a, row, g.seq, i0 & ~31)) sh.bad_page = g.req;
         const int keys = min(kCacheTile, g.seq - tile * kCacheTile);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
-        if (lane == 0) tc::mbar_arrive_expect_tx(&sh.kv_full[sb], boxes * a.box * D * 4);
-        __syncwarp();
-        if (lane < boxes) {
-          if (page < 0 || page >= a.n_pages) {  // outside the pool: recorded, and another read in its place
-            sh.bad_page = g.req;
-            page = 0;
+        if (tc::elect_one()) {
+          if (n >= kStages && !tc::mbar_wait(&sh.kv_empty[sb], (n / kStages - 1) & 1)) {
+            *abort_flag = 1;
+          } else {
+            tc::mbar_arrive_expect_tx(&sh.kv_full[sb], boxes * a.box * D * 4);
+            unsigned char* dst = smem + sb * stage_bytes(D);
+            for (int b = 0; b < boxes; ++b, dst += a.box * D * 2) {
+              const int2 at = sh.window.at[(i0 + b) & 31];
+              tma_load_5d(dst, &mapK, at.y, g.head, at.x, &sh.kv_full[sb]);
+              tma_load_5d(dst + stage_bytes(D) / 2, &mapV, at.y, g.head, at.x, &sh.kv_full[sb]);
+            }
           }
-          unsigned char* dst = smem + sb * stage_bytes(D) + lane * a.box * D * 2;
-          const int in_page = (tile * kCacheTile + lane * a.box) % a.page_size;
-          tma_load_5d(dst, &mapK, in_page, g.head, page, &sh.kv_full[sb]);
-          tma_load_5d(dst + stage_bytes(D) / 2, &mapV, in_page, g.head, page, &sh.kv_full[sb]);
         }
         __syncwarp();
-        page = next;
       }
       if (!fine || *abort_flag) {
         fine = false;
@@ -493,8 +491,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         if (pieces == 1) {
           store_row<D>(a, g, row, col, v, M, L);
         } else {
-          __stcg(reinterpret_cast<float4*>(a.part_o + (static_cast<int64_t>(g.slot) * kRows + row) * D + col), v);
-          if (sub == 0) __stcg(a.part_ml + static_cast<int64_t>(g.slot) * kRows + row, make_float2(M, L));
+          const int64_t at = static_cast<int64_t>(piece_place(blockIdx.x, g.tile0 == 0)) * kRows + row;
+          __stcg(reinterpret_cast<float4*>(a.part_o + at * D + col), v);
+          if (sub == 0) __stcg(a.part_ml + at, make_float2(M, L));
         }
       }
       if (pieces == 1) continue;
@@ -510,43 +509,63 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       bar_consumers();
       if (!sh.last) continue;
       __threadfence();
-      for (int row = tid / kLanes; row < rows; row += kAtOnce) {
-        auto slot = [&](int k) { return (k == 0 ? g.slot0 : 2 * (g.c0 + k)) * static_cast<int64_t>(kRows) + row; };
-        // eight pieces' loads at a time, one trip to L2 each; the reference moves between them
-        float M = -INFINITY, L = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k0 = 0; k0 < pieces; k0 += 8) {
-          float2 ml[8];
-          float4 x[8];
+      // Few rows: eight pieces of a row at a time; many: two pieces of four rows. Either way the
+      // loads of a turn are one trip to L2; a row's reference moves between turns.
+      auto join = [&](auto at_once, auto of_rows) {
+        constexpr int P = decltype(at_once)::value, N = decltype(of_rows)::value;
+        for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
+          float M[N], L[N];
+          float4 v[N];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            if (k0 + k < pieces) {
-              ml[k] = __ldcg(a.part_ml + slot(k0 + k));
-              x[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + slot(k0 + k) * D + col));
-            } else {
-              ml[k] = make_float2(-INFINITY, 0.f);
-              x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int i = 0; i < N; ++i) {
+            M[i] = -INFINITY;
+            L[i] = 0.f;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          for (int k0 = 0; k0 < pieces; k0 += P) {
+            float2 ml[N][P];
+            float4 x[N][P];
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+              const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
+#pragma unroll
+              for (int i = 0; i < N; ++i) {
+                ml[i][k] = make_float2(-INFINITY, 0.f);
+                x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
+                  ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
+                  x[i][k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + i * kAtOnce) * D + col));
+                }
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              float mn = M[i];
+#pragma unroll
+              for (int k = 0; k < P; ++k) mn = fmaxf(mn, ml[i][k].x);
+              const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
+              M[i] = mn;
+              L[i] *= old;
+              v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
+#pragma unroll
+              for (int k = 0; k < P; ++k) {
+                const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
+                L[i] = fmaf(f, ml[i][k].y, L[i]);
+                v[i].x = fmaf(f, x[i][k].x, v[i].x);
+                v[i].y = fmaf(f, x[i][k].y, v[i].y);
+                v[i].z = fmaf(f, x[i][k].z, v[i].z);
+                v[i].w = fmaf(f, x[i][k].w, v[i].w);
+              }
             }
           }
-          float mn = M;
 #pragma unroll
-          for (int k = 0; k < 8; ++k) mn = fmaxf(mn, ml[k].x);
-          const float old = M == -INFINITY ? 0.f : tc::ex2(M - mn);
-          M = mn;
-          L *= old;
-          v = make_float4(v.x * old, v.y * old, v.z * old, v.w * old);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float f = ml[k].x == -INFINITY ? 0.f : tc::ex2(ml[k].x - M);
-            L = fmaf(f, ml[k].y, L);
-            v.x = fmaf(f, x[k].x, v.x);
-            v.y = fmaf(f, x[k].y, v.y);
-            v.z = fmaf(f, x[k].z, v.z);
-            v.w = fmaf(f, x[k].w, v.w);
-          }
+          for (int i = 0; i < N; ++i)
+            if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i]);
         }
-        store_row<D>(a, g, row, col, v, M, L);
-      }
+      };
+      using std::integral_constant;
+      if (rows <= kAtOnce) join(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+      else join(integral_constant<int, 2>{}, integral_constant<int, 4>{});
     }
   }
   pdl_wait();  // this grid's end implies the validation kernel's, which resets the status word

@@ -11,8 +11,8 @@
 //   O  += P_j V_j           tcgen05, A (P) from TMEM, V the MN-major operand as the pages hold it
 // with the softmax, the order of MMAs and the ring of k_attn_fwd.cu (which see for what they
 // measured): while one slot's softmax runs, the tensor core has the other slot's products.
-// Keys come as TMA boxes of a page's rows, a lane a box, each after a look at the block table a block
-// ahead.
+// Keys and values come as TMA boxes of a page's rows, 32 boxes' places looked up in the block table
+// at a time, by a warp each (one warp for both, looking up every block's, took 3000 cycles a block).
 //
 // Units are few (a chunk of 512 tokens, G = 4: eight a KV head) and of unequal length, so
 // their key blocks, taken as one line (request, unit, head, block), are cut into equal runs, a
@@ -24,10 +24,8 @@
 // of that), and for short calls the pieces' way through L2.
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
-// segments, table, TMA. Warp 9: TMEM and the MMAs. Every wait is bounded; a CTA whose wait gives up
-// records AVTP_ERR_TIMEOUT and leaves.
-#include <type_traits>
-
+// segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
+// CTA whose wait gives up records AVTP_ERR_TIMEOUT and leaves.
 #include "avtp_cache_attn.cuh"
 
 namespace avtp {
@@ -35,12 +33,15 @@ namespace {
 
 constexpr int kQT = 128;  // rows of a slot (MMA M, TMEM lanes)
 constexpr int kKB = 128;  // keys of a block (MMA N of Q K^T, K of P V)
-constexpr int kThreads = 320;
+constexpr int kThreads = 352;
 constexpr int kSlotWarps = 4;
-constexpr int kTmaWarp = 8;
+constexpr int kKeyWarp = 8;
 constexpr int kMmaWarp = 9;
+constexpr int kValueWarp = 10;
 constexpr int kStages = 4;      // key or value blocks in shared memory
-constexpr int kLeastBlocks = 4; // key blocks of a run, at least
+// A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first
+// softmax with nothing to overlap, its rows' way out): its steps on the line are its blocks and these.
+constexpr int kUnitSteps = 2;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSCol = 0;    // S (and P) of slot s at kSCol + 128 s
 constexpr uint32_t kOCol = 256;  // O of slot s at kOCol + 128 s
@@ -48,6 +49,8 @@ constexpr uint32_t kOCol = 256;  // O of slot s at kOCol + 128 s
 // reference by more than kRescaleTau (log2 units).
 constexpr float kRescaleSum = 16384.f;
 constexpr float kRescaleTau = 8.f;
+// A row whose sum is below this has no reference yet, or one too far above its logits.
+constexpr float kLeastSum = 1.f / 1024.f;
 constexpr float kLn2 = 0.6931471805599453f;
 static_assert(kChunkRows == 2 * kQT, "two slots a unit");
 
@@ -93,6 +96,7 @@ struct ChunkSync {
   uint64_t drain;
   Segment seg[2];
   CachePlan<kThreads> plan;
+  CacheWindow window[2];  // of the keys' warp, of the values'
   uint32_t tmem;
   int abort, bad_page;
 };
@@ -131,7 +135,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&sy.seg_full[s], 1);
-      tc::mbar_init(&sy.seg_empty[s], 2 * kSlotWarps + 1);
+      tc::mbar_init(&sy.seg_empty[s], 2 * kSlotWarps + 2);
       tc::mbar_init(&sy.s_full[s], 1);
       for (int h = 0; h < 2; ++h) {
         tc::mbar_init(&sy.p_full[s][h], kSlotWarps);
@@ -152,8 +156,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     tc::tmem_alloc(&sy.tmem, kTmemCols);
     tc::tmem_relinquish();
   }
+  CacheRequest mine;  // a lane's request of a call of few: on its way while the barriers are made
+  bool mine_ok = true;
+  if (warp == kKeyWarp && lane < a.R) mine_ok = mine.load(a, lane);
   // the rows behind a slot's nt * G, which no box writes: zeros
-  for (uint32_t i = threadIdx.x; i < 2 * kTile / 16; i += kThreads) reinterpret_cast<uint4*>(sQ)[i] = make_uint4(0u, 0u, 0u, 0u);
+  const int spare = kQT - nt * a.G;
+  for (int i = threadIdx.x; i < 2 * (D / 64) * spare * 8; i += kThreads) {
+    const int panel = i / (spare * 8), e = i - panel * spare * 8;
+    *reinterpret_cast<uint4*>(sQ + panel * kPanel + nt * a.G * 128 + e * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
   tc::fence_proxy_async();
   tc::fence_before_sync();
   __syncthreads();
@@ -162,23 +173,71 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   const uint32_t tmem = sy.tmem;
   volatile int* abort_flag = &sy.abort;
 
-  sy.plan.form(a, [&](const CacheRequest& q, int& most) {
+  auto steps = [&](const CacheRequest& q, int& most) {
     const int U = units_of(a, q, nt);
     int64_t sum = 0;
-    for (int u = 0; u < U; ++u) sum += unit_blocks(q, nt, u);
-    if (U > 0) most = max(most, unit_blocks(q, nt, U - 1));
+#pragma unroll 1
+    for (int u = 0; u < U; ++u) sum += kUnitSteps + unit_blocks(q, nt, u);
+    if (U > 0) most = max(most, kUnitSteps + unit_blocks(q, nt, U - 1));
     return sum * a.Hkv;
-  });
-  const CacheRuns runs(sy.plan.pre[kThreads], sy.plan.most, kLeastBlocks);
-  const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
+  };
+  if (a.R > kNearRequests) sy.plan.form(a, steps);
 
-  if (warp == kTmaWarp) {
-    // ------------------------------------------------------------ segments and TMA loads
+  // The copies of one segment's keys or values, into every other stage of the ring (kv = 0 or 1), n
+  // so far; between(): behind the first block's copy is under way.
+  auto stream = [&](const Segment& g, int kv, const CUtensorMap* map, int& n, auto between) {
+    const int32_t* row = a.table + g.req * a.table_stride;
+    const int per_block = kKB / a.box;
+    for (int j = g.j0; j < g.j1 && !*abort_flag; ++j, ++n) {
+      const int i0 = j * per_block, sb = 2 * (n & 1) + kv;
+      if (j == g.j0 || (i0 & 31) == 0)
+        if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
+      const int keys = min(kKB, g.seq - j * kKB);  // none: an empty cache
+      const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
+      if (tc::elect_one()) {
+        if (n >= 2 && !tc::mbar_wait(&sy.kv_empty[sb], ((n >> 1) - 1) & 1)) {
+          *abort_flag = 1;
+        } else {
+          tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
+          unsigned char* dst = sKV + sb * kTile;
+#pragma unroll 1
+          for (int b = 0; b < boxes; ++b, dst += a.box * 128) {
+            const int2 at = sy.window[kv].at[(i0 + b) & 31];
+#pragma unroll
+            for (int p = 0; p < D / 64; ++p)
+              tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, &sy.kv_full[sb]);
+          }
+        }
+      }
+      __syncwarp();
+      if (j == g.j0) between();
+    }
+    // the ring's places are constants of a step: an odd one is passed on empty
+    if ((n & 1) != 0 && !*abort_flag) {
+      const int sb = 2 + kv;
+      if (tc::elect_one()) {
+        if (n >= 2 && !tc::mbar_wait(&sy.kv_empty[sb], ((n >> 1) - 1) & 1)) *abort_flag = 1;
+        else tc::mbar_arrive(&sy.kv_full[sb]);
+      }
+      __syncwarp();
+      ++n;
+    }
+  };
+  // let the copies in flight land before the CTA may exit
+  auto land = [&](int kv, int n) {
+    for (int k = (n >= 2 ? n - 2 : 0); k < n; ++k) tc::mbar_wait_warp(&sy.kv_full[2 * (k & 1) + kv], (k >> 1) & 1);
+  };
+
+  if (warp == kKeyWarp) {
+    // ------------------------------------------------------------ segments, queries and keys
+    const CacheLine line(a, sy.plan, mine, mine_ok, steps);
+    const CacheRuns runs(line.total, line.most, kUnitSteps + 1, gridDim.x);
+    const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
     int64_t pre = 0;  // steps before unit u of request r
-    int r = t0 < t1 ? sy.plan.find(a, t0, &pre) : 0, u = 0;
+    int r = t0 < t1 ? line.find(a, sy.plan, t0, &pre) : 0, u = 0;
     CacheChunkSplit split{};
     split.c1 = -1;
-    int sc = 0, n = 0;  // segments published, ring places used (K, V, K, V, ...)
+    int sc = 0, qn = 0, n = 0;  // segments published, queries loaded, key blocks loaded
     bool ok = true;
     for (int64_t t = t0;; ++sc) {
       Segment g{};
@@ -186,33 +245,36 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       int64_t end = t;
       if (t < t1) {
         CacheRequest q;
-        int nb;
+        int nb = 0;
+        int64_t s = 0;  // the unit's first step
         for (;; ++r, u = 0) {
           q.load(a, r);
           const int U = units_of(a, q, nt);
+#pragma unroll 1
           for (; u < U; ++u) {
             nb = unit_blocks(q, nt, u);
-            if (t < pre + static_cast<int64_t>(nb) * a.Hkv) break;
-            pre += static_cast<int64_t>(nb) * a.Hkv;
+            if (t < pre + static_cast<int64_t>(kUnitSteps + nb) * a.Hkv) break;
+            pre += static_cast<int64_t>(kUnitSteps + nb) * a.Hkv;
           }
           if (u < U) break;
         }
+        const int head = static_cast<int>(cache_div(t - pre, kUnitSteps + nb));
+        s = pre + static_cast<int64_t>(head) * (kUnitSteps + nb);
+        end = min(t1, s + kUnitSteps + nb);
+        // a run that ends in a unit's first steps leaves its blocks to the next
+        g.head = end > s + kUnitSteps ? head : -1;
         g.row0 = q.row0;
         g.n = q.n;
         g.seq = q.seq;
         g.nt = nt;
         g.unit = u;
         g.req = r;
-        g.head = static_cast<int>((t - pre) / nb);
-        const int64_t s = pre + static_cast<int64_t>(g.head) * nb;  // the unit's first step
-        end = min(t1, s + nb);
-        g.j0 = static_cast<int>(t - s);
-        g.j1 = static_cast<int>(end - s);
-        const int c0 = runs.cta(s), c1 = runs.cta(s + nb - 1);
-        // a CTA's first segment goes to its even place, its last (the only other that can be a piece) to its odd one
-        g.place = c0 == c1 ? -1 : 2 * static_cast<int>(blockIdx.x) + (t == t0 ? 0 : 1);
-        if (c0 < c1 && c0 == static_cast<int>(blockIdx.x))
-          split = CacheChunkSplit{g.row0, g.n, g.head, g.unit, c0, c1, g.place, 0};
+        g.j0 = static_cast<int>(max(int64_t(0), t - s - kUnitSteps));
+        g.j1 = static_cast<int>(end - s - kUnitSteps);
+        const int me = static_cast<int>(blockIdx.x);
+        const int c0 = g.j0 == 0 ? me : runs.run(s + kUnitSteps), c1 = g.j1 == nb ? me : runs.run(s + kUnitSteps + nb - 1);
+        g.place = c0 == c1 ? -1 : piece_place(me, g.j0 == 0);
+        if (g.head >= 0 && c0 < c1 && c0 == me) split = CacheChunkSplit{g.row0, g.n, g.head, g.unit, c0, c1};
       }
       if (sc >= 2) ok = tc::mbar_wait_warp(&sy.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
       if (!ok) break;
@@ -222,71 +284,52 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       }
       __syncwarp();
       if (g.head < 0) break;
-      if (sc >= 1) ok = tc::mbar_wait_warp(&sy.q_empty, (sc - 1) & 1);
-      if (!ok) break;
-      const int nq = g.live(1) ? 2 : 1;
-      if (lane == 0) {
-        tc::mbar_arrive_expect_tx(&sy.q_full, nq * (D / 64) * nt * a.G * 128);
-        for (int s = 0; s < nq; ++s)
-          for (int ac = 0; ac < D / 64; ++ac)
-            tc::tma_load_3d(sQ + s * kTile + ac * kPanel, &mapQ, ac * 64, g.head * a.G, g.row0 + g.tok0(s), &sy.q_full);
-      }
-      __syncwarp();
-      const int32_t* row = a.table + g.req * a.table_stride;
-      auto page_of = [&](int j) {
-        const int64_t key = static_cast<int64_t>(j) * kKB + lane * a.box;
-        return (lane * a.box < kKB && key < g.seq) ? row[key / a.page_size] : 0;
-      };
-      int page = page_of(g.j0);
-      for (int j = g.j0; j < g.j1 && ok; ++j) {
-        const int next = j + 1 < g.j1 ? page_of(j + 1) : 0;
-        const int keys = min(kKB, g.seq - j * kKB);  // none: an empty cache
-        const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
-        if (lane < boxes && (page < 0 || page >= a.n_pages)) {  // outside the pool: recorded, another read in its place
-          sy.bad_page = g.req;
-          page = 0;
-        }
-        const int in_page = (j * kKB + lane * a.box) % a.page_size;
-        for (int kv = 0; kv < 2; ++kv, ++n) {
-          const int sb = n % kStages;
-          ok = n < kStages || tc::mbar_wait_warp(&sy.kv_empty[sb], (n / kStages - 1) & 1);
-          if (!ok || *abort_flag) {
-            ok = false;
-            break;
+      auto queries = [&]() {
+        if (tc::elect_one()) {
+          if (qn >= 1 && !tc::mbar_wait(&sy.q_empty, (qn - 1) & 1)) {
+            *abort_flag = 1;
+          } else {
+            const int nq = g.live(1) ? 2 : 1;
+            tc::mbar_arrive_expect_tx(&sy.q_full, nq * (D / 64) * nt * a.G * 128);
+#pragma unroll 1
+            for (int s = 0; s < nq; ++s)
+#pragma unroll 1
+              for (int ac = 0; ac < D / 64; ++ac)
+                tc::tma_load_3d(sQ + s * kTile + ac * kPanel, &mapQ, ac * 64, g.head * a.G, g.row0 + g.tok0(s), &sy.q_full);
           }
-          if (lane == 0) tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
-          __syncwarp();
-          if (lane < boxes) {
-#pragma unroll
-            for (int p = 0; p < D / 64; ++p)
-              tma_load_4d(sKV + sb * kTile + p * kPanel + lane * a.box * 128, kv ? &mapV : &mapK, p * 64,
-                          in_page, g.head, page, &sy.kv_full[sb]);
-          }
-          __syncwarp();
         }
-        page = next;
-      }
-      // the ring's places are constants of a step: an odd pair is passed on empty
-      for (; ok && n % kStages != 0; ++n) {
-        const int sb = n % kStages;
-        ok = n < kStages || tc::mbar_wait_warp(&sy.kv_empty[sb], (n / kStages - 1) & 1);
-        if (ok && lane == 0) tc::mbar_arrive(&sy.kv_full[sb]);
+        ++qn;
         __syncwarp();
-      }
-      if (!ok) {
-        ++sc;
-        break;
-      }
+      };
+      // the first queries wait for nothing; later ones come behind the segment's first keys, which
+      // need not wait for the last product with the queries before
+      const bool first = qn == 0;
+      if (first) queries();
+      stream(g, 0, &mapK, n, [&] {
+        if (!first) queries();
+      });
+      ok = !*abort_flag;
+      if (!ok) break;
       t = end;
     }
     if (lane == 0) {
       if (!ok) *abort_flag = 1;
       a.split[blockIdx.x] = split;
     }
-    // let the copies in flight land before the CTA may exit
-    if (sc >= 1) tc::mbar_wait_warp(&sy.q_full, (sc - 1) & 1);
-    for (int k = (n >= kStages ? n - kStages : 0); k < n; ++k)
-      tc::mbar_wait_warp(&sy.kv_full[k % kStages], (k / kStages) & 1);
+    if (qn >= 1) tc::mbar_wait_warp(&sy.q_full, (qn - 1) & 1);
+    land(0, n);
+  } else if (warp == kValueWarp) {
+    // ------------------------------------------------------------ values
+    int n = 0;
+    for (int sc = 0; !*abort_flag; ++sc) {
+      if (!tc::mbar_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1)) break;
+      const Segment g = sy.seg[sc & 1];
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
+      if (g.head < 0) break;
+      stream(g, 1, &mapV, n, [] {});
+    }
+    land(1, n);
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ MMA issuer
     // One elected lane issues (see elect_one), serving both slots in turn, which keeps their
@@ -311,68 +354,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // half of O of slot s += P_j V_j, 16 keys an MMA; only the first `steps` of the block's eight
       // where the request's keys end in it
       auto pv_mmas = [&](int s, int j, int stage, int steps, int half) {
-        const uint64_t dv = tc::desc_mn_sw128(kv_base + stage * kTile, kPanel);
-        const uint32_t tP = tmem + kSCol + s * 128, tO = tmem + kOCol + s * 128;
-        if (steps == kKB / 16) {
+        const uint64_t dv = tc::desc_mn_sw128(kv_base + stage * kTile, kPanel) + half * (4 * 2048 / 16);
+        const uint32_t tP = tmem + kSCol + s * 128 + half * 32, tO = tmem + kOCol + s * 128;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int ks = half * 4 + k;
-            tc::mma_bf16_ts(tO, tP + ks * 8, dv + ks * (2048 / 16), idO, (j > 0 || ks > 0) ? 1u : 0u);
-          }
-        } else {
-#pragma unroll 1
-          for (int ks = half * 4; ks < min(half * 4 + 4, steps); ++ks)
-            tc::mma_bf16_ts(tO, tP + ks * 8, dv + ks * (2048 / 16), idO, (j > 0 || ks > 0) ? 1u : 0u);
-        }
+        for (int k = 0; k < 4; ++k)
+          if (half * 4 + k < steps)
+            tc::mma_bf16_ts(tO, tP + k * 8, dv + k * (2048 / 16), idO, (j > 0 || half > 0 || k > 0) ? 1u : 0u);
       };
-      using std::integral_constant;
-      // Step j, odd or even: V_j sits in stage 1 or 3, K_{j + 1} in stage 2 or 0, and the next
-      // step's blocks in the other two (kStages is 4); ph: the ring phase of V_j; pb[s]: the
-      // phase of slot s's barriers at the segment's block 0. p0, kv, kk: whether the first half
-      // of the next P and the next V and K were seen complete.
-      static_assert(kStages == 4, "stages of a step are compile-time constants");
-      bool p0 = false, kv = false, kk = false;
-      uint32_t pb[2] = {0, 0};
-      int n0 = 0, n1 = 0, nm = 0, last_steps = 0;
-      auto slot_group = [&](auto odd, auto slot, int j, uint32_t ph, bool more) {
-        constexpr int kOdd = decltype(odd)::value, s = decltype(slot)::value;
-        constexpr int sv = kOdd ? 3 : 1, sk = kOdd ? 0 : 2, sv1 = kOdd ? 1 : 3, sk1 = kOdd ? 2 : 0;
-        const int steps = j == nm - 1 ? last_steps : kKB / 16;
-        const uint32_t pp = kOdd ^ pb[s];
-        if (s == 0 || n0 <= j) {  // the first group of the step: V_j and K_{j + 1}
-          wait(&sy.kv_full[sv], ph, kv);
-          if (j + 1 < nm) wait(&sy.kv_full[sk], kOdd ? ph ^ 1 : ph, kk);
-        }
-        wait(&sy.p_full[s][0], pp, p0);
-        tc::fence_after_sync();
-        pv_mmas(s, j, sv, steps, 0);
-        const bool p1 = tc::mbar_test_wait(&sy.p_full[s][1], pp);
-        tc::mma_commit(&sy.pv_done[s][0]);
-        wait(&sy.p_full[s][1], pp, p1);
-        tc::fence_after_sync();
-        pv_mmas(s, j, sv, steps, 1);
-        tc::mma_commit(&sy.pv_done[s][1]);
-        const bool last = s == 1 || n1 <= j;
-        if (last) tc::mma_commit(&sy.kv_empty[sv]);
-        if (more) s_mmas(s, sk);
-        // the next group's barriers
-        const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
-        p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? !kOdd : kOdd) ^ (s1 ? pb[1] : pb[0]));
-        if (last) {
-          kv = tc::mbar_test_wait(&sy.kv_full[sv1], kOdd ? ph ^ 1 : ph);
-          kk = tc::mbar_test_wait(&sy.kv_full[sk1], ph ^ 1);
-        }
-        if (more) tc::mma_commit(&sy.s_full[s]);
-        if (last && j + 1 < nm) {  // the step's last group: K_{j + 1} has been read, by whom it had to be
-          tc::mma_commit(&sy.kv_empty[sk]);
-          if (j + 2 == nm) tc::mma_commit(&sy.q_empty);  // the segment's last S
-        }
-      };
-      auto step = [&](auto odd, int j, uint32_t ph) {
-        if (j < n0) slot_group(odd, integral_constant<int, 0>{}, j, ph, j + 1 < n0);
-        if (j < n1) slot_group(odd, integral_constant<int, 1>{}, j, ph, j + 1 < n1);
-      };
-      uint32_t ph = 0;
+      uint32_t ph = 0;           // phase of the ring at the segment's current pair of blocks
+      uint32_t pb0 = 0, pb1 = 0; // phase of each slot's barriers at the segment's block 0
 #pragma unroll 1
       for (int sc = 0; !bad; ++sc) {
         wait(&sy.seg_full[sc & 1], (sc >> 1) & 1, false);
@@ -380,38 +370,67 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         const Segment g = sy.seg[sc & 1];
         tc::mbar_arrive(&sy.seg_empty[sc & 1]);
         if (g.head < 0) break;
-        n0 = g.blocks(0);
-        n1 = g.blocks(1);
-        nm = max(n0, n1);
-        last_steps = max(0, (min(kKB, g.seq - (g.j1 - 1) * kKB) + 15) >> 4);
-        p0 = kv = kk = false;
+        const int n0 = g.blocks(0), n1 = g.blocks(1), nm = max(n0, n1);
+        const int last_steps = max(0, (min(kKB, g.seq - (g.j1 - 1) * kKB) + 15) >> 4);
         wait(&sy.q_full, sc & 1, false);
         wait(&sy.kv_full[0], ph, false);
         tc::fence_after_sync();
-        if (n0 > 0) {
-          s_mmas(0, 0);
-          tc::mma_commit(&sy.s_full[0]);
-        }
-        if (n1 > 0) {
-          s_mmas(1, 0);
-          tc::mma_commit(&sy.s_full[1]);
-        }
-        tc::mma_commit(&sy.kv_empty[0]);
-        if (nm == 1) tc::mma_commit(&sy.q_empty);
+        // Step -1 is S_0 of both slots alone. Step j, odd or even: V_j sits in stage 1 or 3, K_{j + 1} in
+        // stage 2 or 0, and the next step's blocks in the other two. One copy of a slot's products for
+        // both slots and either parity: four took more of the instruction cache than the roles'
+        // loops leave. p0, kv, kk: whether the first half of the next P and the next V and K were
+        // seen complete.
+        bool p0 = false, kv = false, kk = false;
 #pragma unroll 1
-        for (int j = 0; j < nm; j += 2, ph ^= 1) {
-          step(integral_constant<int, 0>{}, j, ph);
-          if (j + 1 < nm) {
-            step(integral_constant<int, 1>{}, j + 1, ph);
-          } else {  // the odd pair of stages, passed on
-            wait(&sy.kv_full[2], ph, false);
-            tc::mbar_arrive(&sy.kv_empty[2]);
-            wait(&sy.kv_full[3], ph, false);
-            tc::mbar_arrive(&sy.kv_empty[3]);
+        for (int j = -1; j < nm; ++j) {
+          const int odd = j & 1, sv = 1 + 2 * odd, sk = 2 - 2 * odd;
+          const int steps = j == nm - 1 ? last_steps : kKB / 16;
+          const bool keys = j + 1 < nm;
+#pragma unroll 1
+          for (int s = n0 > j ? 0 : 1; s < (n1 > j ? 2 : 1); ++s) {
+            const bool more = j + 1 < (s ? n1 : n0), last = s == 1 || n1 <= j;
+            if (j >= 0) {
+              const uint32_t pp = odd ^ (s ? pb1 : pb0);
+              if (s == 0 || n0 <= j) {  // the first group of the step: V_j and K_{j + 1}
+                wait(&sy.kv_full[sv], ph, kv);
+                if (keys) wait(&sy.kv_full[sk], ph ^ odd, kk);
+              }
+              wait(&sy.p_full[s][0], pp, p0);
+              tc::fence_after_sync();
+              pv_mmas(s, j, sv, steps, 0);
+              const bool p1 = tc::mbar_test_wait(&sy.p_full[s][1], pp);
+              tc::mma_commit(&sy.pv_done[s][0]);
+              wait(&sy.p_full[s][1], pp, p1);
+              tc::fence_after_sync();
+              pv_mmas(s, j, sv, steps, 1);
+              tc::mma_commit(&sy.pv_done[s][1]);
+              if (last) tc::mma_commit(&sy.kv_empty[sv]);
+            }
+            if (more) s_mmas(s, sk);
+            // the next group's barriers
+            const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
+            if (j >= 0) p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? odd ^ 1 : odd) ^ (s1 ? pb1 : pb0));
+            if (last && j >= 0) {
+              kv = tc::mbar_test_wait(&sy.kv_full[4 - sv], ph ^ odd);
+              kk = tc::mbar_test_wait(&sy.kv_full[2 - sk], ph ^ 1);
+            }
+            if (more) tc::mma_commit(&sy.s_full[s]);
+            if (last && keys) {  // the step's last group: K_{j + 1} has been read, by whom it had to be
+              tc::mma_commit(&sy.kv_empty[sk]);
+              if (j + 2 == nm) tc::mma_commit(&sy.q_empty);  // the segment's last S
+            }
           }
+          if (j >= 0) ph ^= odd;
         }
-        pb[0] ^= n0 & 1;
-        pb[1] ^= n1 & 1;
+        if ((nm & 1) != 0) {  // the odd pair of stages, passed on
+          wait(&sy.kv_full[2], ph, false);
+          tc::mbar_arrive(&sy.kv_empty[2]);
+          wait(&sy.kv_full[3], ph, false);
+          tc::mbar_arrive(&sy.kv_empty[3]);
+          ph ^= 1;
+        }
+        pb0 ^= n0 & 1;
+        pb1 ^= n1 & 1;
       }
       if (bad) *abort_flag = 1;
       // every MMA issued has completed once this arrives
@@ -444,7 +463,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // keys this row sees (all of them for a row that is not stored), and every row of the warp
       const int limit = live ? max(0, g.seq - g.n + tok + 1) : 0x7fffffff;
       const int all_see = __reduce_min_sync(0xffffffffu, limit);
-      float m = -INFINITY, l = 0.f;  // row reference (log2 units); sum of exp2(c2 s - m)
+      // row reference (log2 units), sum of exp2(c2 s - m). The reference begins as the maximum of the
+      // first half, which is in registers anyway (the whole block's, with the half's exponentials
+      // taken twice, cost 1400 cycles a segment; beginning at 0, sharp queries moved it too often).
+      float m = 0.f, l = 0.f;
       for (int j = 0; j < nblk; ++j) {
         ok = tc::mbar_wait_warp(&sy.s_full[slot], (done + j) & 1);
         if (!ok) break;
@@ -468,22 +490,68 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           }
           tc::fence_proxy_async();
         }
-#pragma unroll
+// One copy of the load, the maximum and the exponentials, for both halves and for a half that is
+// started again: the kernel's roles share an instruction cache that their loops fill.
+#pragma unroll 1
         for (int hf = 0; hf < 2; ++hf) {
-          uint32_t su[64];  // the row's logits of this half
+          uint32_t su[64];  // the row's logits of a half
           uint32_t pk[32];
-          auto load = [&](int half) {
+          float sum = 0.f, mb = -INFINITY;
+          // The segment's first half gives the reference it begins with. Later a half takes none: only
+          // values far above the reference or, as yet, all far below it, or a NaN, make the warp take
+          // the maximum of what is left of the block and start the half again (its logits are in TMEM).
+          bool scan = j == 0 && hf == 0, again = false;
+          int half = hf;
+#pragma unroll 1
+          for (;;) {
             tc::tmem_ld64_async(tS + half * 64, su);
             tc::tmem_wait64(su);
             if (masked) {
 #pragma unroll
               for (int c = 0; c < 64; ++c) su[c] = (half * 64 + c < seen) ? su[c] : 0xff800000u;
             }
-          };
-          // P of the half against the reference m, and its sum
-          auto exps = [&]() {
-            const float nm = (m == -INFINITY) ? 0.f : -m;
-            const float2 nn = make_float2(nm, nm);
+            if (scan) {
+              float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+              for (int c = 0; c < 64; c += 8) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                  t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
+              }
+              mb = fmaxf(mb, fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2);  // -inf when nothing is visible
+              if (half > hf) {
+                half = hf;
+                continue;
+              }
+              scan = false;
+              float factor = 1.f;
+              // A reference moves down before a row's first term alone, so nothing was lost to underflow
+              // (l = 0, and O is zero or not yet written); behind that l stays above kLeastSum, but for
+              // a half whose block's maximum, then the reference, is in the other half.
+              if (mb > m + kRescaleTau || (l < kLeastSum && mb != -INFINITY)) {
+                factor = l > 0.f ? tc::ex2(m - mb) : 1.f;
+                l *= factor;
+                m = mb;
+              }
+              if (__any_sync(0xffffffffu, factor != 1.f)) {
+                // O is final up to the previous half once its P V is done
+                ok = tc::mbar_wait_warp(&sy.pv_done[slot][hf ^ 1], (done + j + hf + 1) & 1);
+                if (!ok) break;
+                tc::fence_after_sync();
+#pragma unroll 1
+                for (int oc = 0; oc < D; oc += 32) {
+                  uint32_t ov[32];
+                  tc::tmem_ld32_async(tO + oc, ov);
+                  tc::tmem_wait(ov);
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
+                  tc::tmem_st32(tO + oc, ov);
+                }
+                tc::tmem_wait_st();
+              }
+            }
+            // P of the half against the reference m, and its sum
+            const float2 nn = make_float2(-m, -m);
             float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
 #pragma unroll
             for (int c = 0; c < 64; c += 4) {
@@ -495,49 +563,13 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
               pk[c / 2] = tc::pack_bf16x2(p0, p1);
               pk[c / 2 + 1] = tc::pack_bf16x2(p2, p3);
             }
-            return (acc0.x + acc0.y) + (acc1.x + acc1.y);
-          };
-          load(hf);
-          float sum = exps();
-          // no reference yet, a value far above it, or a NaN: take the maximum of what is left
-          // of the block as the reference and start the half again (its logits are in TMEM)
-          if (__any_sync(0xffffffffu, live && (m == -INFINITY || !(sum <= kRescaleSum)))) {
-            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-            for (int half = 1; half >= hf; --half) {
-              load(half);
-#pragma unroll
-              for (int c = 0; c < 64; c += 8) {
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                  t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
-              }
-            }
-            const float mb = fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2;  // -inf when nothing is visible
-            float factor = 1.f;
-            if (mb > m + kRescaleTau) {
-              if (m != -INFINITY) factor = tc::ex2(m - mb);
-              l *= factor;
-              m = mb;
-            }
-            if (__any_sync(0xffffffffu, factor != 1.f)) {
-              // O is final up to the previous half once its P V is done
-              ok = tc::mbar_wait_warp(&sy.pv_done[slot][hf ^ 1], (done + j + hf + 1) & 1);
-              if (!ok) break;
-              tc::fence_after_sync();
-#pragma unroll 1
-              for (int oc = 0; oc < D; oc += 32) {
-                uint32_t ov[32];
-                tc::tmem_ld32_async(tO + oc, ov);
-                tc::tmem_wait(ov);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
-                tc::tmem_st32(tO + oc, ov);
-              }
-              tc::tmem_wait_st();
-            }
-            sum = exps();
+            sum = (acc0.x + acc0.y) + (acc1.x + acc1.y);
+            if (again || !__any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum))) break;
+            again = scan = true;
+            mb = -INFINITY;
+            half = 1;
           }
+          if (!ok) break;
           l += sum;
           tc::tmem_st32(tS + hf * 32, pk);
           tc::tmem_wait_st();
@@ -620,9 +652,12 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
 }
 
 // ---------------------------------------------------------------- the units in pieces
-// CTA (c, y): the unit whose first piece is CTA c's last, eight columns of its 256 rows, a
-// row a thread. O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i with M the largest reference.
+// CTA (c, y): the unit that goes on behind run c and began in it, 16 columns of its 256 rows, a row a
+// thread. O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i with M the largest reference of the
+// pieces that saw a key. The weights are formed first, all their loads at once, so that four
+// pieces' columns are under way together.
 __global__ void __launch_bounds__(kChunkRows) k_cache_join(CacheAttnDev a, int d) {
+  __shared__ float s_weight[kCacheMaxPieces][kChunkRows];
   pdl_wait();
   pdl_trigger();
   const CacheChunkSplit u = a.split[blockIdx.x];
@@ -630,34 +665,65 @@ __global__ void __launch_bounds__(kChunkRows) k_cache_join(CacheAttnDev a, int d
   const int slot = threadIdx.x / kQT, row = threadIdx.x % kQT, nt = kQT / a.G;
   const int in_tile = row / a.G, tok = (2 * u.unit + slot) * nt + in_tile;
   if (in_tile >= nt || tok >= u.n) return;
-  const int pieces = u.c1 - u.c0 + 1, col4 = 2 * blockIdx.y;
-  auto piece = [&](int k) { return static_cast<int64_t>(k == 0 ? u.slot0 : 2 * (u.c0 + k)) * 2 + slot; };
-  float M = -INFINITY;
-#pragma unroll 4
-  for (int k = 0; k < pieces; ++k) M = fmaxf(M, __ldcg(a.chunk_ml + piece(k) * kQT + row).x);
-  float L = 0.f;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
-  const float4* part = reinterpret_cast<const float4*>(a.chunk_o);
-#pragma unroll 4
-  for (int k = 0; k < pieces; ++k) {
-    const float2 ml = __ldcg(a.chunk_ml + piece(k) * kQT + row);
-    if (ml.x == -INFINITY && ml.y == 0.f) continue;  // saw nothing, or holds no block of this slot
-    const float f = tc::ex2(ml.x - M);
-    const float4* src = part + (piece(k) * (d / 4) + col4) * kQT + row;
-    const float4 p = __ldcg(src), q = __ldcg(src + kQT);
-    L = fmaf(f, ml.y, L);
-    x = make_float4(fmaf(f, p.x, x.x), fmaf(f, p.y, x.y), fmaf(f, p.z, x.z), fmaf(f, p.w, x.w));
-    y = make_float4(fmaf(f, q.x, y.x), fmaf(f, q.y, y.y), fmaf(f, q.z, y.z), fmaf(f, q.w, y.w));
+  const int pieces = min(u.c1 - u.c0 + 1, kCacheMaxPieces), col4 = 4 * blockIdx.y;
+  auto piece = [&](int k) { return static_cast<int64_t>(piece_place(u.c0 + k, k == 0)) * 2 + slot; };
+  float M = -INFINITY, L = 0.f;
+  for (int k0 = 0; k0 < pieces; k0 += 8) {
+    float2 ml[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      ml[k] = k0 + k < pieces ? __ldcg(a.chunk_ml + piece(k0 + k) * kQT + row) : make_float2(0.f, 0.f);
+    float mn = M;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (ml[k].y != 0.f) mn = fmaxf(mn, ml[k].x);  // a sum of zero: it saw no key, or holds no block of this slot
+    const float old = M == -INFINITY ? 0.f : tc::ex2(M - mn);
+    if (old != 1.f)
+      for (int k = 0; k < k0; ++k) s_weight[k][threadIdx.x] *= old;
+    L *= old;
+    M = mn;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float f = ml[k].y == 0.f ? 0.f : tc::ex2(ml[k].x - M);
+      if (k0 + k < pieces) s_weight[k0 + k][threadIdx.x] = f;
+      L = fmaf(f, ml[k].y, L);
+    }
+  }
+  float4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < pieces; k0 += 4) {
+    float4 p[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4* src =
+          reinterpret_cast<const float4*>(a.chunk_o) + (piece(min(k0 + k, pieces - 1)) * (d / 4) + col4) * kQT + row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[k][i] = __ldcg(src + i * kQT);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float f = k0 + k < pieces ? s_weight[k0 + k][threadIdx.x] : 0.f;
+      if (f == 0.f) continue;  // its O may never have been written
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = make_float4(fmaf(f, p[k][i].x, v[i].x), fmaf(f, p[k][i].y, v[i].y), fmaf(f, p[k][i].z, v[i].z),
+                           fmaf(f, p[k][i].w, v[i].w));
+    }
   }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   const int64_t t = static_cast<int64_t>(u.row0) + tok;
   const int head = u.head * a.G + (row - in_tile * a.G);
-  uint4 w;
-  w.x = tc::pack_bf16x2(x.x * inv, x.y * inv);
-  w.y = tc::pack_bf16x2(x.z * inv, x.w * inv);
-  w.z = tc::pack_bf16x2(y.x * inv, y.y * inv);
-  w.w = tc::pack_bf16x2(y.z * inv, y.w * inv);
-  *reinterpret_cast<uint4*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * d + col4 * 4) = w;
+  uint4* out = reinterpret_cast<uint4*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * d + col4 * 4);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint4 w;
+    w.x = tc::pack_bf16x2(v[2 * i].x * inv, v[2 * i].y * inv);
+    w.y = tc::pack_bf16x2(v[2 * i].z * inv, v[2 * i].w * inv);
+    w.z = tc::pack_bf16x2(v[2 * i + 1].x * inv, v[2 * i + 1].y * inv);
+    w.w = tc::pack_bf16x2(v[2 * i + 1].z * inv, v[2 * i + 1].w * inv);
+    out[i] = w;
+  }
   if (blockIdx.y == 0 && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (M + log2f(L)) * kLn2;
 }
 
@@ -672,7 +738,7 @@ cudaError_t launch(int grid, const CUtensorMap& mq, const CUtensorMap& mk, const
   if (e != cudaSuccess) return e;
   e = launch_kernel(k_cache_chunk<D>, dim3(grid), dim3(kThreads), chunk_smem_bytes(D), s, /*pdl=*/true, mq, mk, mv, a);
   if (e != cudaSuccess) return e;
-  return launch_kernel(k_cache_join, dim3(grid, D / 8), dim3(kChunkRows), 0, s, /*pdl=*/true, a, D);
+  return launch_kernel(k_cache_join, dim3(grid, D / 16), dim3(kChunkRows), 0, s, /*pdl=*/true, a, D);
 }
 
 }  // namespace
