@@ -89,10 +89,12 @@ struct Segment {
 struct ChunkSync {
   uint64_t seg_full[2], seg_empty[2];
   uint64_t q_full, q_empty;
-  uint64_t kv_full[kStages], kv_empty[kStages];
-  uint64_t s_full[2];      // S of a slot written by the MMA
+  uint64_t kv_full[kStages];
+  uint64_t kv_empty[2];    // V_j and K_{j + 1} read, j even, odd (or -1: K_0)
+  uint64_t s_full[2];      // S of a slot written by the MMA, and P V of the block before complete
   uint64_t p_full[2][2];   // half of a slot's P written by the softmax (and S read out)
-  uint64_t pv_done[2][2];  // P V complete up to that half of a block
+  uint64_t half_done[2];   // P V of a block's first half complete (when someone may wait for that)
+  uint64_t o_done[2];      // P V of a slot's last block in the segment complete
   uint64_t drain;
   Segment seg[2];
   CachePlan<kThreads> plan;
@@ -129,18 +131,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   const int nt = kQT / a.G;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      tc::mbar_init(&sy.kv_full[s], 1);
-      tc::mbar_init(&sy.kv_empty[s], 1);
-    }
+    for (int s = 0; s < kStages; ++s) tc::mbar_init(&sy.kv_full[s], 1);
     for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(&sy.kv_empty[s], 1);
+      tc::mbar_init(&sy.half_done[s], 1);
+      tc::mbar_init(&sy.o_done[s], 1);
       tc::mbar_init(&sy.seg_full[s], 1);
       tc::mbar_init(&sy.seg_empty[s], 2 * kSlotWarps + 2);
       tc::mbar_init(&sy.s_full[s], 1);
-      for (int h = 0; h < 2; ++h) {
-        tc::mbar_init(&sy.p_full[s][h], kSlotWarps);
-        tc::mbar_init(&sy.pv_done[s][h], 1);
-      }
+      for (int h = 0; h < 2; ++h) tc::mbar_init(&sy.p_full[s][h], kSlotWarps);
     }
     tc::mbar_init(&sy.q_full, 1);
     tc::mbar_init(&sy.q_empty, 1);
@@ -183,19 +182,49 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   };
   if (a.R > kNearRequests) sy.plan.form(a, steps);
 
-  // The copies of one segment's keys or values, into every other stage of the ring (kv = 0 or 1), n
-  // so far; between(): behind the first block's copy is under way.
-  auto stream = [&](const Segment& g, int kv, const CUtensorMap* map, int& n, auto between) {
+  // The ring. K_j and V_j of a segment lie in stages 2 (j % 2) and 2 (j % 2) + 1. The MMA thread
+  // releases V_j and K_{j + 1} together, behind the last product with either: kv_empty[j % 2], once
+  // a step but the last, and kv_empty[1] once before, for K_0. The last values are released with the
+  // segment's O. The copies of a segment's keys (kv = 0) or values; between(): called behind the
+  // first block's copy.
+  struct Ring {
+    int fired0 = 0, fired1 = 0;    // completions of kv_empty[0] and [1] in the segments before
+    int outs0 = 0, outs1 = 0;      // of o_done[0] and [1]
+    int loads0 = 0, loads1 = 0;    // into the even and the odd blocks' stage
+    __device__ __forceinline__ void pass(const Segment& g) {
+      const int blocks = g.j1 - g.j0;
+      fired0 += blocks >> 1;
+      fired1 += 1 + ((blocks - 1) >> 1);
+      outs0 += g.blocks(0) > 0 ? 1 : 0;
+      outs1 += g.blocks(1) > 0 ? 1 : 0;
+      loads0 += (blocks + 1) >> 1;
+      loads1 += blocks >> 1;
+    }
+  };
+  auto stream = [&](const Segment& g, int kv, const CUtensorMap* map, Ring& ring, auto between) {
     const int32_t* row = a.table + g.req * a.table_stride;
-    const int per_block = kKB / a.box;
-    for (int j = g.j0; j < g.j1 && !*abort_flag; ++j, ++n) {
-      const int i0 = j * per_block, sb = 2 * (n & 1) + kv;
-      if (j == g.j0 || (i0 & 31) == 0)
+    const int per_block = kKB / a.box, blocks = g.j1 - g.j0;
+#pragma unroll 1
+    for (int j = 0; j < blocks && !*abort_flag; ++j) {
+      const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
+      if (j == 0 || (i0 & 31) == 0)
         if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
-      const int keys = min(kKB, g.seq - j * kKB);  // none: an empty cache
+      const int keys = min(kKB, g.seq - (g.j0 + j) * kKB);  // none: an empty cache
       const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
+      // the stage's last occupant, block j - 2: V_{j - 2} is released in step j - 2, K_{j - 2} in step
+      // j - 3; before the first two keys, the last release of the segment before, before the first
+      // two values, its O
+      const int bar = (j & 1) ^ (kv ? 0 : 1);
+      const int which = (bar ? ring.fired1 : ring.fired0) + (j < 2 ? -1 : (j >> 1) - 1 + (kv & bar));
       if (tc::elect_one()) {
-        if (n >= 2 && !tc::mbar_wait(&sy.kv_empty[sb], ((n >> 1) - 1) & 1)) {
+        bool fine = true;
+        if (kv == 0 || j >= 2) {
+          fine = which < 0 || tc::mbar_wait(&sy.kv_empty[bar], which & 1);
+        } else if (j == 0) {
+          fine = (ring.outs0 == 0 || tc::mbar_wait(&sy.o_done[0], (ring.outs0 - 1) & 1)) &&
+                 (ring.outs1 == 0 || tc::mbar_wait(&sy.o_done[1], (ring.outs1 - 1) & 1));
+        }
+        if (!fine) {
           *abort_flag = 1;
         } else {
           tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
@@ -210,22 +239,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
       }
       __syncwarp();
-      if (j == g.j0) between();
+      if (j == 0) between();
     }
-    // the ring's places are constants of a step: an odd one is passed on empty
-    if ((n & 1) != 0 && !*abort_flag) {
-      const int sb = 2 + kv;
-      if (tc::elect_one()) {
-        if (n >= 2 && !tc::mbar_wait(&sy.kv_empty[sb], ((n >> 1) - 1) & 1)) *abort_flag = 1;
-        else tc::mbar_arrive(&sy.kv_full[sb]);
-      }
-      __syncwarp();
-      ++n;
-    }
+    ring.pass(g);
   };
+
   // let the copies in flight land before the CTA may exit
-  auto land = [&](int kv, int n) {
-    for (int k = (n >= 2 ? n - 2 : 0); k < n; ++k) tc::mbar_wait_warp(&sy.kv_full[2 * (k & 1) + kv], (k >> 1) & 1);
+  auto land = [&](int kv, const Ring& ring) {
+    if (ring.loads0 > 0) tc::mbar_wait_warp(&sy.kv_full[kv], (ring.loads0 - 1) & 1);
+    if (ring.loads1 > 0) tc::mbar_wait_warp(&sy.kv_full[2 + kv], (ring.loads1 - 1) & 1);
   };
 
   if (warp == kKeyWarp) {
@@ -237,7 +259,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     int r = t0 < t1 ? line.find(a, sy.plan, t0, &pre) : 0, u = 0;
     CacheChunkSplit split{};
     split.c1 = -1;
-    int sc = 0, qn = 0, n = 0;  // segments published, queries loaded, key blocks loaded
+    int sc = 0, qn = 0;  // segments published, queries loaded
+    Ring ring;
     bool ok = true;
     for (int64_t t = t0;; ++sc) {
       Segment g{};
@@ -305,7 +328,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // need not wait for the last product with the queries before
       const bool first = qn == 0;
       if (first) queries();
-      stream(g, 0, &mapK, n, [&] {
+      stream(g, 0, &mapK, ring, [&] {
         if (!first) queries();
       });
       ok = !*abort_flag;
@@ -317,19 +340,19 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       a.split[blockIdx.x] = split;
     }
     if (qn >= 1) tc::mbar_wait_warp(&sy.q_full, (qn - 1) & 1);
-    land(0, n);
+    land(0, ring);
   } else if (warp == kValueWarp) {
     // ------------------------------------------------------------ values
-    int n = 0;
+    Ring ring;
     for (int sc = 0; !*abort_flag; ++sc) {
       if (!tc::mbar_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1)) break;
       const Segment g = sy.seg[sc & 1];
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
       if (g.head < 0) break;
-      stream(g, 1, &mapV, n, [] {});
+      stream(g, 1, &mapV, ring, [] {});
     }
-    land(1, n);
+    land(1, ring);
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ MMA issuer
     // One elected lane issues (see elect_one), serving both slots in turn, which keeps their
@@ -361,8 +384,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           if (half * 4 + k < steps)
             tc::mma_bf16_ts(tO, tP + k * 8, dv + k * (2048 / 16), idO, (j > 0 || half > 0 || k > 0) ? 1u : 0u);
       };
-      uint32_t ph = 0;           // phase of the ring at the segment's current pair of blocks
-      uint32_t pb0 = 0, pb1 = 0; // phase of each slot's barriers at the segment's block 0
+      uint32_t ph0 = 0, ph1 = 0;  // phases of stages 0 and 1, and of 2 and 3, at the segment's block 0
+      uint32_t pb0 = 0, pb1 = 0;  // phase of each slot's barriers at the segment's block 0
 #pragma unroll 1
       for (int sc = 0; !bad; ++sc) {
         wait(&sy.seg_full[sc & 1], (sc >> 1) & 1, false);
@@ -373,17 +396,19 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         const int n0 = g.blocks(0), n1 = g.blocks(1), nm = max(n0, n1);
         const int last_steps = max(0, (min(kKB, g.seq - (g.j1 - 1) * kKB) + 15) >> 4);
         wait(&sy.q_full, sc & 1, false);
-        wait(&sy.kv_full[0], ph, false);
+        wait(&sy.kv_full[0], ph0, false);
         tc::fence_after_sync();
-        // Step -1 is S_0 of both slots alone. Step j, odd or even: V_j sits in stage 1 or 3, K_{j + 1} in
-        // stage 2 or 0, and the next step's blocks in the other two. One copy of a slot's products for
-        // both slots and either parity: four took more of the instruction cache than the roles'
-        // loops leave. p0, kv, kk: whether the first half of the next P and the next V and K were
-        // seen complete.
+        // Step -1 is S_0 of both slots alone. One copy of a slot's products for both slots and either
+        // parity of the step: four took more of the instruction cache than the roles' loops leave.
+        // And few commits: the thread stands still for most of one, longer than the two MMAs that the
+        // tensor core queues. p0, kv, kk: whether the first half of the next P and the next V and
+        // K were seen complete.
         bool p0 = false, kv = false, kk = false;
 #pragma unroll 1
         for (int j = -1; j < nm; ++j) {
-          const int odd = j & 1, sv = 1 + 2 * odd, sk = 2 - 2 * odd;
+          const int odd = j & 1;
+          const uint32_t turn = static_cast<uint32_t>(j) >> 1;  // of V_j's stage in this segment
+          const uint32_t pv = (odd ? ph1 : ph0) ^ (turn & 1), pk = (odd ? ph0 : ph1) ^ ((turn + odd) & 1);
           const int steps = j == nm - 1 ? last_steps : kKB / 16;
           const bool keys = j + 1 < nm;
 #pragma unroll 1
@@ -392,43 +417,43 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             if (j >= 0) {
               const uint32_t pp = odd ^ (s ? pb1 : pb0);
               if (s == 0 || n0 <= j) {  // the first group of the step: V_j and K_{j + 1}
-                wait(&sy.kv_full[sv], ph, kv);
-                if (keys) wait(&sy.kv_full[sk], ph ^ odd, kk);
+                wait(&sy.kv_full[2 * odd + 1], pv, kv);
+                if (keys) wait(&sy.kv_full[2 - 2 * odd], pk, kk);
               }
               wait(&sy.p_full[s][0], pp, p0);
               tc::fence_after_sync();
-              pv_mmas(s, j, sv, steps, 0);
-              const bool p1 = tc::mbar_test_wait(&sy.p_full[s][1], pp);
-              tc::mma_commit(&sy.pv_done[s][0]);
-              wait(&sy.p_full[s][1], pp, p1);
+              pv_mmas(s, j, 2 * odd + 1, steps, 0);
+              // a softmax that is still at the second half may have to wait for the first half's P V;
+              // where it is through, a plain arrival keeps the barrier's phase
+              if (tc::mbar_test_wait(&sy.p_full[s][1], pp)) {
+                tc::mbar_arrive(&sy.half_done[s]);
+              } else {
+                tc::mma_commit(&sy.half_done[s]);
+                wait(&sy.p_full[s][1], pp, false);
+              }
               tc::fence_after_sync();
-              pv_mmas(s, j, sv, steps, 1);
-              tc::mma_commit(&sy.pv_done[s][1]);
-              if (last) tc::mma_commit(&sy.kv_empty[sv]);
+              pv_mmas(s, j, 2 * odd + 1, steps, 1);
             }
-            if (more) s_mmas(s, sk);
+            if (more) s_mmas(s, 2 - 2 * odd);
             // the next group's barriers
-            const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
-            if (j >= 0) p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? odd ^ 1 : odd) ^ (s1 ? pb1 : pb0));
-            if (last && j >= 0) {
-              kv = tc::mbar_test_wait(&sy.kv_full[4 - sv], ph ^ odd);
-              kk = tc::mbar_test_wait(&sy.kv_full[2 - sk], ph ^ 1);
+            if (j >= 0) {
+              const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
+              p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? odd ^ 1 : odd) ^ (s1 ? pb1 : pb0));
+              if (last) {  // V_{j + 1} and K_{j + 2}, in the other two stages
+                kv = tc::mbar_test_wait(&sy.kv_full[3 - 2 * odd], pk);
+                kk = tc::mbar_test_wait(&sy.kv_full[2 * odd], pv ^ 1);
+              }
             }
             if (more) tc::mma_commit(&sy.s_full[s]);
-            if (last && keys) {  // the step's last group: K_{j + 1} has been read, by whom it had to be
-              tc::mma_commit(&sy.kv_empty[sk]);
+            else if (j >= 0) tc::mma_commit(&sy.o_done[s]);
+            if (last && keys) {
+              tc::mma_commit(&sy.kv_empty[odd]);
               if (j + 2 == nm) tc::mma_commit(&sy.q_empty);  // the segment's last S
             }
           }
-          if (j >= 0) ph ^= odd;
         }
-        if ((nm & 1) != 0) {  // the odd pair of stages, passed on
-          wait(&sy.kv_full[2], ph, false);
-          tc::mbar_arrive(&sy.kv_empty[2]);
-          wait(&sy.kv_full[3], ph, false);
-          tc::mbar_arrive(&sy.kv_empty[3]);
-          ph ^= 1;
-        }
+        ph0 ^= ((nm + 1) >> 1) & 1;
+        ph1 ^= (nm >> 1) & 1;
         pb0 ^= n0 & 1;
         pb1 ^= n1 & 1;
       }
@@ -448,7 +473,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     unsigned char* stage = sO + warp * kOutStage;
     const int tok_of_row = row / a.G, head_of_row = row - tok_of_row * a.G;
     bool ok = true;
-    int done = 0, turns = 0;  // blocks of this slot and turns of the ring in earlier segments
+    int done = 0, outs = 0;         // blocks of this slot, and segments that held some, so far
+    int loads0 = 0, loads1 = 0;     // blocks in the even and the odd stages in earlier segments
 #pragma unroll 1
     for (int sc = 0;; ++sc) {
       ok = tc::mbar_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1);
@@ -479,10 +505,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           // the request's keys end in this block: the values behind them that share the last
           // 16-key step are whatever the page held and are multiplied by P = 0; they are
           // cleared, so that nothing there (an infinity or a NaN) reaches a row
-          const int n = 2 * j + 1;
-          ok = tc::mbar_wait_warp(&sy.kv_full[n % kStages], (turns + n / kStages) & 1);
+          const int sb = 2 * (j & 1) + 1;
+          ok = tc::mbar_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
           if (!ok) break;
-          unsigned char* v = sKV + (n % kStages) * kTile;
+          unsigned char* v = sKV + sb * kTile;
           const int dead = ((valid + 15) & ~15) - valid;
           for (int e = lane; e < dead * 8 * (D / 64); e += 32) {
             const int ac = e / (dead * 8), w = e - ac * dead * 8;
@@ -534,8 +560,9 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
                 m = mb;
               }
               if (__any_sync(0xffffffffu, factor != 1.f)) {
-                // O is final up to the previous half once its P V is done
-                ok = tc::mbar_wait_warp(&sy.pv_done[slot][hf ^ 1], (done + j + hf + 1) & 1);
+                // O holds the blocks before (S came behind their P V) and, at the second half, the
+                // first once its P V is done
+                if (hf == 1) ok = tc::mbar_wait_warp(&sy.half_done[slot], (done + j) & 1);
                 if (!ok) break;
                 tc::fence_after_sync();
 #pragma unroll 1
@@ -579,10 +606,12 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
         if (!ok) break;
       }
-      if (ok && nblk > 0) ok = tc::mbar_wait_warp(&sy.pv_done[slot][1], (done + nblk - 1) & 1);
+      if (ok && nblk > 0) ok = tc::mbar_wait_warp(&sy.o_done[slot], outs & 1);
       if (!ok) break;
       done += nblk;
-      turns += (2 * max(g.blocks(0), g.blocks(1)) + kStages - 1) / kStages;
+      outs += nblk > 0 ? 1 : 0;
+      loads0 += (g.j1 - g.j0 + 1) >> 1;
+      loads1 += (g.j1 - g.j0) >> 1;
       if (!g.live(slot)) continue;
       tc::fence_after_sync();
       // ---- the segment's rows out. The next segment's S may run meanwhile; its P V, which
