@@ -18,6 +18,7 @@ struct CacheAttnDev {
   int64_t n_tokens, n_pages;
   int R, max_new, max_pages, Hq, Hkv, G, page_size;
   int box;           // rows of a TMA box: a power of two that divides the page size, at most a tile
+  int step_shift;    // see CachePlan
   int64_t few_rows;  // requests of at most this many rows a KV head are k_cache_attn's, the others k_cache_chunk's
   float c2;
   __nv_bfloat16* o;
@@ -47,22 +48,40 @@ struct CacheRequest {
   __device__ __forceinline__ int64_t rows(const CacheAttnDev& a) const { return static_cast<int64_t>(n) * a.G; }
 };
 
-// a / b of non-negative numbers, b > 0: in 32 bits where they fit, as they nearly always do. One copy
-// of it in a kernel, whose first pass over its code waits for instructions.
-static __device__ __noinline__ int64_t cache_div(int64_t a, int64_t b) {
-  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
-  return a / b;
+// The roles of a CTA share an instruction cache, which a second copy of their loops has cost more than
+// half of a kernel's speed, and a first pass over code waits for it. So what is not a role's inner
+// loop exists once a kernel: the waits (behind a first look), warp sums.
+static __device__ __noinline__ bool cache_wait_on(uint64_t* bar, uint32_t parity) { return tc::mbar_wait(bar, parity); }
+static __device__ __noinline__ bool cache_wait_warp_on(uint64_t* bar, uint32_t parity) {
+  return tc::mbar_wait_warp(bar, parity);
+}
+__device__ __forceinline__ bool cache_wait(uint64_t* bar, uint32_t parity) {
+  return tc::mbar_test_wait(bar, parity) || cache_wait_on(bar, parity);
+}
+__device__ __forceinline__ bool cache_wait_warp(uint64_t* bar, uint32_t parity) {
+  return __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity)) || cache_wait_warp_on(bar, parity);
+}
+// Inclusive sums over a warp.
+static __device__ __noinline__ int cache_scan(int x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
 }
 
-// A call's work as one line of steps, request by request, cut into equal runs. Every CTA forms the
-// cut for itself, its loading warp alone for up to 32 requests (a lane each), else all its threads
-// (NT of them, equal shares of the requests; pre[i] is the steps before thread i's share).
+// A call's work as one line of steps, request by request, cut into equal runs. A step is
+// 2^step_shift tiles of keys of a row block (0 but for calls whose bounds would let the line pass
+// 2^31 steps). Every CTA forms the cut for itself, its loading warp alone for up to 32 requests (a
+// lane each), else all its threads (NT of them, equal shares of the requests; pre[i] is the steps
+// before thread i's share).
 constexpr int kNearRequests = 32;
 template <int NT>
 struct CachePlan {
-  int64_t pre[NT + 1];
-  int64_t total;
-  int32_t most, ok;
+  int32_t pre[NT + 1];
+  int32_t total, most, ok;
 
   __device__ __forceinline__ static int share(const CacheAttnDev& a) { return (a.R + NT - 1) / NT; }
   // For more than kNearRequests requests, all threads: steps(request, most) gives a request's steps,
@@ -75,9 +94,9 @@ struct CachePlan {
       ok = 1;
     }
     __syncthreads();
-    int64_t sum = 0;
-    int longest = 1;
+    int sum = 0, longest = 1;
     bool fine = true;
+#pragma unroll 1
     for (int r = tid * each; r < min(a.R, (tid + 1) * each); ++r) {
       CacheRequest q;
       fine = q.load(a, r) && fine;
@@ -89,10 +108,11 @@ struct CachePlan {
     pre[tid + 1] = sum;
     __syncthreads();
     if (tid < 32) {
-      int64_t carry = 0;
+      int carry = 0;
       const int used = min(NT, a.R);  // threads with a share
+#pragma unroll 1
       for (int b = 0; b < used; b += 32) {
-        const int64_t x = scan(pre[b + lane + 1]) + carry;
+        const int x = cache_scan(pre[b + lane + 1]) + carry;
         pre[b + lane + 1] = x;
         carry = __shfl_sync(0xffffffffu, x, 31);
       }
@@ -103,22 +123,12 @@ struct CachePlan {
     }
     __syncthreads();
   }
-  // Inclusive sums over a warp.
-  __device__ __forceinline__ static int64_t scan(int64_t x) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    return x;
-  }
 };
 // The loading warp's view of the line.
 struct CacheLine {
-  int64_t total;  // 0 if validation refuses a length
-  int32_t most;   // steps of the longest row block (a row block's steps are one after the other on the line)
-  int64_t incl;   // up to kNearRequests requests: steps up to this lane's, its own included
+  int total;  // 0 if validation refuses a length
+  int most;   // steps of the longest row block (a row block's steps are one after the other on the line)
+  int incl;   // up to kNearRequests requests: steps up to this lane's, its own included
 
   template <int NT, class F>
   __device__ __forceinline__ CacheLine(const CacheAttnDev& a, const CachePlan<NT>& plan, const CacheRequest& mine,
@@ -130,17 +140,17 @@ struct CacheLine {
     } else {
       const int lane = threadIdx.x & 31;
       int longest = 1;
-      incl = CachePlan<NT>::scan(lane < a.R && mine_ok ? steps(mine, longest) : 0);
+      incl = cache_scan(lane < a.R && mine_ok ? steps(mine, longest) : 0);
       most = __reduce_max_sync(0xffffffffu, longest);
       total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
     }
   }
   // A request at or before that of step t, t < total, and the steps before it.
   template <int NT>
-  __device__ __forceinline__ int find(const CacheAttnDev& a, const CachePlan<NT>& plan, int64_t t, int64_t* before) const {
+  __device__ __forceinline__ int find(const CacheAttnDev& a, const CachePlan<NT>& plan, int t, int* before) const {
     if (a.R <= kNearRequests) {
       const int r = __popc(__ballot_sync(0xffffffffu, incl <= t));
-      const int64_t x = __shfl_sync(0xffffffffu, incl, r > 0 ? r - 1 : 0);
+      const int x = __shfl_sync(0xffffffffu, incl, r > 0 ? r - 1 : 0);
       *before = r > 0 ? x : 0;
       return r;
     }
@@ -158,19 +168,21 @@ struct CacheLine {
 // CTAs, fewer where a run would be shorter than `least` steps or a block would be in more than
 // kCacheMaxPieces pieces.
 struct CacheRuns {
-  int64_t total, each, longer;  // steps of a run, runs of one step more
-  int64_t N;
-  __device__ __forceinline__ CacheRuns(int64_t total_, int most, int least, int ctas) : total(total_) {
-    const int64_t run = max((most + kCacheMaxPieces - 3) / (kCacheMaxPieces - 2), least);
-    N = total >= run * ctas ? ctas : max(int64_t(1), cache_div(total, run));
-    each = cache_div(total, N);
+  int total, each, longer;  // steps of a run, runs of one step more
+  int N;
+  CacheRuns() = default;
+  __device__ __forceinline__ CacheRuns(int total_, int most, int least, int ctas) : total(total_) {
+    const int run = max((most + kCacheMaxPieces - 3) / (kCacheMaxPieces - 2), least);
+    N = max(1, min(ctas, static_cast<int>(static_cast<uint32_t>(total) / static_cast<uint32_t>(run))));
+    each = static_cast<uint32_t>(total) / static_cast<uint32_t>(N);
     longer = total - each * N;
   }
-  __device__ __forceinline__ int64_t begin(int64_t c) const { return c < N ? c * each + min(c, longer) : total; }
+  __device__ __forceinline__ int begin(int c) const { return c < N ? c * each + min(c, longer) : total; }
   // the run of step t
-  __device__ __forceinline__ int run(int64_t t) const {
-    const int64_t edge = longer * (each + 1);
-    return static_cast<int>(t < edge ? cache_div(t, each + 1) : longer + cache_div(t - edge, each));
+  __device__ __forceinline__ int run(int t) const {
+    const int edge = longer * (each + 1);
+    return t < edge ? static_cast<uint32_t>(t) / static_cast<uint32_t>(each + 1)
+                    : longer + static_cast<uint32_t>(t - edge) / static_cast<uint32_t>(each);
   }
 };
 // Where a run leaves a piece of a block: a block that began in an earlier run in its even place, one

@@ -154,6 +154,10 @@ __device__ __forceinline__ int tiles_of(const CacheAttnDev& a, const CacheReques
   return q.n == 0 || q.rows(a) > a.few_rows ? 0 : max(1, (q.seq - 1) / kCacheTile + 1);
 }
 
+__device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
+  return (tiles + (1 << a.step_shift) - 1) >> a.step_shift;
+}
+
 // mapK, mapV: the cache as {64 elements, row of the page, panel of 64, head, page}, box of `box` rows
 // and all panels of one head and page: one TMA instruction a page piece. (One a panel, at pages of 16
 // rows 16 of them a tile, issued too slowly: 4.4 TB/s.) kWM warps share the keys of a slice of the tile, 16
@@ -193,9 +197,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   pdl_trigger();
   __syncthreads();
   auto steps = [&](const CacheRequest& q, int& most) {
-    const int t = tiles_of(a, q);
+    const int t = steps_of(a, tiles_of(a, q));
     most = max(most, t);
-    return static_cast<int64_t>(t) * a.Hkv;
+    return t * a.Hkv;
   };
   if (a.R > kNearRequests) sh.plan.form(a, steps);
   volatile int* abort_flag = &sh.abort;
@@ -204,39 +208,41 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     // ------------------------------------------------------------ segments and loads
     const CacheLine line(a, sh.plan, mine, mine_ok, steps);
     const CacheRuns runs(line.total, line.most, 1, gridDim.x);
-    const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
+    const int t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
     const int per_tile = kCacheTile / a.box;
-    int64_t pre = 0;  // tiles before request r
+    int pre = 0;  // steps before request r
     int r = t0 < t1 ? line.find(a, sh.plan, t0, &pre) : 0;
     int n = 0, sc = 0;
     bool fine = true;
-    for (int64_t t = t0; fine; ++sc) {
+#pragma unroll 1
+    for (int t = t0; fine; ++sc) {
       Segment g{};
       g.head = -1;
-      int64_t end = t;
+      int end = t;
       if (t < t1) {
         CacheRequest q;
-        int tiles;
+        int tiles, len;  // tiles and steps of a row block
+#pragma unroll 1
         for (;; ++r) {
           q.load(a, r);
           tiles = tiles_of(a, q);
-          const int64_t len = static_cast<int64_t>(tiles) * a.Hkv;
-          if (t < pre + len) break;
-          pre += len;
+          len = steps_of(a, tiles);
+          if (t < pre + len * a.Hkv) break;
+          pre += len * a.Hkv;
         }
-        g.head = static_cast<int>(cache_div(t - pre, tiles));
-        const int64_t s = pre + static_cast<int64_t>(g.head) * tiles;  // the block's first step
-        end = min(t1, s + tiles);
+        g.head = static_cast<int>(static_cast<uint32_t>(t - pre) / static_cast<uint32_t>(len));
+        const int s = pre + g.head * len;  // the block's first step
+        end = min(t1, s + len);
         g.row0 = q.row0;
         g.n = q.n;
         g.seq = q.seq;
-        g.tile0 = static_cast<int>(t - s);
-        g.tile1 = static_cast<int>(end - s);
+        g.tile0 = (t - s) << a.step_shift;
+        g.tile1 = min(tiles, (end - s) << a.step_shift);
         g.c0 = t == s ? static_cast<int>(blockIdx.x) : runs.run(s);
-        g.c1 = end == s + tiles ? static_cast<int>(blockIdx.x) : runs.run(s + tiles - 1);
+        g.c1 = end == s + len ? static_cast<int>(blockIdx.x) : runs.run(s + len - 1);
         g.req = r;
       }
-      if (sc >= 2) fine = tc::mbar_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
+      if (sc >= 2) fine = cache_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
       if (!fine) break;
       if (lane == 0) {
         sh.seg[sc & 1] = g;
@@ -252,7 +258,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         const int keys = min(kCacheTile, g.seq - tile * kCacheTile);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
         if (tc::elect_one()) {
-          if (n >= kStages && !tc::mbar_wait(&sh.kv_empty[sb], (n / kStages - 1) & 1)) {
+          if (n >= kStages && !cache_wait(&sh.kv_empty[sb], (n / kStages - 1) & 1)) {
             *abort_flag = 1;
           } else {
             tc::mbar_arrive_expect_tx(&sh.kv_full[sb], boxes * a.box * D * 4);
@@ -275,7 +281,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     if (!fine && lane == 0) *abort_flag = 1;
     // let the copies in flight land before the CTA may exit
     for (int k = (n >= kStages ? n - kStages : 0); k < n; ++k)
-      tc::mbar_wait_warp(&sh.kv_full[k % kStages], (k / kStages) & 1);
+      cache_wait_warp(&sh.kv_full[k % kStages], (k / kStages) & 1);
   } else {
     // ------------------------------------------------------------ products, softmax, output
     const int wm = warp % kWM, slice = warp / kWM;
@@ -285,7 +291,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     bool waited = false;
     int n = 0;
     for (int sc = 0;; ++sc) {
-      if (!tc::mbar_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1)) *abort_flag = 1;
+      if (!cache_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1)) *abort_flag = 1;
       bar_consumers();
       if (*abort_flag) break;
       const Segment g = sh.seg[sc & 1];
@@ -320,7 +326,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 
       for (int tile = g.tile0; tile < g.tile1; ++tile, ++n) {
         const int sb = n % kStages;
-        if (!tc::mbar_wait_warp(&sh.kv_full[sb], (n / kStages) & 1)) {
+        if (!cache_wait_warp(&sh.kv_full[sb], (n / kStages) & 1)) {
           *abort_flag = 1;
           break;
         }
@@ -718,6 +724,13 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.chunk_o = ws_at<float>(ws, p.chunk_o);
   d.chunk_ml = ws_at<float2>(ws, p.chunk_ml);
   d.split = ws_at<CacheChunkSplit>(ws, p.split);
+  // steps of the longest line the bounds allow, below 2^31
+  auto shift = [&](int64_t blocks, int64_t tiles) {
+    int sft = 0;
+    while (static_cast<double>(blocks) * static_cast<double>((tiles >> sft) + 4) * c.n_kv_heads >= 2147483648.0) ++sft;
+    return sft;
+  };
+  const int64_t keys = static_cast<int64_t>(a.max_pages) * c.page_size;
   const int grid = device_sm_count();
   cudaError_t e = launch_kernel(k_cache_prep, dim3(1), dim3(kPrepThreads), 0, s, /*pdl=*/true, d, grid);
   if (e != cudaSuccess || a.n_tokens == 0) return e;
@@ -734,6 +747,7 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   CUtensorMap mk, mv, mq;
   if (sh.few) {
     d.box = box(kCacheTile);
+    d.step_shift = shift(a.n_requests, keys / kCacheTile);
     if (!rows_map(&mk, pk, c, d.box) || !rows_map(&mv, pv, c, d.box)) return cudaErrorInvalidValue;
     const int wm = sh.row_warps;
     auto launch = c.head_dim == 128
@@ -743,6 +757,7 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   }
   if (!sh.chunks) return cudaSuccess;
   d.box = box(2 * kCacheTile);
+  d.step_shift = shift(a.n_tokens / (2 * (kChunkRows / 2 / d.G)) + a.n_requests, keys / (2 * kCacheTile));
   if (!panel_map(&mk, pk, c, d.box) || !panel_map(&mv, pv, c, d.box) || !query_map(&mq, a, c.head_dim, d.G))
     return cudaErrorInvalidValue;
   return launch_cache_chunk(c.head_dim, grid, mq, mk, mv, d, s);

@@ -112,6 +112,29 @@ __device__ __forceinline__ int units_of(const CacheAttnDev& a, const CacheReques
   return q.rows(a) > a.few_rows ? (q.n + 2 * nt - 1) / (2 * nt) : 0;
 }
 
+// Behind the queries before (qn of them), a segment's, by one thread of the calling warp; false if the
+// wait gave up.
+template <int D>
+__device__ __noinline__ bool load_queries(const CUtensorMap* map, unsigned char* sQ, const Segment& g, int G, ChunkSync& sy,
+                                          int qn) {
+  bool ok = true;
+  if (tc::elect_one()) {
+    ok = qn == 0 || cache_wait(&sy.q_empty, (qn - 1) & 1);
+    if (ok) {
+      const int nq = g.live(1) ? 2 : 1;
+      tc::mbar_arrive_expect_tx(&sy.q_full, nq * (D / 64) * g.nt * G * 128);
+#pragma unroll 1
+      for (int i = 0; i < nq * (D / 64); ++i)
+        tc::tma_load_3d(sQ + i * kPanel, map, i % (D / 64) * 64, g.head * G, g.row0 + g.tok0(i / (D / 64)), &sy.q_full);
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
+__device__ __forceinline__ int steps_of(const CacheAttnDev& a, int blocks) {
+  return kUnitSteps + ((blocks + (1 << a.step_shift) - 1) >> a.step_shift);
+}
+
 // ---------------------------------------------------------------- attention
 // mapQ: q {d, Hq, T}, box 64 x G x floor(128 / G); mapK, mapV: the cache as
 // {d, row of the page, head, page}, box of 64 elements and `box` rows.
@@ -174,10 +197,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
 
   auto steps = [&](const CacheRequest& q, int& most) {
     const int U = units_of(a, q, nt);
-    int64_t sum = 0;
+    int sum = 0;
 #pragma unroll 1
-    for (int u = 0; u < U; ++u) sum += kUnitSteps + unit_blocks(q, nt, u);
-    if (U > 0) most = max(most, kUnitSteps + unit_blocks(q, nt, U - 1));
+    for (int u = 0; u < U; ++u) sum += steps_of(a, unit_blocks(q, nt, u));
+    if (U > 0) most = max(most, steps_of(a, unit_blocks(q, nt, U - 1)));
     return sum * a.Hkv;
   };
   if (a.R > kNearRequests) sy.plan.form(a, steps);
@@ -187,12 +210,134 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   // a step but the last, and kv_empty[1] once before, for K_0. The last values are released with the
   // segment's O. The copies of a segment's keys (kv = 0) or values; between(): called behind the
   // first block's copy.
-  struct Ring {
-    int fired0 = 0, fired1 = 0;    // completions of kv_empty[0] and [1] in the segments before
-    int outs0 = 0, outs1 = 0;      // of o_done[0] and [1]
-    int loads0 = 0, loads1 = 0;    // into the even and the odd blocks' stage
-    __device__ __forceinline__ void pass(const Segment& g) {
+  if (warp == kKeyWarp || warp == kValueWarp) {
+    // ------------------------------------------------------------ segments, queries, keys; values
+    const int kv = warp == kKeyWarp ? 0 : 1;
+    const CUtensorMap* map = kv ? &mapV : &mapK;
+    const int per_block = kKB / a.box;
+    int fired0 = 0, fired1 = 0;  // completions of kv_empty[0] and [1] in the segments before
+    int outs0 = 0, outs1 = 0;    // of o_done[0] and [1]
+    int loads0 = 0, loads1 = 0;  // into the even and the odd blocks' stage
+    int qn = 0;                  // queries loaded
+    bool ok = true;
+    int t = 0, t1 = 0, pre = 0;  // steps: next, the run's end, before unit u of request r
+    int r = 0, u = 0;
+    CacheRuns runs;
+    CacheChunkSplit split{};
+    split.c1 = -1;
+    if (kv == 0) {
+      const CacheLine line(a, sy.plan, mine, mine_ok, steps);
+      runs = CacheRuns(line.total, line.most, kUnitSteps + 1, gridDim.x);
+      t = runs.begin(blockIdx.x);
+      t1 = runs.begin(blockIdx.x + 1);
+      if (t < t1) r = line.find(a, sy.plan, t, &pre);
+    }
+#pragma unroll 1
+    for (int sc = 0;; ++sc) {
+      Segment g{};
+      if (kv == 0) {
+        g.head = -1;
+        int end = t;
+        if (t < t1) {
+          CacheRequest q;
+          int nb = 0, len = 0;  // key blocks and steps of the unit
+#pragma unroll 1
+          for (;; ++r, u = 0) {
+            q.load(a, r);
+            const int U = units_of(a, q, nt);
+#pragma unroll 1
+            for (; u < U; ++u) {
+              nb = unit_blocks(q, nt, u);
+              len = steps_of(a, nb);
+              if (t < pre + len * a.Hkv) break;
+              pre += len * a.Hkv;
+            }
+            if (u < U) break;
+          }
+          const int head = static_cast<int>(static_cast<uint32_t>(t - pre) / static_cast<uint32_t>(len));
+          const int s = pre + head * len;  // the unit's first step
+          end = min(t1, s + len);
+          // a run that ends in a unit's first steps leaves its blocks to the next
+          g.head = end > s + kUnitSteps ? head : -1;
+          g.row0 = q.row0;
+          g.n = q.n;
+          g.seq = q.seq;
+          g.nt = nt;
+          g.unit = u;
+          g.req = r;
+          g.j0 = max(0, t - s - kUnitSteps) << a.step_shift;
+          g.j1 = min(nb, (end - s - kUnitSteps) << a.step_shift);
+          const int me = static_cast<int>(blockIdx.x);
+          const int c0 = g.j0 == 0 ? me : runs.run(s + kUnitSteps);
+          const int c1 = end == s + len ? me : runs.run(s + len - 1);
+          g.place = c0 == c1 ? -1 : piece_place(me, g.j0 == 0);
+          if (g.head >= 0 && c0 < c1 && c0 == me) split = CacheChunkSplit{g.row0, g.n, g.head, g.unit, c0, c1};
+        }
+        t = end;
+        if (sc >= 2) ok = cache_wait_warp(&sy.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
+        if (!ok) break;
+        if (lane == 0) {
+          sy.seg[sc & 1] = g;
+          tc::mbar_arrive(&sy.seg_full[sc & 1]);
+        }
+        __syncwarp();
+      } else {
+        ok = cache_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1);
+        if (!ok) break;
+        g = sy.seg[sc & 1];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
+      }
+      if (g.head < 0) break;
+      // The ring. K_j and V_j of a segment lie in stages 2 (j % 2) and 2 (j % 2) + 1. The MMA thread
+      // releases V_j and K_{j + 1} together, behind the last product with either: kv_empty[j % 2],
+      // once a step but the last, and kv_empty[1] once before, for K_0. The last values are released
+      // with the segment's O.
+      const int32_t* row = a.table + g.req * a.table_stride;
       const int blocks = g.j1 - g.j0;
+      // the first queries wait for nothing; later ones come behind the segment's first keys, which
+      // need not wait for the last product with the queries before
+      if (kv == 0 && qn == 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
+#pragma unroll 1
+      for (int j = 0; j < blocks && !*abort_flag; ++j) {
+        const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
+        if (j == 0 || (i0 & 31) == 0)
+          if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
+        const int keys = min(kKB, g.seq - (g.j0 + j) * kKB);  // none: an empty cache
+        const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
+        // the stage's last occupant, block j - 2: V_{j - 2} is released in step j - 2, K_{j - 2} in
+        // step j - 3; before the first two keys, the last release of the segment before, before the
+        // first two values, its O
+        const int bar = (j & 1) ^ (kv ^ 1);
+        const int which = (bar ? fired1 : fired0) + (j < 2 ? -1 : (j >> 1) - 1 + (kv & bar));
+        if (tc::elect_one()) {
+          bool fine = true;
+          if (kv == 0 || j >= 2) {
+            fine = which < 0 || cache_wait(&sy.kv_empty[bar], which & 1);
+          } else if (j == 0) {
+            fine = (outs0 == 0 || cache_wait(&sy.o_done[0], (outs0 - 1) & 1)) &&
+                   (outs1 == 0 || cache_wait(&sy.o_done[1], (outs1 - 1) & 1));
+          }
+          if (!fine) {
+            *abort_flag = 1;
+          } else {
+            tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
+            unsigned char* dst = sKV + sb * kTile;
+#pragma unroll 1
+            for (int b = 0; b < boxes; ++b, dst += a.box * 128) {
+              const int2 at = sy.window[kv].at[(i0 + b) & 31];
+#pragma unroll
+              for (int p = 0; p < D / 64; ++p)
+                tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, &sy.kv_full[sb]);
+            }
+          }
+        }
+        __syncwarp();
+        if (kv == 0 && j == 0 && qn > 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
+      }
+      ok = ok && !*abort_flag;
+      if (!ok) break;
+      ++qn;
       fired0 += blocks >> 1;
       fired1 += 1 + ((blocks - 1) >> 1);
       outs0 += g.blocks(0) > 0 ? 1 : 0;
@@ -200,159 +345,14 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       loads0 += (blocks + 1) >> 1;
       loads1 += blocks >> 1;
     }
-  };
-  auto stream = [&](const Segment& g, int kv, const CUtensorMap* map, Ring& ring, auto between) {
-    const int32_t* row = a.table + g.req * a.table_stride;
-    const int per_block = kKB / a.box, blocks = g.j1 - g.j0;
-#pragma unroll 1
-    for (int j = 0; j < blocks && !*abort_flag; ++j) {
-      const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
-      if (j == 0 || (i0 & 31) == 0)
-        if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
-      const int keys = min(kKB, g.seq - (g.j0 + j) * kKB);  // none: an empty cache
-      const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
-      // the stage's last occupant, block j - 2: V_{j - 2} is released in step j - 2, K_{j - 2} in step
-      // j - 3; before the first two keys, the last release of the segment before, before the first
-      // two values, its O
-      const int bar = (j & 1) ^ (kv ? 0 : 1);
-      const int which = (bar ? ring.fired1 : ring.fired0) + (j < 2 ? -1 : (j >> 1) - 1 + (kv & bar));
-      if (tc::elect_one()) {
-        bool fine = true;
-        if (kv == 0 || j >= 2) {
-          fine = which < 0 || tc::mbar_wait(&sy.kv_empty[bar], which & 1);
-        } else if (j == 0) {
-          fine = (ring.outs0 == 0 || tc::mbar_wait(&sy.o_done[0], (ring.outs0 - 1) & 1)) &&
-                 (ring.outs1 == 0 || tc::mbar_wait(&sy.o_done[1], (ring.outs1 - 1) & 1));
-        }
-        if (!fine) {
-          *abort_flag = 1;
-        } else {
-          tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
-          unsigned char* dst = sKV + sb * kTile;
-#pragma unroll 1
-          for (int b = 0; b < boxes; ++b, dst += a.box * 128) {
-            const int2 at = sy.window[kv].at[(i0 + b) & 31];
-#pragma unroll
-            for (int p = 0; p < D / 64; ++p)
-              tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, &sy.kv_full[sb]);
-          }
-        }
-      }
-      __syncwarp();
-      if (j == 0) between();
-    }
-    ring.pass(g);
-  };
-
-  // let the copies in flight land before the CTA may exit
-  auto land = [&](int kv, const Ring& ring) {
-    if (ring.loads0 > 0) tc::mbar_wait_warp(&sy.kv_full[kv], (ring.loads0 - 1) & 1);
-    if (ring.loads1 > 0) tc::mbar_wait_warp(&sy.kv_full[2 + kv], (ring.loads1 - 1) & 1);
-  };
-
-  if (warp == kKeyWarp) {
-    // ------------------------------------------------------------ segments, queries and keys
-    const CacheLine line(a, sy.plan, mine, mine_ok, steps);
-    const CacheRuns runs(line.total, line.most, kUnitSteps + 1, gridDim.x);
-    const int64_t t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
-    int64_t pre = 0;  // steps before unit u of request r
-    int r = t0 < t1 ? line.find(a, sy.plan, t0, &pre) : 0, u = 0;
-    CacheChunkSplit split{};
-    split.c1 = -1;
-    int sc = 0, qn = 0;  // segments published, queries loaded
-    Ring ring;
-    bool ok = true;
-    for (int64_t t = t0;; ++sc) {
-      Segment g{};
-      g.head = -1;
-      int64_t end = t;
-      if (t < t1) {
-        CacheRequest q;
-        int nb = 0;
-        int64_t s = 0;  // the unit's first step
-        for (;; ++r, u = 0) {
-          q.load(a, r);
-          const int U = units_of(a, q, nt);
-#pragma unroll 1
-          for (; u < U; ++u) {
-            nb = unit_blocks(q, nt, u);
-            if (t < pre + static_cast<int64_t>(kUnitSteps + nb) * a.Hkv) break;
-            pre += static_cast<int64_t>(kUnitSteps + nb) * a.Hkv;
-          }
-          if (u < U) break;
-        }
-        const int head = static_cast<int>(cache_div(t - pre, kUnitSteps + nb));
-        s = pre + static_cast<int64_t>(head) * (kUnitSteps + nb);
-        end = min(t1, s + kUnitSteps + nb);
-        // a run that ends in a unit's first steps leaves its blocks to the next
-        g.head = end > s + kUnitSteps ? head : -1;
-        g.row0 = q.row0;
-        g.n = q.n;
-        g.seq = q.seq;
-        g.nt = nt;
-        g.unit = u;
-        g.req = r;
-        g.j0 = static_cast<int>(max(int64_t(0), t - s - kUnitSteps));
-        g.j1 = static_cast<int>(end - s - kUnitSteps);
-        const int me = static_cast<int>(blockIdx.x);
-        const int c0 = g.j0 == 0 ? me : runs.run(s + kUnitSteps), c1 = g.j1 == nb ? me : runs.run(s + kUnitSteps + nb - 1);
-        g.place = c0 == c1 ? -1 : piece_place(me, g.j0 == 0);
-        if (g.head >= 0 && c0 < c1 && c0 == me) split = CacheChunkSplit{g.row0, g.n, g.head, g.unit, c0, c1};
-      }
-      if (sc >= 2) ok = tc::mbar_wait_warp(&sy.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
-      if (!ok) break;
-      if (lane == 0) {
-        sy.seg[sc & 1] = g;
-        tc::mbar_arrive(&sy.seg_full[sc & 1]);
-      }
-      __syncwarp();
-      if (g.head < 0) break;
-      auto queries = [&]() {
-        if (tc::elect_one()) {
-          if (qn >= 1 && !tc::mbar_wait(&sy.q_empty, (qn - 1) & 1)) {
-            *abort_flag = 1;
-          } else {
-            const int nq = g.live(1) ? 2 : 1;
-            tc::mbar_arrive_expect_tx(&sy.q_full, nq * (D / 64) * nt * a.G * 128);
-#pragma unroll 1
-            for (int s = 0; s < nq; ++s)
-#pragma unroll 1
-              for (int ac = 0; ac < D / 64; ++ac)
-                tc::tma_load_3d(sQ + s * kTile + ac * kPanel, &mapQ, ac * 64, g.head * a.G, g.row0 + g.tok0(s), &sy.q_full);
-          }
-        }
-        ++qn;
-        __syncwarp();
-      };
-      // the first queries wait for nothing; later ones come behind the segment's first keys, which
-      // need not wait for the last product with the queries before
-      const bool first = qn == 0;
-      if (first) queries();
-      stream(g, 0, &mapK, ring, [&] {
-        if (!first) queries();
-      });
-      ok = !*abort_flag;
-      if (!ok) break;
-      t = end;
-    }
     if (lane == 0) {
       if (!ok) *abort_flag = 1;
-      a.split[blockIdx.x] = split;
+      if (kv == 0) a.split[blockIdx.x] = split;
     }
-    if (qn >= 1) tc::mbar_wait_warp(&sy.q_full, (qn - 1) & 1);
-    land(0, ring);
-  } else if (warp == kValueWarp) {
-    // ------------------------------------------------------------ values
-    Ring ring;
-    for (int sc = 0; !*abort_flag; ++sc) {
-      if (!tc::mbar_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1)) break;
-      const Segment g = sy.seg[sc & 1];
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
-      if (g.head < 0) break;
-      stream(g, 1, &mapV, ring, [] {});
-    }
-    land(1, ring);
+    // let the copies in flight land before the CTA may exit
+    if (kv == 0 && qn > 0) cache_wait_warp(&sy.q_full, (qn - 1) & 1);
+    if (loads0 > 0) cache_wait_warp(&sy.kv_full[kv], (loads0 - 1) & 1);
+    if (loads1 > 0) cache_wait_warp(&sy.kv_full[2 + kv], (loads1 - 1) & 1);
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ MMA issuer
     // One elected lane issues (see elect_one), serving both slots in turn, which keeps their
@@ -364,7 +364,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       const uint32_t q_base = tc::smem_u32(sQ), kv_base = tc::smem_u32(sKV);
       bool bad = false;
       auto wait = [&](uint64_t* bar, uint32_t parity, bool seen) {
-        if (!seen && !bad) bad = !tc::mbar_wait(bar, parity);
+        if (!seen && !bad) bad = !cache_wait(bar, parity);
       };
       auto s_mmas = [&](int s, int stage) {
         const uint64_t dq = tc::desc_k_sw128(q_base + s * kTile), dk = tc::desc_k_sw128(kv_base + stage * kTile);
@@ -460,7 +460,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       if (bad) *abort_flag = 1;
       // every MMA issued has completed once this arrives
       tc::mma_commit(&sy.drain);
-      tc::mbar_wait(&sy.drain, 0);
+      cache_wait(&sy.drain, 0);
     }
   } else {
     // ------------------------------------------------------------ softmax and output (warps 0-7)
@@ -477,7 +477,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     int loads0 = 0, loads1 = 0;     // blocks in the even and the odd stages in earlier segments
 #pragma unroll 1
     for (int sc = 0;; ++sc) {
-      ok = tc::mbar_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1);
+      ok = cache_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1);
       if (!ok) break;
       const Segment g = sy.seg[sc & 1];
       __syncwarp();
@@ -494,19 +494,19 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // taken twice, cost 1400 cycles a segment; beginning at 0, sharp queries moved it too often).
       float m = 0.f, l = 0.f;
       for (int j = 0; j < nblk; ++j) {
-        ok = tc::mbar_wait_warp(&sy.s_full[slot], (done + j) & 1);
+        ok = cache_wait_warp(&sy.s_full[slot], (done + j) & 1);
         if (!ok) break;
         tc::fence_after_sync();
         const int key0 = (g.j0 + j) * kKB;
         const bool masked = key0 + kKB > all_see;
         const int seen = limit - key0;  // of the block's keys
         const int valid = g.seq - key0;
-        if (quad == 0 && valid < kKB && valid > 0) {
+        if (masked && quad == 0 && valid < kKB && valid > 0) {
           // the request's keys end in this block: the values behind them that share the last
           // 16-key step are whatever the page held and are multiplied by P = 0; they are
           // cleared, so that nothing there (an infinity or a NaN) reaches a row
           const int sb = 2 * (j & 1) + 1;
-          ok = tc::mbar_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
+          ok = cache_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
           if (!ok) break;
           unsigned char* v = sKV + sb * kTile;
           const int dead = ((valid + 15) & ~15) - valid;
@@ -516,68 +516,30 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           }
           tc::fence_proxy_async();
         }
-// One copy of the load, the maximum and the exponentials, for both halves and for a half that is
-// started again: the kernel's roles share an instruction cache that their loops fill.
-#pragma unroll 1
+#pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          uint32_t su[64];  // the row's logits of a half
+          uint32_t su[64];  // the row's logits of this half
           uint32_t pk[32];
-          float sum = 0.f, mb = -INFINITY;
-          // The segment's first half gives the reference it begins with. Later a half takes none: only
-          // values far above the reference or, as yet, all far below it, or a NaN, make the warp take
-          // the maximum of what is left of the block and start the half again (its logits are in TMEM).
-          bool scan = j == 0 && hf == 0, again = false;
-          int half = hf;
-#pragma unroll 1
-          for (;;) {
+          auto load = [&](int half) {
             tc::tmem_ld64_async(tS + half * 64, su);
             tc::tmem_wait64(su);
             if (masked) {
 #pragma unroll
               for (int c = 0; c < 64; ++c) su[c] = (half * 64 + c < seen) ? su[c] : 0xff800000u;
             }
-            if (scan) {
-              float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          };
+          auto row_max = [&]() {
+            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-              for (int c = 0; c < 64; c += 8) {
+            for (int c = 0; c < 64; c += 8) {
 #pragma unroll
-                for (int w = 0; w < 4; ++w)
-                  t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
-              }
-              mb = fmaxf(mb, fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2);  // -inf when nothing is visible
-              if (half > hf) {
-                half = hf;
-                continue;
-              }
-              scan = false;
-              float factor = 1.f;
-              // A reference moves down before a row's first term alone, so nothing was lost to underflow
-              // (l = 0, and O is zero or not yet written); behind that l stays above kLeastSum, but for
-              // a half whose block's maximum, then the reference, is in the other half.
-              if (mb > m + kRescaleTau || (l < kLeastSum && mb != -INFINITY)) {
-                factor = l > 0.f ? tc::ex2(m - mb) : 1.f;
-                l *= factor;
-                m = mb;
-              }
-              if (__any_sync(0xffffffffu, factor != 1.f)) {
-                // O holds the blocks before (S came behind their P V) and, at the second half, the
-                // first once its P V is done
-                if (hf == 1) ok = tc::mbar_wait_warp(&sy.half_done[slot], (done + j) & 1);
-                if (!ok) break;
-                tc::fence_after_sync();
-#pragma unroll 1
-                for (int oc = 0; oc < D; oc += 32) {
-                  uint32_t ov[32];
-                  tc::tmem_ld32_async(tO + oc, ov);
-                  tc::tmem_wait(ov);
-#pragma unroll
-                  for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
-                  tc::tmem_st32(tO + oc, ov);
-                }
-                tc::tmem_wait_st();
-              }
+              for (int w = 0; w < 4; ++w)
+                t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
             }
-            // P of the half against the reference m, and its sum
+            return fmaxf(tc::max3(t[0], t[1], t[2]), t[3]);
+          };
+          // P of the half against the reference m, and its sum
+          auto exps = [&]() {
             const float2 nn = make_float2(-m, -m);
             float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
 #pragma unroll
@@ -590,13 +552,50 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
               pk[c / 2] = tc::pack_bf16x2(p0, p1);
               pk[c / 2 + 1] = tc::pack_bf16x2(p2, p3);
             }
-            sum = (acc0.x + acc0.y) + (acc1.x + acc1.y);
-            if (again || !__any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum))) break;
-            again = scan = true;
-            mb = -INFINITY;
-            half = 1;
+            return (acc0.x + acc0.y) + (acc1.x + acc1.y);
+          };
+          load(hf);
+          if (hf == 0 && j == 0) {
+            const float mb = row_max() * c2;
+            m = mb == -INFINITY ? 0.f : mb;
           }
-          if (!ok) break;
+          float sum = exps();
+          // values far above the reference or, as yet, all far below it, or a NaN: take the maximum
+          // of what is left of the block as the reference and start the half again (its logits
+          // are in TMEM)
+          if (__any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum))) {
+            float mb = -INFINITY;  // stays so when nothing is visible
+#pragma unroll 1
+            for (int half = 1; half >= hf; --half) {
+              load(half);
+              mb = fmaxf(mb, row_max() * c2);
+            }
+            float factor = 1.f;
+            // A reference moves down before a row's first term alone, so nothing was lost to underflow
+            // (l = 0, and O is zero or not yet written); behind that l stays above kLeastSum, but for
+            // a half whose block's maximum, then the reference, is in the other half.
+            if (mb > m + kRescaleTau || (l < kLeastSum && mb != -INFINITY)) {
+              factor = l > 0.f ? tc::ex2(m - mb) : 1.f;
+              l *= factor;
+              m = mb;
+            }
+            if (__any_sync(0xffffffffu, factor != 1.f)) {
+              if (hf == 1) ok = cache_wait_warp(&sy.half_done[slot], (done + j) & 1);
+              if (!ok) break;
+              tc::fence_after_sync();
+#pragma unroll 1
+              for (int oc = 0; oc < D; oc += 32) {
+                uint32_t ov[32];
+                tc::tmem_ld32_async(tO + oc, ov);
+                tc::tmem_wait(ov);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
+                tc::tmem_st32(tO + oc, ov);
+              }
+              tc::tmem_wait_st();
+            }
+            sum = exps();
+          }
           l += sum;
           tc::tmem_st32(tS + hf * 32, pk);
           tc::tmem_wait_st();
@@ -606,7 +605,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
         if (!ok) break;
       }
-      if (ok && nblk > 0) ok = tc::mbar_wait_warp(&sy.o_done[slot], outs & 1);
+      if (ok && nblk > 0) ok = cache_wait_warp(&sy.o_done[slot], outs & 1);
       if (!ok) break;
       done += nblk;
       outs += nblk > 0 ? 1 : 0;
