@@ -733,6 +733,28 @@ def _block_table(where: str, t: torch.Tensor, n_requests: int) -> Tuple[int, int
     return t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
+class _CacheCall:
+    """A prepared call of one entry point: what ``run`` passes is made once, so that a step's call costs
+    the C call and little else (2 us of 6 for a small one)."""
+
+    def _prepare(self, name: str, workspace: torch.Tensor, *structs) -> None:
+        self.workspace = workspace
+        self._name = name
+        self._fn = getattr(load(), name)
+        self._device = workspace.device.index
+        self._args = tuple(ctypes.byref(x) for x in structs) + (
+            c_void_p(_ptr(workspace)), c_size_t(workspace.numel() * workspace.element_size()))
+
+    def run(self, stream=None):
+        """Launches the prepared call on ``stream`` (default: the current one); returns self."""
+        if torch._C._cuda_getDevice() != self._device:
+            raise ValueError(f"{self._name}: prepared for device {self._device}, the current device is another")
+        code = self._fn(*self._args, _stream(stream))
+        if code != OK:
+            raise AVTPError(code, self._name)
+        return self
+
+
 @dataclass
 class PagedCache:
     """One layer's keys and values in pages: bf16 [n_pages, page_size, Hkv, head_dim], the last
@@ -774,7 +796,7 @@ class PagedCache:
         return _Cache(_ptr(self.k), _ptr(self.v), n, p, h, d, *strides(self.k), *strides(self.v))
 
 
-class CacheSlotsCall:
+class CacheSlotsCall(_CacheCall):
     """A prepared avtp_cache_slots call: block-table entries, slots and lengths of a step's new
     tokens from ``cu_new`` (int32 [R+1], for example ``out_cu_seqlens`` of a prune) and the cached
     tokens ``past_len`` (int32 [R], default none). New pages come from ``free_pages`` (int32), from
@@ -810,12 +832,7 @@ class CacheSlotsCall:
             _check(load().avtp_cache_slots_workspace_size(ctypes.byref(self._a), ctypes.byref(n)),
                    "avtp_cache_slots_workspace_size")
             workspace = new_workspace(int(n.value), dev)
-        self.workspace = workspace
-
-    def run(self, stream=None) -> "CacheSlotsCall":
-        _check(load().avtp_cache_slots(ctypes.byref(self._a), _ptr(self.workspace), self.workspace.numel(),
-                                       _stream(stream)), "avtp_cache_slots")
-        return self
+        self._prepare("avtp_cache_slots", workspace, self._a)
 
 
 def cache_slots(cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages: int, block_table: torch.Tensor,
@@ -827,7 +844,7 @@ def cache_slots(cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages:
     return c.slot_map, c.seq_len, c.free_head_out
 
 
-class CacheWriteCall:
+class CacheWriteCall(_CacheCall):
     """A prepared avtp_cache_write call: row ``kept_idx[j]`` (default j) of ``k`` and ``v`` (bf16
     [n_rows, Hkv, head_dim]) to slot ``slot_map[j]`` of the cache, -1 for none."""
 
@@ -851,12 +868,8 @@ class CacheWriteCall:
         self._c = cache.c()
         self._a = _CacheWriteArgs(_ptr(k), _ptr(v), k.stride(0) if k.shape[0] > 1 else h * d,
                                   v.stride(0) if v.shape[0] > 1 else h * d, k.shape[0], _ptr(kept_idx), _ptr(slot_map), n)
-        self.workspace = workspace if workspace is not None else new_workspace(256, dev)
-
-    def run(self, stream=None) -> "CacheWriteCall":
-        _check(load().avtp_cache_write(ctypes.byref(self._c), ctypes.byref(self._a), _ptr(self.workspace),
-                                       self.workspace.numel(), _stream(stream)), "avtp_cache_write")
-        return self
+        self._prepare("avtp_cache_write", workspace if workspace is not None else new_workspace(256, dev), self._c,
+                      self._a)
 
 
 def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, kept_idx=None,
@@ -865,7 +878,7 @@ def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: t
     CacheWriteCall(cache, slot_map, k, v, kept_idx=kept_idx, workspace=workspace).run(stream)
 
 
-class CacheAttentionCall:
+class CacheAttentionCall(_CacheCall):
     """A prepared avtp_cache_attention call: causal attention of a step's new tokens ``q`` (bf16 [T,
     Hq, head_dim], request r's rows ``cu_new[r] .. cu_new[r+1]``, at most ``max_new`` of them) over
     the cache, where each request has ``seq_len[r]`` tokens, the new ones among them. ``o`` (bf16, as
@@ -907,12 +920,7 @@ class CacheAttentionCall:
             _check(load().avtp_cache_attention_workspace_size(ctypes.byref(self._c), ctypes.byref(self._a),
                                                               ctypes.byref(n)), "avtp_cache_attention_workspace_size")
             workspace = new_workspace(int(n.value), dev)
-        self.workspace = workspace
-
-    def run(self, stream=None) -> "CacheAttentionCall":
-        _check(load().avtp_cache_attention(ctypes.byref(self._c), ctypes.byref(self._a), _ptr(self.workspace),
-                                           self.workspace.numel(), _stream(stream)), "avtp_cache_attention")
-        return self
+        self._prepare("avtp_cache_attention", workspace, self._c, self._a)
 
 
 def cache_attention(cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,

@@ -19,6 +19,7 @@ struct CacheAttnDev {
   int R, max_new, max_pages, Hq, Hkv, G, page_size;
   int box;           // rows of a TMA box: a power of two that divides the page size, at most a tile
   int step_shift;    // see CachePlan
+  int both;          // both kernels are at work and share the SMs (see cache_ctas)
   int64_t few_rows;  // requests of at most this many rows a KV head are k_cache_attn's, the others k_cache_chunk's
   float c2;
   __nv_bfloat16* o;
@@ -61,6 +62,28 @@ __device__ __forceinline__ bool cache_wait(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ bool cache_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity)) || cache_wait_warp_on(bar, parity);
 }
+// What a request costs k_cache_attn (x) and k_cache_chunk (y), in units of about 0.15 us of an SM: a tile
+// of 64 keys 3 while the other SMs are not all streaming, a block of 128 keys of a unit, or its
+// beginning, 10. Clamped so that the sum over the requests is a 32-bit number.
+__device__ __forceinline__ int2 cache_weights(const CacheAttnDev& a, const CacheRequest& q) {
+  const int64_t most = 0x7fffffff / a.R;
+  if (q.rows(a) <= a.few_rows) return make_int2(static_cast<int>(min(most, int64_t(3) * a.Hkv * ((q.seq + 63) / 64))), 0);
+  const int rows = 2 * (kChunkRows / 2 / a.G);
+  const int64_t units = static_cast<int64_t>((q.n + rows - 1) / rows) * a.Hkv;
+  return make_int2(0, static_cast<int>(min(most, 10 * units * (2 + max(0, q.seq - q.n / 2) / 128))));
+}
+// The CTAs that work in k_cache_attn (`few`) or k_cache_chunk, of the grid's. The first is bound by
+// memory, the second by the tensor cores, and a CTA of either fills an SM: where a call needs both
+// they share the SMs by their work, and the second kernel's CTAs start on those that the first
+// leaves. (One behind the other: two chunks of 450 tokens beside 22 single tokens 77 us.)
+__device__ __forceinline__ int cache_ctas(const CacheAttnDev& a, int2 w, bool few) {
+  const int grid = static_cast<int>(gridDim.x);
+  if (!a.both || w.x == 0 || w.y == 0) return grid;
+  const float part = static_cast<float>(w.x) / (static_cast<float>(w.x) + static_cast<float>(w.y));
+  const int n = max(1, min(grid - 1, static_cast<int>(part * grid + 0.5f)));
+  return few ? n : grid - n;
+}
+
 // Inclusive sums over a warp.
 static __device__ __noinline__ int cache_scan(int x) {
   const int lane = threadIdx.x & 31;
@@ -82,6 +105,7 @@ template <int NT>
 struct CachePlan {
   int32_t pre[NT + 1];
   int32_t total, most, ok;
+  int32_t few, chunk;  // summed cache_weights
 
   __device__ __forceinline__ static int share(const CacheAttnDev& a) { return (a.R + NT - 1) / NT; }
   // For more than kNearRequests requests, all threads: steps(request, most) gives a request's steps,
@@ -92,6 +116,7 @@ struct CachePlan {
     if (tid == 0) {
       most = 1;
       ok = 1;
+      few = chunk = 0;
     }
     __syncthreads();
     int sum = 0, longest = 1;
@@ -100,7 +125,14 @@ struct CachePlan {
     for (int r = tid * each; r < min(a.R, (tid + 1) * each); ++r) {
       CacheRequest q;
       fine = q.load(a, r) && fine;
-      if (fine) sum += steps(q, longest);
+      if (fine) {
+        sum += steps(q, longest);
+        if (a.both) {
+          const int2 w = cache_weights(a, q);
+          atomicAdd(&few, w.x);
+          atomicAdd(&chunk, w.y);
+        }
+      }
     }
     if (!fine) ok = 0;
     longest = __reduce_max_sync(0xffffffffu, longest);
@@ -129,6 +161,7 @@ struct CacheLine {
   int total;  // 0 if validation refuses a length
   int most;   // steps of the longest row block (a row block's steps are one after the other on the line)
   int incl;   // up to kNearRequests requests: steps up to this lane's, its own included
+  int2 weights;
 
   template <int NT, class F>
   __device__ __forceinline__ CacheLine(const CacheAttnDev& a, const CachePlan<NT>& plan, const CacheRequest& mine,
@@ -137,12 +170,18 @@ struct CacheLine {
       total = plan.ok ? plan.total : 0;
       most = plan.most;
       incl = 0;
+      weights = make_int2(plan.few, plan.chunk);
     } else {
       const int lane = threadIdx.x & 31;
       int longest = 1;
       incl = cache_scan(lane < a.R && mine_ok ? steps(mine, longest) : 0);
       most = __reduce_max_sync(0xffffffffu, longest);
       total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
+      weights = make_int2(0, 0);
+      if (a.both) {
+        const int2 w = lane < a.R && mine_ok ? cache_weights(a, mine) : make_int2(0, 0);
+        weights = make_int2(__reduce_add_sync(0xffffffffu, w.x), __reduce_add_sync(0xffffffffu, w.y));
+      }
     }
   }
   // A request at or before that of step t, t < total, and the steps before it.

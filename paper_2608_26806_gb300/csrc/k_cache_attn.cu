@@ -207,7 +207,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   if (warp == kLoadWarp) {
     // ------------------------------------------------------------ segments and loads
     const CacheLine line(a, sh.plan, mine, mine_ok, steps);
-    const CacheRuns runs(line.total, line.most, 1, gridDim.x);
+    const CacheRuns runs(line.total, line.most, 1, cache_ctas(a, line.weights, true));
     const int t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
     const int per_tile = kCacheTile / a.box;
     int pre = 0;  // steps before request r
@@ -712,6 +712,7 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.G = a.n_q_heads / c.n_kv_heads;
   d.page_size = c.page_size;
   d.few_rows = sh.few_rows;
+  d.both = sh.few && sh.chunks ? 1 : 0;
   d.c2 = a.softmax_scale * kLog2e;
   d.o = static_cast<__nv_bfloat16*>(a.o);
   d.o_stride = a.o_stride;

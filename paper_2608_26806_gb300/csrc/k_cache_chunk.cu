@@ -227,7 +227,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     split.c1 = -1;
     if (kv == 0) {
       const CacheLine line(a, sy.plan, mine, mine_ok, steps);
-      runs = CacheRuns(line.total, line.most, kUnitSteps + 1, gridDim.x);
+      runs = CacheRuns(line.total, line.most, kUnitSteps + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
       if (t < t1) r = line.find(a, sy.plan, t, &pre);

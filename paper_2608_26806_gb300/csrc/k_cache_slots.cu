@@ -9,7 +9,9 @@
 // One CTA checks everything before anything is written (offsets, lengths, the free list's end and
 // every page that will be used), so a refused call changes nothing. It keeps past_r and first_r
 // in the workspace: seq_len and free_head_out may be past_len and free_head themselves. Up to
-// kOneCtaTokens tokens the same CTA writes the maps; beyond, a second kernel over the whole GPU.
+// kOneCtaTokens tokens the same CTA writes the maps; beyond, a second kernel over the whole GPU. What
+// bounds either is latency, a chain of dependent loads: a step of 8 requests 4.1 us a call, of 256
+// 4.6; 5815 tokens 7.8 us in one CTA and 6.1 in two kernels, 15938 17.3 and 6.6, 142331 7.9.
 #include "avtp_cache.cuh"
 
 namespace avtp {
@@ -19,6 +21,8 @@ constexpr int kThreads = 1024;
 constexpr int kMapThreads = 256;
 constexpr int64_t kOneCtaTokens = 8192;
 
+constexpr int kStaged = 1024;  // requests whose lengths fit into shared memory
+
 struct SlotsDev {
   avtp_cache_slots_args_t a;
   DevStatus* st;
@@ -26,53 +30,56 @@ struct SlotsDev {
   int32_t* first;
 };
 
+// Per request: offset, cached tokens, entry of its first new page in the free list. In shared memory
+// for up to kStaged requests: a token's request is then found by ten quick loads, not ten trips to L2.
+struct Lengths {
+  const int32_t *cu, *past, *first;
+};
+
 __device__ __forceinline__ int64_t ceil_div(int64_t x, int64_t p) { return (x + p - 1) / p; }
 
-// New pages of request r into its table row; the lanes of a group of n threads share them.
-__device__ __forceinline__ void write_pages(const SlotsDev& d, int r, int lane, int n) {
-  const int64_t past = d.past[r], len = past + d.a.cu_new[r + 1] - d.a.cu_new[r];
-  const int64_t have = ceil_div(past, d.a.page_size), need = ceil_div(len, d.a.page_size);
-  int32_t* row = d.a.block_table + r * d.a.table_stride;
-  const int32_t* src = d.a.free_pages + d.first[r];
-  for (int64_t j = have + lane; j < need; j += n) row[j] = src[j - have];
+// New pages k, k + step, ... of `total`, from entry `head` of the free list on. (Page by page, not
+// request by request: a step brings 256 requests a page or none each, a prefill eight of them hundreds.)
+__device__ __forceinline__ void write_pages(const SlotsDev& d, const Lengths& l, int64_t head, int64_t total, int64_t k,
+                                            int64_t step) {
+  for (; k < total; k += step) {
+    const int r = upper_index(l.first, d.a.n_requests, head + k);
+    const int64_t have = ceil_div(l.past[r], d.a.page_size);
+    d.a.block_table[r * d.a.table_stride + have + head + k - l.first[r]] = d.a.free_pages[head + k];
+  }
 }
 
-// The slot of token t, which belongs to request r. New pages are read from the free list (their
-// table entries may be another thread's to write).
-__device__ __forceinline__ int32_t slot_of(const SlotsDev& d, int r, int64_t t) {
-  const int64_t past = d.past[r];
-  const int64_t pos = past + t - d.a.cu_new[r];
-  const int32_t page = static_cast<int32_t>(pos / d.a.page_size);
-  const int32_t have = static_cast<int32_t>(ceil_div(past, d.a.page_size));
-  const int32_t id = page < have ? d.a.block_table[r * d.a.table_stride + page] : d.a.free_pages[d.first[r] + page - have];
-  return id * d.a.page_size + static_cast<int32_t>(pos - static_cast<int64_t>(page) * d.a.page_size);
-}
-
-// Slots of tokens t, t + step, ... A thread's requests only go up, so it searches for the first
-// and walks to the next.
-__device__ void write_slots(const SlotsDev& d, int64_t t, int64_t step) {
-  const int R = d.a.n_requests;
-  const int64_t live = d.a.cu_new[R];
+// Slots of tokens t, t + step, ... New pages are read from the free list (their table entries may
+// be another thread's to write).
+__device__ __forceinline__ void write_slots(const SlotsDev& d, const Lengths& l, int64_t t, int64_t step) {
+  const int R = d.a.n_requests, P = d.a.page_size;
+  const int64_t live = l.cu[R];
   int r = -1;
   for (; t < d.a.n_tokens; t += step) {
     if (t >= live) {
       d.a.slot_map[t] = -1;
       continue;
     }
-    if (r < 0 || t >= d.a.cu_new[r + 1]) r = upper_index(d.a.cu_new, R, t);
-    d.a.slot_map[t] = slot_of(d, r, t);
+    if (r < 0 || t >= l.cu[r + 1]) r = upper_index(l.cu, R, t);
+    // a request's length is a 32-bit number
+    const uint32_t past = l.past[r], pos = past + static_cast<uint32_t>(t - l.cu[r]);
+    const uint32_t page = pos / P, have = (past + P - 1u) / P;
+    const int32_t id = page < have ? d.a.block_table[r * d.a.table_stride + page] : d.a.free_pages[l.first[r] + page - have];
+    d.a.slot_map[t] = id * P + static_cast<int32_t>(pos - page * P);
   }
 }
 
 __global__ void __launch_bounds__(kThreads) k_cache_slots(SlotsDev d, int write_all) {
   __shared__ int s_err, s_detail;
   __shared__ int64_t s_warp[32], s_carry;
+  __shared__ int32_t s_cu[kStaged + 1], s_past[kStaged], s_first[kStaged];
   pdl_wait();
   pdl_trigger();
   const avtp_cache_slots_args_t& a = d.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int R = a.n_requests;
   const int64_t P = a.page_size;
+  const bool staged = R <= kStaged;
   const int64_t head = a.free_head != nullptr ? *a.free_head : 0;
   if (tid == 0) {
     s_err = (head < 0 || a.cu_new[0] != 0) ? 1 : 0;
@@ -113,8 +120,17 @@ __global__ void __launch_bounds__(kThreads) k_cache_slots(SlotsDev d, int write_
     if (r < R) {
       // below n_free (checked before it is used), which is below 2^31
       const int64_t first = head + before + incl - take;
-      d.past[r] = static_cast<int32_t>(past);
-      d.first[r] = static_cast<int32_t>(first < a.n_free ? first : a.n_free);
+      const int32_t f = static_cast<int32_t>(first < a.n_free ? first : a.n_free);
+      if (staged) {
+        s_cu[r] = a.cu_new[r];
+        s_past[r] = static_cast<int32_t>(past);
+        s_first[r] = f;
+        if (r == R - 1) s_cu[R] = a.cu_new[R];
+      }
+      if (!staged || !write_all) {
+        d.past[r] = static_cast<int32_t>(past);
+        d.first[r] = f;
+      }
     }
     __syncthreads();
     if (tid == kThreads - 1) s_carry = before + incl;
@@ -124,10 +140,16 @@ __global__ void __launch_bounds__(kThreads) k_cache_slots(SlotsDev d, int write_
   if (tid == 0 && head + total > a.n_free) fail(R);
   __syncthreads();
   if (!s_err) {
-    for (int64_t j = tid; j < total; j += kThreads) {
-      const int32_t id = a.free_pages[head + j];
-      if (id < 0 || id >= a.n_pages) fail(R);
+    // eight loads at a time: 8900 pages one after the other had taken 3 us
+    bool bad = false;
+    for (int64_t j0 = tid; j0 < total; j0 += 8 * kThreads) {
+      int32_t id[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) id[i] = j0 + i * kThreads < total ? a.free_pages[head + j0 + i * kThreads] : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) bad = bad || id[i] < 0 || id[i] >= a.n_pages;
     }
+    if (bad) fail(R);
   }
   __syncthreads();
   const bool ok = s_err == 0;
@@ -136,22 +158,39 @@ __global__ void __launch_bounds__(kThreads) k_cache_slots(SlotsDev d, int write_
     if (ok && a.free_head_out != nullptr) *a.free_head_out = static_cast<int32_t>(head + total);
   }
   if (!ok) return;
-  for (int r = tid; r < R; r += kThreads)
-    a.seq_len[r] = d.past[r] + a.cu_new[r + 1] - a.cu_new[r];
+  const Lengths l = staged ? Lengths{s_cu, s_past, s_first} : Lengths{a.cu_new, d.past, d.first};
+  for (int r = tid; r < R; r += kThreads) a.seq_len[r] = l.past[r] + l.cu[r + 1] - l.cu[r];
   if (!write_all) return;
-  for (int r = warp; r < R; r += kThreads / 32) write_pages(d, r, lane, 32);
-  write_slots(d, tid, kThreads);
+  write_pages(d, l, head, total, tid, kThreads);
+  write_slots(d, l, tid, kThreads);
 }
 
+// The maps of a call whose lengths k_cache_slots has checked.
 __global__ void __launch_bounds__(kMapThreads) k_cache_slots_map(SlotsDev d) {
+  __shared__ int32_t s_cu[kStaged + 1], s_past[kStaged], s_first[kStaged];
+  const int R = d.a.n_requests;
+  const bool staged = R <= kStaged;
+  if (staged)  // an input: it need not wait for the kernel ahead
+    for (int i = threadIdx.x; i <= R; i += kMapThreads) s_cu[i] = d.a.cu_new[i];
   pdl_wait();
   pdl_trigger();
   if (!d.st->layout_ok) return;
+  if (staged) {
+    for (int i = threadIdx.x; i < R; i += kMapThreads) {
+      s_past[i] = d.past[i];
+      s_first[i] = d.first[i];
+    }
+    __syncthreads();
+  }
+  const Lengths l = staged ? Lengths{s_cu, s_past, s_first} : Lengths{d.a.cu_new, d.past, d.first};
   const int64_t at = static_cast<int64_t>(blockIdx.x) * kMapThreads + threadIdx.x;
   const int64_t threads = static_cast<int64_t>(gridDim.x) * kMapThreads;
-  for (int64_t r = at >> 5; r < d.a.n_requests; r += threads >> 5)
-    write_pages(d, static_cast<int>(r), threadIdx.x & 31, 32);
-  write_slots(d, at, threads);
+  const int64_t head = l.first[0];
+  // the last request's pages end the list's part
+  const int64_t past = l.past[R - 1], len = past + l.cu[R] - l.cu[R - 1];
+  const int64_t total = l.first[R - 1] + ceil_div(len, d.a.page_size) - ceil_div(past, d.a.page_size) - head;
+  write_pages(d, l, head, total, at, threads);
+  write_slots(d, l, at, threads);
 }
 
 }  // namespace

@@ -52,8 +52,9 @@ SLOT_CASES = {
     "mixed": ([5, 300, 16, 15, 17], [0, 1, 16, 17, 300], 16),
     "page_of_one": ([3, 0], [4, 2], 1),
     "odd_page": ([100, 3], [29, 41], 7),
-    "one_cta_most": ([0, 11], [8000, 192], 32),
-    "two_kernels": ([0, 11, 5], [8000, 192, 1], 32),
+    "one_cta_most": ([0, 11], [1900, 148], 32),
+    "two_kernels": ([0, 11, 5], [1900, 148, 1], 32),
+    "two_kernels_more": ([0, 11, 5], [8000, 192, 1], 32),
     "large": ([0, 11, 5, 0, 1000], [40000, 0, 3, 9000, 777], 48),
 }
 
@@ -73,7 +74,7 @@ def test_slots_match_the_plain_form(name):
     assert np.array_equal(dev["past"].cpu().numpy(), c["past"])
 
 
-@pytest.mark.parametrize("R", [1, 31, 1023, 1024, 1025, 3000])
+@pytest.mark.parametrize("R", [1, 31, 1024, 1025, 2048, 2049, 3000])
 def test_slots_of_many_requests(R):
     rng = np.random.default_rng(R)
     c = _slots_case(rng.integers(0, 90, R), rng.integers(0, 12, R), 16, seed=R)
