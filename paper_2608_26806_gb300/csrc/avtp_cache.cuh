@@ -24,9 +24,12 @@ cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_arg
 constexpr int kCacheTile = 64;        // keys of a tile of k_cache_attn
 constexpr int kCacheMaxPieces = 32;   // pieces that a row block's keys are split into, at most
 constexpr int kChunkRows = 256;       // rows of a unit of k_cache_chunk, two slots of 128
-// Requests of at most this many rows a KV head are k_cache_attn's, when no request of the call has
-// more; beside larger ones (max_new is the call's bound) those of at most kCacheFewMixed.
-constexpr int kCacheFewRows = 64;
+// Requests of at most kCacheFewRows rows a KV head are k_cache_attn's, when no request of the call can
+// have more; beside larger ones (max_new is the call's bound) those of at most kCacheFewMixed, one
+// warp's. Sixteen requests of 700-4000 tokens, four heads a group, us a call there and in
+// k_cache_chunk: 20 rows 34.9 / 41.7, 32 rows 37.6 / 42.1, 36 rows (by four warps a slice of keys) 49.0 /
+// 42.4, 64 rows 55.4 / 42.8.
+constexpr int kCacheFewRows = 32;
 constexpr int kCacheFewMixed = 16;
 
 // A unit of k_cache_chunk in several pieces, for the kernel that joins them; c1 < c0: none.

@@ -163,6 +163,7 @@ struct CacheLine {
   int incl;   // up to kNearRequests requests: steps up to this lane's, its own included
   int2 weights;
 
+  CacheLine() = default;
   template <int NT, class F>
   __device__ __forceinline__ CacheLine(const CacheAttnDev& a, const CachePlan<NT>& plan, const CacheRequest& mine,
                                        bool mine_ok, F steps) {
@@ -183,6 +184,18 @@ struct CacheLine {
         weights = make_int2(__reduce_add_sync(0xffffffffu, w.x), __reduce_add_sync(0xffffffffu, w.y));
       }
     }
+  }
+  // Request r, by the whole warp: of up to kNearRequests a lane holds it (a load takes 800 cycles).
+  __device__ __forceinline__ CacheRequest request(const CacheAttnDev& a, const CacheRequest& mine, int r) const {
+    CacheRequest q;
+    if (a.R <= kNearRequests) {
+      q.row0 = __shfl_sync(0xffffffffu, mine.row0, r);
+      q.n = __shfl_sync(0xffffffffu, mine.n, r);
+      q.seq = __shfl_sync(0xffffffffu, mine.seq, r);
+    } else {
+      q.load(a, r);
+    }
+    return q;
   }
   // A request at or before that of step t, t < total, and the steps before it.
   template <int NT>

@@ -56,9 +56,8 @@ static_assert(kChunkRows == 2 * kQT, "two slots a unit");
 
 __host__ __device__ constexpr uint32_t tile_bytes(int d) { return static_cast<uint32_t>(kQT) * d * 2; }
 constexpr uint32_t kPanel = kQT * 128;
-constexpr uint32_t kOutStage = 32 * 64;  // a warp's 32 rows x 32 columns of O on their way out
 __host__ __device__ constexpr size_t chunk_smem_bytes(int d) {
-  const size_t need = 1024 + static_cast<size_t>(2 + kStages) * tile_bytes(d) + 2 * kSlotWarps * kOutStage;
+  const size_t need = 1024 + static_cast<size_t>(2 + kStages) * tile_bytes(d);
   // more than half the SM's shared memory, so that no second CTA (and its 512 TMEM columns)
   // shares an SM
   return need > 116 * 1024 ? need : 116 * 1024;
@@ -149,7 +148,6 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   constexpr uint32_t kTile = tile_bytes(D);
   unsigned char* sQ = smem;                   // slot s at sQ + s * kTile
   unsigned char* sKV = smem + 2 * kTile;      // stage b at sKV + b * kTile
-  unsigned char* sO = sKV + kStages * kTile;  // warp w at sO + w * kOutStage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int nt = kQT / a.G;
 
@@ -178,7 +176,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     tc::tmem_alloc(&sy.tmem, kTmemCols);
     tc::tmem_relinquish();
   }
-  CacheRequest mine;  // a lane's request of a call of few: on its way while the barriers are made
+  CacheRequest mine{};  // a lane's request of a call of few: on its way while the barriers are made
   bool mine_ok = true;
   if (warp == kKeyWarp && lane < a.R) mine_ok = mine.load(a, lane);
   // the rows behind a slot's nt * G, which no box writes: zeros
@@ -191,7 +189,6 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
-  pdl_trigger();
   const uint32_t tmem = sy.tmem;
   volatile int* abort_flag = &sy.abort;
 
@@ -223,10 +220,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     int t = 0, t1 = 0, pre = 0;  // steps: next, the run's end, before unit u of request r
     int r = 0, u = 0;
     CacheRuns runs;
+    CacheLine line;
     CacheChunkSplit split{};
     split.c1 = -1;
     if (kv == 0) {
-      const CacheLine line(a, sy.plan, mine, mine_ok, steps);
+      line = CacheLine(a, sy.plan, mine, mine_ok, steps);
       runs = CacheRuns(line.total, line.most, kUnitSteps + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
@@ -243,7 +241,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           int nb = 0, len = 0;  // key blocks and steps of the unit
 #pragma unroll 1
           for (;; ++r, u = 0) {
-            q.load(a, r);
+            q = line.request(a, mine, r);
             const int U = units_of(a, q, nt);
 #pragma unroll 1
             for (; u < U; ++u) {
@@ -470,7 +468,6 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     const uint32_t tS = tl + kSCol + slot * 128, tO = tl + kOCol + slot * 128;
     const float c2 = a.c2;
     const float2 cc = make_float2(c2, c2);
-    unsigned char* stage = sO + warp * kOutStage;
     const int tok_of_row = row / a.G, head_of_row = row - tok_of_row * a.G;
     bool ok = true;
     int done = 0, outs = 0;         // blocks of this slot, and segments that held some, so far
@@ -631,36 +628,22 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
         continue;
       }
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      // a lane stores its own row, 16 bytes at a time: through shared memory, whole lines at a time, took
+      // twice as long, nearly all of it waiting for that code's instructions
+      const float inv = 1.f / l;
+      const uint32_t sees = l == 0.f ? 0u : 0xffffffffu;  // a row that sees nothing is zero whatever its accumulator holds
       const int64_t t = static_cast<int64_t>(g.row0) + tok;
       const int head = g.head * a.G + head_of_row;
-      const int64_t at = live ? t * a.o_stride + static_cast<int64_t>(head) * D : -1;
       if (live && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (m + log2f(l)) * kLn2;
-      // 32 columns at a time through this warp's stage, 16-byte pieces in the 64-byte swizzle; four
-      // lanes then store a row's 64 bytes
+      uint4* out = reinterpret_cast<uint4*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D);
 #pragma unroll 1
-      for (int oc = 0; oc < D; oc += 32) {
+      for (int oc = 0; oc < D; oc += 32, out += 4) {
         float v[32];
         tc::tmem_ld32(tO + oc, v);
-        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          uint4 w;
-          // a row that sees nothing is zero whatever its accumulator holds
-          auto two = [&](int c) { return l == 0.f ? 0u : tc::pack_bf16x2(v[c] * inv, v[c + 1] * inv); };
-          w.x = two(8 * i);
-          w.y = two(8 * i + 2);
-          w.z = two(8 * i + 4);
-          w.w = two(8 * i + 6);
-          *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) = w;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int rr = 8 * i + (lane >> 2), piece = lane & 3;
-          const int64_t to = __shfl_sync(0xffffffffu, at, rr);
-          const uint4 w = *reinterpret_cast<const uint4*>(stage + rr * 64 + ((piece ^ ((rr >> 1) & 3)) << 4));
-          if (to >= 0) *reinterpret_cast<uint4*>(a.o + to + oc + piece * 8) = w;
+          auto two = [&](int c) { return tc::pack_bf16x2(v[8 * i + c] * inv, v[8 * i + c + 1] * inv) & sees; };
+          if (live) out[i] = make_uint4(two(0), two(2), two(4), two(6));
         }
       }
     }
@@ -672,6 +655,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, kTmemCols);
   }
+  // only now: a grid waiting to start beside this one costs it 3 %
+  pdl_trigger();
   pdl_wait();  // this grid's end implies the validation kernel's, which resets the status word
   if (threadIdx.x == 0) {
     if (sy.abort) record_error(a.st, AVTP_ERR_TIMEOUT, static_cast<int32_t>(blockIdx.x));
