@@ -42,7 +42,7 @@ struct CacheAttnWs {
   size_t status;    // DevStatus
   size_t count;     // int32 [grid]: pieces done of the row block whose first piece is the CTA's last
   size_t part_o;    // float [2 * grid][rows][d]: a piece's O, not yet divided by its sum
-  size_t part_ml;   // float2 [2 * grid][rows]: a piece's reference and sum (log2 units)
+  size_t part_ml;   // float4 [2 * grid][rows]: a piece's reference (log2 units), sum of P, of its rounded values
   // of k_cache_chunk, when max_new allows a request for it
   size_t chunk_o;   // float4 [2 * grid][2 slots][d / 4][128 rows]
   size_t chunk_ml;  // float2 [2 * grid][2 slots][128 rows]

@@ -29,7 +29,7 @@ struct CacheAttnDev {
   DevStatus* st;
   int32_t* count;        // see CacheAttnWs
   float* part_o;
-  float2* part_ml;
+  float4* part_ml;
   float* chunk_o;
   float2* chunk_ml;
   CacheChunkSplit* split;

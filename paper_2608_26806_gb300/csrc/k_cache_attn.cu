@@ -14,11 +14,14 @@
 // leaves a piece (O, reference, sum) in the workspace; the CTA that finishes a block's last
 // piece joins them, in their order, so results do not depend on who came last.
 //
-// Per tile and warp: S = Q K^T on the warp's 64 / (4 / kWM) keys and 16 rows, the running
-// maximum m and sum l of exp2(c2 S - m) per row in registers, P in bf16 straight from S's
-// registers as the A operand of P V. Rows' values are summed over the four warps' keys at the end
-// of a row block. m, l and O are fp32; P is rounded to bf16 as the tensor core takes it (2^-9 of
-// a weight, averaged over the keys), O once at the end.
+// Per tile and warp: S = Q K^T on the warp's 64 / (4 / kWM) keys and 16 rows, P = exp2(c2 S - m)
+// against the row's reference m, in bf16 straight from S's registers as the A operand of P V, and
+// the sum l of P. The warps' shares meet at the end of a row block. m, l and O are fp32. P is
+// rounded to bf16 for its product (2^-9 of a weight), O once at the end; O is divided by the sum of
+// the rounded P, which one more product with a column of ones gives, so that a row that one key
+// dominates loses nothing to the rounding (error of O against 64 bits, 2-norm, one request of 3425
+// tokens with some sharp queries: 2.5e-3 divided by l, 1.9e-3 so; 1.6e-3 is O's own rounding), and the
+// LSE takes l.
 //
 // Warps 0-3 compute, warp 4 loads. Every wait is bounded; a CTA whose wait gives up records
 // AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and their
@@ -70,7 +73,7 @@ struct Shared {
   Segment seg[2];
   CachePlan<kThreads> plan;
   CacheWindow window;
-  float m[4][16], l[4][16];
+  float m[4][16], l[4][16], w[4][16];  // reference, sum of P, of its rounded values
   int32_t last;
   int abort, bad_page;
 };
@@ -136,14 +139,13 @@ __device__ __forceinline__ float quad_sum(float x) {
 
 // A row's result, four columns a lane: O divided by its sum and rounded, and the LSE.
 template <int D>
-__device__ __forceinline__ void store_row(const CacheAttnDev& a, const Segment& g, int row, int col, float4 v, float m, float l) {
+__device__ __forceinline__ void store_row(const CacheAttnDev& a, const Segment& g, int row, int col, float4 v, float m, float l,
+                                          float w) {
   const int tok = row / a.G, head = g.head * a.G + (row - tok * a.G);
   const int64_t t = static_cast<int64_t>(g.row0) + tok;
-  const float inv = l == 0.f ? 0.f : 1.f / l;  // no key visible: zeros
-  uint2 w;
-  w.x = tc::pack_bf16x2(v.x * inv, v.y * inv);
-  w.y = tc::pack_bf16x2(v.z * inv, v.w * inv);
-  *reinterpret_cast<uint2*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D + col) = w;
+  const float inv = w == 0.f ? 0.f : 1.f / w;  // no key visible: zeros
+  const uint2 x = make_uint2(tc::pack_bf16x2(v.x * inv, v.y * inv), tc::pack_bf16x2(v.z * inv, v.w * inv));
+  *reinterpret_cast<uint2*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D + col) = x;
   if (col == 0 && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (m + log2f(l)) * kLn2;
 }
 
@@ -319,6 +321,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       const int all_see = g.seq - g.n + 1;  // keys that every row sees
 
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      float rs[4] = {0.f, 0.f, 0.f, 0.f};  // P times ones: rows gr and gr + 8 in rs[0] and rs[2]
       float o[D / 8][4];
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -414,6 +417,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
                 m[i] = mb;
               }
               l[i] *= f2[i];
+              rs[2 * i] *= f2[i];
+              rs[2 * i + 1] *= f2[i];
             }
 #pragma unroll
             for (int i = 0; i < D / 8; ++i) {
@@ -448,6 +453,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
               mma_16816(o[2 * c], p[kk], f[c][0], f[c][1]);
               mma_16816(o[2 * c + 1], p[kk], f[c][2], f[c][3]);
             }
+            mma_16816(rs, p[kk], 0x3f803f80u, 0x3f803f80u);
           }
         }
         __syncwarp();
@@ -467,6 +473,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         if (tq == 0) {
           sh.m[warp][gr + 8 * i] = m[i];
           sh.l[warp][gr + 8 * i] = sum;
+          sh.w[warp][gr + 8 * i] = rs[2 * i];
         }
       }
       bar_consumers();
@@ -480,7 +487,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         float M = -INFINITY;
 #pragma unroll
         for (int s = 0; s < kSlices; ++s) M = fmaxf(M, sh.m[s * kWM + w][rr]);
-        float L = 0.f;
+        float L = 0.f, W = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int s = 0; s < kSlices; ++s) {
@@ -488,17 +495,18 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           const float f = ms == -INFINITY ? 0.f : tc::ex2(ms - M);
           const float4 x = *reinterpret_cast<const float4*>(s_out + ((s * kWM + w) * 16 + rr) * out_row(D) + col);
           L += f * sh.l[s * kWM + w][rr];
+          W += f * sh.w[s * kWM + w][rr];
           v.x = fmaf(f, x.x, v.x);
           v.y = fmaf(f, x.y, v.y);
           v.z = fmaf(f, x.z, v.z);
           v.w = fmaf(f, x.w, v.w);
         }
         if (pieces == 1) {
-          store_row<D>(a, g, row, col, v, M, L);
+          store_row<D>(a, g, row, col, v, M, L, W);
         } else {
           const int64_t at = static_cast<int64_t>(piece_place(blockIdx.x, g.tile0 == 0)) * kRows + row;
           __stcg(reinterpret_cast<float4*>(a.part_o + at * D + col), v);
-          if (sub == 0) __stcg(a.part_ml + at, make_float2(M, L));
+          if (sub == 0) __stcg(a.part_ml + at, make_float4(M, L, W, 0.f));
         }
       }
       if (pieces == 1) continue;
@@ -519,24 +527,24 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       // code costs more than its loads.)
       constexpr int P = kWM == 1 ? 8 : 2, N = kWM == 1 ? 1 : 4;
       for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
-        float M[N], L[N];
+        float M[N], L[N], W[N];
         float4 v[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           M[i] = -INFINITY;
-          L[i] = 0.f;
+          L[i] = W[i] = 0.f;
           v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
 #pragma unroll 1
         for (int k0 = 0; k0 < pieces; k0 += P) {
-          float2 ml[N][P];
+          float4 ml[N][P];
           float4 x[N][P];
 #pragma unroll
           for (int k = 0; k < P; ++k) {
             const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-              ml[i][k] = make_float2(-INFINITY, 0.f);
+              ml[i][k] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
               x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
               if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
                 ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
@@ -552,11 +560,13 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
             const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
             M[i] = mn;
             L[i] *= old;
+            W[i] *= old;
             v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
 #pragma unroll
             for (int k = 0; k < P; ++k) {
               const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
               L[i] = fmaf(f, ml[i][k].y, L[i]);
+              W[i] = fmaf(f, ml[i][k].z, W[i]);
               v[i].x = fmaf(f, x[i][k].x, v[i].x);
               v[i].y = fmaf(f, x[i][k].y, v[i].y);
               v[i].z = fmaf(f, x[i][k].z, v[i].z);
@@ -566,7 +576,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         }
 #pragma unroll
         for (int i = 0; i < N; ++i)
-          if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i]);
+          if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
       }
     }
   }
@@ -677,7 +687,7 @@ CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_ar
   if (sh.few) {
     const size_t rows = 16 * static_cast<size_t>(sh.row_warps);
     p.part_o = take(2 * grid * rows * d * 4);
-    p.part_ml = take(2 * grid * rows * 8);
+    p.part_ml = take(2 * grid * rows * 16);
   }
   if (sh.chunks) {
     p.chunk_o = take(2 * grid * kChunkRows * d * 4);
@@ -717,7 +727,7 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.st = ws_at<DevStatus>(ws, p.status);
   d.count = ws_at<int32_t>(ws, p.count);
   d.part_o = ws_at<float>(ws, p.part_o);
-  d.part_ml = ws_at<float2>(ws, p.part_ml);
+  d.part_ml = ws_at<float4>(ws, p.part_ml);
   d.chunk_o = ws_at<float>(ws, p.chunk_o);
   d.chunk_ml = ws_at<float2>(ws, p.chunk_ml);
   d.split = ws_at<CacheChunkSplit>(ws, p.split);

@@ -74,11 +74,14 @@ class Batch:
         """O and LSE of every row against 64 bits.
 
         Bounds, per element, with A = sum_u p_u |v_u| (p the 64-bit probabilities), n the keys of the
-        row and S the largest sum |q_i k_i| scale of it: P is rounded to bf16 (2^-8 of each weight,
-        so 2^-8 A), O is (2^-8 |O| <= 2^-8 A of the rounded sum); a logit is d fp32 products and
-        sums, off by at most e = (d + 4) 2^-24 S, times 2 in a ratio of exponentials; the
-        exponential itself 2^-22, twice; sums of n terms n 2^-24, twice. ln(sum) is off by e, the sum's
-        relative error, and three roundings of numbers no larger than |lse| + S + ln n.
+        row and S the largest sum |q_i k_i| scale of it. P is rounded to bf16, each weight off by
+        d_u, |d_u| <= 2^-8. Divided by the sum of the exact weights, O is off by sum p_u d_u v_u, at
+        most 2^-8 A; divided by the sum of the rounded ones, by sum p_u d_u (v_u - O) to first order,
+        at most 2^-8 (A + |O|). O's own rounding adds 2^-8 |O|. Second order: a factor 1 + 2^-7. A
+        logit is d fp32 products and sums, off by at most e = (d + 4) 2^-24 S, times 2 in a ratio of
+        exponentials; the exponential itself 2^-22, twice; sums of n terms n 2^-24, twice. ln(sum) is
+        off by e, the sum's relative error, and three roundings of numbers no larger than |lse| + S +
+        ln n.
         """
         scale = scale if scale is not None else self.d ** -0.5
         o, lse = o.float().cpu().double(), None if lse is None else lse.cpu().double()
@@ -103,7 +106,8 @@ class Batch:
             A = torch.einsum("nhgs,shd->nhgd", p, v.abs()).reshape(n, self.Hq, self.d)
             e = (self.d + 4) * 2.0 ** -24 * S.reshape(n, self.Hq)
             cnt = seen.double()[:, None]
-            tol = A * (2.0 ** -7 * (1 + 2.0 ** -7) + (2 * e + 2.0 ** -21 + 2 * cnt * 2.0 ** -24)[..., None])
+            tol = (2.0 ** -8 * (1 + 2.0 ** -7) * (A + 2 * want.abs())
+                   + A * (2 * e + 2.0 ** -21 + 2 * cnt * 2.0 ** -24)[..., None])
             got = o[a:a + n]
             assert torch.isfinite(got).all(), f"request {r}: not finite"
             off = (got - want).abs() - tol
