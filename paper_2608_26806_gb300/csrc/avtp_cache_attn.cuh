@@ -62,20 +62,21 @@ __device__ __forceinline__ bool cache_wait(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ bool cache_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity)) || cache_wait_warp_on(bar, parity);
 }
-// What a request costs k_cache_attn (x) and k_cache_chunk (y), in units of about 0.15 us of an SM: a tile
-// of 64 keys 3 while the other SMs are not all streaming, a block of 128 keys of a unit, or its
-// beginning, 10. Clamped so that the sum over the requests is a 32-bit number.
+// What a request costs k_cache_attn (x) and k_cache_chunk (y), in units of about 0.07 us of an SM: a tile
+// of 64 keys 7, a block of 128 keys of a unit, or its beginning, 20 (a tile 6, 8 or 10: two chunks
+// beside 22 single tokens 70, 65, 66 us, one of 2048 beside 63 255, 255, 289, one of 100 beside 63
+// 270, 293, 369). Clamped so that the sum over the requests is a 32-bit number.
 __device__ __forceinline__ int2 cache_weights(const CacheAttnDev& a, const CacheRequest& q) {
   const int64_t most = 0x7fffffff / a.R;
-  if (q.rows(a) <= a.few_rows) return make_int2(static_cast<int>(min(most, int64_t(3) * a.Hkv * ((q.seq + 63) / 64))), 0);
+  if (q.rows(a) <= a.few_rows) return make_int2(static_cast<int>(min(most, int64_t(7) * a.Hkv * ((q.seq + 63) / 64))), 0);
   const int rows = 2 * (kChunkRows / 2 / a.G);
   const int64_t units = static_cast<int64_t>((q.n + rows - 1) / rows) * a.Hkv;
-  return make_int2(0, static_cast<int>(min(most, 10 * units * (2 + max(0, q.seq - q.n / 2) / 128))));
+  return make_int2(0, static_cast<int>(min(most, 20 * units * (2 + max(0, q.seq - q.n / 2) / 128))));
 }
 // The CTAs that work in k_cache_attn (`few`) or k_cache_chunk, of the grid's. The first is bound by
 // memory, the second by the tensor cores, and a CTA of either fills an SM: where a call needs both
 // they share the SMs by their work, and the second kernel's CTAs start on those that the first
-// leaves. (One behind the other: two chunks of 450 tokens beside 22 single tokens 77 us.)
+// leaves. (One behind the other, each on all SMs: 74, 292 and 293 us for the three above.)
 __device__ __forceinline__ int cache_ctas(const CacheAttnDev& a, int2 w, bool few) {
   const int grid = static_cast<int>(gridDim.x);
   if (!a.both || w.x == 0 || w.y == 0) return grid;
