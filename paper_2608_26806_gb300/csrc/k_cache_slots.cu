@@ -19,9 +19,9 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kMapThreads = 256;
-constexpr int64_t kOneCtaTokens = 8192;
+constexpr int64_t kOneCtaTokens = 2048;
 
-constexpr int kStaged = 1024;  // requests whose lengths fit into shared memory
+constexpr int kStaged = 2048;  // requests whose lengths fit into shared memory
 
 struct SlotsDev {
   avtp_cache_slots_args_t a;
@@ -31,7 +31,7 @@ struct SlotsDev {
 };
 
 // Per request: offset, cached tokens, entry of its first new page in the free list. In shared memory
-// for up to kStaged requests: a token's request is then found by ten quick loads, not ten trips to L2.
+// for up to kStaged requests: a token's request is then found by eleven quick loads, not eleven trips to L2.
 struct Lengths {
   const int32_t *cu, *past, *first;
 };
