@@ -79,6 +79,9 @@ avtp_status_t check_attn(const avtp_cache_t* c, const avtp_cache_attn_args_t* a)
     return AVTP_ERR_UNSUPPORTED;
   // rows of a KV head, and new tokens beside cached ones, are 32-bit numbers
   if (static_cast<int64_t>(a->max_new) * (a->n_q_heads / c->n_kv_heads) > kInt32Max) return AVTP_ERR_RANGE;
+  // so are the blocks of rows that the requests may have, with a few steps each (see CachePlan)
+  const int64_t slot = kChunkRows / 2 / (a->n_q_heads / c->n_kv_heads);
+  if (a->n_requests + a->n_tokens / (2 * slot) > (int64_t(1) << 27) / c->n_kv_heads) return AVTP_ERR_RANGE;
   if (a->cu_new == nullptr || a->seq_len == nullptr || a->block_table == nullptr) return AVTP_ERR_INVALID_ARG;
   if (a->n_tokens > 0 && (a->q == nullptr || a->o == nullptr)) return AVTP_ERR_INVALID_ARG;
   if (a->table_stride < a->max_pages) return AVTP_ERR_INVALID_ARG;

@@ -35,6 +35,9 @@ struct CacheAttnDev {
   CacheChunkSplit* split;
 };
 
+// A request's keys, at most: positions up to a block behind its last one are 32-bit numbers.
+constexpr int32_t kCacheMostKeys = 0x7fffffff - 255;
+
 struct CacheRequest {
   int32_t row0, n, seq;  // first packed row, new tokens, cached tokens
   // False for what validation refuses.
@@ -44,7 +47,7 @@ struct CacheRequest {
     n = static_cast<int32_t>(hi - lo);
     seq = a.seq[r];
     return lo >= 0 && hi >= lo && hi <= a.n_tokens && hi - lo <= a.max_new && seq >= 0 &&
-           seq <= static_cast<int64_t>(a.max_pages) * a.page_size && (r > 0 || lo == 0);
+           seq <= kCacheMostKeys && seq <= static_cast<int64_t>(a.max_pages) * a.page_size && (r > 0 || lo == 0);
   }
   __device__ __forceinline__ int64_t rows(const CacheAttnDev& a) const { return static_cast<int64_t>(n) * a.G; }
 };
@@ -62,6 +65,9 @@ __device__ __forceinline__ bool cache_wait(uint64_t* bar, uint32_t parity) {
 __device__ __forceinline__ bool cache_wait_warp(uint64_t* bar, uint32_t parity) {
   return __all_sync(0xffffffffu, tc::mbar_test_wait(bar, parity)) || cache_wait_warp_on(bar, parity);
 }
+// Whether a CTA gives up, one answer for the calling warp.
+__device__ __forceinline__ bool cache_raised(const volatile int* flag) { return __any_sync(0xffffffffu, *flag) != 0; }
+
 // What a request costs k_cache_attn (x) and k_cache_chunk (y), in units of about 0.07 us of an SM: a tile
 // of 64 keys 7, a block of 128 keys of a unit, or its beginning, 20 (a tile 6, 8 or 10: two chunks
 // beside 22 single tokens 70, 65, 66 us, one of 2048 beside 63 255, 255, 289, one of 100 beside 63

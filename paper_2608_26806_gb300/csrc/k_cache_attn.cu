@@ -101,6 +101,17 @@ __global__ void __launch_bounds__(kPrepThreads) k_cache_prep(CacheAttnDev a, int
 
 // ---------------------------------------------------------------- building blocks
 __device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// The same, and whether x holds for any of them: what decides whether they go on has to be one answer
+// for all, or some would wait for others that have left.
+__device__ __forceinline__ bool bar_consumers_any(bool x) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"(x ? 1u : 0u)
+      : "memory");
+  return any != 0;
+}
 __device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int row, int head, int page, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::
@@ -253,7 +264,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       __syncwarp();
       if (g.head < 0) break;
       const int32_t* row = a.table + g.req * a.table_stride;
-      for (int tile = g.tile0; tile < g.tile1 && !*abort_flag; ++tile, ++n) {
+      for (int tile = g.tile0; tile < g.tile1 && !cache_raised(abort_flag); ++tile, ++n) {
         const int i0 = tile * per_tile, sb = n % kStages;
         if (tile == g.tile0 || (i0 & 31) == 0)
           if (sh.window.load(a, row, g.seq, i0 & ~31)) sh.bad_page = g.req;
@@ -274,10 +285,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         }
         __syncwarp();
       }
-      if (!fine || *abort_flag) {
-        fine = false;
-        break;
-      }
+      fine = !cache_raised(abort_flag);
       t = end;
     }
     if (!fine && lane == 0) *abort_flag = 1;
@@ -293,8 +301,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     int n = 0;
     for (int sc = 0;; ++sc) {
       if (!cache_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1)) *abort_flag = 1;
-      bar_consumers();
-      if (*abort_flag) break;
+      if (bar_consumers_any(*abort_flag != 0)) break;
       const Segment g = sh.seg[sc & 1];
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sh.seg_empty[sc & 1]);
@@ -476,8 +483,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           sh.w[warp][gr + 8 * i] = rs[2 * i];
         }
       }
-      bar_consumers();
-      if (*abort_flag) break;
+      if (bar_consumers_any(*abort_flag != 0)) break;
       const int pieces = g.c1 - g.c0 + 1;
       constexpr int kLanes = D / 4;               // lanes of a row, four columns each
       constexpr int kAtOnce = kConsumers / kLanes;  // rows at once

@@ -205,8 +205,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   // The ring. K_j and V_j of a segment lie in stages 2 (j % 2) and 2 (j % 2) + 1. The MMA thread
   // releases V_j and K_{j + 1} together, behind the last product with either: kv_empty[j % 2], once
   // a step but the last, and kv_empty[1] once before, for K_0. The last values are released with the
-  // segment's O. The copies of a segment's keys (kv = 0) or values; between(): called behind the
-  // first block's copy.
+  // segment's O.
   if (warp == kKeyWarp || warp == kValueWarp) {
     // ------------------------------------------------------------ segments, queries, keys; values
     const int kv = warp == kKeyWarp ? 0 : 1;
@@ -287,17 +286,13 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
       }
       if (g.head < 0) break;
-      // The ring. K_j and V_j of a segment lie in stages 2 (j % 2) and 2 (j % 2) + 1. The MMA thread
-      // releases V_j and K_{j + 1} together, behind the last product with either: kv_empty[j % 2],
-      // once a step but the last, and kv_empty[1] once before, for K_0. The last values are released
-      // with the segment's O.
       const int32_t* row = a.table + g.req * a.table_stride;
       const int blocks = g.j1 - g.j0;
       // the first queries wait for nothing; later ones come behind the segment's first keys, which
       // need not wait for the last product with the queries before
       if (kv == 0 && qn == 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
 #pragma unroll 1
-      for (int j = 0; j < blocks && !*abort_flag; ++j) {
+      for (int j = 0; j < blocks && !cache_raised(abort_flag); ++j) {
         const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
         if (j == 0 || (i0 & 31) == 0)
           if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
@@ -333,7 +328,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         __syncwarp();
         if (kv == 0 && j == 0 && qn > 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
       }
-      ok = ok && !*abort_flag;
+      ok = ok && !cache_raised(abort_flag);
       if (!ok) break;
       ++qn;
       fired0 += blocks >> 1;

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_write(WriteDev w) {
   pdl_trigger();
   if (kCluster) {
     if (blockIdx.x == 0 && threadIdx.x == 0) *w.st = DevStatus{0, 0, 0, 0u};
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
   }
   int64_t bad = -1;
   const int sub = threadIdx.x & (w.lanes - 1);
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_write(WriteDev w) {
       }
     }
   }
-  if (kCluster) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (kCluster) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
   else pdl_wait();
   if (bad >= 0) record_error(w.st, AVTP_ERR_DEVICE_INPUT, static_cast<int32_t>(bad));
 }

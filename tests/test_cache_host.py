@@ -112,6 +112,19 @@ def test_attention_arguments(lib, field, value, code):
     assert lib.avtp_cache_attention(ctypes.byref(_cache()), ctypes.byref(a), FAKE, BIG, None) == code
 
 
+def test_attention_refuses_more_rows_than_its_line_of_work_counts(lib):
+    """2^27 blocks of rows over all KV heads, from the requests or from the new tokens."""
+    size = ctypes.c_size_t()
+    for fields, code in (({"n_requests": 1 << 27}, G), ({"n_requests": 1 << 24}, G),
+                         ({"n_requests": (1 << 24) - 1}, avtp.OK),
+                         ({"n_tokens": (1 << 31) - 1, "lse_stride": 1 << 31, "n_q_heads": 8 * 128, "q_stride": 1 << 17,
+                           "o_stride": 1 << 17}, G)):
+        a = _with(_attn(), **fields)
+        assert lib.avtp_cache_attention_workspace_size(ctypes.byref(_cache()), ctypes.byref(a), ctypes.byref(size)) == code
+        if code != avtp.OK:
+            assert lib.avtp_cache_attention(ctypes.byref(_cache()), ctypes.byref(a), FAKE, BIG, None) == code
+
+
 @pytest.mark.parametrize("page", [1, 8, 24, 40])
 def test_attention_wants_pages_of_whole_sixteens(lib, page):
     assert lib.avtp_cache_attention(ctypes.byref(_cache(page=page)), ctypes.byref(_attn()), FAKE, BIG, None) == U

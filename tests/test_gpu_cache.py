@@ -250,6 +250,41 @@ def test_many_requests(R):
     b.check(c.o, c.lse)
 
 
+def _kinds(R, seed, chunk, few):
+    """R requests: one in five a chunk of up to ``chunk`` tokens, the others up to ``few``."""
+    rng = np.random.default_rng(seed)
+    new = [int(rng.integers(1, chunk) if r % 5 == 2 else rng.integers(0, few + 1)) for r in range(R)]
+    return [(int(rng.integers(0, 400)) + (n if r % 11 else 0), n) for r, n in enumerate(new)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,chunk,few", [(8, 2, 64, 90, 3), (28, 4, 128, 50, 1), (6, 6, 64, 300, 20)])
+@pytest.mark.parametrize("R", [33, 64, 200])
+def test_many_requests_of_either_kind(R, Hq, Hkv, d, chunk, few):
+    b = Batch(_kinds(R, R + d, chunk, few), Hq, Hkv, d, 16, seed=R)
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
+def test_many_requests_of_two_row_warps():
+    b = Batch(_kinds(70, 3, 8, 8), 8, 2, 128, 32, seed=12)
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
+@pytest.mark.parametrize("requests", [STEP, CHUNK, _kinds(36, 4, 60, 2)], ids=["step", "chunk", "many"])
+def test_a_table_of_more_keys_than_steps(requests):
+    """Rows of the table for 2^31 tokens: bounds with which a line of single tiles would pass 2^31."""
+    b = Batch(requests, 16, 8, 64, 1024, seed=13, spare_pages=1)
+    wide = torch.full((len(requests), 1 << 21), -7, dtype=torch.int32, device="cuda")
+    wide[:, :b.table.shape[1]] = b.dev["table"]
+    b.dev["table"] = wide
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
 @pytest.mark.parametrize("scale,k_scale", [(1.0, 4.0), (1e-3, 1.0), (None, 0.0)])
 def test_sharp_and_flat_softmax(scale, k_scale):
     for requests in (STEP, CHUNK):
@@ -366,6 +401,56 @@ def test_attention_refuses_bad_lengths_and_writes_nothing(what, requests):
     c = b.call(o=o, **kw).run()
     assert status(c) == avtp.ERR_DEVICE_INPUT
     assert (o == -3.0).all()
+
+
+@pytest.mark.parametrize("chunk", [2, 60], ids=["step", "chunk"])
+@pytest.mark.parametrize("what", ["offsets_fall", "negative", "table_short", "max_new"])
+def test_attention_refuses_bad_lengths_among_many_requests(what, chunk):
+    b = Batch(_kinds(40, 5, chunk, 1), 8, 2, 128, 32, seed=14)
+    kw = {}
+    if what == "offsets_fall":
+        b.dev["cu"][20] = int(b.cu[19]) - 1
+    elif what == "negative":
+        b.dev["seq"][37] = -1
+    elif what == "table_short":
+        b.dev["seq"][39] = b.table.shape[1] * 32 + 1
+    elif what == "max_new":
+        kw["max_new"] = b.max_new - 1
+    o = torch.full_like(b.dev["q"], -3.0)
+    c = b.call(o=o, **kw).run()
+    assert status(c) == avtp.ERR_DEVICE_INPUT
+    assert (o == -3.0).all()
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_attention_refuses_positions_of_more_than_32_bits(new):
+    """2^31 - 1 keys of a table that has the pages for them: the block behind the last key would not
+    have a 32-bit position."""
+    b = Batch([(90, new), (70, 1)], 2, 1, 64, 1 << 20, seed=15, spare_pages=0)
+    wide = torch.zeros(2, 1 << 11, dtype=torch.int32, device="cuda")
+    b.dev["table"] = wide
+    for most in ((1 << 31) - 1, (1 << 31) - 255):
+        b.dev["seq"][0] = most
+        o = torch.full_like(b.dev["q"], -3.0)
+        c = b.call(o=o).run()
+        assert status(c) == avtp.ERR_DEVICE_INPUT
+        assert (o == -3.0).all()
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Each with a workspace of its own, over the same cache."""
+    b = Batch([(700, 300), (70, 1), (0, 2), (900, 129), (2500, 1)], 16, 4, 128, 64, seed=16)
+    calls = [b.call() for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for c, s in zip(calls, streams):
+            c.run(stream=s)
+    torch.cuda.synchronize()
+    for c in calls:
+        assert status(c) == avtp.OK
+        b.check(c.o, c.lse)
+    assert torch.equal(calls[0].o, calls[1].o) and torch.equal(calls[0].lse, calls[1].lse)
 
 
 @pytest.mark.parametrize("requests", [[(70, 1), (100, 1), (300, 1)], [(200, 100), (100, 40), (300, 129)]],
