@@ -9,8 +9,8 @@
 //   S_j = Q K_j^T           tcgen05, M = 128 rows, N = 128 keys, operands in shared memory
 //   P_j = exp2(c2 S_j - m)  a thread per row; bf16, over S_j's first 64 TMEM columns
 //   O  += P_j V_j           tcgen05, A (P) from TMEM, V the MN-major operand as the pages hold it
-// with the softmax, the order of MMAs and the ring of k_attn_fwd.cu (which see for what they
-// measured): while one slot's softmax runs, the tensor core has the other slot's products.
+// with the softmax, the order of MMAs and the ring of k_attn_fwd.cu: while one slot's softmax runs, the
+// tensor core has the other slot's products.
 // Keys and values come as TMA boxes of a page's rows, 32 boxes' places looked up in the block table
 // at a time, by a warp each (one warp for both, looking up every block's, took 3000 cycles a block).
 //
@@ -20,12 +20,28 @@
 // workspace, and k_cache_join puts them together in their order: results do not depend on which
 // came first.
 //
-// What bounds it: the tensor core (2048 cycles a block and unit at d = 128, the exponentials half
-// of that), and for short calls the pieces' way through L2.
+// What bounds it: the tensor core, 2048 cycles a block and unit at d = 128 of the 2550 that one takes (a
+// slot's softmax, its last P V, its next S and the hand-overs between are one chain of that length; the
+// exponentials alone would take half of it), at full load the power limit, and a unit's ends: 9000 cycles
+// from its last S to the next unit's first, of which its masked block's softmax 2600 and its rows' way out.
+// Short calls are launches and the way to the first S (10000 cycles), and the pieces' way through L2.
+//
+// Instructions are what this kernel is short of: eleven warps in four roles go through more of them than
+// the SM's nearest instruction cache holds, and a first pass over code waits for it line by line. So the
+// softmax has its usual path in one piece and everything else once behind it, waits and sums are calls,
+// one-time code is rolled; a second copy of the loads, or waits compiled into the issuing loop, cost 10 to
+// 60 %. The issuing loop is the exception: a copy a slot, whose descriptors are constants, is faster than
+// one for both (32 query heads, 8 KV heads, 8192 tokens behind 2176: 507 us against 533; a copy a slot and
+// parity 500, but eight requests of 700 tokens behind 300 take 90 us instead of 84 then).
+//
+// Measured (32 query heads, 8 KV heads, d = 128, pages of 64 tokens): 9856 tokens 490 us, 1620 TFLOP/s;
+// 8192 behind 2176 507 us, 1660 TFLOP/s; 512 behind 9300 63 us, 1280 TFLOP/s.
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
 // CTA whose wait gives up records AVTP_ERR_TIMEOUT and leaves.
+#include <type_traits>
+
 #include "avtp_cache_attn.cuh"
 
 namespace avtp {
@@ -41,6 +57,7 @@ constexpr int kValueWarp = 10;
 constexpr int kStages = 4;      // key or value blocks in shared memory
 // A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first
 // softmax with nothing to overlap, its rows' way out): its steps on the line are its blocks and these.
+// (With three, 9856 tokens 488 us instead of 494, 512 behind 9300 63.6 instead of 62.8.)
 constexpr int kUnitSteps = 2;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSCol = 0;    // S (and P) of slot s at kSCol + 128 s
@@ -56,8 +73,9 @@ static_assert(kChunkRows == 2 * kQT, "two slots a unit");
 
 __host__ __device__ constexpr uint32_t tile_bytes(int d) { return static_cast<uint32_t>(kQT) * d * 2; }
 constexpr uint32_t kPanel = kQT * 128;
+constexpr uint32_t kOutStage = 2048;  // a warp's 32 rows x 32 columns of O on their way out
 __host__ __device__ constexpr size_t chunk_smem_bytes(int d) {
-  const size_t need = 1024 + static_cast<size_t>(2 + kStages) * tile_bytes(d);
+  const size_t need = 1024 + static_cast<size_t>(2 + kStages) * tile_bytes(d) + 2 * kSlotWarps * kOutStage;
   // more than half the SM's shared memory, so that no second CTA (and its 512 TMEM columns)
   // shares an SM
   return need > 116 * 1024 ? need : 116 * 1024;
@@ -102,6 +120,23 @@ struct ChunkSync {
   int abort, bad_page;
 };
 
+// sum_{i < n} floor((a i + b) / m), by Euclid's steps on (a, m); a n + b is below 2^32, the sum below 2^31.
+__host__ __device__ inline uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
+  uint32_t sum = 0;
+  while (true) {
+    sum += static_cast<uint32_t>(static_cast<uint64_t>(n) * (n - 1) / 2 * (a / m)) + n * (b / m);
+    a %= m;
+    b %= m;
+    const uint32_t top = a * n + b;
+    if (top < m) return sum;
+    n = top / m;
+    b = top % m;
+    const uint32_t t = m;
+    m = a;
+    a = t;
+  }
+}
+
 // Key blocks of a request's unit: those of its last token, one for a token that sees nothing.
 __device__ __forceinline__ int unit_blocks(const CacheRequest& q, int nt, int u) {
   return max(1, (q.seq - q.n + static_cast<int>(min((u + 1) * static_cast<int64_t>(2 * nt), static_cast<int64_t>(q.n))) +
@@ -134,6 +169,19 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int blocks) {
   return kUnitSteps + ((blocks + (1 << a.step_shift) - 1) >> a.step_shift);
 }
 
+// Steps of the first u units of a request's head, the last of all not among them, in closed form: unit i's
+// last token sees x = past + rows (i + 1) keys, for which it has kUnitSteps + max(1, ceil(x / (128 * 2^step_shift))) of them. For
+// requests of more than kNearUnits units: 128 of them, added up one by one and passed one by one, took up to
+// 24000 cycles before a CTA's first product and take 9000 so; eight of them 2500 and 5300.
+constexpr int kNearUnits = 32;
+static __device__ __noinline__ int steps_before(int past, int rows, int step_shift, int u) {
+  const int blind = past >= 0 ? 0 : min(u, -past / rows);  // units that see nothing
+  const uint32_t keys = static_cast<uint32_t>(kKB) << step_shift;
+  int sum = kUnitSteps * u + blind;
+  if (u > blind) sum += floor_sum(u - blind, keys, rows, past + (blind + 1) * rows + keys - 1);
+  return sum;
+}
+
 // ---------------------------------------------------------------- attention
 // mapQ: q {d, Hq, T}, box 64 x G x floor(128 / G); mapK, mapV: the cache as
 // {d, row of the page, head, page}, box of 64 elements and `box` rows.
@@ -148,6 +196,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   constexpr uint32_t kTile = tile_bytes(D);
   unsigned char* sQ = smem;                   // slot s at sQ + s * kTile
   unsigned char* sKV = smem + 2 * kTile;      // stage b at sKV + b * kTile
+  unsigned char* sO = sKV + kStages * kTile;  // warp w at sO + w * kOutStage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int nt = kQT / a.G;
 
@@ -194,10 +243,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
 
   auto steps = [&](const CacheRequest& q, int& most) {
     const int U = units_of(a, q, nt);
-    int sum = 0;
+    if (U == 0) return 0;
+    int sum = steps_of(a, unit_blocks(q, nt, U - 1));  // the last unit may be short
+    most = max(most, sum);
+    if (U > kNearUnits) {
+      sum += steps_before(q.seq - q.n, 2 * nt, a.step_shift, U - 1);
+    } else {
 #pragma unroll 1
-    for (int u = 0; u < U; ++u) sum += steps_of(a, unit_blocks(q, nt, u));
-    if (U > 0) most = max(most, steps_of(a, unit_blocks(q, nt, U - 1)));
+      for (int u = 0; u < U - 1; ++u) sum += steps_of(a, unit_blocks(q, nt, u));
+    }
     return sum * a.Hkv;
   };
   if (a.R > kNearRequests) sy.plan.form(a, steps);
@@ -227,7 +281,24 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       runs = CacheRuns(line.total, line.most, kUnitSteps + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
-      if (t < t1) r = line.find(a, sy.plan, t, &pre);
+      if (t < t1) {
+        r = line.find(a, sy.plan, t, &pre);
+        // a request of many units: its last one that begins at or before step t, 32 tries at a time (the
+        // units of few, and the requests behind r, are passed one by one below)
+        const CacheRequest q = line.request(a, mine, r);
+        const int past = q.seq - q.n, U = units_of(a, q, nt);
+        if (U > kNearUnits) {
+#pragma unroll 1
+          for (int n = U; n > 1;) {  // it is among units u .. u + n - 1
+            const int each = (n + 31) / 32, at = lane * each;
+            const bool before = at < n && pre + steps_before(past, 2 * nt, a.step_shift, u + at) * a.Hkv <= t;
+            const int on = (__popc(__ballot_sync(0xffffffffu, before)) - 1) * each;
+            u += on;
+            n = min(each, n - on);
+          }
+          pre += steps_before(past, 2 * nt, a.step_shift, u) * a.Hkv;
+        }
+      }
     }
 #pragma unroll 1
     for (int sc = 0;; ++sc) {
@@ -391,59 +462,61 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         wait(&sy.q_full, sc & 1, false);
         wait(&sy.kv_full[0], ph0, false);
         tc::fence_after_sync();
-        // Step -1 is S_0 of both slots alone. One copy of a slot's products for both slots and either
-        // parity of the step: four took more of the instruction cache than the roles' loops leave.
-        // And few commits: the thread stands still for most of one, longer than the two MMAs that the
-        // tensor core queues. p0, kv, kk: whether the first half of the next P and the next V and
-        // K were seen complete.
         bool p0 = false, kv = false, kk = false;
+        // S_0 of both slots. Few commits, here and below: the thread stands still for most of one, longer
+        // than the two MMAs that the tensor core queues. p0, kv, kk: whether the first half of the next P and
+        // the next V and K were seen complete.
 #pragma unroll 1
-        for (int j = -1; j < nm; ++j) {
-          const int odd = j & 1;
+        for (int s = n0 > 0 ? 0 : 1; s < (n1 > 0 ? 2 : 1); ++s) {
+          s_mmas(s, 0);
+          tc::mma_commit(&sy.s_full[s]);
+        }
+        tc::mma_commit(&sy.kv_empty[1]);
+        if (nm == 1) tc::mma_commit(&sy.q_empty);
+        auto group = [&](auto odd_, auto slot_, int j) {
+          const int odd = odd_, s = slot_;
           const uint32_t turn = static_cast<uint32_t>(j) >> 1;  // of V_j's stage in this segment
           const uint32_t pv = (odd ? ph1 : ph0) ^ (turn & 1), pk = (odd ? ph0 : ph1) ^ ((turn + odd) & 1);
           const int steps = j == nm - 1 ? last_steps : kKB / 16;
           const bool keys = j + 1 < nm;
-#pragma unroll 1
-          for (int s = n0 > j ? 0 : 1; s < (n1 > j ? 2 : 1); ++s) {
-            const bool more = j + 1 < (s ? n1 : n0), last = s == 1 || n1 <= j;
-            if (j >= 0) {
-              const uint32_t pp = odd ^ (s ? pb1 : pb0);
-              if (s == 0 || n0 <= j) {  // the first group of the step: V_j and K_{j + 1}
-                wait(&sy.kv_full[2 * odd + 1], pv, kv);
-                if (keys) wait(&sy.kv_full[2 - 2 * odd], pk, kk);
-              }
-              wait(&sy.p_full[s][0], pp, p0);
-              tc::fence_after_sync();
-              pv_mmas(s, j, 2 * odd + 1, steps, 0);
-              // a softmax that is still at the second half may have to wait for the first half's P V;
-              // where it is through, a plain arrival keeps the barrier's phase
-              if (tc::mbar_test_wait(&sy.p_full[s][1], pp)) {
-                tc::mbar_arrive(&sy.half_done[s]);
-              } else {
-                tc::mma_commit(&sy.half_done[s]);
-                wait(&sy.p_full[s][1], pp, false);
-              }
-              tc::fence_after_sync();
-              pv_mmas(s, j, 2 * odd + 1, steps, 1);
-            }
-            if (more) s_mmas(s, 2 - 2 * odd);
-            // the next group's barriers
-            if (j >= 0) {
-              const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
-              p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? odd ^ 1 : odd) ^ (s1 ? pb1 : pb0));
-              if (last) {  // V_{j + 1} and K_{j + 2}, in the other two stages
-                kv = tc::mbar_test_wait(&sy.kv_full[3 - 2 * odd], pk);
-                kk = tc::mbar_test_wait(&sy.kv_full[2 * odd], pv ^ 1);
-              }
-            }
-            if (more) tc::mma_commit(&sy.s_full[s]);
-            else if (j >= 0) tc::mma_commit(&sy.o_done[s]);
-            if (last && keys) {
-              tc::mma_commit(&sy.kv_empty[odd]);
-              if (j + 2 == nm) tc::mma_commit(&sy.q_empty);  // the segment's last S
-            }
+          const bool more = j + 1 < (s ? n1 : n0), last = s == 1 || n1 <= j;
+          const uint32_t pp = odd ^ (s ? pb1 : pb0);
+          if (s == 0 || n0 <= j) {  // the first group of the step: V_j and K_{j + 1}
+            wait(&sy.kv_full[2 * odd + 1], pv, kv);
+            if (keys) wait(&sy.kv_full[2 - 2 * odd], pk, kk);
           }
+          wait(&sy.p_full[s][0], pp, p0);
+          tc::fence_after_sync();
+          pv_mmas(s, j, 2 * odd + 1, steps, 0);
+          // a softmax that is still at the second half may have to wait for the first half's P V;
+          // where it is through, a plain arrival keeps the barrier's phase
+          if (tc::mbar_test_wait(&sy.p_full[s][1], pp)) {
+            tc::mbar_arrive(&sy.half_done[s]);
+          } else {
+            tc::mma_commit(&sy.half_done[s]);
+            wait(&sy.p_full[s][1], pp, false);
+          }
+          tc::fence_after_sync();
+          pv_mmas(s, j, 2 * odd + 1, steps, 1);
+          if (more) s_mmas(s, 2 - 2 * odd);
+          // the next group's barriers
+          const int s1 = (s == 0 && j < n1) ? 1 : (n0 > j + 1 ? 0 : 1);
+          p0 = tc::mbar_test_wait(&sy.p_full[s1][0], (last ? odd ^ 1 : odd) ^ (s1 ? pb1 : pb0));
+          if (last) {  // V_{j + 1} and K_{j + 2}, in the other two stages
+            kv = tc::mbar_test_wait(&sy.kv_full[3 - 2 * odd], pk);
+            kk = tc::mbar_test_wait(&sy.kv_full[2 * odd], pv ^ 1);
+          }
+          if (more) tc::mma_commit(&sy.s_full[s]);
+          else tc::mma_commit(&sy.o_done[s]);
+          if (last && keys) {
+            tc::mma_commit(&sy.kv_empty[odd]);
+            if (j + 2 == nm) tc::mma_commit(&sy.q_empty);  // the segment's last S
+          }
+        };
+#pragma unroll 1
+        for (int j = 0; j < nm; ++j) {
+          if (j < n0) group(j & 1, std::integral_constant<int, 0>{}, j);
+          if (j < n1) group(j & 1, std::integral_constant<int, 1>{}, j);
         }
         ph0 ^= ((nm + 1) >> 1) & 1;
         ph1 ^= (nm >> 1) & 1;
@@ -508,92 +581,119 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           }
           tc::fence_proxy_async();
         }
+        uint32_t su[64];  // the row's logits of a half
+        uint32_t pk[32];  // its P
+        // P of the half in su against the reference m; its sum
+        auto exps = [&]() {
+          const float2 nn = make_float2(-m, -m);
+          float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t su[64];  // the row's logits of this half
-          uint32_t pk[32];
-          auto load = [&](int half) {
-            tc::tmem_ld64_async(tS + half * 64, su);
-            tc::tmem_wait64(su);
-            if (masked) {
-#pragma unroll
-              for (int c = 0; c < 64; ++c) su[c] = (half * 64 + c < seen) ? su[c] : 0xff800000u;
-            }
-          };
-          auto row_max = [&]() {
-            float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int c = 0; c < 64; c += 8) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
-            }
-            return fmaxf(tc::max3(t[0], t[1], t[2]), t[3]);
-          };
-          // P of the half against the reference m, and its sum
-          auto exps = [&]() {
-            const float2 nn = make_float2(-m, -m);
-            float2 acc0 = make_float2(0.f, 0.f), acc1 = acc0;
-#pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-              const float2 z01 = tc::ffma2(make_float2(__uint_as_float(su[c]), __uint_as_float(su[c + 1])), cc, nn);
-              const float2 z23 = tc::ffma2(make_float2(__uint_as_float(su[c + 2]), __uint_as_float(su[c + 3])), cc, nn);
-              const float p0 = tc::ex2(z01.x), p1 = tc::ex2(z01.y), p2 = tc::ex2(z23.x), p3 = tc::ex2(z23.y);
-              acc0 = tc::add2(acc0, make_float2(p0, p1));
-              acc1 = tc::add2(acc1, make_float2(p2, p3));
-              pk[c / 2] = tc::pack_bf16x2(p0, p1);
-              pk[c / 2 + 1] = tc::pack_bf16x2(p2, p3);
-            }
-            return (acc0.x + acc0.y) + (acc1.x + acc1.y);
-          };
-          load(hf);
-          if (hf == 0 && j == 0) {
-            const float mb = row_max() * c2;
-            m = mb == -INFINITY ? 0.f : mb;
+          for (int c = 0; c < 64; c += 4) {
+            const float2 z01 = tc::ffma2(make_float2(__uint_as_float(su[c]), __uint_as_float(su[c + 1])), cc, nn);
+            const float2 z23 = tc::ffma2(make_float2(__uint_as_float(su[c + 2]), __uint_as_float(su[c + 3])), cc, nn);
+            const float p0 = tc::ex2(z01.x), p1 = tc::ex2(z01.y), p2 = tc::ex2(z23.x), p3 = tc::ex2(z23.y);
+            acc0 = tc::add2(acc0, make_float2(p0, p1));
+            acc1 = tc::add2(acc1, make_float2(p2, p3));
+            pk[c / 2] = tc::pack_bf16x2(p0, p1);
+            pk[c / 2 + 1] = tc::pack_bf16x2(p2, p3);
           }
-          float sum = exps();
-          // values far above the reference or, as yet, all far below it, or a NaN: take the maximum
-          // of what is left of the block as the reference and start the half again (its logits
-          // are in TMEM)
-          if (__any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum))) {
-            float mb = -INFINITY;  // stays so when nothing is visible
-#pragma unroll 1
-            for (int half = 1; half >= hf; --half) {
-              load(half);
-              mb = fmaxf(mb, row_max() * c2);
-            }
-            float factor = 1.f;
-            // A reference moves down before a row's first term alone, so nothing was lost to underflow
-            // (l = 0, and O is zero or not yet written); behind that l stays above kLeastSum, but for
-            // a half whose block's maximum, then the reference, is in the other half.
-            if (mb > m + kRescaleTau || (l < kLeastSum && mb != -INFINITY)) {
-              factor = l > 0.f ? tc::ex2(m - mb) : 1.f;
-              l *= factor;
-              m = mb;
-            }
-            if (__any_sync(0xffffffffu, factor != 1.f)) {
-              if (hf == 1) ok = cache_wait_warp(&sy.half_done[slot], (done + j) & 1);
-              if (!ok) break;
-              tc::fence_after_sync();
-#pragma unroll 1
-              for (int oc = 0; oc < D; oc += 32) {
-                uint32_t ov[32];
-                tc::tmem_ld32_async(tO + oc, ov);
-                tc::tmem_wait(ov);
-#pragma unroll
-                for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
-                tc::tmem_st32(tO + oc, ov);
-              }
-              tc::tmem_wait_st();
-            }
-            sum = exps();
-          }
+          return (acc0.x + acc0.y) + (acc1.x + acc1.y);
+        };
+        // values far above the reference or, as yet, all far below it, or a NaN
+        auto off = [&](float sum) { return __any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum)); };
+        auto hand_over = [&](int hf, float sum) {
           l += sum;
           tc::tmem_st32(tS + hf * 32, pk);
           tc::tmem_wait_st();
           tc::fence_before_sync();
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(&sy.p_full[slot][hf]);
+        };
+        // Nearly every block: no mask, and a reference that stays. Its instructions lie one behind the
+        // other; what the others need comes behind, once.
+        int hf = 0;
+        if (!masked && j > 0) {
+          tc::tmem_ld64_async(tS, su);
+          tc::tmem_wait64(su);
+          float sum = exps();
+          if (!off(sum)) {
+            hand_over(0, sum);
+            hf = 1;
+            tc::tmem_ld64_async(tS + 64, su);
+            tc::tmem_wait64(su);
+            sum = exps();
+            if (!off(sum)) {
+              hand_over(1, sum);
+              hf = 2;
+            }
+          }
+        }
+#pragma unroll 1
+        for (; hf < 2; ++hf) {
+          float sum, mb = -INFINITY;
+          // Once through the loop but for a reference to be found: the half's maximum as a segment's
+          // first one (kFirst), the maximum of what is left of the block where a sum asks for it (kMove).
+          enum { kPlain, kFirst, kMove };
+          int mode = hf == 0 && j == 0 ? kFirst : kPlain;
+          int at = hf;  // the half in su
+#pragma unroll 1
+          for (;;) {
+            tc::tmem_ld64_async(tS + at * 64, su);
+            tc::tmem_wait64(su);
+            if (masked) {
+              const int left = seen - at * 64;
+#pragma unroll
+              for (int c = 0; c < 64; ++c) su[c] = c < left ? su[c] : 0xff800000u;
+            }
+            if (mode != kPlain) {
+              float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+              for (int c = 0; c < 64; c += 8) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                  t[w] = tc::max3(t[w], __uint_as_float(su[c + 2 * w]), __uint_as_float(su[c + 2 * w + 1]));
+              }
+              mb = fmaxf(mb, fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2);  // stays -inf when nothing is visible
+              if (mode == kFirst) {
+                m = mb == -INFINITY ? 0.f : mb;
+              } else if (at > hf) {
+                at = hf;
+                continue;
+              } else {
+                float factor = 1.f;
+                // A reference moves down before a row's first term alone, so nothing was lost to underflow
+                // (l = 0, and O is zero or not yet written); behind that l stays above kLeastSum, but for
+                // a half whose block's maximum, then the reference, is in the other half.
+                if (mb > m + kRescaleTau || (l < kLeastSum && mb != -INFINITY)) {
+                  factor = l > 0.f ? tc::ex2(m - mb) : 1.f;
+                  l *= factor;
+                  m = mb;
+                }
+                if (__any_sync(0xffffffffu, factor != 1.f)) {
+                  if (hf == 1) ok = cache_wait_warp(&sy.half_done[slot], (done + j) & 1);
+                  if (!ok) break;
+                  tc::fence_after_sync();
+#pragma unroll 1
+                  for (int oc = 0; oc < D; oc += 32) {
+                    uint32_t ov[32];
+                    tc::tmem_ld32_async(tO + oc, ov);
+                    tc::tmem_wait(ov);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) ov[i] = __float_as_uint(__uint_as_float(ov[i]) * factor);
+                    tc::tmem_st32(tO + oc, ov);
+                  }
+                  tc::tmem_wait_st();
+                }
+              }
+            }
+            sum = exps();
+            if (mode == kMove || !off(sum)) break;
+            mode = kMove;
+            mb = -INFINITY;
+            at = 1;
+          }
+          if (!ok) break;
+          hand_over(hf, sum);
         }
         if (!ok) break;
       }
@@ -623,23 +723,41 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
         continue;
       }
-      // a lane stores its own row, 16 bytes at a time: through shared memory, whole lines at a time, took
-      // twice as long, nearly all of it waiting for that code's instructions
       const float inv = 1.f / l;
       const uint32_t sees = l == 0.f ? 0u : 0xffffffffu;  // a row that sees nothing is zero whatever its accumulator holds
       const int64_t t = static_cast<int64_t>(g.row0) + tok;
       const int head = g.head * a.G + head_of_row;
       if (live && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (m + log2f(l)) * kLn2;
-      uint4* out = reinterpret_cast<uint4*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D);
+      // 32 columns at a time through shared memory (16-byte pieces, swizzled), so that four lanes store 64
+      // bytes of a row: a lane a row, 16 bytes at a time, each store takes 32 turns of the memory pipe
+      unsigned char* stage = sO + warp * kOutStage;
+      const int piece = lane & 3;
+      const unsigned long long dst =
+          live ? reinterpret_cast<unsigned long long>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D) : 0ull;
+      unsigned long long to[4];  // rows lane / 4, + 8, ...
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        to[i] = __shfl_sync(0xffffffffu, dst, i * 8 + (lane >> 2));
+        if (to[i] != 0) to[i] += piece * 16;
+      }
 #pragma unroll 1
-      for (int oc = 0; oc < D; oc += 32, out += 4) {
+      for (int oc = 0; oc < D; oc += 32) {
         float v[32];
         tc::tmem_ld32(tO + oc, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           auto two = [&](int c) { return tc::pack_bf16x2(v[8 * i + c] * inv, v[8 * i + c + 1] * inv) & sees; };
-          if (live) out[i] = make_uint4(two(0), two(2), two(4), two(6));
+          *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4)) =
+              make_uint4(two(0), two(2), two(4), two(6));
         }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = i * 8 + (lane >> 2);
+          const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 64 + ((piece ^ ((r >> 1) & 3)) << 4));
+          if (to[i] != 0) *reinterpret_cast<uint4*>(to[i] + oc * 2) = x;
+        }
+        __syncwarp();
       }
     }
     if (!ok && lane == 0) *abort_flag = 1;

@@ -273,6 +273,19 @@ def test_many_requests_of_two_row_warps():
     b.check(c.o, c.lse)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,requests", [
+    (16, 1, 128, [(900, 700)]),                                       # 16 tokens a block of rows, 44 of them
+    (128, 1, 64, [(40, 130), (500, 120), (1, 1), (67, 67)]),          # two; some see nothing
+    (32, 2, 64, [(300, 700), (513, 513), (20, 530), (0, 529), (600, 1)]),
+    (34, 1, 128, [(400, 260)] * 35),                                  # three, 87 of them, many requests
+], ids=["one", "all_heads", "blind", "many"])
+def test_chunks_of_many_blocks_of_rows(Hq, Hkv, d, requests):
+    b = Batch(requests, Hq, Hkv, d, 32, seed=17)
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
 @pytest.mark.parametrize("requests", [STEP, CHUNK, _kinds(36, 4, 60, 2)], ids=["step", "chunk", "many"])
 def test_a_table_of_more_keys_than_steps(requests):
     """Rows of the table for 2^31 tokens: bounds with which a line of single tiles would pass 2^31."""
