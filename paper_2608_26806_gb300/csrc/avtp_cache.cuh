@@ -21,9 +21,9 @@ cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_arg
 
 // ---------------------------------------------------------------- attention
 // Rows of a (request, KV head) are its (new token, head of the group) pairs, token by token.
-constexpr int kCacheTile = 64;        // keys of a tile of k_cache_attn
 constexpr int kCacheMaxPieces = 32;   // pieces that a row block's keys are split into, at most
 constexpr int kChunkRows = 256;       // rows of a unit of k_cache_chunk, two slots of 128
+constexpr int kChunkKeys = 128;       // keys of its blocks
 // Requests of at most kCacheFewRows rows a KV head are k_cache_attn's, when no request of the call can
 // have more; beside larger ones (max_new is the call's bound) those of at most kCacheFewMixed, one
 // warp's. Sixteen requests of 700-4000 tokens, four heads a group, us a call there and in

@@ -48,7 +48,7 @@ namespace avtp {
 namespace {
 
 constexpr int kQT = 128;  // rows of a slot (MMA M, TMEM lanes)
-constexpr int kKB = 128;  // keys of a block (MMA N of Q K^T, K of P V)
+constexpr int kKB = kChunkKeys;  // MMA N of Q K^T, K of P V
 constexpr int kThreads = 352;
 constexpr int kSlotWarps = 4;
 constexpr int kKeyWarp = 8;
