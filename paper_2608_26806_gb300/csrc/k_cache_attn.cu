@@ -532,63 +532,69 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       }
       bar_consumers();
       if (!sh.last) continue;
-      // Few rows: eight pieces of a row at a time; many: two pieces of four rows. Either way the loads
-      // of a turn are one trip to L2; a row's reference moves between turns. (Sixteen pieces at a time
-      // took longer, 10.2 against 9.6 us for a request of 3425 tokens: the first pass over straight-line
-      // code costs more than its loads.)
-      constexpr int P = kWM == 1 ? 8 : 2, N = kWM == 1 ? 1 : 4;
-      for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
-        float M[N], L[N], W[N];
-        float4 v[N];
+      // Eight pieces of a row at a time or two of four rows, whichever takes fewer turns, each of which is one
+      // trip to L2; a row's reference moves between turns. (One request of 3425 tokens, 7 rows a head in 27
+      // pieces: 12.8 us the one way, 14.6 the other; 16 of 700-4000, 16 rows in 2 or 3: 39.5 and 37.9. Sixteen
+      // pieces at a time took longer, 10.2 against 9.6 us: the first pass over straight-line code costs more
+      // than its loads.)
+      auto join = [&](auto rows_at_once) {
+        constexpr int N = decltype(rows_at_once)::value, P = 8 / N;
+        for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
+          float M[N], L[N], W[N];
+          float4 v[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          M[i] = -INFINITY;
-          L[i] = W[i] = 0.f;
-          v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+          for (int i = 0; i < N; ++i) {
+            M[i] = -INFINITY;
+            L[i] = W[i] = 0.f;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
 #pragma unroll 1
-        for (int k0 = 0; k0 < pieces; k0 += P) {
-          float4 ml[N][P];
-          float4 x[N][P];
+          for (int k0 = 0; k0 < pieces; k0 += P) {
+            float4 ml[N][P];
+            float4 x[N][P];
 #pragma unroll
-          for (int k = 0; k < P; ++k) {
-            const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
+            for (int k = 0; k < P; ++k) {
+              const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
+#pragma unroll
+              for (int i = 0; i < N; ++i) {
+                ml[i][k] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
+                  ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
+                  x[i][k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + i * kAtOnce) * D + col));
+                }
+              }
+            }
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-              ml[i][k] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-              x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
-                ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
-                x[i][k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + i * kAtOnce) * D + col));
+              float mn = M[i];
+#pragma unroll
+              for (int k = 0; k < P; ++k) mn = fmaxf(mn, ml[i][k].x);
+              const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
+              M[i] = mn;
+              L[i] *= old;
+              W[i] *= old;
+              v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
+#pragma unroll
+              for (int k = 0; k < P; ++k) {
+                const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
+                L[i] = fmaf(f, ml[i][k].y, L[i]);
+                W[i] = fmaf(f, ml[i][k].z, W[i]);
+                v[i].x = fmaf(f, x[i][k].x, v[i].x);
+                v[i].y = fmaf(f, x[i][k].y, v[i].y);
+                v[i].z = fmaf(f, x[i][k].z, v[i].z);
+                v[i].w = fmaf(f, x[i][k].w, v[i].w);
               }
             }
           }
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            float mn = M[i];
-#pragma unroll
-            for (int k = 0; k < P; ++k) mn = fmaxf(mn, ml[i][k].x);
-            const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
-            M[i] = mn;
-            L[i] *= old;
-            W[i] *= old;
-            v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-              const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
-              L[i] = fmaf(f, ml[i][k].y, L[i]);
-              W[i] = fmaf(f, ml[i][k].z, W[i]);
-              v[i].x = fmaf(f, x[i][k].x, v[i].x);
-              v[i].y = fmaf(f, x[i][k].y, v[i].y);
-              v[i].z = fmaf(f, x[i][k].z, v[i].z);
-              v[i].w = fmaf(f, x[i][k].w, v[i].w);
-            }
-          }
+          for (int i = 0; i < N; ++i)
+            if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
-      }
+      };
+      const int turns = (rows + kAtOnce - 1) / kAtOnce;  // of one row a thread
+      if ((turns + 3) / 4 * ((pieces + 1) / 2) < turns * ((pieces + 7) / 8)) join(std::integral_constant<int, 4>{});
+      else join(std::integral_constant<int, 1>{});
     }
   }
   pdl_wait();  // this grid's end implies the validation kernel's, which resets the status word
