@@ -102,11 +102,12 @@ static __device__ __noinline__ int cache_scan(int x) {
   return x;
 }
 
-// A call's work as one line of steps, request by request, cut into equal runs. A step is
-// 2^step_shift tiles of keys of a row block (0 but for calls whose bounds would let the line pass
-// 2^31 steps). Every CTA forms the cut for itself, its loading warp alone for up to 32 requests (a
-// lane each), else all its threads (NT of them, equal shares of the requests; pre[i] is the steps
-// before thread i's share).
+// A call's work as one line of steps, request by request, row block by row block (rows served by one pass
+// over their keys: a request's of a KV head in k_cache_attn, a unit in k_cache_chunk), cut into equal
+// runs. A step is 2^step_shift tiles of keys of a row block (0 but for calls whose bounds would let the
+// line pass 2^31 steps). Every CTA forms the cut for itself, its loading warp alone for up to 32 requests
+// (a lane each), else all its threads (NT of them, equal shares of the requests; pre[i] is the steps before
+// thread i's share).
 constexpr int kNearRequests = 32;
 template <int NT>
 struct CachePlan {
