@@ -11,6 +11,7 @@ the same name.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from ctypes import POINTER, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
@@ -733,9 +734,18 @@ def _block_table(where: str, t: torch.Tensor, n_requests: int) -> Tuple[int, int
     return t.shape[1], t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
+def _on_stream(stream):
+    """The stream as the current one, so that buffers made for a call on it come from its memory."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)))
+
+
 class _CacheCall:
     """A prepared call of one entry point: what ``run`` passes is made once, so that a step's call costs
-    the C call and little else (2 us of 6 for a small one)."""
+    the C call and little else (2 us of 6 for a small one). Buffers that it makes (outputs, the workspace)
+    belong to the stream that is current then: to run it on another, order that stream behind it, and keep
+    the call until it is through."""
 
     def _prepare(self, name: str, workspace: torch.Tensor, *structs) -> None:
         self.workspace = workspace
@@ -839,8 +849,9 @@ def cache_slots(cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages:
                 free_pages: torch.Tensor, free_head=None, past_len=None, stream=None, **buffers):
     """avtp_cache_slots: (slot_map int32 [n_tokens], seq_len int32 [R], free_head int32 [1]); the new
     pages' entries go into ``block_table``. See :class:`CacheSlotsCall`."""
-    c = CacheSlotsCall(cu_new, n_tokens, page_size=page_size, n_pages=n_pages, block_table=block_table,
-                       free_pages=free_pages, free_head=free_head, past_len=past_len, **buffers).run(stream)
+    with _on_stream(stream):
+        c = CacheSlotsCall(cu_new, n_tokens, page_size=page_size, n_pages=n_pages, block_table=block_table,
+                           free_pages=free_pages, free_head=free_head, past_len=past_len, **buffers).run()
     return c.slot_map, c.seq_len, c.free_head_out
 
 
@@ -875,7 +886,8 @@ class CacheWriteCall(_CacheCall):
 def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, kept_idx=None,
                 workspace=None, stream=None) -> None:
     """avtp_cache_write: K and V rows to their slots; with a prune's ``kept_idx`` only the kept ones."""
-    CacheWriteCall(cache, slot_map, k, v, kept_idx=kept_idx, workspace=workspace).run(stream)
+    with _on_stream(stream):
+        CacheWriteCall(cache, slot_map, k, v, kept_idx=kept_idx, workspace=workspace).run()
 
 
 class CacheAttentionCall(_CacheCall):
@@ -928,6 +940,7 @@ def cache_attention(cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, se
                     stream=None):
     """avtp_cache_attention: (o, lse) of a chunk of new tokens, or a single one, a request over the
     paged cache. See :class:`CacheAttentionCall`."""
-    c = CacheAttentionCall(cache, q, cu_new, seq_len, block_table, max_new=max_new, softmax_scale=softmax_scale, o=o,
-                           lse=lse, workspace=workspace).run(stream)
+    with _on_stream(stream):
+        c = CacheAttentionCall(cache, q, cu_new, seq_len, block_table, max_new=max_new, softmax_scale=softmax_scale,
+                               o=o, lse=lse, workspace=workspace).run()
     return c.o, c.lse

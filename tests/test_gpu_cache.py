@@ -450,6 +450,26 @@ def test_attention_refuses_positions_of_more_than_32_bits(new):
         assert (o == -3.0).all()
 
 
+def test_buffers_of_a_call_on_another_stream_are_that_streams():
+    """Work still queued on the current stream writes memory that it has given back; a call on a side
+    stream must not be handed that memory for its outputs or workspace."""
+    b = Batch(CHUNK, 8, 2, 128, 32, seed=18)
+    d = b.dev
+    side = torch.cuda.Stream()
+    size = b.call().workspace.numel()
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        dead = [torch.empty_like(d["q"]), torch.empty(8, b.T, device="cuda"),
+                torch.empty(size, dtype=torch.uint8, device="cuda")]
+        torch.cuda._sleep(20_000_000)
+        for t in dead:
+            t.fill_(7)
+        del dead, t
+        o, lse = avtp.cache_attention(b.cache, d["q"], d["cu"], d["seq"], d["table"], max_new=b.max_new, stream=stream)
+        torch.cuda.synchronize()
+        b.check(o, lse)
+
+
 def test_two_calls_at_once_on_two_streams():
     """Each with a workspace of its own, over the same cache."""
     b = Batch([(700, 300), (70, 1), (0, 2), (900, 129), (2500, 1)], 16, 4, 128, 64, seed=16)
