@@ -183,7 +183,8 @@ struct CacheLine {
     } else {
       const int lane = threadIdx.x & 31;
       int longest = 1;
-      incl = cache_scan(lane < a.R && mine_ok ? steps(mine, longest) : 0);
+      incl = lane < a.R && mine_ok ? steps(mine, longest) : 0;
+      incl = a.R > 1 ? cache_scan(incl) : __shfl_sync(0xffffffffu, incl, 0);
       most = __reduce_max_sync(0xffffffffu, longest);
       total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
       weights = make_int2(0, 0);

@@ -361,7 +361,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       const int blocks = g.j1 - g.j0;
       // the first queries wait for nothing; later ones come behind the segment's first keys, which
       // need not wait for the last product with the queries before
-      if (kv == 0 && qn == 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
+      if (kv == 0 && sc == 0) {
+        ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
+        qn = ok ? 1 : 0;
+      }
 #pragma unroll 1
       for (int j = 0; j < blocks && !cache_raised(abort_flag); ++j) {
         const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
@@ -397,17 +400,18 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           }
         }
         __syncwarp();
-        if (kv == 0 && j == 0 && qn > 0) ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, qn);
+        if (j & 1) ++loads1; else ++loads0;
+        if (kv == 0 && j == 0 && sc > 0) {
+          ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
+          if (ok) qn = sc + 1;
+        }
       }
       ok = ok && !cache_raised(abort_flag);
       if (!ok) break;
-      ++qn;
       fired0 += blocks >> 1;
       fired1 += 1 + ((blocks - 1) >> 1);
       outs0 += g.blocks(0) > 0 ? 1 : 0;
       outs1 += g.blocks(1) > 0 ? 1 : 0;
-      loads0 += (blocks + 1) >> 1;
-      loads1 += blocks >> 1;
     }
     if (lane == 0) {
       if (!ok) *abort_flag = 1;
