@@ -27,8 +27,8 @@
 // heads, 124-127 us, 6.5 TB/s; 64 of 200-8000, 4 KV heads, pages of 16, 98-102 us, 5.8 TB/s, the cache's bytes
 // read once and nothing else. 64 of 700-4000 with 16 heads of 64: 140 us, 4.4 TB/s, where the pages hold a
 // head's rows 128 bytes at a time among the others'; 5.8 TB/s where they hold them one behind the other. One
-// request of 3425 tokens, 8 KV heads, 9.8 us: 5800 cycles to the first load, three tiles in 3600, 2900 for the
-// piece and its count, 4500 for the join.
+// request of 3425 tokens, 8 KV heads, 9.4 us: 5700 cycles to the first load, two tiles in 3600, 2500 for the
+// piece and its count, 3500 for the join.
 //
 // Warps 0-3 compute, warp 4 loads. Every wait is bounded; a CTA whose wait gives up records
 // AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and their
@@ -541,9 +541,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       if (!sh.last) continue;
       // Eight pieces of a row at a time or two of four rows, whichever takes fewer turns, each of which is one
       // trip to L2; a row's reference moves between turns. (One request of 3425 tokens, 7 rows a head in 27
-      // pieces: 12.8 us the one way, 14.6 the other; 16 of 700-4000, 16 rows in 2 or 3: 39.5 and 37.9. Sixteen
-      // pieces at a time took longer, 10.2 against 9.6 us: the first pass over straight-line code costs more
-      // than its loads.)
+      // pieces: 12.6 us the one way, 14.6 the other; 16 of 700-4000, 16 rows in 2 or 3: 39.5 and 37.9.) Beyond
+      // 16 pieces, join_many: the first 11.0 us so, five tokens of 32 heads 18.7 -> 16.5. (For the second, and
+      // for ten pieces a head, it would take 0.3 to 1.2 us more.)
       auto join = [&](auto rows_at_once) {
         constexpr int N = decltype(rows_at_once)::value, P = 8 / N;
         for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
@@ -599,8 +599,71 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
             if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
         }
       };
+      // A row in many pieces: their references and sums lie with the row's lanes, one or two a lane, and the
+      // weights are formed once, while the first sixteen pieces' rows are on their way.
+      auto join_many = [&]() {
+        constexpr int P = 16, E = kCacheMaxPieces / kLanes;
+        auto place = [&](int piece, int row) {
+          return piece_place(g.c0 + piece, piece == 0) * static_cast<int64_t>(kRows) + row;
+        };
+        // the warp stays together: row0 of its first lanes
+#pragma unroll 1
+        for (int row0 = warp * 32 / kLanes; row0 < rows; row0 += kAtOnce) {
+          const int row = row0 + lane / kLanes;
+          const bool here = row < rows;
+          float4 ml[E];
+          float weight[E];
+          float M = -INFINITY, L = 0.f, W = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int piece = sub + e * kLanes;
+            ml[e] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            if (piece < pieces && here) ml[e] = __ldcg(a.part_ml + place(piece, row));
+          }
+#pragma unroll 1
+          for (int k0 = 0; k0 < pieces; k0 += P) {
+            float4 x[P];
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+              x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (k0 + k < pieces && here)
+                x[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + place(k0 + k, row) * D + col));
+            }
+            if (k0 == 0) {
+#pragma unroll
+              for (int e = 0; e < E; ++e) M = fmaxf(M, ml[e].x);
+#pragma unroll 1
+              for (int o = kLanes / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+#pragma unroll
+              for (int e = 0; e < E; ++e) {
+                weight[e] = ml[e].x == -INFINITY ? 0.f : tc::ex2(ml[e].x - M);
+                L = fmaf(weight[e], ml[e].y, L);
+                W = fmaf(weight[e], ml[e].z, W);
+              }
+#pragma unroll 1
+              for (int o = kLanes / 2; o > 0; o >>= 1) {
+                L += __shfl_xor_sync(0xffffffffu, L, o);
+                W += __shfl_xor_sync(0xffffffffu, W, o);
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+              const float mine = E == 2 && k0 + k >= kLanes ? weight[E - 1] : weight[0];
+              const float f = __shfl_sync(0xffffffffu, mine, k0 + k, kLanes);
+              v.x = fmaf(f, x[k].x, v.x);
+              v.y = fmaf(f, x[k].y, v.y);
+              v.z = fmaf(f, x[k].z, v.z);
+              v.w = fmaf(f, x[k].w, v.w);
+            }
+          }
+          if (here) store_row<D>(a, g, row, col, v, M, L, W);
+        }
+      };
       const int turns = (rows + kAtOnce - 1) / kAtOnce;  // of one row a thread
-      if ((turns + 3) / 4 * ((pieces + 1) / 2) < turns * ((pieces + 7) / 8)) join(std::integral_constant<int, 4>{});
+      const int few = (turns + 3) / 4 * ((pieces + 1) / 2);
+      if (pieces > 16 && turns * 2 < few) join_many();
+      else if (few < turns * ((pieces + 7) / 8)) join(std::integral_constant<int, 4>{});
       else join(std::integral_constant<int, 1>{});
     }
   }

@@ -241,6 +241,15 @@ def test_long_requests(Hq, Hkv, d, requests):
     b.check(c.o, c.lse)
 
 
+@pytest.mark.parametrize("Hq,Hkv,d", [(7, 1, 64), (2, 2, 64), (28, 4, 128), (5, 1, 128)])
+@pytest.mark.parametrize("seq,new", [(1500, 1), (2111, 1), (3425, 4), (5000, 2), (20000, 1)])
+def test_one_request_in_few_and_many_pieces(Hq, Hkv, d, seq, new):
+    b = Batch([(seq, new)], Hq, Hkv, d, 48, seed=seq)
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
 @pytest.mark.parametrize("R", [159, 160, 161, 700])
 def test_many_requests(R):
     rng = np.random.default_rng(R)
