@@ -499,7 +499,9 @@ AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* c
  * pages or 2^31 - 256 tokens, or more than max_new new tokens are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing
  * is written; a page outside [0, n_pages) is recorded too, is not read, and leaves its request's rows
  * unspecified. Slots behind a request's last token may hold anything; a value of a later new token
- * that is not finite may reach the earlier tokens of its chunk (0 * inf). Asynchronous on `stream`. */
+ * that is not finite may reach the earlier tokens of its chunk (0 * inf). n_requests + n_tokens /
+ * (2 * (128 / G)), G query heads a KV head, times n_kv_heads, above 2^27 returns AVTP_ERR_RANGE.
+ * Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                             void* workspace, size_t workspace_bytes, avtp_stream_t stream);
 
