@@ -496,11 +496,12 @@ AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* c
 /* Products on bf16 operands with fp32 accumulation, softmax in fp32, P rounded to bf16 before
  * P V as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run.
  * Offsets that decrease or pass n_tokens, a length that is negative or longer than max_pages
- * pages or 2^31 - 256 tokens, or more than max_new new tokens are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing
- * is written; a page outside [0, n_pages) is recorded too, is not read, and leaves its request's rows
- * unspecified. Slots behind a request's last token may hold anything; a value of a later new token
- * that is not finite may reach the earlier tokens of its chunk (0 * inf). n_requests + n_tokens /
- * (2 * (128 / G)), G query heads a KV head, times n_kv_heads, above 2^27 returns AVTP_ERR_RANGE.
+ * pages or 2^31 - 256 tokens, or more than max_new new tokens are recorded as
+ * AVTP_ERR_DEVICE_INPUT, and then nothing is written; a page outside [0, n_pages) is recorded too,
+ * is not read, and leaves its request's rows unspecified. Slots behind a request's last token may
+ * hold anything; a value of a later new token that is not finite may reach the earlier tokens of its
+ * chunk (0 * inf). With G query heads a KV head, (n_requests + n_tokens / (2 * (128 / G))) *
+ * n_kv_heads above 2^27 returns AVTP_ERR_RANGE.
  * Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                             void* workspace, size_t workspace_bytes, avtp_stream_t stream);
