@@ -824,7 +824,8 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
     while (static_cast<double>(blocks) * static_cast<double>((tiles >> sft) + 4) * c.n_kv_heads >= 2147483648.0) ++sft;
     return sft;
   };
-  const int64_t keys = static_cast<int64_t>(a.max_pages) * c.page_size;
+  // a request's keys, at most (CacheRequest refuses more)
+  const int64_t table = static_cast<int64_t>(a.max_pages) * c.page_size, keys = table < kCacheMostKeys ? table : kCacheMostKeys;
   const int grid = device_sm_count();
   cudaError_t e = launch_kernel(k_cache_prep, dim3(1), dim3(kPrepThreads), 0, s, /*pdl=*/true, d, grid);
   if (e != cudaSuccess || a.n_tokens == 0) return e;

@@ -459,6 +459,18 @@ def test_attention_refuses_positions_of_more_than_32_bits(new):
         assert (o == -3.0).all()
 
 
+@pytest.mark.parametrize("new", [1, 300])
+def test_a_table_bound_of_2_to_51_keys(new):
+    """The bound alone, of which a request uses one page: steps stay as short as 2^31 keys need."""
+    b = Batch([(5000, new)], 4, 1, 128, 1 << 20, seed=19, spare_pages=0)
+    c = b.call()
+    c._a.max_pages = (1 << 31) - 1
+    c._a.table_stride = (1 << 31) - 1
+    c.run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+
+
 def test_buffers_of_a_call_on_another_stream_are_that_streams():
     """Work still queued on the current stream writes memory that it has given back; a call on a side
     stream must not be handed that memory for its outputs or workspace."""
