@@ -27,10 +27,11 @@
 // heads, 124-127 us, 6.5 TB/s; 64 of 200-8000, 4 KV heads, pages of 16, 98-102 us, 5.8 TB/s, the cache's bytes
 // read once and nothing else. 64 of 700-4000 with 16 heads of 64: 140 us, 4.4 TB/s, where the pages hold a
 // head's rows 128 bytes at a time among the others'; 5.8 TB/s where they hold them one behind the other. One
-// request of 3425 tokens, 8 KV heads, 9.4 us: 5700 cycles to the first load, two tiles in 3600, 2500 for the
+// request of 3425 tokens, 8 KV heads, 9.1 us: 5700 cycles to the first load, two tiles in 3600, 2500 for the
 // piece and its count, 3500 for the join.
 //
-// Warps 0-3 compute, warp 4 loads. Every wait is bounded; a CTA whose wait gives up records
+// Warps 0-3 compute, warp 4 makes segments and loads keys, warp 5 values (one warp for both: one request of
+// 3425 tokens 9.3 us instead of 9.05, four of 50000 124.3 instead of 123.6). Every wait is bounded; a CTA whose wait gives up records
 // AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and their
 // values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 #include <cudaTypedefs.h>
@@ -42,9 +43,9 @@
 namespace avtp {
 namespace {
 
-constexpr int kThreads = 160;
+constexpr int kThreads = 192;
 constexpr int kConsumers = 128;
-constexpr int kLoadWarp = 4;
+constexpr int kKeyWarp = 4;  // and the one behind it for the values
 constexpr int kPrepThreads = 256;
 // A tile's share of a row's sum above kRescaleSum moves the row's reference, if its maximum exceeds
 // the reference by more than kRescaleTau (log2 units).
@@ -82,7 +83,7 @@ struct Shared {
   uint64_t seg_full[2], seg_empty[2];
   Segment seg[2];
   CachePlan<kThreads> plan;
-  CacheWindow window;
+  CacheWindow window[2];  // of the keys' warp, of the values'
   float m[4][16], l[4][16], w[4][16];  // reference, sum of P, of its rounded values
   int32_t last;
   int abort, bad_page;
@@ -202,12 +203,12 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
-      tc::mbar_init(&sh.kv_full[s], 1);
+      tc::mbar_init(&sh.kv_full[s], 2);
       tc::mbar_init(&sh.kv_empty[s], 4);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&sh.seg_full[s], 1);
-      tc::mbar_init(&sh.seg_empty[s], 4);
+      tc::mbar_init(&sh.seg_empty[s], 5);
     }
     sh.abort = 0;
     sh.bad_page = -1;
@@ -217,7 +218,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   }
   CacheRequest mine{};  // a lane's request of a call of few: on its way while the barriers are made
   bool mine_ok = true;
-  if (warp == kLoadWarp && lane < a.R) mine_ok = mine.load(a, lane);
+  if (warp == kKeyWarp && lane < a.R) mine_ok = mine.load(a, lane);
   pdl_trigger();
   __syncthreads();
   auto steps = [&](const CacheRequest& q, int& most) {
@@ -228,76 +229,91 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   if (a.R > kNearRequests) sh.plan.form(a, steps);
   volatile int* abort_flag = &sh.abort;
 
-  if (warp == kLoadWarp) {
-    // ------------------------------------------------------------ segments and loads
-    const CacheLine line(a, sh.plan, mine, mine_ok, steps);
-    const CacheRuns runs(line.total, line.most, 1, cache_ctas(a, line.weights, true));
-    const int t0 = runs.begin(blockIdx.x), t1 = runs.begin(blockIdx.x + 1);
+  if (warp >= kKeyWarp) {
+    // ------------------------------------------------------------ segments and keys; values
+    const int kv = warp == kKeyWarp ? 0 : 1;
+    const CUtensorMap* map = kv ? &mapV : &mapK;
     const int per_tile = kTile / a.box;
-    int pre = 0;  // steps before request r
-    int r = t0 < t1 ? line.find(a, sh.plan, t0, &pre) : 0;
-    int n = 0, sc = 0;
+    CacheLine line;
+    CacheRuns runs;
+    int t = 0, t1 = 0, pre = 0, r = 0;  // steps: next, the run's end, before request r
+    if (kv == 0) {
+      line = CacheLine(a, sh.plan, mine, mine_ok, steps);
+      runs = CacheRuns(line.total, line.most, 1, cache_ctas(a, line.weights, true));
+      t = runs.begin(blockIdx.x);
+      t1 = runs.begin(blockIdx.x + 1);
+      if (t < t1) r = line.find(a, sh.plan, t, &pre);
+    }
+    int n = 0;
     bool fine = true;
 #pragma unroll 1
-    for (int t = t0; fine; ++sc) {
+    for (int sc = 0; fine; ++sc) {
       Segment g{};
-      g.head = -1;
-      int end = t;
-      if (t < t1) {
-        CacheRequest q;
-        int tiles, len;  // tiles and steps of a row block
+      if (kv == 1) {
+        fine = cache_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1);
+        if (!fine) break;
+        g = sh.seg[sc & 1];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.seg_empty[sc & 1]);
+      } else {
+        g.head = -1;
+        int end = t;
+        if (t < t1) {
+          CacheRequest q;
+          int tiles, len;  // tiles and steps of a row block
 #pragma unroll 1
-        for (;; ++r) {
-          q = line.request(a, mine, r);
-          tiles = tiles_of<D>(a, q);
-          len = steps_of(a, tiles);
-          if (t < pre + len * a.Hkv) break;
-          pre += len * a.Hkv;
+          for (;; ++r) {
+            q = line.request(a, mine, r);
+            tiles = tiles_of<D>(a, q);
+            len = steps_of(a, tiles);
+            if (t < pre + len * a.Hkv) break;
+            pre += len * a.Hkv;
+          }
+          g.head = static_cast<int>(static_cast<uint32_t>(t - pre) / static_cast<uint32_t>(len));
+          const int s = pre + g.head * len;  // the block's first step
+          end = min(t1, s + len);
+          g.row0 = q.row0;
+          g.n = q.n;
+          g.seq = q.seq;
+          g.tile0 = (t - s) << a.step_shift;
+          g.tile1 = min(tiles, (end - s) << a.step_shift);
+          g.c0 = t == s ? static_cast<int>(blockIdx.x) : runs.run(s);
+          g.c1 = end == s + len ? static_cast<int>(blockIdx.x) : runs.run(s + len - 1);
+          g.req = r;
         }
-        g.head = static_cast<int>(static_cast<uint32_t>(t - pre) / static_cast<uint32_t>(len));
-        const int s = pre + g.head * len;  // the block's first step
-        end = min(t1, s + len);
-        g.row0 = q.row0;
-        g.n = q.n;
-        g.seq = q.seq;
-        g.tile0 = (t - s) << a.step_shift;
-        g.tile1 = min(tiles, (end - s) << a.step_shift);
-        g.c0 = t == s ? static_cast<int>(blockIdx.x) : runs.run(s);
-        g.c1 = end == s + len ? static_cast<int>(blockIdx.x) : runs.run(s + len - 1);
-        g.req = r;
+        if (sc >= 2) fine = cache_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
+        if (!fine) break;
+        if (lane == 0) {
+          sh.seg[sc & 1] = g;
+          tc::mbar_arrive(&sh.seg_full[sc & 1]);
+        }
+        __syncwarp();
+        t = end;
       }
-      if (sc >= 2) fine = cache_wait_warp(&sh.seg_empty[sc & 1], ((sc >> 1) - 1) & 1);
-      if (!fine) break;
-      if (lane == 0) {
-        sh.seg[sc & 1] = g;
-        tc::mbar_arrive(&sh.seg_full[sc & 1]);
-      }
-      __syncwarp();
       if (g.head < 0) break;
       const int32_t* row = a.table + g.req * a.table_stride;
       for (int tile = g.tile0; tile < g.tile1 && !cache_raised(abort_flag); ++tile, ++n) {
         const int i0 = tile * per_tile, sb = n % kStages;
         if (tile == g.tile0 || (i0 & 31) == 0)
-          if (sh.window.load(a, row, g.seq, i0 & ~31)) sh.bad_page = g.req;
+          if (sh.window[kv].load(a, row, g.seq, i0 & ~31)) sh.bad_page = g.req;
         const int keys = min(kTile, g.seq - tile * kTile);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
         if (tc::elect_one()) {
           if (n >= kStages && !cache_wait(&sh.kv_empty[sb], (n / kStages - 1) & 1)) {
             *abort_flag = 1;
           } else {
-            tc::mbar_arrive_expect_tx(&sh.kv_full[sb], boxes * a.box * D * 4);
-            unsigned char* dst = smem + sb * stage_bytes(D);
+            tc::mbar_arrive_expect_tx(&sh.kv_full[sb], boxes * a.box * D * 2);
+            unsigned char* dst = smem + sb * stage_bytes(D) + kv * (stage_bytes(D) / 2);
+#pragma unroll 1
             for (int b = 0; b < boxes; ++b, dst += a.box * D * 2) {
-              const int2 at = sh.window.at[(i0 + b) & 31];
-              tma_load_5d(dst, &mapK, at.y, g.head, at.x, &sh.kv_full[sb]);
-              tma_load_5d(dst + stage_bytes(D) / 2, &mapV, at.y, g.head, at.x, &sh.kv_full[sb]);
+              const int2 at = sh.window[kv].at[(i0 + b) & 31];
+              tma_load_5d(dst, map, at.y, g.head, at.x, &sh.kv_full[sb]);
             }
           }
         }
         __syncwarp();
       }
       fine = !cache_raised(abort_flag);
-      t = end;
     }
     if (!fine && lane == 0) *abort_flag = 1;
     // let the copies in flight land before the CTA may exit
