@@ -350,7 +350,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           qa[ks][i] = row < rows ? src[ks * 8 + tq] : 0u;
           qa[ks][i + 2] = row < rows ? src[ks * 8 + tq + 4] : 0u;
         }
-        if (row >= rows) limit[i] = 0x7fffffff;  // a row that is not stored: q = 0, and no mask
+        // A row that is not stored: q = 0. It sees no more than the others, or 0 x NaN behind the request's
+        // last key would have its warp look for the maximum and move stored rows' references.
+        if (row >= rows) limit[i] = g.seq;
       }
       const int all_see = g.seq - g.n + 1;  // keys that every row sees
 
