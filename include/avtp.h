@@ -411,7 +411,7 @@ typedef struct {
  * from entry *free_head on, request by request. cu_new may be out_cu_seqlens of avtp_prune: the
  * pruned lengths are used where they were made, with no host round trip. */
 typedef struct {
-  int32_t n_requests;          /* R >= 1                                                     */
+  int32_t n_requests;          /* R >= 1, at most 2^31 - 1025                                */
   int64_t n_tokens;            /* length of slot_map, >= cu_new[R] (host); < 2^31            */
   int32_t page_size;           /* >= 1                                                       */
   int64_t n_pages;             /* of the pool; n_pages * page_size < 2^31                    */

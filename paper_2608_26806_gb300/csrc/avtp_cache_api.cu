@@ -51,6 +51,8 @@ avtp_status_t check_slots(const avtp_cache_slots_args_t* a) {
   const avtp_status_t st = check_pool_size(a->n_pages, a->page_size);
   if (st != AVTP_OK) return st;
   if (a->n_tokens > kInt32Max || a->n_free > kInt32Max) return AVTP_ERR_RANGE;
+  // the kernel's 32-bit loops over the requests step 1024 at a time, past the last
+  if (a->n_requests > kInt32Max - 1024) return AVTP_ERR_RANGE;
   if (a->n_free < 0 || a->table_stride < a->max_pages) return AVTP_ERR_INVALID_ARG;
   if (a->cu_new == nullptr || a->block_table == nullptr || a->seq_len == nullptr) return AVTP_ERR_INVALID_ARG;
   if ((a->n_tokens > 0 && a->slot_map == nullptr) || (a->n_free > 0 && a->free_pages == nullptr))

@@ -60,6 +60,14 @@ def test_slots_arguments(lib, field, value, code):
     assert lib.avtp_cache_slots_workspace_size(ctypes.byref(a), ctypes.byref(size)) == code
 
 
+@pytest.mark.parametrize("R,code", [((1 << 31) - 1, G), ((1 << 31) - 1024, G), ((1 << 31) - 1025, avtp.OK)])
+def test_slots_refuse_more_requests_than_their_loops_count(lib, R, code):
+    a, size = _with(_slots(), n_requests=R), ctypes.c_size_t()
+    assert lib.avtp_cache_slots_workspace_size(ctypes.byref(a), ctypes.byref(size)) == code
+    if code != avtp.OK:
+        assert lib.avtp_cache_slots(ctypes.byref(a), FAKE, BIG, None) == code
+
+
 def test_workspaces_are_checked(lib):
     c, s, w, a = _cache(), _slots(), _write(), _attn()
     size = ctypes.c_size_t()
