@@ -1,13 +1,17 @@
 """The paged cache on the GPU: what lies outside the requests' tokens, bounds far above them, and the
 forms of slots and writes that large calls take."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2608_26806_gb300 import avtp
+from paper_2608_26806_gb300 import avtp, synth
 from tests.cache_util import Batch
-from tests.gpu_util import ensure_built
+from tests.gpu_util import DevWorkload, ensure_built
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 pytestmark = pytest.mark.gpu
 
 
@@ -45,3 +49,36 @@ def test_slots_behind_a_requests_last_token_change_no_bit(Hq, Hkv, d):
         got.append((c.o, c.lse))
     for o, lse in got[1:]:
         assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1])
+
+
+# ---------------------------------------------------------------- the documented calls
+def test_the_readme_example_attends_to_the_kept_tokens_and_the_new_ones():
+    """The example run as it stands: the new tokens' rows against 64 bits over the kept rows and their own."""
+    with open(os.path.join(ROOT, "README.md"), encoding="utf-8") as f:
+        code = [c for c in re.findall(r"```python\n(.*?)```", f.read(), re.S) if "cache_attention" in c]
+    assert len(code) == 1
+    segs = [[("t", 5), ("i", 300), ("t", 9)], [("i", 64), ("t", 7)], [("t", 12), ("i", 500), ("t", 2)]]
+    wl = synth.make_custom(segs, keep_ratio=0.3, n_q_heads=32, n_kv_heads=8, head_dim=128, hidden=256, pos_planes=3)
+    dw = DevWorkload(wl)
+    g = torch.Generator(device="cuda").manual_seed(5)
+
+    def rand(*shape):
+        return torch.randn(*shape, device="cuda", generator=g).to(torch.bfloat16)
+
+    R, T, n_pages = 3, wl.layout.n_tokens, 40
+    env = dict(q=dw.t["q"], k=dw.t["k"], v=rand(T, 8, 128), h_cur=dw.t["h_cur"], h_prior=dw.t["h_prior"],
+               pos=dw.t["pos"], keep_ratio=dw.keep_ratio, keep_ratio_np=wl.keep_ratio, cu_seqlens=wl.layout.cu_seqlens,
+               img_cu=wl.layout.img_cu, img_start=wl.layout.img_start, img_len=wl.layout.img_len, n_pages=n_pages,
+               table=torch.full((R, 12), -1, dtype=torch.int32, device="cuda"),
+               free=torch.randperm(n_pages, device="cuda", generator=g).to(torch.int32),
+               q_new=rand(R, 32, 128), k_new=rand(R, 8, 128), v_new=rand(R, 8, 128),
+               cu_new=torch.arange(R + 1, dtype=torch.int32, device="cuda"))
+    exec(compile(code[0], "README.md", "exec"), env)  # noqa: S102
+    kept, cu = env["out"].kept_idx.long(), env["out"].out_cu_seqlens.cpu().numpy()
+    rows = [tuple(torch.cat([env[x][kept[cu[r]:cu[r + 1]]], env[x + "_new"][r:r + 1]]).cpu() for x in ("k", "v"))
+            for r in range(R)]
+    b = Batch.__new__(Batch)
+    b.__dict__.update(requests=[(len(kr), 1) for kr, _ in rows], Hq=32, Hkv=8, d=128, cu=np.arange(R + 1),
+                      q=env["q_new"].cpu(), rows=rows)
+    assert env["seq_len"].tolist() == [s for s, _ in b.requests]
+    b.check(env["o"], env["lse"])
