@@ -471,7 +471,8 @@ AVTP_API avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_ca
 typedef struct {
   int32_t n_requests;          /* R >= 1                                                     */
   int64_t n_tokens;            /* rows of q and o, >= cu_new[R] (host); < 2^31. Rows behind
-                                * cu_new[R] are neither read nor written                     */
+                                * cu_new[R] are not written; those of q may be read, and
+                                * change no result                                           */
   int32_t max_new;             /* n_r is at most this (host)                                 */
   int32_t n_q_heads;           /* a multiple of n_kv_heads, at most 128 times as many        */
   const void* q;               /* device bf16 [n_tokens, n_q_heads, head_dim], contiguous heads;

@@ -16,7 +16,7 @@ struct CacheAttnDev {
   const int32_t* table;
   int64_t table_stride;
   int64_t n_tokens, n_pages;
-  int R, max_new, max_pages, Hq, Hkv, G, page_size;
+  int R, max_new, max_pages, Hkv, G, page_size;
   int box;           // rows of a TMA box: a power of two that divides the page size, at most a tile
   int step_shift;    // see CachePlan
   int both;          // both kernels are at work and share the SMs (see cache_ctas)

@@ -818,7 +818,6 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
   d.R = a.n_requests;
   d.max_new = a.max_new;
   d.max_pages = a.max_pages;
-  d.Hq = a.n_q_heads;
   d.Hkv = c.n_kv_heads;
   d.G = a.n_q_heads / c.n_kv_heads;
   d.page_size = c.page_size;

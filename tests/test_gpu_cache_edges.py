@@ -51,6 +51,32 @@ def test_slots_behind_a_requests_last_token_change_no_bit(Hq, Hkv, d):
         assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1])
 
 
+@pytest.mark.parametrize("Hq,Hkv,d,requests", [
+    (2, 2, 64, [(33, 33)]),  # fewer rows than a tile's tokens
+    (8, 2, 128, [(300, 129), (40, 40), (513, 200)]),
+    (34, 1, 128, [(70, 70), (9, 5)]),
+], ids=["short", "chunks", "odd_group"])
+def test_chunks_take_no_bit_from_slots_or_queries_behind_the_last(Hq, Hkv, d, requests):
+    """A chunk's last tile of queries reaches behind the last request, its last block of keys behind the last
+    token: zeros, NaN and infinities there."""
+    b = Batch(requests, Hq, Hkv, d, 64, seed=Hq, tail=70)
+    live = int(b.cu[-1])
+    spare_k, spare_v = torch.isnan(b.cache.k), torch.isnan(b.cache.v)
+    got = []
+    for fill in (0.0, float("nan"), float("inf"), -3e38):
+        b.cache.k[spare_k] = fill
+        b.cache.v[spare_v] = fill
+        b.dev["q"][live:] = fill
+        o = torch.full_like(b.dev["q"], 5.0)
+        c = b.call(o=o).run()
+        assert status(c) == avtp.OK
+        b.check(c.o, c.lse)
+        assert (o[live:] == 5.0).all()
+        got.append((o[:live].clone(), c.lse[:, :live].clone()))
+    for o, lse in got[1:]:
+        assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1])
+
+
 # ---------------------------------------------------------------- the documented calls
 def test_the_readme_example_attends_to_the_kept_tokens_and_the_new_ones():
     """The example run as it stands: the new tokens' rows against 64 bits over the kept rows and their own."""
