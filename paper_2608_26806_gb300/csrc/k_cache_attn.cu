@@ -43,9 +43,11 @@
 namespace avtp {
 namespace {
 
-constexpr int kThreads = 192;
-constexpr int kConsumers = 128;
-constexpr int kKeyWarp = 4;  // and the one behind it for the values
+constexpr int kWarps = 4;  // that compute
+constexpr int kConsumers = 32 * kWarps;
+constexpr int kKeyWarp = kWarps;  // and the one behind it for the values
+constexpr int kThreads = kConsumers + 64;
+constexpr int kConsumerBar = 1;  // named barrier of the computing warps
 constexpr int kPrepThreads = 256;
 // A tile's share of a row's sum above kRescaleSum moves the row's reference, if its maximum exceeds
 // the reference by more than kRescaleTau (log2 units).
@@ -73,10 +75,8 @@ constexpr int kStages = 5;
 // rows of an accumulator's column pair fall into different banks.
 __host__ __device__ constexpr int out_row(int d) { return d + 8; }
 __host__ __device__ constexpr size_t smem_bytes(int d) {
-  return 1024 + static_cast<size_t>(kStages) * stage_bytes(d) + 4 * 16 * out_row(d) * 4;
+  return 1024 + static_cast<size_t>(kStages) * stage_bytes(d) + kWarps * 16 * out_row(d) * 4;
 }
-static_assert(smem_bytes(128) <= 200 * 1024 && smem_bytes(64) <= 200 * 1024, "shared memory of one CTA");
-
 template <int D>
 struct Shared {
   uint64_t kv_full[kStages], kv_empty[kStages];
@@ -84,10 +84,13 @@ struct Shared {
   Segment seg[2];
   CachePlan<kThreads> plan;
   CacheWindow window[2];  // of the keys' warp, of the values'
-  float m[4][16], l[4][16], w[4][16];  // reference, sum of P, of its rounded values
+  float m[kWarps][16], l[kWarps][16], w[kWarps][16];  // reference, sum of P, of its rounded values
   int32_t last;
   int abort, bad_page;
 };
+constexpr size_t kMostShared = 227 * 1024;  // of a CTA
+static_assert(smem_bytes(128) + sizeof(Shared<128>) <= kMostShared && smem_bytes(64) + sizeof(Shared<64>) <= kMostShared,
+              "shared memory of one CTA");
 
 // ---------------------------------------------------------------- validation
 // The first kernel of a call: the status word, the counters, and what the lengths have wrong. The
@@ -111,15 +114,17 @@ __global__ void __launch_bounds__(kPrepThreads) k_cache_prep(CacheAttnDev a, int
 }
 
 // ---------------------------------------------------------------- building blocks
-__device__ __forceinline__ void bar_consumers() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void bar_consumers() {
+  asm volatile("bar.sync %0, %1;" ::"n"(kConsumerBar), "n"(kConsumers) : "memory");
+}
 // The same, and whether x holds for any of them: what decides whether they go on has to be one answer
 // for all, or some would wait for others that have left.
 __device__ __forceinline__ bool bar_consumers_any(bool x) {
   uint32_t any;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(any)
-      : "r"(x ? 1u : 0u)
+      : "r"(x ? 1u : 0u), "n"(kConsumerBar), "n"(kConsumers)
       : "memory");
   return any != 0;
 }
@@ -183,6 +188,11 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
   return (tiles + (1 << a.step_shift) - 1) >> a.step_shift;
 }
 
+// A wait looks at one bit of a barrier's phase, so a warp may be at most one phase behind what it waits for.
+// Every computing warp therefore waits for every tile of the ring, in order, and both loading warps for every
+// release. (Warps that took tiles in turn, each waiting for its own alone, could find the ring's turn before
+// still on its way, pass, release the stage early and have the loader arrive on a phase with no arrival left.)
+//
 // mapK, mapV: the cache as {64 elements, row of the page, panel of 64, head, page}, box of `box` rows
 // and all panels of one head and page: one TMA instruction a page piece. (One a panel, at pages of 16
 // rows 16 of them a tile, issued too slowly: 4.4 TB/s.) kWM warps share the keys of a slice of the tile, 16
@@ -193,9 +203,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   extern __shared__ unsigned char smem_raw[];
   __shared__ Shared<D> sh;
   constexpr int kRows = 16 * kWM;
-  constexpr int kSlices = 4 / kWM;            // slices of a tile's keys
+  constexpr int kSlices = kWarps / kWM;       // slices of a tile's keys
   constexpr int kTile = tile_keys(D);
   constexpr int kKeys = kTile / kSlices;      // keys of a slice
+  static_assert(kWarps % kWM == 0 && kKeys % 16 == 0 && kConsumers % (D / 4) == 0, "the computing warps' shares");
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   float* s_out = reinterpret_cast<float*>(smem + kStages * stage_bytes(D));
@@ -203,12 +214,12 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
-      tc::mbar_init(&sh.kv_full[s], 2);
-      tc::mbar_init(&sh.kv_empty[s], 4);
+      tc::mbar_init(&sh.kv_full[s], 2);  // the keys' copies and the values'
+      tc::mbar_init(&sh.kv_empty[s], kWarps);
     }
     for (int s = 0; s < 2; ++s) {
       tc::mbar_init(&sh.seg_full[s], 1);
-      tc::mbar_init(&sh.seg_empty[s], 5);
+      tc::mbar_init(&sh.seg_empty[s], kWarps + 1);  // and the values' warp
     }
     sh.abort = 0;
     sh.bad_page = -1;

@@ -55,11 +55,12 @@ namespace {
 
 constexpr int kQT = 128;  // rows of a slot (MMA M, TMEM lanes)
 constexpr int kKB = kChunkKeys;  // MMA N of Q K^T, K of P V
-constexpr int kThreads = 352;
 constexpr int kSlotWarps = 4;
-constexpr int kKeyWarp = 8;
-constexpr int kMmaWarp = 9;
-constexpr int kValueWarp = 10;
+constexpr int kKeyWarp = 2 * kSlotWarps;
+constexpr int kMmaWarp = kKeyWarp + 1;
+constexpr int kValueWarp = kMmaWarp + 1;
+constexpr int kThreads = 32 * (kValueWarp + 1);
+static_assert(kSlotWarps * 32 == kQT, "a thread a row of a slot");
 constexpr int kStages = 4;      // key or value blocks in shared memory
 // A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first
 // softmax with nothing to overlap, its rows' way out): its steps on the line are its blocks and these.
@@ -86,7 +87,6 @@ __host__ __device__ constexpr size_t chunk_smem_bytes(int d) {
   // shares an SM
   return need > 116 * 1024 ? need : 116 * 1024;
 }
-static_assert(chunk_smem_bytes(128) + sizeof(int64_t) * (kThreads + 1) <= 224 * 1024, "shared memory of one CTA");
 
 // A run's part of one unit: key blocks j0 .. j1 - 1.
 struct Segment {
@@ -125,6 +125,7 @@ struct ChunkSync {
   uint32_t tmem;
   int abort, bad_page;
 };
+static_assert(chunk_smem_bytes(128) + sizeof(ChunkSync) <= 227 * 1024, "shared memory of one CTA");
 
 // sum_{i < n} floor((a i + b) / m), by Euclid's steps on (a, m); a n + b is below 2^32, the sum below 2^31.
 __host__ __device__ inline uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
@@ -579,7 +580,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         if (masked && quad == 0 && valid < kKB && valid > 0) {
           // the request's keys end in this block: the values behind them that share the last
           // 16-key step are whatever the page held and are multiplied by P = 0; they are
-          // cleared, so that nothing there (an infinity or a NaN) reaches a row
+          // cleared, so that nothing there (an infinity or a NaN) reaches a row. (The stage's values
+          // before these have been multiplied, or S_j would not be here: the phase waited for is the next.)
           const int sb = 2 * (j & 1) + 1;
           ok = cache_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
           if (!ok) break;
