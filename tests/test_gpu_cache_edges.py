@@ -77,6 +77,51 @@ def test_chunks_take_no_bit_from_slots_or_queries_behind_the_last(Hq, Hkv, d, re
         assert torch.equal(o, got[0][0]) and torch.equal(lse, got[0][1])
 
 
+def _step_shift(blocks, keys, tile, Hkv):
+    """The library's rule: steps of a line of `blocks` row blocks a KV head stay below 2^31."""
+    shift = 0
+    while blocks * ((keys // tile >> shift) + 4) * Hkv >= 1 << 31:
+        shift += 1
+    return shift
+
+
+MANY = [(int(n), 1) for n in np.random.default_rng(8).integers(0, 3000, 34)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hkv,requests", [
+    (8, [(4100, 1), (0, 1), (3000, 1)] + [(700, 1)] * 14),
+    (8, [(2500, 1), (2300, 560), (900, 40)] + [(1500, 1)] * 14),  # 560 tokens of 16 heads: 35 blocks of rows
+    (4, MANY + [(1, 1), (3500, 1)]),
+    (4, MANY + [(2200, 544), (1200, 30)]),
+], ids=["step", "chunk", "many", "many_chunks"])
+def test_steps_of_several_tiles(Hkv, requests, d):
+    """A table for 2^31 keys, with which a line of single tiles would pass 2^31 steps in either kernel: steps of
+    two or more, several of them a row block and more than there are CTAs, so that runs end inside blocks."""
+    G, page, columns = 16, 1024, 1 << 21
+    R, T = len(requests), sum(n for _, n in requests)
+    keys = min(columns * page, (1 << 31) - 256)
+    few = _step_shift(R, keys, 64 if d == 128 else 128, Hkv)
+    assert few > 0
+    ctas = torch.cuda.get_device_properties(0).multi_processor_count
+    if max(n for _, n in requests) > 1:
+        chunk = _step_shift(R + T // (2 * (128 // G)), keys, 128, Hkv)
+        assert chunk > 0 and max(n for _, n in requests) > 32 * 2 * (128 // G)
+        assert max(s for s, n in requests if n > 1) > 4 * (128 << chunk)
+    else:
+        tile = (64 if d == 128 else 128) << few
+        assert sum(-(-s // tile) for s, _ in requests) * Hkv > ctas and max(s for s, _ in requests) > 4 * tile
+    b = Batch(requests, G * Hkv, Hkv, d, page, seed=21, spare_pages=1)
+    wide = torch.full((R, columns), -7, dtype=torch.int32, device="cuda")
+    wide[:, :b.table.shape[1]] = b.dev["table"]
+    b.dev["table"] = wide
+    c = b.call().run()
+    assert status(c) == avtp.OK
+    b.check(c.o, c.lse)
+    again = b.call().run()
+    assert torch.equal(c.o, again.o) and torch.equal(c.lse, again.lse)
+
+
 # ---------------------------------------------------------------- the documented calls
 def test_the_readme_example_attends_to_the_kept_tokens_and_the_new_ones():
     """The example run as it stands: the new tokens' rows against 64 bits over the kept rows and their own."""
