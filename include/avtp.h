@@ -433,8 +433,10 @@ AVTP_API avtp_status_t avtp_cache_slots_workspace_size(const avtp_cache_slots_ar
 /* Writes block_table's new entries (the others stay as they are), seq_len, slot_map and
  * free_head_out. Offsets that decrease or pass n_tokens, negative lengths, a request longer than
  * max_pages pages, a free list that runs out, or a page to be used outside [0, n_pages) are
- * recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. With past_len and free_head
- * given as seq_len and free_head_out, replays of a captured call append step after step.
+ * recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written: an avtp_cache_write behind it on
+ * the stream uses the slots that slot_map held before, so fill it with -1 where no one looks at the
+ * status between. With past_len and free_head given as seq_len and free_head_out, replays of a
+ * captured call append step after step.
  * Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_slots(const avtp_cache_slots_args_t* args, void* workspace, size_t workspace_bytes,
                                         avtp_stream_t stream);

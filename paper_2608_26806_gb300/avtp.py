@@ -812,7 +812,9 @@ class CacheSlotsCall(_CacheCall):
     tokens ``past_len`` (int32 [R], default none). New pages come from ``free_pages`` (int32), from
     entry ``free_head`` (int32 [1], default 0) on. ``n_tokens``: at least ``cu_new[-1]``, the length
     of ``slot_map``. ``seq_len=past_len`` and ``free_head_out=free_head`` advance them in place, so
-    that replays of a captured call append step after step."""
+    that replays of a captured call append step after step. A refused call (read_device_status) writes
+    nothing: outputs of its own hold -1, or what an earlier run left, and a ``cache_write`` behind that
+    run writes to those slots again."""
 
     def __init__(self, cu_new: torch.Tensor, n_tokens: int, *, page_size: int, n_pages: int, block_table: torch.Tensor,
                  free_pages: torch.Tensor, free_head=None, past_len=None, seq_len=None, slot_map=None,
@@ -825,10 +827,14 @@ class CacheSlotsCall(_CacheCall):
         dev = _on_one_device(name, cu_new, block_table, free_pages, free_head, past_len, seq_len, slot_map,
                              free_head_out, workspace)
         self.block_table = block_table
-        self.seq_len = seq_len if seq_len is not None else torch.empty(R, dtype=torch.int32, device=dev)
-        self.slot_map = slot_map if slot_map is not None else torch.empty(int(n_tokens), dtype=torch.int32, device=dev)
-        self.free_head_out = (free_head_out if free_head_out is not None
-                              else torch.empty(1, dtype=torch.int32, device=dev))
+        # One buffer for the outputs that are made here, -1 until a call that is not refused writes them: a slot that
+        # cache_write skips, a length and a head that the next call refuses.
+        made = (0 if slot_map is not None else int(n_tokens), 0 if seq_len is not None else R,
+                0 if free_head_out is not None else 1)
+        made = torch.full((sum(made),), -1, dtype=torch.int32, device=dev).split(made)
+        self.slot_map = slot_map if slot_map is not None else made[0]
+        self.seq_len = seq_len if seq_len is not None else made[1]
+        self.free_head_out = free_head_out if free_head_out is not None else made[2]
         for what, t, shape in (("past_len", past_len, (R,)), ("seq_len", self.seq_len, (R,)),
                                ("slot_map", self.slot_map, (int(n_tokens),)), ("free_head", free_head, (1,)),
                                ("free_head_out", self.free_head_out, (1,))):

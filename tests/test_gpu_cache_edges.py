@@ -199,6 +199,24 @@ def test_slots_of_many_idle_requests_in_one_cta(R, in_place):
     assert int(c.free_head_out.item()) == want[3]
 
 
+@pytest.mark.parametrize("new", [40, 3000])
+def test_a_write_behind_refused_slots_leaves_the_cache_alone(new):
+    """A free list that runs out, found on the device: the slot map that the call made names no slot, whatever its
+    memory held before."""
+    cache = avtp.PagedCache.new(300, 16, 2, 64)
+    for t in (cache.k, cache.v):
+        t.fill_(3.0)
+    k = torch.ones(new, 2, 64, dtype=torch.bfloat16, device="cuda")
+    cu = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    table = torch.full((1, 300), -1, dtype=torch.int32, device="cuda")
+    free = torch.arange(2, dtype=torch.int32, device="cuda")
+    old = [torch.arange(new, dtype=torch.int32, device="cuda") for _ in range(4)]  # slots of another step
+    del old
+    slots, _, _ = avtp.cache_slots(cu, new, page_size=16, n_pages=300, block_table=table, free_pages=free)
+    avtp.cache_write(cache, slots, k, k)
+    assert (cache.k == 3.0).all() and (cache.v == 3.0).all() and (table == -1).all()
+
+
 # ---------------------------------------------------------------- write
 @pytest.mark.parametrize("n", [257, 600, 40000])  # more CTAs than a cluster's, up to several rows a group of lanes
 @pytest.mark.parametrize("what", ["slot_end", "slot_negative", "row_end", "row_negative"])
