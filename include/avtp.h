@@ -497,7 +497,9 @@ AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* c
                                                            const avtp_cache_attn_args_t* args, size_t* bytes);
 
 /* Products on bf16 operands with fp32 accumulation, softmax in fp32, P rounded to bf16 before
- * P V as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run.
+ * P V as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run. Two
+ * kernels share the requests by their rows a KV head and the call's bounds, and divide O by the sum of
+ * the rounded or of the exact weights: last bits may change with the batch that a request is in.
  * Offsets that decrease or pass n_tokens, a length that is negative or longer than max_pages
  * pages or 2^31 - 256 tokens, or more than max_new new tokens are recorded as
  * AVTP_ERR_DEVICE_INPUT, and then nothing is written; a page outside [0, n_pages) is recorded too,

@@ -6,13 +6,13 @@
 // for a block of 16 kWM rows.
 //
 // What bounds it: the cache's bytes. A tile of keys and values is 32 KiB (64 keys at d = 128, 128 at d = 64),
-// 1400 cycles of an SM's share of HBM; its products, by warp-level mma.sync (32 rows are too few for a
-// tcgen05 tile), take less up to 16 rows and about as long for 32. So everything serves the stream of
-// loads: a CTA per SM, a ring of tiles filled by TMA (a box per page piece, the pages' numbers looked
-// up 32 boxes at a time), and the whole call's tiles, taken as one line (request, KV head, tile), cut into
-// equal runs, one a CTA, whatever the requests' lengths. A run that begins or ends inside a KV head's keys
-// leaves a piece (O, reference, sums) in the workspace; the CTA that finishes a head's last piece joins
-// them, in their order, so results do not depend on who came last.
+// 1400 cycles of an SM's share of HBM; its products, by warp-level mma.sync (32 rows are too few for a tcgen05
+// tile), take less up to 16 rows and about as long for 32. So everything serves the stream of loads: a CTA per
+// SM, a ring of tiles filled by TMA (a box per page piece, the pages' numbers looked up 32 boxes at a time),
+// and the whole call's tiles, taken as one line (request, KV head, tile), cut into equal runs, one a CTA, none
+// shorter than a thirtieth of the longest head's (kCacheMaxPieces). A run that begins or ends inside a KV
+// head's keys leaves a piece (O, reference, sums) in the workspace; the CTA that finishes a head's last piece
+// joins them, in their order, so results do not depend on who came last.
 //
 // Per tile and warp: S = Q K^T on the warp's kTile kWM / 4 keys and 16 rows, P = exp2(c2 S - m)
 // against the row's reference m, in bf16 straight from S's registers as the A operand of P V, and
@@ -23,17 +23,18 @@
 // tokens with some sharp queries: 2.5e-3 divided by l, 1.9e-3 so; 1.6e-3 is O's own rounding), and the
 // LSE takes l.
 //
-// Measured, calls one behind the other (d = 128, a token a request): four requests of 50000 tokens, 8 KV
-// heads, 124-127 us, 6.5 TB/s; 64 of 200-8000, 4 KV heads, pages of 16, 98-102 us, 5.8 TB/s, the cache's bytes
-// read once and nothing else. 64 of 700-4000 with 16 heads of 64: 140 us, 4.4 TB/s, where the pages hold a
-// head's rows 128 bytes at a time among the others'; 5.8 TB/s where they hold them one behind the other. One
-// request of 3425 tokens, 8 KV heads, 9.1 us: 5700 cycles to the first load, two tiles in 3600, 2500 for the
-// piece and its count, 3500 for the join.
+// Measured, calls one behind the other (d = 128, a token a request): four requests of 50000 tokens, 8 KV heads,
+// 124-127 us, 6.5 TB/s; 64 of 200-8000, 4 KV heads, pages of 16, 98-102 us, 5.8 TB/s, the cache's bytes read
+// once and nothing else. 64 of 700-4000 with 16 heads of 64: 146 us, 4.3 TB/s, where the pages hold a head's
+// rows 128 bytes at a time among the others' (of the 256 bytes that a fetch brings, half have left L2 when the
+// other head wants them: 1.43 times the keys and values come from DRAM); 111 us, 5.7 TB/s where they hold them
+// one behind the other. One request of 3425 tokens, 8 KV heads, 9.2 us: 5700 cycles to the first load, two
+// tiles in 3600, 2500 for the piece and its count, 3500 for the join.
 //
 // Warps 0-3 compute, warp 4 makes segments and loads keys, warp 5 values (one warp for both: one request of
-// 3425 tokens 9.3 us instead of 9.05, four of 50000 124.3 instead of 123.6). Every wait is bounded; a CTA whose wait gives up records
-// AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and their
-// values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
+// 3425 tokens 9.3 us instead of 9.05, four of 50000 124.3 instead of 123.6). Every wait is bounded; a CTA whose
+// wait gives up records AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and
+// their values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 #include <cudaTypedefs.h>
 
 #include <type_traits>

@@ -31,8 +31,8 @@
 // softmax has its usual path in one piece and everything else once behind it, waits and sums are calls,
 // one-time code is rolled; a second copy of the loads, or waits compiled into the issuing loop, cost 10 to
 // 60 %. The issuing loop is the exception: a copy a slot, whose descriptors are constants, is faster than
-// one for both (32 query heads, 8 KV heads, 8192 tokens behind 2176: 507 us against 533; a copy a slot and
-// parity 500, but eight requests of 700 tokens behind 300 take 90 us instead of 84 then).
+// one for both (32 query heads, 8 KV heads, 8192 tokens behind 2176, one call at full clock: 507 us against 533; a
+// copy a slot and parity 500, but eight requests of 700 tokens behind 300 take 90 us instead of 84 then).
 //
 // P is rounded to bf16 for its product and O divided by the sum l of the weights before that rounding: an
 // error of O of 2.3e-3 (2-norm, with some sharp queries; 1.6e-3 is O's own rounding). The sum of the
@@ -40,8 +40,10 @@
 // of the kernel's time here (504 -> 549 us, 491 -> 566), having no column of the accumulators left to come
 // from the tensor core.
 //
-// Measured (32 query heads, 8 KV heads, d = 128, pages of 64 tokens): 9856 tokens 490 us, 1620 TFLOP/s;
-// 8192 behind 2176 507 us, 1660 TFLOP/s; 512 behind 9300 63 us, 1280 TFLOP/s.
+// Measured, calls one behind the other (32 query heads, 8 KV heads, d = 128, pages of 64 tokens): 9856 tokens 500-530
+// us, 1500-1590 TFLOP/s; 8192 behind 2176 529-552 us, 1525-1590 TFLOP/s; 512 behind 9300 65-67 us, 1205-1230
+// TFLOP/s. (With 30 ms between the calls, at full clock, 497 and 511 us.) At d = 64 8192 behind 2176 takes 443 us:
+// 2510 cycles a block, since that chain does not depend on d, with the tensor pipe 41 % active.
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a

@@ -12,7 +12,7 @@
 // kOneCtaTokens tokens the same CTA writes the maps; beyond, a second kernel over the whole GPU. What
 // bounds either is latency, a chain of dependent loads: a step of 8 requests 4.0-4.5 us a call, of 256
 // 4.6-5.1, of 1024 6.7; 2000 tokens of 64 requests 6.3 in one CTA, 2100 6.3 in two kernels, 5815 7.8 and 6.1,
-// 15938 17.3 and 6.6, 142331 7.9 in two.
+// 15938 17.3 and 6.6, 142331 8.9 in two.
 #include "avtp_cache.cuh"
 
 namespace avtp {
