@@ -462,6 +462,84 @@ typedef struct {
 AVTP_API avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_cache_write_args_t* args, void* workspace,
                                         size_t workspace_bytes, avtp_stream_t stream);
 
+/* Rotary positions of a step's queries and keys, behind the norm of each head where the model has
+ * one, with the keys and values to their slots of the cache. For token t and every head, x a row of q
+ * or k:
+ *   y = x * rsqrt(mean(x^2) + eps) * w         (w: q_norm or k_norm; NULL: y = x)
+ *   (y_a, y_b) -> attn_factor * (y_a cos z - y_b sin z, y_b cos z + y_a sin z),
+ *   z = pos[pair_plane[i]][t] * inv_freq[i]
+ * for the pairs i < rot_dim / 2 of a head's first rot_dim elements, (a, b) = (i, i + rot_dim / 2) or
+ * (2 i, 2 i + 1); the other elements stay y. In 32 bits, angles exact to 2^-53 * pos * inv_freq beside
+ * that; rounded to bf16 once. Position ids of several planes (M-RoPE) are gathered by avtp_prune like
+ * any others: pos may be its output planes. */
+typedef enum {
+  AVTP_ROPE_HALF = 0,        /* pairs (i, i + rot_dim / 2) */
+  AVTP_ROPE_INTERLEAVED = 1  /* pairs (2 i, 2 i + 1)       */
+} avtp_rope_style_t;
+
+typedef struct {
+  int64_t n_tokens;          /* T < 2^31                                                          */
+  int32_t n_q_heads;         /* 0: no queries                                                     */
+  int32_t n_kv_heads;        /* 0: no keys                                                        */
+  int32_t head_dim;          /* 64 or 128                                                         */
+  const void* q;             /* device bf16 [T, n_q_heads, head_dim], contiguous heads; 16-byte   */
+  int64_t q_stride;          /* aligned, token stride a multiple of 8 elements                    */
+  void* q_out;               /* as q: written; may be q with its stride                           */
+  int64_t q_out_stride;
+  const void* k;             /* device bf16 [T, n_kv_heads, head_dim], as q                       */
+  int64_t k_stride;
+  void* k_out;               /* as k: written; may be k with its stride; NULL: the cache alone    */
+  int64_t k_out_stride;
+  const void* v;             /* as k: copied to the cache; not read without one                   */
+  int64_t v_stride;
+  const int32_t* slot_map;   /* device [T], with a cache: as in avtp_cache_write                  */
+  int32_t rot_dim;           /* a multiple of 8, 0 (no rotation) to head_dim                      */
+  int32_t style;             /* avtp_rope_style_t                                                 */
+  const float* inv_freq;     /* device [rot_dim / 2], radians a position; finite                  */
+  const int32_t* pos;        /* device [n_planes, T], rows pos_stride elements apart              */
+  int64_t pos_stride;        /* >= T                                                              */
+  int32_t n_planes;          /* >= 1                                                              */
+  const int32_t* pair_plane; /* device [rot_dim / 2], each in [0, n_planes); NULL: plane 0        */
+  float attn_factor;         /* of the rotated elements (context scalings use it); finite, 1: none */
+  const void* q_norm;        /* device bf16 [head_dim], 16-byte aligned, or NULL                  */
+  const void* k_norm;
+  float eps;                 /* >= 0                                                              */
+} avtp_rope_args_t;
+
+/* cache: NULL, or where the keys and values go (n_kv_heads and head_dim as in args). A slot outside
+ * [-1, n_pages * page_size) is skipped and recorded as AVTP_ERR_DEVICE_INPUT; a frequency that is not
+ * finite or a plane outside [0, n_planes) is recorded too, and then nothing is written. workspace:
+ * 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_rope(const avtp_rope_args_t* args, const avtp_cache_t* cache, void* workspace,
+                                 size_t workspace_bytes, avtp_stream_t stream);
+
+/* Frequencies for avtp_rope, with th_i = base^(-2 i / rot_dim) the unscaled ones, for contexts `factor` times as
+ * long as the original_len positions that a model was trained on:
+ *   NONE     th_i
+ *   LINEAR   th_i / factor (positions interpolated)
+ *   NTK      th_i with base * factor^(rot_dim / (rot_dim - 2)): the slowest pair as in LINEAR, the fastest kept
+ *   YARN     (1 - g_i) th_i / factor + g_i th_i, g_i = clamp((r_i - slow) / (fast - slow), 0, 1) with r_i =
+ *            original_len * th_i / (2 pi) turns of the pair over the original context, and an attn_factor of
+ *            0.1 ln(factor) + 1 (arXiv 2309.00071) */
+typedef enum {
+  AVTP_ROPE_SCALE_NONE = 0,
+  AVTP_ROPE_SCALE_LINEAR = 1,
+  AVTP_ROPE_SCALE_NTK = 2,
+  AVTP_ROPE_SCALE_YARN = 3
+} avtp_rope_scale_t;
+
+typedef struct {
+  int32_t rot_dim;       /* even, >= 2; NTK: >= 4                                 */
+  int32_t scale;         /* avtp_rope_scale_t                                     */
+  double base;           /* > 1                                                   */
+  double factor;         /* >= 1; NONE: not read                                  */
+  double original_len;   /* > 0, YARN                                             */
+  double slow, fast;     /* 0 <= slow < fast, YARN; the paper uses 1 and 32       */
+} avtp_rope_freq_args_t;
+
+/* Host arrays: inv_freq [rot_dim / 2], rounded to fp32 once, and attn_factor [1] (1 but for YARN; NULL to skip). */
+AVTP_API avtp_status_t avtp_rope_frequencies(const avtp_rope_freq_args_t* args, float* inv_freq, float* attn_factor);
+
 /* Causal attention of a step's new tokens over the cache, which holds their own keys and values
  * already: for the i-th of request r's n_r = cu_new[r+1] - cu_new[r] new tokens, its packed row
  * t = cu_new[r] + i, and every query head h,

@@ -14,7 +14,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
-from ctypes import POINTER, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 from dataclasses import dataclass, field
 from typing import Dict, Iterable, List, Optional, Sequence, Tuple
 
@@ -40,8 +40,11 @@ N_STEP_EVENTS = 5
 _CRITERIA = {"hidden_variation": CRIT_HIDDEN_VARIATION, "text_attention": CRIT_TEXT_ATTENTION}
 # avtp_query_set_t and avtp_attn_path_t
 QUERIES_TEXT, QUERIES_LAST = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 PATH_AUTO, PATH_TENSOR, PATH_CUDA = 0, 1, 2
 _QUERY_SETS = {"text": QUERIES_TEXT, "last": QUERIES_LAST}
+_ROPE_STYLES = {"half": ROPE_HALF, "interleaved": ROPE_INTERLEAVED}
+_ROPE_SCALES = {None: 0, "linear": 1, "ntk": 2, "yarn": 3}
 _PATHS = {"auto": PATH_AUTO, "tensor": PATH_TENSOR, "cuda": PATH_CUDA}
 
 
@@ -95,6 +98,21 @@ class _CacheWriteArgs(ctypes.Structure):
                 ("kept_idx", c_void_p), ("slot_map", c_void_p), ("n", c_int64)]
 
 
+class _RopeArgs(ctypes.Structure):
+    _fields_ = [("n_tokens", c_int64), ("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
+                ("q", c_void_p), ("q_stride", c_int64), ("q_out", c_void_p), ("q_out_stride", c_int64),
+                ("k", c_void_p), ("k_stride", c_int64), ("k_out", c_void_p), ("k_out_stride", c_int64),
+                ("v", c_void_p), ("v_stride", c_int64), ("slot_map", c_void_p), ("rot_dim", c_int32),
+                ("style", c_int32), ("inv_freq", c_void_p), ("pos", c_void_p), ("pos_stride", c_int64),
+                ("n_planes", c_int32), ("pair_plane", c_void_p), ("attn_factor", c_float), ("q_norm", c_void_p),
+                ("k_norm", c_void_p), ("eps", c_float)]
+
+
+class _RopeFreqArgs(ctypes.Structure):
+    _fields_ = [("rot_dim", c_int32), ("scale", c_int32), ("base", c_double), ("factor", c_double),
+                ("original_len", c_double), ("slow", c_double), ("fast", c_double)]
+
+
 class _CacheAttnArgs(ctypes.Structure):
     _fields_ = [("n_requests", c_int32), ("n_tokens", c_int64), ("max_new", c_int32), ("n_q_heads", c_int32),
                 ("q", c_void_p), ("q_stride", c_int64), ("cu_new", c_void_p), ("seq_len", c_void_p),
@@ -137,6 +155,8 @@ SIGNATURES = {
     "avtp_cache_slots_workspace_size": (c_int, [POINTER(_CacheSlotsArgs), POINTER(c_size_t)]),
     "avtp_cache_slots": (c_int, [POINTER(_CacheSlotsArgs), c_void_p, c_size_t, c_void_p]),
     "avtp_cache_write": (c_int, [POINTER(_Cache), POINTER(_CacheWriteArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_rope": (c_int, [POINTER(_RopeArgs), POINTER(_Cache), c_void_p, c_size_t, c_void_p]),
+    "avtp_rope_frequencies": (c_int, [POINTER(_RopeFreqArgs), POINTER(c_float), POINTER(c_float)]),
     "avtp_cache_attention_workspace_size": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), POINTER(c_size_t)]),
     "avtp_cache_attention": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), c_void_p, c_size_t, c_void_p]),
     "avtp_wait_selftest": (c_int, [c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
@@ -752,7 +772,7 @@ class _CacheCall:
         self._name = name
         self._fn = getattr(load(), name)
         self._device = workspace.device.index
-        self._args = tuple(ctypes.byref(x) for x in structs) + (
+        self._args = tuple(None if x is None else ctypes.byref(x) for x in structs) + (
             c_void_p(_ptr(workspace)), c_size_t(workspace.numel() * workspace.element_size()))
 
     def run(self, stream=None):
@@ -894,6 +914,92 @@ def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: t
     """avtp_cache_write: K and V rows to their slots; with a prune's ``kept_idx`` only the kept ones."""
     with _on_stream(stream):
         CacheWriteCall(cache, slot_map, k, v, kept_idx=kept_idx, workspace=workspace).run()
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, *, factor: float = 1.0,
+                     original_len: float = 0.0, slow: float = 1.0, fast: float = 32.0) -> Tuple[np.ndarray, float]:
+    """avtp_rope_frequencies: (inv_freq fp32 [rot_dim / 2], attn_factor) on the host, for ``scaling`` None,
+    "linear", "ntk" or "yarn"."""
+    if scaling not in _ROPE_SCALES:
+        raise ValueError(f"rope_frequencies: scaling must be one of {list(_ROPE_SCALES)}")
+    out = np.empty(max(int(rot_dim) // 2, 1), dtype=np.float32)
+    attn = c_float()
+    a = _RopeFreqArgs(int(rot_dim), _ROPE_SCALES[scaling], float(base), float(factor), float(original_len), float(slow),
+                      float(fast))
+    _check(load().avtp_rope_frequencies(ctypes.byref(a), out.ctypes.data_as(POINTER(c_float)), ctypes.byref(attn)),
+           "avtp_rope_frequencies")
+    return out, float(attn.value)
+
+
+class RopeCall(_CacheCall):
+    """A prepared avtp_rope call: rotary positions of ``q`` and ``k`` (bf16 [T, H, head_dim]; either may be None), behind
+    their norms of each head where ``q_norm`` / ``k_norm`` (bf16 [head_dim]) are given. ``pos``: int32 [T], or
+    [n_planes, T] with ``pair_plane`` (int32 [rot_dim / 2]) naming each pair's plane; ``inv_freq``: fp32 [rot_dim /
+    2] (:func:`rope_frequencies`). With ``cache``, ``v`` and ``slot_map`` the keys and values go to their slots, and
+    to ``k_out`` only if one is given. ``q_out`` and ``k_out`` may be ``q`` and ``k`` themselves."""
+
+    def __init__(self, pos: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], *, q=None, k=None, v=None, q_out=None,
+                 k_out=None, style="half", pair_plane=None, attn_factor=1.0, q_norm=None, k_norm=None, eps=1e-6,
+                 cache: Optional[PagedCache] = None, slot_map=None, workspace=None):
+        name = "rope"
+        some = q if q is not None else k
+        if some is None or some.dim() != 3:
+            raise ValueError(f"{name}: q or k must be bf16 [T, H, head_dim] with contiguous heads")
+        T, d = some.shape[0], some.shape[2]
+        if (cache is None) != (slot_map is None) or (cache is None) != (v is None) or (cache is not None and k is None):
+            raise ValueError(f"{name}: cache, slot_map and v go together, with k")
+        dev = _on_one_device(name, pos, inv_freq, q, k, v, q_out, k_out, pair_plane, q_norm, k_norm, slot_map, workspace,
+                             cache.k if cache is not None else None)
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        if k is not None and k_out is None and cache is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+        for what, t, like in (("q", q, q), ("q_out", q_out, q), ("k", k, k), ("k_out", k_out, k), ("v", v, k)):
+            if t is None:
+                continue
+            if (like is None or t.dtype != torch.bfloat16 or t.dim() != 3 or tuple(t.shape) != (T, like.shape[1], d)
+                    or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
+                raise ValueError(f"{name}: {what} must be bf16 [T, H, head_dim] with contiguous heads")
+        if cache is not None and tuple(cache.k.shape[2:]) != tuple(k.shape[1:]):
+            raise ValueError(f"{name}: the cache has other heads than k")
+        rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+        planes = 1
+        if rot:
+            if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+                raise ValueError(f"{name}: inv_freq must be a contiguous fp32 tensor with one dimension")
+            if (pos is None or pos.dtype != torch.int32 or pos.dim() not in (1, 2) or pos.shape[-1] != T
+                    or (T > 1 and pos.stride(-1) != 1)):
+                raise ValueError(f"{name}: pos must be int32 [T] or [n_planes, T] with a contiguous last dim")
+            planes = pos.shape[0] if pos.dim() == 2 else 1
+            if pair_plane is not None:
+                _int32(name, "pair_plane", pair_plane, (rot // 2,))
+        for what, t in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if t is not None and (t.dtype != torch.bfloat16 or tuple(t.shape) != (d,) or not t.is_contiguous()):
+                raise ValueError(f"{name}: {what} must be a contiguous bf16 tensor of shape [head_dim]")
+        if slot_map is not None:
+            _int32(name, "slot_map", slot_map, (T,))
+        self.q_out, self.k_out, self.cache = q_out, k_out, cache
+        self._keep = (pos, inv_freq, q, k, v, pair_plane, q_norm, k_norm, slot_map)
+
+        def stride(t):
+            return 0 if t is None else (t.stride(0) if T > 1 else t.shape[1] * d)
+
+        self._c = cache.c() if cache is not None else None
+        self._a = _RopeArgs(
+            T, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], d, _ptr(q), stride(q), _ptr(q_out),
+            stride(q_out), _ptr(k), stride(k), _ptr(k_out), stride(k_out), _ptr(v), stride(v), _ptr(slot_map), rot,
+            _ROPE_STYLES[style] if isinstance(style, str) else int(style), _ptr(inv_freq), _ptr(pos),
+            pos.stride(0) if rot and planes > 1 else T, planes, _ptr(pair_plane), float(attn_factor), _ptr(q_norm),
+            _ptr(k_norm), float(eps))
+        self._prepare("avtp_rope", workspace if workspace is not None else new_workspace(256, dev), self._a, self._c)
+
+
+def rope(pos: Optional[torch.Tensor], inv_freq: Optional[torch.Tensor], *, q=None, k=None, stream=None, **more):
+    """avtp_rope: (q_out, k_out) rotated, the keys and values in the cache where one is given. See
+    :class:`RopeCall`."""
+    with _on_stream(stream):
+        c = RopeCall(pos, inv_freq, q=q, k=k, **more).run()
+    return c.q_out, c.k_out
 
 
 class CacheAttentionCall(_CacheCall):

@@ -19,6 +19,9 @@ cudaError_t launch_cache_slots(const avtp_cache_slots_args_t& a, void* ws, const
 // ---------------------------------------------------------------- write
 cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_args_t& a, void* ws, cudaStream_t s);
 
+// ---------------------------------------------------------------- rotary positions
+cudaError_t launch_rope(const avtp_rope_args_t& a, const avtp_cache_t* c, void* ws, cudaStream_t s);
+
 // ---------------------------------------------------------------- attention
 // Rows of a (request, KV head) are its (new token, head of the group) pairs, token by token.
 constexpr int kCacheMaxPieces = 32;   // pieces that a row block's keys are split into, at most

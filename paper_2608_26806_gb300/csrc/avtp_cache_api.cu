@@ -1,5 +1,5 @@
 // C ABI of the paged cache: argument validation, workspace plans and launches of
-// avtp_cache_slots, avtp_cache_write and avtp_cache_attention.
+// avtp_cache_slots, avtp_cache_write, avtp_rope and avtp_cache_attention; the frequencies of avtp_rope.
 #include <math.h>
 
 #include "avtp_cache.cuh"
@@ -70,6 +70,48 @@ SlotsWs plan_slots(const avtp_cache_slots_args_t& a) {
   return p;
 }
 
+// One tensor of rows: head_dim elements a head, contiguous heads.
+avtp_status_t check_rows(const void* p, int64_t stride, int64_t row) {
+  if (p == nullptr || stride < row) return AVTP_ERR_INVALID_ARG;
+  return aligned16(p) && stride % 8 == 0 ? AVTP_OK : AVTP_ERR_UNSUPPORTED;
+}
+
+avtp_status_t check_rope(const avtp_rope_args_t* a, const avtp_cache_t* c) {
+  if (a == nullptr || a->n_tokens < 0 || a->n_q_heads < 0 || a->n_kv_heads < 0) return AVTP_ERR_INVALID_ARG;
+  if (a->n_tokens > kInt32Max || a->n_q_heads > 65536 || a->n_kv_heads > 65536) return AVTP_ERR_RANGE;
+  if (a->head_dim != 64 && a->head_dim != 128) return AVTP_ERR_UNSUPPORTED;
+  if (a->rot_dim < 0 || a->rot_dim > a->head_dim) return AVTP_ERR_INVALID_ARG;
+  if (a->rot_dim % 8 != 0) return AVTP_ERR_UNSUPPORTED;
+  if (a->style != AVTP_ROPE_HALF && a->style != AVTP_ROPE_INTERLEAVED) return AVTP_ERR_INVALID_ARG;
+  if (!isfinite(a->attn_factor) || !isfinite(a->eps) || a->eps < 0.f) return AVTP_ERR_INVALID_ARG;
+  if (c != nullptr) {
+    const avtp_status_t st = check_cache(c);
+    if (st != AVTP_OK) return st;
+    if (c->n_kv_heads != a->n_kv_heads || c->head_dim != a->head_dim) return AVTP_ERR_INVALID_ARG;
+  }
+  if (a->n_tokens == 0) return AVTP_OK;
+  const int64_t d = a->head_dim;
+  struct Rows {
+    const void* p;
+    int64_t stride, heads;
+    bool wanted;
+  } const rows[5] = {{a->q, a->q_stride, a->n_q_heads, true},
+                     {a->q_out, a->q_out_stride, a->n_q_heads, true},
+                     {a->k, a->k_stride, a->n_kv_heads, true},
+                     {a->k_out, a->k_out_stride, a->n_kv_heads, c == nullptr || a->k_out != nullptr},
+                     {a->v, a->v_stride, a->n_kv_heads, c != nullptr}};
+  for (const Rows& r : rows) {
+    if (r.heads == 0 || !r.wanted) continue;
+    const avtp_status_t st = check_rows(r.p, r.stride, r.heads * d);
+    if (st != AVTP_OK) return st;
+  }
+  if (c != nullptr && a->slot_map == nullptr) return AVTP_ERR_INVALID_ARG;
+  if (a->rot_dim > 0 && (a->inv_freq == nullptr || a->pos == nullptr || a->n_planes < 1 || a->pos_stride < a->n_tokens))
+    return AVTP_ERR_INVALID_ARG;
+  if (!aligned16(a->q_norm) || !aligned16(a->k_norm)) return AVTP_ERR_UNSUPPORTED;
+  return AVTP_OK;
+}
+
 avtp_status_t check_attn(const avtp_cache_t* c, const avtp_cache_attn_args_t* a) {
   avtp_status_t st = check_cache(c);
   if (st != AVTP_OK) return st;
@@ -134,6 +176,40 @@ avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_cache_write
   if (!aligned16(args->k) || !aligned16(args->v)) return AVTP_ERR_UNSUPPORTED;
   if ((st = check_ws(workspace, workspace_bytes, sizeof(DevStatus))) != AVTP_OK) return st;
   return from_cuda(launch_cache_write(*cache, *args, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_rope(const avtp_rope_args_t* args, const avtp_cache_t* cache, void* workspace, size_t workspace_bytes,
+                        avtp_stream_t stream) {
+  avtp_status_t st = check_rope(args, cache);
+  if (st != AVTP_OK) return st;
+  if ((st = check_ws(workspace, workspace_bytes, sizeof(DevStatus))) != AVTP_OK) return st;
+  return from_cuda(launch_rope(*args, cache, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_rope_frequencies(const avtp_rope_freq_args_t* a, float* inv_freq, float* attn_factor) {
+  if (a == nullptr || inv_freq == nullptr || a->rot_dim < 2 || a->rot_dim % 2 != 0 || !(a->base > 1.0) ||
+      !isfinite(a->base) || a->scale < AVTP_ROPE_SCALE_NONE || a->scale > AVTP_ROPE_SCALE_YARN)
+    return AVTP_ERR_INVALID_ARG;
+  const bool yarn = a->scale == AVTP_ROPE_SCALE_YARN;
+  if (a->scale != AVTP_ROPE_SCALE_NONE && (!(a->factor >= 1.0) || !isfinite(a->factor))) return AVTP_ERR_INVALID_ARG;
+  if (a->scale == AVTP_ROPE_SCALE_NTK && a->rot_dim < 4) return AVTP_ERR_INVALID_ARG;
+  if (yarn && (!(a->original_len > 0.0) || !isfinite(a->original_len) || !(a->slow >= 0.0) || !(a->slow < a->fast) ||
+               !isfinite(a->fast)))
+    return AVTP_ERR_INVALID_ARG;
+  const double n = a->rot_dim;
+  const double base = a->scale == AVTP_ROPE_SCALE_NTK ? a->base * pow(a->factor, n / (n - 2.0)) : a->base;
+  for (int32_t i = 0; i < a->rot_dim / 2; ++i) {
+    double f = pow(base, -2.0 * i / n);
+    if (a->scale == AVTP_ROPE_SCALE_LINEAR) f /= a->factor;
+    if (yarn) {
+      const double turns = a->original_len * f / 6.283185307179586;
+      const double g = fmin(fmax((turns - a->slow) / (a->fast - a->slow), 0.0), 1.0);
+      f = (1.0 - g) * f / a->factor + g * f;
+    }
+    inv_freq[i] = static_cast<float>(f);
+  }
+  if (attn_factor != nullptr) *attn_factor = yarn ? static_cast<float>(0.1 * log(a->factor) + 1.0) : 1.f;
+  return AVTP_OK;
 }
 
 avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
