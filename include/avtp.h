@@ -589,6 +589,130 @@ AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* c
 AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                             void* workspace, size_t workspace_bytes, avtp_stream_t stream);
 
+/* Upkeep of the cache's pages: cached prompts pruned further, several requests on one prompt, pages given back.
+ *
+ * Pages may have several holders. `shared` (device int32 [n_pages], zeros at first) is the number of a page's
+ * holders beyond the first: avtp_cache_fork adds to it, avtp_cache_free takes from it, and a page that
+ * avtp_cache_slots takes from the free list has one holder. Calls without `shared` treat every page as held once.
+ *
+ * Requests may let go of pages that a sliding window has left (see avtp_cache_window_attention): with `window` > 0 a
+ * request that was `held_len` tokens long at its last such call holds the pages of its first n_sinks tokens, and
+ * of those from held_len - window + 1 on, the first that the window of its next token needs. held_len (device
+ * [R], zeros at first) goes with the lengths: avtp_cache_free writes it, avtp_cache_fork copies it. Table entries of
+ * pages let go of stay as they were and are not read. window 0: every request holds all its pages. */
+
+/* The kept tokens of cached requests moved together, in one layer's cache: for j < n_r = keep_cu[r+1] -
+ * keep_cu[r], the rows of token keep_idx[keep_cu[r] + j] - base of request r go to the place of its token j, in
+ * the pages of dst_table, or without one in its own (then base + j <= keep_idx: a prune of the cache in place). base
+ * is 0, or base_cu[r]: with avtp_prune's kept_idx, out_cu_seqlens and the batch's cu_seqlens the positions are used
+ * where they were made. Whoever holds one table for several layers calls this for each, then, in place,
+ * avtp_cache_free once with len_out. */
+typedef struct {
+  int32_t n_requests;          /* R >= 1, at most 2^31 - 1025                                        */
+  int64_t n_kept;              /* length of keep_idx, >= keep_cu[R] (host); < 2^31                   */
+  const int32_t* keep_cu;      /* device [R+1], keep_cu[0] = 0, non-decreasing                       */
+  const int32_t* keep_idx;     /* device [n_kept]                                                    */
+  const int32_t* base_cu;      /* device [R] or NULL: 0                                              */
+  const int32_t* seq_len;      /* device [R]: cached tokens                                          */
+  const int32_t* block_table;  /* device [R, max_pages]                                              */
+  int32_t max_pages;
+  int64_t table_stride;        /* elements, >= max_pages                                             */
+  const int32_t* dst_table;    /* device [R, dst_max_pages], of pages that hold no row to be read; NULL: in place */
+  int32_t dst_max_pages;
+  int64_t dst_stride;
+  const int32_t* shared;       /* device [n_pages] or NULL; read in place                            */
+  int32_t window;              /* see above; 0: none                                                 */
+  int32_t n_sinks;
+  const int32_t* held_len;     /* device [R], with a window                                          */
+  int32_t* len_out;            /* device [R] or NULL: n_r, written; not seq_len                      */
+} avtp_cache_compact_args_t;
+
+/* Offsets that decrease or pass n_kept are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. Recorded too:
+ * - with dst_table, a position outside its request's tokens or on a page let go of, or a page outside [0, n_pages) or the
+ *   table: that token is not moved;
+ * - in place, the same, positions that do not ascend, or a row to be moved to a page let go of or with shared > 0 (others
+ *   hold it): that request is left as it was.
+ * workspace: 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,
+                                          size_t workspace_bytes, avtp_stream_t stream);
+
+/* Whole pages of one layer's cache: for i < n with src[i] >= 0 and dst[i] >= 0, page src[i] to page dst[i] (a page that no
+ * other pair names). A page outside [-1, n_pages) is skipped and recorded as AVTP_ERR_DEVICE_INPUT. workspace: 256-byte
+ * aligned, at least 16 bytes. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_copy(const avtp_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n,
+                                       void* workspace, size_t workspace_bytes, avtp_stream_t stream);
+
+/* Requests that go on from others' cached tokens: child i, row child[i] of the table, becomes the first
+ * fork_len[i] tokens of row parent[i]. Their full pages get a holder more; a last one that is not full is copied, since
+ * both will write to it: the child's table gets a page of the free list (from entry *free_head on, child by child),
+ * and copy_src / copy_dst name the two for avtp_cache_copy, once a layer (-1 where nothing is to be copied). */
+typedef struct {
+  int32_t n_requests;          /* R >= 1: rows of the table; at most 2^31 - 1025                    */
+  int32_t n_children;          /* >= 0, at most 2^31 - 1025                                         */
+  int32_t page_size;
+  int64_t n_pages;             /* of the pool; n_pages * page_size < 2^31                           */
+  int32_t max_pages;
+  int64_t table_stride;        /* elements, >= max_pages                                            */
+  const int32_t* parent;       /* device [n_children]                                               */
+  const int32_t* child;        /* device [n_children]: each once, none of them a parent, holding no page */
+  const int32_t* fork_len;     /* device [n_children], at most the parent's length; NULL: all of it */
+  const int32_t* free_pages;   /* device [n_free], as in avtp_cache_slots                           */
+  int64_t n_free;
+  const int32_t* free_head;    /* device [1]; NULL: 0                                               */
+  int32_t* block_table;        /* device [R, max_pages]: the children's entries written             */
+  int32_t* seq_len;            /* device [R]: the children's lengths written                        */
+  int32_t* shared;             /* device [n_pages]: counts of the pages shared go up                */
+  int32_t window;              /* see above; 0: none                                                */
+  int32_t n_sinks;
+  int32_t* held_len;           /* device [R], with a window: the children's written                 */
+  int32_t* copy_src;           /* device [n_children]: written                                      */
+  int32_t* copy_dst;
+  int32_t* free_head_out;      /* device [1] or NULL: written; may be free_head                     */
+} avtp_cache_fork_args_t;
+
+AVTP_API avtp_status_t avtp_cache_fork_workspace_size(const avtp_cache_fork_args_t* args, size_t* bytes);
+
+/* A row outside the table, a child given twice or that is a parent, a length that is negative, longer than the parent or
+ * max_pages pages or, with a window, so short that it needs a page let go of, a page outside [0, n_pages), or a free list that runs out are
+ * recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_fork(const avtp_cache_fork_args_t* args, void* workspace, size_t workspace_bytes,
+                                       avtp_stream_t stream);
+
+/* Pages back to the free list: request r goes from seq_len[r] to new_len[r] tokens (0: it is done; fewer: drafted
+ * tokens taken back, or a cache compacted in place; the same: only what the window has left) and lets go of the pages that
+ * it needs no more. Those whose last holder lets go are put before entry *free_head of the free list, in the table's
+ * order (row by row, a row's entries ascending; a page that several rows of the call let go of at the last of
+ * them): results do not change from run to run. */
+typedef struct {
+  int32_t n_requests;          /* R >= 1, at most 2^31 - 1025                                       */
+  int32_t page_size;
+  int64_t n_pages;
+  int32_t max_pages;
+  int64_t table_stride;        /* elements, >= max_pages                                            */
+  const int32_t* seq_len;      /* device [R]                                                        */
+  const int32_t* new_len;      /* device [R], 0 to seq_len                                          */
+  const int32_t* block_table;  /* device [R, max_pages]: not written                                */
+  int32_t* free_pages;         /* device [n_free]: entries before *free_head written                */
+  int64_t n_free;
+  const int32_t* free_head;    /* device [1]                                                        */
+  int32_t* shared;             /* device [n_pages] or NULL: counts go down                          */
+  int32_t window;              /* 0: none                                                           */
+  int32_t n_sinks;
+  const int32_t* held_len;     /* device [R], with a window                                         */
+  int32_t* seq_len_out;        /* device [R]: new_len, written; may be seq_len                      */
+  int32_t* held_len_out;       /* device [R], with a window: written; may be held_len               */
+  int32_t* free_head_out;      /* device [1]: written; may be free_head                             */
+} avtp_cache_free_args_t;
+
+AVTP_API avtp_status_t avtp_cache_free_workspace_size(const avtp_cache_free_args_t* args, size_t* bytes);
+
+/* Lengths out of range (as above; a held_len beyond seq_len), a page outside [0, n_pages), one that more rows let go of than hold
+ * it, a new_len inside a page with shared > 0 (the request's next tokens would be written over the others'; whoever
+ * wants that forks the request first), or a free list with too few entries before *free_head are recorded as
+ * AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_free(const avtp_cache_free_args_t* args, void* workspace, size_t workspace_bytes,
+                                       avtp_stream_t stream);
+
 /* Check of the failure path every pipeline kernel takes when a wait on an mbarrier (a
  * TMA copy, a tensor-core commit, a hand-off between warps) does not complete: one CTA
  * of 64 threads waits on a fresh count-1 mbarrier with the library's bounded waits,

@@ -121,6 +121,31 @@ class _CacheAttnArgs(ctypes.Structure):
                 ("lse_stride", c_int64)]
 
 
+class _CacheCompactArgs(ctypes.Structure):
+    _fields_ = [("n_requests", c_int32), ("n_kept", c_int64), ("keep_cu", c_void_p), ("keep_idx", c_void_p),
+                ("base_cu", c_void_p), ("seq_len", c_void_p), ("block_table", c_void_p), ("max_pages", c_int32),
+                ("table_stride", c_int64), ("dst_table", c_void_p), ("dst_max_pages", c_int32), ("dst_stride", c_int64),
+                ("shared", c_void_p), ("window", c_int32), ("n_sinks", c_int32), ("held_len", c_void_p),
+                ("len_out", c_void_p)]
+
+
+class _CacheForkArgs(ctypes.Structure):
+    _fields_ = [("n_requests", c_int32), ("n_children", c_int32), ("page_size", c_int32), ("n_pages", c_int64),
+                ("max_pages", c_int32), ("table_stride", c_int64), ("parent", c_void_p), ("child", c_void_p),
+                ("fork_len", c_void_p), ("free_pages", c_void_p), ("n_free", c_int64), ("free_head", c_void_p),
+                ("block_table", c_void_p), ("seq_len", c_void_p), ("shared", c_void_p), ("window", c_int32),
+                ("n_sinks", c_int32), ("held_len", c_void_p), ("copy_src", c_void_p), ("copy_dst", c_void_p),
+                ("free_head_out", c_void_p)]
+
+
+class _CacheFreeArgs(ctypes.Structure):
+    _fields_ = [("n_requests", c_int32), ("page_size", c_int32), ("n_pages", c_int64), ("max_pages", c_int32),
+                ("table_stride", c_int64), ("seq_len", c_void_p), ("new_len", c_void_p), ("block_table", c_void_p),
+                ("free_pages", c_void_p), ("n_free", c_int64), ("free_head", c_void_p), ("shared", c_void_p),
+                ("window", c_int32), ("n_sinks", c_int32), ("held_len", c_void_p), ("seq_len_out", c_void_p),
+                ("held_len_out", c_void_p), ("free_head_out", c_void_p)]
+
+
 class _ForwardArgs(ctypes.Structure):
     _fields_ = [("v", c_void_p), ("v_stride", c_int64), ("o", c_void_p), ("o_stride", c_int64), ("lse", c_void_p),
                 ("lse_stride", c_int64)]
@@ -159,6 +184,12 @@ SIGNATURES = {
     "avtp_rope_frequencies": (c_int, [POINTER(_RopeFreqArgs), POINTER(c_float), POINTER(c_float)]),
     "avtp_cache_attention_workspace_size": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), POINTER(c_size_t)]),
     "avtp_cache_attention": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_compact": (c_int, [POINTER(_Cache), POINTER(_CacheCompactArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_copy": (c_int, [POINTER(_Cache), c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_fork_workspace_size": (c_int, [POINTER(_CacheForkArgs), POINTER(c_size_t)]),
+    "avtp_cache_fork": (c_int, [POINTER(_CacheForkArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_free_workspace_size": (c_int, [POINTER(_CacheFreeArgs), POINTER(c_size_t)]),
+    "avtp_cache_free": (c_int, [POINTER(_CacheFreeArgs), c_void_p, c_size_t, c_void_p]),
     "avtp_wait_selftest": (c_int, [c_int64, c_int32, c_void_p, c_size_t, c_void_p]),
     "avtp_layer_attention": (c_int, [POINTER(_Layout), c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_size_t,
                                      c_void_p]),
@@ -772,7 +803,7 @@ class _CacheCall:
         self._name = name
         self._fn = getattr(load(), name)
         self._device = workspace.device.index
-        self._args = tuple(None if x is None else ctypes.byref(x) for x in structs) + (
+        self._args = tuple(ctypes.byref(x) if isinstance(x, ctypes.Structure) else x for x in structs) + (
             c_void_p(_ptr(workspace)), c_size_t(workspace.numel() * workspace.element_size()))
 
     def run(self, stream=None):
@@ -1056,3 +1087,176 @@ def cache_attention(cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, se
         c = CacheAttentionCall(cache, q, cu_new, seq_len, block_table, max_new=max_new, softmax_scale=softmax_scale,
                                o=o, lse=lse, workspace=workspace).run()
     return c.o, c.lse
+
+
+# ---------------------------------------------------------------- upkeep of the pages
+def _window(where: str, window: int, sinks: int, n_requests: int, held_len: Optional[torch.Tensor]) -> Tuple[int, int]:
+    if int(window) > 0 and held_len is None:
+        raise ValueError(f"{where}: a window goes with held_len")
+    _int32(where, "held_len", held_len, (n_requests,))
+    return int(window), int(sinks)
+
+
+class CacheCompactCall(_CacheCall):
+    """A prepared avtp_cache_compact call: the kept tokens of cached requests moved together in one layer's cache, to
+    the pages of ``dst_table`` (int32 [R, columns]) or, without one, in place. ``keep_idx`` (int32): request r's kept
+    positions at ``keep_cu[r] .. keep_cu[r+1]``, less ``base_cu[r]`` where that is given (a prune's ``kept_idx``,
+    ``out_cu_seqlens`` and the batch's ``cu_seqlens``). ``len_out`` (int32 [R]) receives the kept tokens; the pages
+    behind them go back with :class:`CacheFreeCall`. ``shared``, ``window``, ``sinks`` and ``held_len``: as there."""
+
+    def __init__(self, cache: PagedCache, keep_cu: torch.Tensor, keep_idx: torch.Tensor, seq_len: torch.Tensor,
+                 block_table: torch.Tensor, *, dst_table=None, base_cu=None, shared=None, window=0, sinks=0, held_len=None,
+                 len_out=None, workspace=None):
+        name = "cache_compact"
+        _int32_list(name, "keep_cu", keep_cu)
+        _int32_list(name, "keep_idx", keep_idx)
+        R = keep_cu.shape[0] - 1
+        max_pages, stride = _block_table(name, block_table, R)
+        dst = _block_table(name, dst_table, R) if dst_table is not None else (0, 0)
+        dev = _on_one_device(name, cache.k, keep_cu, keep_idx, seq_len, block_table, dst_table, base_cu, shared, held_len,
+                             len_out, workspace)
+        self.len_out = len_out if len_out is not None else torch.full((R,), -1, dtype=torch.int32, device=dev)
+        if base_cu is not None:  # a batch's offsets: R of them, or with its end
+            _int32_list(name, "base_cu", base_cu)
+            if base_cu.shape[0] not in (R, R + 1):
+                raise ValueError(f"{name}: base_cu must have an offset a request")
+        for what, t, n in (("seq_len", seq_len, R), ("len_out", self.len_out, R), ("shared", shared, cache.n_pages)):
+            _int32(name, what, t, (n,))
+        window, sinks = _window(name, window, sinks, R, held_len)
+        self.cache = cache
+        self._keep = (keep_cu, keep_idx, seq_len, block_table, dst_table, base_cu, shared, held_len)
+        self._c = cache.c()
+        self._a = _CacheCompactArgs(R, keep_idx.shape[0], _ptr(keep_cu), _ptr(keep_idx), _ptr(base_cu), _ptr(seq_len),
+                                    _ptr(block_table), max_pages, stride, _ptr(dst_table), *dst, _ptr(shared), window, sinks,
+                                    _ptr(held_len), _ptr(self.len_out))
+        self._prepare("avtp_cache_compact", workspace if workspace is not None else new_workspace(256, dev), self._c,
+                      self._a)
+
+
+def cache_compact(cache: PagedCache, keep_cu: torch.Tensor, keep_idx: torch.Tensor, seq_len: torch.Tensor,
+                  block_table: torch.Tensor, *, stream=None, **more) -> torch.Tensor:
+    """avtp_cache_compact: kept tokens together; returns their counts (int32 [R]). See :class:`CacheCompactCall`."""
+    with _on_stream(stream):
+        return CacheCompactCall(cache, keep_cu, keep_idx, seq_len, block_table, **more).run().len_out
+
+
+class CacheCopyCall(_CacheCall):
+    """A prepared avtp_cache_copy call: pages ``src[i]`` to pages ``dst[i]`` (int32; -1 in either: none) of one
+    layer's cache."""
+
+    def __init__(self, cache: PagedCache, src: torch.Tensor, dst: torch.Tensor, *, workspace=None):
+        name = "cache_copy"
+        _int32_list(name, "src", src)
+        _int32(name, "dst", dst, tuple(src.shape))
+        dev = _on_one_device(name, cache.k, src, dst, workspace)
+        self.cache = cache
+        self._keep = (src, dst)
+        self._c = cache.c()
+        self._prepare("avtp_cache_copy", workspace if workspace is not None else new_workspace(256, dev), self._c,
+                      c_void_p(_ptr(src)), c_void_p(_ptr(dst)), c_int64(src.shape[0]))
+
+
+def cache_copy(cache: PagedCache, src: torch.Tensor, dst: torch.Tensor, *, workspace=None, stream=None) -> None:
+    """avtp_cache_copy: whole pages to other pages. See :class:`CacheCopyCall`."""
+    with _on_stream(stream):
+        CacheCopyCall(cache, src, dst, workspace=workspace).run()
+
+
+class CacheForkCall(_CacheCall):
+    """A prepared avtp_cache_fork call: rows ``child`` of ``block_table`` and ``seq_len`` go on from the cached tokens
+    of rows ``parent`` (int32 [C] each), or the first ``fork_len`` of them. Full pages are shared (``shared``, int32
+    [n_pages], zeros at first, counts the holders beyond the first); a last page that is not full is to be copied,
+    from ``copy_src`` to ``copy_dst`` (:class:`CacheCopyCall`, once a layer), to a page of the free list. A
+    refused call (read_device_status) writes nothing: copy lists of its own then hold -1."""
+
+    def __init__(self, parent: torch.Tensor, child: torch.Tensor, seq_len: torch.Tensor, block_table: torch.Tensor, *,
+                 page_size: int, n_pages: int, free_pages: torch.Tensor, shared: torch.Tensor, free_head=None, fork_len=None,
+                 window=0, sinks=0, held_len=None, copy_src=None, copy_dst=None, free_head_out=None, workspace=None):
+        name = "cache_fork"
+        _int32_list(name, "parent", parent)
+        _int32_list(name, "free_pages", free_pages)
+        _int32_list(name, "seq_len", seq_len)
+        C, R = parent.shape[0], seq_len.shape[0]
+        max_pages, stride = _block_table(name, block_table, R)
+        dev = _on_one_device(name, parent, child, seq_len, block_table, free_pages, shared, free_head, fork_len, held_len,
+                             copy_src, copy_dst, free_head_out, workspace)
+        made = torch.full((2 * C + 1,), -1, dtype=torch.int32, device=dev).split([C, C, 1])
+        self.copy_src = copy_src if copy_src is not None else made[0]
+        self.copy_dst = copy_dst if copy_dst is not None else made[1]
+        self.free_head_out = free_head_out if free_head_out is not None else made[2]
+        if shared is None:
+            raise ValueError(f"{name}: shared is needed")
+        for what, t, n in (("child", child, C), ("fork_len", fork_len, C), ("copy_src", self.copy_src, C),
+                           ("copy_dst", self.copy_dst, C), ("shared", shared, int(n_pages)), ("free_head", free_head, 1),
+                           ("free_head_out", self.free_head_out, 1)):
+            _int32(name, what, t, (n,))
+        window, sinks = _window(name, window, sinks, R, held_len)
+        self.block_table, self.seq_len = block_table, seq_len
+        self._keep = (parent, child, free_pages, shared, free_head, fork_len, held_len)
+        self._a = _CacheForkArgs(R, C, int(page_size), int(n_pages), max_pages, stride, _ptr(parent), _ptr(child),
+                                 _ptr(fork_len), _ptr(free_pages), free_pages.shape[0], _ptr(free_head), _ptr(block_table),
+                                 _ptr(seq_len), _ptr(shared), window, sinks, _ptr(held_len), _ptr(self.copy_src),
+                                 _ptr(self.copy_dst), _ptr(self.free_head_out))
+        if workspace is None:
+            n = c_size_t()
+            _check(load().avtp_cache_fork_workspace_size(ctypes.byref(self._a), ctypes.byref(n)),
+                   "avtp_cache_fork_workspace_size")
+            workspace = new_workspace(int(n.value), dev)
+        self._prepare("avtp_cache_fork", workspace, self._a)
+
+
+def cache_fork(parent: torch.Tensor, child: torch.Tensor, seq_len: torch.Tensor, block_table: torch.Tensor, *, stream=None,
+               **more):
+    """avtp_cache_fork: (copy_src, copy_dst, free_head). See :class:`CacheForkCall`."""
+    with _on_stream(stream):
+        c = CacheForkCall(parent, child, seq_len, block_table, **more).run()
+    return c.copy_src, c.copy_dst, c.free_head_out
+
+
+class CacheFreeCall(_CacheCall):
+    """A prepared avtp_cache_free call: requests go from ``seq_len`` to ``new_len`` tokens (int32 [R]; 0: done) and the
+    pages that they need no more go back to ``free_pages``, before its entry ``free_head``. With ``shared``
+    (:class:`CacheForkCall`) a page goes back with its last holder. With ``window`` (and ``sinks``, ``held_len`` int32
+    [R], zeros at first) what a sliding window has left goes back too. ``seq_len_out=seq_len``,
+    ``held_len_out=held_len`` and ``free_head_out=free_head`` advance them in place. A refused call
+    (read_device_status) writes nothing: outputs of its own then hold -1."""
+
+    def __init__(self, seq_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, *, page_size: int,
+                 n_pages: int, free_pages: torch.Tensor, free_head: torch.Tensor, shared=None, window=0, sinks=0,
+                 held_len=None, seq_len_out=None, held_len_out=None, free_head_out=None, workspace=None):
+        name = "cache_free"
+        _int32_list(name, "seq_len", seq_len)
+        _int32_list(name, "free_pages", free_pages)
+        _int32_list(name, "free_head", free_head)
+        R = seq_len.shape[0]
+        max_pages, stride = _block_table(name, block_table, R)
+        dev = _on_one_device(name, seq_len, new_len, block_table, free_pages, free_head, shared, held_len, seq_len_out,
+                             held_len_out, free_head_out, workspace)
+        window, sinks = _window(name, window, sinks, R, held_len)
+        made = torch.full((2 * R + 1,), -1, dtype=torch.int32, device=dev).split([R, R, 1])
+        self.seq_len_out = seq_len_out if seq_len_out is not None else made[0]
+        self.held_out = None if not window else (held_len_out if held_len_out is not None else made[1])
+        self.free_head_out = free_head_out if free_head_out is not None else made[2]
+        self.free_pages = free_pages
+        for what, t, n in (("new_len", new_len, R), ("seq_len_out", self.seq_len_out, R), ("held_len_out", self.held_out, R),
+                           ("shared", shared, int(n_pages)), ("free_head", free_head, 1),
+                           ("free_head_out", self.free_head_out, 1)):
+            _int32(name, what, t, (n,))
+        self._keep = (seq_len, new_len, block_table, free_head, shared, held_len)
+        self._a = _CacheFreeArgs(R, int(page_size), int(n_pages), max_pages, stride, _ptr(seq_len), _ptr(new_len),
+                                 _ptr(block_table), _ptr(free_pages), free_pages.shape[0], _ptr(free_head), _ptr(shared),
+                                 window, sinks, _ptr(held_len), _ptr(self.seq_len_out), _ptr(self.held_out),
+                                 _ptr(self.free_head_out))
+        if workspace is None:
+            n = c_size_t()
+            _check(load().avtp_cache_free_workspace_size(ctypes.byref(self._a), ctypes.byref(n)),
+                   "avtp_cache_free_workspace_size")
+            workspace = new_workspace(int(n.value), dev)
+        self._prepare("avtp_cache_free", workspace, self._a)
+
+
+def cache_free(seq_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, *, stream=None, **more):
+    """avtp_cache_free: (seq_len, free_head), the pages in ``free_pages``. See :class:`CacheFreeCall`."""
+    with _on_stream(stream):
+        c = CacheFreeCall(seq_len, new_len, block_table, **more).run()
+    return c.seq_len_out, c.free_head_out

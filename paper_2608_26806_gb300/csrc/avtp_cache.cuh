@@ -22,6 +22,37 @@ cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_arg
 // ---------------------------------------------------------------- rotary positions
 cudaError_t launch_rope(const avtp_rope_args_t& a, const avtp_cache_t* c, void* ws, cudaStream_t s);
 
+// ---------------------------------------------------------------- pages
+// Which pages a request of n tokens holds (see avtp.h): columns j < up(n) with j < sinks or j >= left(held_len).
+struct CachePages {
+  int32_t P, window, sinks;  // page size, window, pages of the sinks
+  static CachePages of(int32_t page_size, int32_t window, int32_t n_sinks) {
+    return {page_size, window, window > 0 ? static_cast<int32_t>((int64_t(n_sinks) + page_size - 1) / page_size) : 0};
+  }
+  __device__ __forceinline__ int32_t up(int32_t n) const { return (static_cast<uint32_t>(n) + P - 1u) / P; }
+  // the first page that the window of token n needs
+  __device__ __forceinline__ int32_t left(int32_t n) const {
+    return window > 0 && n >= window ? (n - window + 1) / P : 0;
+  }
+  __device__ __forceinline__ bool holds(int32_t column, int32_t held) const {
+    return column < sinks || column >= left(held);
+  }
+};
+
+struct FreeWs {
+  size_t status, first, rel, last, total;  // see FreeDev
+};
+cudaError_t launch_cache_free(const avtp_cache_free_args_t& a, void* ws, const FreeWs& p, cudaStream_t s);
+
+struct ForkWs {
+  size_t status, first, fresh, mark, total;  // see ForkDev
+};
+cudaError_t launch_cache_fork(const avtp_cache_fork_args_t& a, void* ws, const ForkWs& p, cudaStream_t s);
+
+cudaError_t launch_cache_copy(const avtp_cache_t& c, const int32_t* src, const int32_t* dst, int64_t n, void* ws,
+                              cudaStream_t s);
+cudaError_t launch_cache_compact(const avtp_cache_t& c, const avtp_cache_compact_args_t& a, void* ws, cudaStream_t s);
+
 // ---------------------------------------------------------------- attention
 // Rows of a (request, KV head) are its (new token, head of the group) pairs, token by token.
 constexpr int kCacheMaxPieces = 32;   // pieces that a row block's keys are split into, at most

@@ -1,5 +1,6 @@
 // C ABI of the paged cache: argument validation, workspace plans and launches of
-// avtp_cache_slots, avtp_cache_write, avtp_rope and avtp_cache_attention; the frequencies of avtp_rope.
+// avtp_cache_slots, avtp_cache_write, avtp_rope, avtp_cache_attention and the upkeep of pages
+// (avtp_cache_compact, _copy, _fork, _free); the frequencies of avtp_rope.
 #include <math.h>
 
 #include "avtp_cache.cuh"
@@ -138,6 +139,77 @@ avtp_status_t check_attn(const avtp_cache_t* c, const avtp_cache_attn_args_t* a)
   return AVTP_OK;
 }
 
+// The kernels' 32-bit loops over requests or children step 1024 at a time, past the last.
+bool countable(int64_t n) { return n <= kInt32Max - 1024; }
+
+avtp_status_t check_table(const int32_t* table, int32_t max_pages, int64_t stride) {
+  return table != nullptr && max_pages >= 1 && stride >= max_pages ? AVTP_OK : AVTP_ERR_INVALID_ARG;
+}
+
+avtp_status_t check_window(int32_t window, int32_t n_sinks, const void* held_len) {
+  return window >= 0 && n_sinks >= 0 && (window == 0 || held_len != nullptr) ? AVTP_OK : AVTP_ERR_INVALID_ARG;
+}
+
+avtp_status_t check_compact(const avtp_cache_t* c, const avtp_cache_compact_args_t* a) {
+  avtp_status_t st = check_cache(c);
+  if (st != AVTP_OK) return st;
+  if (a == nullptr || a->n_requests < 1 || a->n_kept < 0) return AVTP_ERR_INVALID_ARG;
+  if (a->n_kept > kInt32Max || !countable(a->n_requests)) return AVTP_ERR_RANGE;
+  if (a->keep_cu == nullptr || a->seq_len == nullptr || (a->n_kept > 0 && a->keep_idx == nullptr)) return AVTP_ERR_INVALID_ARG;
+  if ((st = check_table(a->block_table, a->max_pages, a->table_stride)) != AVTP_OK) return st;
+  if (a->dst_table != nullptr && (st = check_table(a->dst_table, a->dst_max_pages, a->dst_stride)) != AVTP_OK) return st;
+  if (a->len_out == a->seq_len) return AVTP_ERR_INVALID_ARG;
+  return check_window(a->window, a->n_sinks, a->held_len);
+}
+
+avtp_status_t check_fork(const avtp_cache_fork_args_t* a) {
+  if (a == nullptr || a->n_requests < 1 || a->n_children < 0) return AVTP_ERR_INVALID_ARG;
+  avtp_status_t st = check_pool_size(a->n_pages, a->page_size);
+  if (st != AVTP_OK) return st;
+  if (!countable(a->n_requests) || !countable(a->n_children) || a->n_free > kInt32Max) return AVTP_ERR_RANGE;
+  if (a->n_free < 0 || (a->n_free > 0 && a->free_pages == nullptr)) return AVTP_ERR_INVALID_ARG;
+  if ((st = check_table(a->block_table, a->max_pages, a->table_stride)) != AVTP_OK) return st;
+  if (a->seq_len == nullptr || a->shared == nullptr) return AVTP_ERR_INVALID_ARG;
+  if (a->n_children > 0 && (a->parent == nullptr || a->child == nullptr || a->copy_src == nullptr || a->copy_dst == nullptr))
+    return AVTP_ERR_INVALID_ARG;
+  return check_window(a->window, a->n_sinks, a->held_len);
+}
+
+ForkWs plan_fork(const avtp_cache_fork_args_t& a) {
+  ForkWs p{};
+  const size_t R = static_cast<size_t>(a.n_requests), C = static_cast<size_t>(a.n_children);
+  p.status = 0;
+  p.first = align_up(sizeof(DevStatus));
+  p.fresh = p.first + align_up((C + 1) * 4);
+  p.mark = p.fresh + align_up(C * 4);
+  p.total = p.mark + align_up(R * 4);
+  return p;
+}
+
+avtp_status_t check_free(const avtp_cache_free_args_t* a) {
+  if (a == nullptr || a->n_requests < 1) return AVTP_ERR_INVALID_ARG;
+  avtp_status_t st = check_pool_size(a->n_pages, a->page_size);
+  if (st != AVTP_OK) return st;
+  if (!countable(a->n_requests) || a->n_free > kInt32Max) return AVTP_ERR_RANGE;
+  if (a->n_free < 0 || (a->n_free > 0 && a->free_pages == nullptr)) return AVTP_ERR_INVALID_ARG;
+  if ((st = check_table(a->block_table, a->max_pages, a->table_stride)) != AVTP_OK) return st;
+  if (a->seq_len == nullptr || a->new_len == nullptr || a->free_head == nullptr || a->seq_len_out == nullptr ||
+      a->free_head_out == nullptr || (a->window > 0 && a->held_len_out == nullptr))
+    return AVTP_ERR_INVALID_ARG;
+  return check_window(a->window, a->n_sinks, a->held_len);
+}
+
+FreeWs plan_free(const avtp_cache_free_args_t& a) {
+  FreeWs p{};
+  const size_t R = static_cast<size_t>(a.n_requests), n = a.shared != nullptr ? static_cast<size_t>(a.n_pages) : 0;
+  p.status = 0;
+  p.first = align_up(sizeof(DevStatus));
+  p.rel = p.first + align_up((R + 1) * 4);
+  p.last = p.rel + align_up(n * 4);
+  p.total = p.last + align_up(n * 4);
+  return p;
+}
+
 }  // namespace
 }  // namespace avtp
 
@@ -228,6 +300,58 @@ avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_a
   const CacheAttnWs p = plan_cache_attention(*cache, *args);
   if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
   return from_cuda(launch_cache_attention(*cache, *args, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,
+                                 size_t workspace_bytes, avtp_stream_t stream) {
+  avtp_status_t st = check_compact(cache, args);
+  if (st != AVTP_OK) return st;
+  if ((st = check_ws(workspace, workspace_bytes, sizeof(DevStatus))) != AVTP_OK) return st;
+  return from_cuda(launch_cache_compact(*cache, *args, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_cache_copy(const avtp_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n, void* workspace,
+                              size_t workspace_bytes, avtp_stream_t stream) {
+  avtp_status_t st = check_cache(cache);
+  if (st != AVTP_OK) return st;
+  if (n < 0 || (n > 0 && (src == nullptr || dst == nullptr))) return AVTP_ERR_INVALID_ARG;
+  if (n > kInt32Max) return AVTP_ERR_RANGE;
+  if ((st = check_ws(workspace, workspace_bytes, sizeof(DevStatus))) != AVTP_OK) return st;
+  return from_cuda(launch_cache_copy(*cache, src, dst, n, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_cache_fork_workspace_size(const avtp_cache_fork_args_t* args, size_t* bytes) {
+  const avtp_status_t st = check_fork(args);
+  if (st != AVTP_OK) return st;
+  if (bytes == nullptr) return AVTP_ERR_INVALID_ARG;
+  *bytes = plan_fork(*args).total;
+  return AVTP_OK;
+}
+
+avtp_status_t avtp_cache_fork(const avtp_cache_fork_args_t* args, void* workspace, size_t workspace_bytes,
+                              avtp_stream_t stream) {
+  avtp_status_t st = check_fork(args);
+  if (st != AVTP_OK) return st;
+  const ForkWs p = plan_fork(*args);
+  if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
+  return from_cuda(launch_cache_fork(*args, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_cache_free_workspace_size(const avtp_cache_free_args_t* args, size_t* bytes) {
+  const avtp_status_t st = check_free(args);
+  if (st != AVTP_OK) return st;
+  if (bytes == nullptr) return AVTP_ERR_INVALID_ARG;
+  *bytes = plan_free(*args).total;
+  return AVTP_OK;
+}
+
+avtp_status_t avtp_cache_free(const avtp_cache_free_args_t* args, void* workspace, size_t workspace_bytes,
+                              avtp_stream_t stream) {
+  avtp_status_t st = check_free(args);
+  if (st != AVTP_OK) return st;
+  const FreeWs p = plan_free(*args);
+  if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
+  return from_cuda(launch_cache_free(*args, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
