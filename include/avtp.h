@@ -589,6 +589,26 @@ AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* c
 AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                             void* workspace, size_t workspace_bytes, avtp_stream_t stream);
 
+/* avtp_cache_attention in a sliding window that keeps the first tokens in sight (sinks): the new token at place p =
+ * seq_len[r] - n_r + i of its request sees the cached tokens u <= p with u > p - window or u < n_sinks, a window of
+ * its own and `window` - 1 tokens before it. Work and bytes go by what is seen. */
+typedef struct {
+  int32_t window;    /* >= 1; one as long as the table's pages leaves nothing out */
+  int32_t n_sinks;   /* >= 0                                                      */
+} avtp_cache_window_t;
+
+AVTP_API avtp_status_t avtp_cache_window_attention_workspace_size(const avtp_cache_t* cache,
+                                                                  const avtp_cache_attn_args_t* args,
+                                                                  const avtp_cache_window_t* window, size_t* bytes);
+
+/* As avtp_cache_attention, with its results, errors and limits. Table entries of pages that no new token of their
+ * request sees a row of are not read (avtp_cache_free gives those pages back). A value that is not finite may reach the
+ * other tokens of its chunk only where one of these sees it (0 * inf). Tokens / (2 * (128 / G)) + n_requests blocks of rows, each of
+ * (window + n_sinks) / 128 + 10 steps or so, times n_kv_heads, above 2^31 return AVTP_ERR_RANGE. Asynchronous on `stream`. */
+AVTP_API avtp_status_t avtp_cache_window_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
+                                                   const avtp_cache_window_t* window, void* workspace,
+                                                   size_t workspace_bytes, avtp_stream_t stream);
+
 /* Upkeep of the cache's pages: cached prompts pruned further, several requests on one prompt, pages given back.
  *
  * Pages may have several holders. `shared` (device int32 [n_pages], zeros at first) is the number of a page's

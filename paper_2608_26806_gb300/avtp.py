@@ -121,6 +121,10 @@ class _CacheAttnArgs(ctypes.Structure):
                 ("lse_stride", c_int64)]
 
 
+class _CacheWindow(ctypes.Structure):
+    _fields_ = [("window", c_int32), ("n_sinks", c_int32)]
+
+
 class _CacheCompactArgs(ctypes.Structure):
     _fields_ = [("n_requests", c_int32), ("n_kept", c_int64), ("keep_cu", c_void_p), ("keep_idx", c_void_p),
                 ("base_cu", c_void_p), ("seq_len", c_void_p), ("block_table", c_void_p), ("max_pages", c_int32),
@@ -184,6 +188,10 @@ SIGNATURES = {
     "avtp_rope_frequencies": (c_int, [POINTER(_RopeFreqArgs), POINTER(c_float), POINTER(c_float)]),
     "avtp_cache_attention_workspace_size": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), POINTER(c_size_t)]),
     "avtp_cache_attention": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), c_void_p, c_size_t, c_void_p]),
+    "avtp_cache_window_attention_workspace_size": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs),
+                                                           POINTER(_CacheWindow), POINTER(c_size_t)]),
+    "avtp_cache_window_attention": (c_int, [POINTER(_Cache), POINTER(_CacheAttnArgs), POINTER(_CacheWindow), c_void_p,
+                                            c_size_t, c_void_p]),
     "avtp_cache_compact": (c_int, [POINTER(_Cache), POINTER(_CacheCompactArgs), c_void_p, c_size_t, c_void_p]),
     "avtp_cache_copy": (c_int, [POINTER(_Cache), c_void_p, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]),
     "avtp_cache_fork_workspace_size": (c_int, [POINTER(_CacheForkArgs), POINTER(c_size_t)]),
@@ -1037,10 +1045,13 @@ class CacheAttentionCall(_CacheCall):
     """A prepared avtp_cache_attention call: causal attention of a step's new tokens ``q`` (bf16 [T,
     Hq, head_dim], request r's rows ``cu_new[r] .. cu_new[r+1]``, at most ``max_new`` of them) over
     the cache, where each request has ``seq_len[r]`` tokens, the new ones among them. ``o`` (bf16, as
-    q) and ``lse`` (fp32 [Hq, T]; False for none) are written for those rows alone."""
+    q) and ``lse`` (fp32 [Hq, T]; False for none) are written for those rows alone. With ``window`` each token
+    sees itself, the ``window`` - 1 tokens before it and the request's first ``sinks``
+    (avtp_cache_window_attention)."""
 
     def __init__(self, cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,
-                 block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, workspace=None):
+                 block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, window=None, sinks=0,
+                 workspace=None):
         name = "cache_attention"
         _int32_list(name, "cu_new", cu_new)
         R = cu_new.shape[0] - 1
@@ -1070,22 +1081,26 @@ class CacheAttentionCall(_CacheCall):
             _ptr(block_table), max_pages, stride, float(softmax_scale if softmax_scale is not None else d ** -0.5),
             _ptr(self.o), self.o.stride(0) if T > 1 else Hq * d, _ptr(self.lse),
             self.lse.stride(0) if self.lse is not None and Hq > 1 else max(T, 1))
+        if window is None and int(sinks) != 0:
+            raise ValueError(f"{name}: sinks go with a window")
+        entry = "avtp_cache_attention" if window is None else "avtp_cache_window_attention"
+        structs = (self._c, self._a) if window is None else (self._c, self._a, _CacheWindow(int(window), int(sinks)))
         if workspace is None:
             n = c_size_t()
-            _check(load().avtp_cache_attention_workspace_size(ctypes.byref(self._c), ctypes.byref(self._a),
-                                                              ctypes.byref(n)), "avtp_cache_attention_workspace_size")
+            _check(getattr(load(), entry + "_workspace_size")(*(ctypes.byref(x) for x in structs), ctypes.byref(n)),
+                   entry + "_workspace_size")
             workspace = new_workspace(int(n.value), dev)
-        self._prepare("avtp_cache_attention", workspace, self._c, self._a)
+        self._prepare(entry, workspace, *structs)
 
 
 def cache_attention(cache: PagedCache, q: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,
-                    block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, workspace=None,
-                    stream=None):
-    """avtp_cache_attention: (o, lse) of a chunk of new tokens, or a single one, a request over the
-    paged cache. See :class:`CacheAttentionCall`."""
+                    block_table: torch.Tensor, *, max_new: int, softmax_scale=None, o=None, lse=None, window=None, sinks=0,
+                    workspace=None, stream=None):
+    """avtp_cache_attention, or with ``window`` avtp_cache_window_attention: (o, lse) of a chunk of new tokens, or a
+    single one, a request over the paged cache. See :class:`CacheAttentionCall`."""
     with _on_stream(stream):
         c = CacheAttentionCall(cache, q, cu_new, seq_len, block_table, max_new=max_new, softmax_scale=softmax_scale,
-                               o=o, lse=lse, workspace=workspace).run()
+                               o=o, lse=lse, window=window, sinks=sinks, workspace=workspace).run()
     return c.o, c.lse
 
 

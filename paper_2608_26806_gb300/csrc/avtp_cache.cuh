@@ -84,11 +84,14 @@ struct CacheAttnWs {
   size_t total;
 };
 CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a);
-cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, void* ws,
-                                   const CacheAttnWs& p, cudaStream_t s);
+// window 0: none
+cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w,
+                                   void* ws, const CacheAttnWs& p, cudaStream_t s);
+// False: a windowed call of more work than its kernels count.
+bool cache_attention_fits(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w);
 
 struct CacheAttnDev;
-cudaError_t launch_cache_chunk(int head_dim, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
+cudaError_t launch_cache_chunk(int head_dim, bool in_window, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
                                const CUtensorMap& mv, const CacheAttnDev& a, cudaStream_t s);
 
 }  // namespace avtp

@@ -1,5 +1,5 @@
 // C ABI of the paged cache: argument validation, workspace plans and launches of
-// avtp_cache_slots, avtp_cache_write, avtp_rope, avtp_cache_attention and the upkeep of pages
+// avtp_cache_slots, avtp_cache_write, avtp_rope, avtp_cache_attention (and _window_attention) and the upkeep of pages
 // (avtp_cache_compact, _copy, _fork, _free); the frequencies of avtp_rope.
 #include <math.h>
 
@@ -137,6 +137,13 @@ avtp_status_t check_attn(const avtp_cache_t* c, const avtp_cache_attn_args_t* a)
   if (a->lse != nullptr && a->lse_stride < a->n_tokens) return AVTP_ERR_INVALID_ARG;
   if (!(a->softmax_scale > 0.f) || !isfinite(a->softmax_scale)) return AVTP_ERR_INVALID_ARG;
   return AVTP_OK;
+}
+
+avtp_status_t check_window_attn(const avtp_cache_t* c, const avtp_cache_attn_args_t* a, const avtp_cache_window_t* w) {
+  const avtp_status_t st = check_attn(c, a);
+  if (st != AVTP_OK) return st;
+  if (w == nullptr || w->window < 1 || w->n_sinks < 0) return AVTP_ERR_INVALID_ARG;
+  return cache_attention_fits(*c, *a, *w) ? AVTP_OK : AVTP_ERR_RANGE;
 }
 
 // The kernels' 32-bit loops over requests or children step 1024 at a time, past the last.
@@ -299,7 +306,27 @@ avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_a
   if (st != AVTP_OK) return st;
   const CacheAttnWs p = plan_cache_attention(*cache, *args);
   if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
-  return from_cuda(launch_cache_attention(*cache, *args, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_cache_attention(*cache, *args, avtp_cache_window_t{0, 0}, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+avtp_status_t avtp_cache_window_attention_workspace_size(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
+                                                         const avtp_cache_window_t* window, size_t* bytes) {
+  const avtp_status_t st = check_window_attn(cache, args, window);
+  if (st != AVTP_OK) return st;
+  if (bytes == nullptr) return AVTP_ERR_INVALID_ARG;
+  *bytes = plan_cache_attention(*cache, *args).total;
+  return AVTP_OK;
+}
+
+avtp_status_t avtp_cache_window_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
+                                          const avtp_cache_window_t* window, void* workspace, size_t workspace_bytes,
+                                          avtp_stream_t stream) {
+  avtp_status_t st = check_window_attn(cache, args, window);
+  if (st != AVTP_OK) return st;
+  const CacheAttnWs p = plan_cache_attention(*cache, *args);
+  if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
+  return from_cuda(
+      launch_cache_attention(*cache, *args, *window, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,

@@ -17,6 +17,7 @@ struct CacheAttnDev {
   int64_t table_stride;
   int64_t n_tokens, n_pages;
   int R, max_new, max_pages, Hkv, G, page_size;
+  int window, sinks;  // a query at place p sees u <= p with u > p - window or u < sinks (kernels of a window alone)
   int box;           // rows of a TMA box: a power of two that divides the page size, at most a tile
   int step_shift;    // see CachePlan
   int both;          // both kernels are at work and share the SMs (see cache_ctas)
@@ -52,6 +53,20 @@ struct CacheRequest {
   __device__ __forceinline__ int64_t rows(const CacheAttnDev& a) const { return static_cast<int64_t>(n) * a.G; }
 };
 
+// In a window, the first key behind the sinks that a token at place p sees (p negative: it sees nothing).
+__device__ __forceinline__ int cache_low(const CacheAttnDev& a, int p) { return p < a.window ? 0 : p - a.window + 1; }
+// The tiles between the sinks' and the first that a row block sees are left out: of those behind the sinks', tile j is
+// the request's tile j + skip.
+struct CacheSkip {
+  int32_t sinks, skip;  // tiles
+  // `first`: place of the row block's first new token
+  __device__ __forceinline__ CacheSkip(const CacheAttnDev& a, int first, int tile_keys) {
+    sinks = (a.sinks + tile_keys - 1) / tile_keys;
+    skip = max(0, cache_low(a, first) / tile_keys - sinks);
+  }
+  __device__ __forceinline__ int tile(int j) const { return j < sinks ? j : j + skip; }
+};
+
 // The roles of a CTA share an instruction cache, which a second copy of their loops has cost more than
 // half of a kernel's speed, and a first pass over code waits for it. So what is not a role's inner
 // loop exists once a kernel: the waits (behind a first look), warp sums.
@@ -72,12 +87,19 @@ __device__ __forceinline__ bool cache_raised(const volatile int* flag) { return 
 // of 64 keys 7, a block of 128 keys of a unit, or its beginning, 20 (a tile 6, 8 or 10: two chunks
 // beside 22 single tokens 70, 65, 66 us, one of 2048 beside 63 255, 255, 289, one of 100 beside 63
 // 270, 293, 369). Clamped so that the sum over the requests is a 32-bit number.
+template <bool kWindow>
 __device__ __forceinline__ int2 cache_weights(const CacheAttnDev& a, const CacheRequest& q) {
   const int64_t most = 0x7fffffff / a.R;
-  if (q.rows(a) <= a.few_rows) return make_int2(static_cast<int>(min(most, int64_t(7) * a.Hkv * ((q.seq + 63) / 64))), 0);
+  // keys that a row block of so many tokens passes, at most
+  auto keys = [&](int all, int tokens) {
+    if (!kWindow) return all;
+    return static_cast<int>(min(static_cast<int64_t>(all), static_cast<int64_t>(a.window) + a.sinks + tokens));
+  };
+  if (q.rows(a) <= a.few_rows)
+    return make_int2(static_cast<int>(min(most, int64_t(7) * a.Hkv * ((keys(q.seq, q.n) + 63) / 64))), 0);
   const int rows = 2 * (kChunkRows / 2 / a.G);
   const int64_t units = static_cast<int64_t>((q.n + rows - 1) / rows) * a.Hkv;
-  return make_int2(0, static_cast<int>(min(most, 20 * units * (2 + max(0, q.seq - q.n / 2) / 128))));
+  return make_int2(0, static_cast<int>(min(most, 20 * units * (2 + keys(max(0, q.seq - q.n / 2), rows) / 128))));
 }
 // The CTAs that work in k_cache_attn (`few`) or k_cache_chunk, of the grid's. The first is bound by
 // memory, the second by the tensor cores, and a CTA of either fills an SM: where a call needs both
@@ -118,7 +140,7 @@ struct CachePlan {
   __device__ __forceinline__ static int share(const CacheAttnDev& a) { return (a.R + NT - 1) / NT; }
   // For more than kNearRequests requests, all threads: steps(request, most) gives a request's steps,
   // with those of its longest row block in `most`. NT is a multiple of 32.
-  template <class F>
+  template <bool kWindow, class F>
   __device__ void form(const CacheAttnDev& a, F steps) {
     const int tid = threadIdx.x, lane = tid & 31, each = share(a);
     if (tid == 0) {
@@ -136,7 +158,7 @@ struct CachePlan {
       if (fine) {
         sum += steps(q, longest);
         if (a.both) {
-          const int2 w = cache_weights(a, q);
+          const int2 w = cache_weights<kWindow>(a, q);
           atomicAdd(&few, w.x);
           atomicAdd(&chunk, w.y);
         }
@@ -165,6 +187,7 @@ struct CachePlan {
   }
 };
 // The loading warp's view of the line.
+template <bool kWindow>
 struct CacheLine {
   int total;  // 0 if validation refuses a length
   int most;   // steps of the longest row block (a row block's steps are one after the other on the line)
@@ -189,7 +212,7 @@ struct CacheLine {
       total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
       weights = make_int2(0, 0);
       if (a.both) {
-        const int2 w = lane < a.R && mine_ok ? cache_weights(a, mine) : make_int2(0, 0);
+        const int2 w = lane < a.R && mine_ok ? cache_weights<kWindow>(a, mine) : make_int2(0, 0);
         weights = make_int2(__reduce_add_sync(0xffffffffu, w.x), __reduce_add_sync(0xffffffffu, w.y));
       }
     }
@@ -252,19 +275,23 @@ __device__ __forceinline__ int piece_place(int run, bool begins) { return 2 * ru
 
 // Where a request's boxes of keys lie, 32 of them at a time: a warp looks them up in the block table, a
 // lane a box, and one thread issues their copies. Box i holds keys i * box ..
-struct CacheWindow {
+struct CacheBoxes {
   int2 at[32];  // page, row of the page
   // Boxes i0 .. i0 + 31 (i0 a multiple of 32) of a request of `seq` tokens; true if a page lies outside
-  // the pool: page 0 then stands in its place.
-  __device__ __forceinline__ bool load(const CacheAttnDev& a, const int32_t* row, int seq, int i0) {
+  // the pool: page 0 then stands in its place. In a window no page is looked up for boxes behind the sinks that end at
+  // or before key `low`, for it may have been let go of: their copies read behind the pool, and bring zeros.
+  template <bool kWindow>
+  __device__ __forceinline__ bool load(const CacheAttnDev& a, const int32_t* row, int seq, int i0, int low = 0) {
     const int lane = threadIdx.x & 31;
     const uint32_t i = static_cast<uint32_t>(i0 + lane), in_page = static_cast<uint32_t>(a.page_size / a.box);
     const uint32_t p = i / in_page;
     int page = 0;
-    if (static_cast<int64_t>(i) * a.box < seq) page = row[p];
+    const int64_t key = static_cast<int64_t>(i) * a.box;
+    const bool seen = !kWindow || key < a.sinks || key + a.box > low;
+    if (key < seq && seen) page = row[p];
     const bool bad = page < 0 || page >= a.n_pages;
-    __syncwarp();  // the window before has been used
-    at[lane] = make_int2(bad ? 0 : page, static_cast<int>(i - p * in_page) * a.box);
+    __syncwarp();  // the boxes before have been used
+    at[lane] = make_int2(!seen ? static_cast<int>(a.n_pages) : bad ? 0 : page, static_cast<int>(i - p * in_page) * a.box);
     __syncwarp();
     return __any_sync(0xffffffffu, bad);
   }

@@ -35,6 +35,9 @@
 // 3425 tokens 9.3 us instead of 9.05, four of 50000 124.3 instead of 123.6). Every wait is bounded; a CTA whose
 // wait gives up records AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and
 // their values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
+//
+// In a window (kWindow, see avtp.h) a row block's tiles are those of the sinks and those from its first token's window on;
+// the line of tiles is as long as what is seen. Keys that none of its rows sees are cleared like those behind the last.
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -84,7 +87,7 @@ struct Shared {
   uint64_t seg_full[2], seg_empty[2];
   Segment seg[2];
   CachePlan<kThreads> plan;
-  CacheWindow window[2];  // of the keys' warp, of the values'
+  CacheBoxes boxes[2];  // of the keys' warp, of the values'
   float m[kWarps][16], l[kWarps][16], w[kWarps][16];  // reference, sum of P, of its rounded values
   int32_t last;
   int abort, bad_page;
@@ -180,9 +183,10 @@ __device__ __forceinline__ void store_row(const CacheAttnDev& a, const Segment& 
 // ---------------------------------------------------------------- attention
 // Tiles of a row block: one for an empty cache, whose rows are zeros; none for requests without new
 // tokens, or with more rows than this kernel takes.
-template <int D>
+template <int D, bool kWindow>
 __device__ __forceinline__ int tiles_of(const CacheAttnDev& a, const CacheRequest& q) {
-  return q.n == 0 || q.rows(a) > a.few_rows ? 0 : max(1, (q.seq - 1) / tile_keys(D) + 1);
+  const int all = max(1, (q.seq - 1) / tile_keys(D) + 1);
+  return q.n == 0 || q.rows(a) > a.few_rows ? 0 : all - (kWindow ? CacheSkip(a, q.seq - q.n, tile_keys(D)).skip : 0);
 }
 
 __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
@@ -198,7 +202,7 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
 // and all panels of one head and page: one TMA instruction a page piece. (One a panel, at pages of 16
 // rows 16 of them a tile, issued too slowly: 4.4 TB/s.) kWM warps share the keys of a slice of the tile, 16
 // rows each: two from 17 rows on.
-template <int D, int kWM>
+template <int D, int kWM, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, CacheAttnDev a) {
   extern __shared__ unsigned char smem_raw[];
@@ -234,11 +238,11 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   pdl_trigger();
   __syncthreads();
   auto steps = [&](const CacheRequest& q, int& most) {
-    const int t = steps_of(a, tiles_of<D>(a, q));
+    const int t = steps_of(a, tiles_of<D, kWindow>(a, q));
     most = max(most, t);
     return t * a.Hkv;
   };
-  if (a.R > kNearRequests) sh.plan.form(a, steps);
+  if (a.R > kNearRequests) sh.plan.template form<kWindow>(a, steps);
   volatile int* abort_flag = &sh.abort;
 
   if (warp >= kKeyWarp) {
@@ -246,11 +250,11 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     const int kv = warp == kKeyWarp ? 0 : 1;
     const CUtensorMap* map = kv ? &mapV : &mapK;
     const int per_tile = kTile / a.box;
-    CacheLine line;
+    CacheLine<kWindow> line;
     CacheRuns runs;
     int t = 0, t1 = 0, pre = 0, r = 0;  // steps: next, the run's end, before request r
     if (kv == 0) {
-      line = CacheLine(a, sh.plan, mine, mine_ok, steps);
+      line = CacheLine<kWindow>(a, sh.plan, mine, mine_ok, steps);
       runs = CacheRuns(line.total, line.most, 1, cache_ctas(a, line.weights, true));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
@@ -276,7 +280,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 #pragma unroll 1
           for (;; ++r) {
             q = line.request(a, mine, r);
-            tiles = tiles_of<D>(a, q);
+            tiles = tiles_of<D, kWindow>(a, q);
             len = steps_of(a, tiles);
             if (t < pre + len * a.Hkv) break;
             pre += len * a.Hkv;
@@ -304,10 +308,13 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       }
       if (g.head < 0) break;
       const int32_t* row = a.table + g.req * a.table_stride;
-      for (int tile = g.tile0; tile < g.tile1 && !cache_raised(abort_flag); ++tile, ++n) {
+      const CacheSkip skip(a, g.seq - g.n, kTile);  // used in a window alone, as low is
+      const int low = cache_low(a, g.seq - g.n);
+      for (int j = g.tile0; j < g.tile1 && !cache_raised(abort_flag); ++j, ++n) {
+        const int tile = kWindow ? skip.tile(j) : j;
         const int i0 = tile * per_tile, sb = n % kStages;
-        if (tile == g.tile0 || (i0 & 31) == 0)
-          if (sh.window[kv].load(a, row, g.seq, i0 & ~31)) sh.bad_page = g.req;
+        if (j == g.tile0 || (i0 & 31) == 0 || (kWindow && j == skip.sinks))
+          if (sh.boxes[kv].template load<kWindow>(a, row, g.seq, i0 & ~31, low)) sh.bad_page = g.req;
         const int keys = min(kTile, g.seq - tile * kTile);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
         if (tc::elect_one()) {
@@ -318,7 +325,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
             unsigned char* dst = smem + sb * stage_bytes(D) + kv * (stage_bytes(D) / 2);
 #pragma unroll 1
             for (int b = 0; b < boxes; ++b, dst += a.box * D * 2) {
-              const int2 at = sh.window[kv].at[(i0 + b) & 31];
+              const int2 at = sh.boxes[kv].at[(i0 + b) & 31];
               tma_load_5d(dst, map, at.y, g.head, at.x, &sh.kv_full[sb]);
             }
           }
@@ -349,6 +356,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       // Q as the A operand; keys visible to this lane's two rows
       uint32_t qa[D / 16][4];
       int limit[2];
+      int low[2];  // in a window, the first keys behind the sinks that they see
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = wm * 16 + gr + 8 * i;
@@ -365,7 +373,10 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         // A row that is not stored: q = 0. It sees no more than the others, or 0 x NaN behind the request's
         // last key would have its warp look for the maximum and move stored rows' references.
         if (row >= rows) limit[i] = g.seq;
+        low[i] = cache_low(a, row >= rows ? g.seq - 1 : g.seq - g.n + tok);
       }
+      const CacheSkip skip(a, g.seq - g.n, kTile);
+      const int first_low = cache_low(a, g.seq - g.n), last_low = cache_low(a, g.seq - 1);  // of the first token and the last
       const int all_see = g.seq - g.n + 1;  // keys that every row sees
 
       float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
@@ -374,7 +385,8 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
 
-      for (int tile = g.tile0; tile < g.tile1; ++tile, ++n) {
+      for (int j = g.tile0; j < g.tile1; ++j, ++n) {
+        const int tile = kWindow ? skip.tile(j) : j;
         const int sb = n % kStages;
         if (!cache_wait_warp(&sh.kv_full[sb], (n / kStages) & 1)) {
           *abort_flag = 1;
@@ -429,6 +441,16 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 if (key0 + i * 8 + 2 * tq + (e & 1) >= limit[e >> 1]) s[i][e] = -INFINITY;
+            }
+          }
+          if (kWindow && key0 < last_low && key0 + kKeys > a.sinks) {
+#pragma unroll
+            for (int i = 0; i < kKeys / 8; ++i) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = key0 + i * 8 + 2 * tq + (e & 1);
+                if (key < low[e >> 1] && key >= a.sinks) s[i][e] = -INFINITY;
+              }
             }
           }
           // P against the rows' references, and its sums. Only a sum above kRescaleSum, a row
@@ -488,6 +510,21 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
               const int left = g.seq - (key0 + kk * 16 + 2 * tq);
               const uint32_t k0 = left > 1 ? 0xffffffffu : (left == 1 ? 0xffffu : 0u);
               const uint32_t k1 = left > 9 ? 0xffffffffu : (left == 9 ? 0xffffu : 0u);
+#pragma unroll
+              for (int c = 0; c < D / 16; ++c) {
+                f[c][0] &= k0;
+                f[c][1] &= k1;
+                f[c][2] &= k0;
+                f[c][3] &= k1;
+              }
+            }
+            if (kWindow && key0 < first_low && key0 + kKeys > a.sinks) {
+              // and those that none of the rows sees
+              auto mask = [&](int key) {  // of two neighbours
+                auto one = [&](int u) { return u < first_low && u >= a.sinks ? 0u : 0xffffu; };
+                return one(key) | (one(key + 1) << 16);
+              };
+              const uint32_t k0 = mask(key0 + kk * 16 + 2 * tq), k1 = mask(key0 + kk * 16 + 2 * tq + 8);
 #pragma unroll
               for (int c = 0; c < D / 16; ++c) {
                 f[c][0] &= k0;
@@ -758,15 +795,34 @@ bool query_map(CUtensorMap* m, const avtp_cache_attn_args_t& a, int d, int G) {
   return encode(m, 3, a.q, dims, strides, box);
 }
 
-template <int D, int kWM>
+template <int D, int kWM, bool kWindow>
 cudaError_t launch_attn(int grid, const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnDev& a, cudaStream_t s) {
   static PerDevice attrs;
   const cudaError_t e = once_per_device(attrs, [](int, int*) {
-    return cudaFuncSetAttribute(k_cache_attn<D, kWM>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(k_cache_attn<D, kWM, kWindow>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 static_cast<int>(smem_bytes(D)));
   });
   if (e != cudaSuccess) return e;
-  return launch_kernel(k_cache_attn<D, kWM>, dim3(grid), dim3(kThreads), smem_bytes(D), s, /*pdl=*/true, mk, mv, a);
+  return launch_kernel(k_cache_attn<D, kWM, kWindow>, dim3(grid), dim3(kThreads), smem_bytes(D), s, /*pdl=*/true, mk, mv, a);
+}
+
+// A request's keys, at most (CacheRequest refuses more).
+int64_t most_keys(const avtp_cache_t& c, const avtp_cache_attn_args_t& a) {
+  const int64_t table = static_cast<int64_t>(a.max_pages) * c.page_size;
+  return table < kCacheMostKeys ? table : kCacheMostKeys;
+}
+// Whether the window may leave a key out: one as long as a request may be is no window.
+bool windowed(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w) {
+  return w.window > 0 && w.window < most_keys(c, a);
+}
+// Steps of k_cache_chunk's line, at most, in a window: its sums of units' blocks in closed form want steps of one block,
+// so that this has to stay below 2^31.
+double chunk_steps(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w) {
+  const int G = a.n_q_heads / c.n_kv_heads;
+  if (static_cast<int64_t>(a.max_new) * G <= kCacheFewRows) return 0.0;
+  const double tokens = 2 * (kChunkRows / 2 / G), all = static_cast<double>(most_keys(c, a));
+  const double seen = static_cast<double>(w.window) + w.n_sinks + tokens;  // keys of a unit, but for blocks' ends
+  return (a.n_tokens / tokens + a.n_requests) * ((seen < all ? seen : all) / kChunkKeys + 8) * c.n_kv_heads;
 }
 
 // What the call's bounds leave to each kernel.
@@ -815,8 +871,12 @@ CacheAttnWs plan_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_ar
   return p;
 }
 
-cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, void* ws,
-                                   const CacheAttnWs& p, cudaStream_t s) {
+bool cache_attention_fits(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w) {
+  return !windowed(c, a, w) || chunk_steps(c, a, w) < 2147483648.0;
+}
+
+cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w,
+                                   void* ws, const CacheAttnWs& p, cudaStream_t s) {
   const Shape sh = shape_of(c, a);
   CacheAttnDev d{};
   d.q = static_cast<const __nv_bfloat16*>(a.q);
@@ -853,8 +913,10 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
     while (static_cast<double>(blocks) * static_cast<double>((tiles >> sft) + 4) * c.n_kv_heads >= 2147483648.0) ++sft;
     return sft;
   };
-  // a request's keys, at most (CacheRequest refuses more)
-  const int64_t table = static_cast<int64_t>(a.max_pages) * c.page_size, keys = table < kCacheMostKeys ? table : kCacheMostKeys;
+  const int64_t keys = most_keys(c, a);
+  const bool in_window = windowed(c, a, w);
+  d.window = w.window;
+  d.sinks = static_cast<int>(w.n_sinks < keys ? w.n_sinks : keys);
   const int grid = device_sm_count();
   cudaError_t e = launch_kernel(k_cache_prep, dim3(1), dim3(kPrepThreads), 0, s, /*pdl=*/true, d, grid);
   if (e != cudaSuccess || a.n_tokens == 0) return e;
@@ -873,16 +935,20 @@ cudaError_t launch_cache_attention(const avtp_cache_t& c, const avtp_cache_attn_
     d.box = box(tile_keys(c.head_dim));
     d.step_shift = shift(a.n_requests, keys / tile_keys(c.head_dim));
     if (!rows_map(&mk, pk, c, d.box) || !rows_map(&mv, pv, c, d.box)) return cudaErrorInvalidValue;
-    auto launch = c.head_dim == 128 ? (sh.row_warps == 1 ? launch_attn<128, 1> : launch_attn<128, 2>)
-                                    : (sh.row_warps == 1 ? launch_attn<64, 1> : launch_attn<64, 2>);
+    auto pick = [&](auto win) {
+      constexpr bool kWindow = decltype(win)::value;
+      return c.head_dim == 128 ? (sh.row_warps == 1 ? launch_attn<128, 1, kWindow> : launch_attn<128, 2, kWindow>)
+                               : (sh.row_warps == 1 ? launch_attn<64, 1, kWindow> : launch_attn<64, 2, kWindow>);
+    };
+    auto launch = in_window ? pick(std::true_type{}) : pick(std::false_type{});
     if ((e = launch(grid, mk, mv, d, s)) != cudaSuccess) return e;
   }
   if (!sh.chunks) return cudaSuccess;
   d.box = box(kChunkKeys);
-  d.step_shift = shift(a.n_tokens / (2 * (kChunkRows / 2 / d.G)) + a.n_requests, keys / kChunkKeys);
+  d.step_shift = in_window ? 0 : shift(a.n_tokens / (2 * (kChunkRows / 2 / d.G)) + a.n_requests, keys / kChunkKeys);
   if (!panel_map(&mk, pk, c, d.box) || !panel_map(&mv, pv, c, d.box) || !query_map(&mq, a, c.head_dim, d.G))
     return cudaErrorInvalidValue;
-  return launch_cache_chunk(c.head_dim, grid, mq, mk, mv, d, s);
+  return launch_cache_chunk(c.head_dim, in_window, grid, mq, mk, mv, d, s);
 }
 
 }  // namespace avtp

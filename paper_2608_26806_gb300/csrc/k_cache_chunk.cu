@@ -45,6 +45,10 @@
 // TFLOP/s. (With 30 ms between the calls, at full clock, 497 and 511 us.) At d = 64 8192 behind 2176 takes 443 us:
 // 2510 cycles a block, since that chain does not depend on d, with the tensor pipe 41 % active.
 //
+// In a window (kWindow, see avtp.h) a unit's blocks are those of the sinks and those from its first token's window on
+// (Segment::block gives a block's place among the request's); its last blocks are masked above and its first ones
+// below, and values that none of its rows sees are cleared as those behind the last key are.
+//
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
 // CTA whose wait gives up records AVTP_ERR_TIMEOUT and leaves.
@@ -90,8 +94,20 @@ __host__ __device__ constexpr size_t chunk_smem_bytes(int d) {
   return need > 116 * 1024 ? need : 116 * 1024;
 }
 
+template <bool kWindow>
+struct SegmentSkip {
+  __device__ __forceinline__ int skipped() const { return 0; }
+  __device__ __forceinline__ int block(int j) const { return j; }
+};
+template <>
+struct SegmentSkip<true> {
+  int32_t sinks, skip;  // see CacheSkip
+  __device__ __forceinline__ int skipped() const { return skip; }
+  __device__ __forceinline__ int block(int j) const { return j < sinks ? j : j + skip; }
+};
 // A run's part of one unit: key blocks j0 .. j1 - 1.
-struct Segment {
+template <bool kWindow>
+struct Segment : SegmentSkip<kWindow> {
   int32_t row0, n, seq;  // the request's first packed row, new and cached tokens
   int32_t head, unit;    // KV head (-1: no more), unit of the request
   int32_t j0, j1;
@@ -107,10 +123,11 @@ struct Segment {
   __device__ __forceinline__ int blocks(int s) const {
     if (!live(s)) return 0;
     const int all = max(1, (seq - n + tok1(s) + kKB - 1) / kKB);
-    return max(0, min(j1, all) - j0);
+    return max(0, min(j1, all - this->skipped()) - j0);
   }
 };
 
+template <bool kWindow>
 struct ChunkSync {
   uint64_t seg_full[2], seg_empty[2];
   uint64_t q_full, q_empty;
@@ -121,13 +138,13 @@ struct ChunkSync {
   uint64_t half_done[2];   // P V of a block's first half complete (when someone may wait for that)
   uint64_t o_done[2];      // P V of a slot's last block in the segment complete
   uint64_t drain;
-  Segment seg[2];
+  Segment<kWindow> seg[2];
   CachePlan<kThreads> plan;
-  CacheWindow window[2];  // of the keys' warp, of the values'
+  CacheBoxes boxes[2];  // of the keys' warp, of the values'
   uint32_t tmem;
   int abort, bad_page;
 };
-static_assert(chunk_smem_bytes(128) + sizeof(ChunkSync) <= 227 * 1024, "shared memory of one CTA");
+static_assert(chunk_smem_bytes(128) + sizeof(ChunkSync<true>) <= 227 * 1024, "shared memory of one CTA");
 
 // sum_{i < n} floor((a i + b) / m), by Euclid's steps on (a, m); a n + b is below 2^32, the sum below 2^31.
 __host__ __device__ inline uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b) {
@@ -147,9 +164,12 @@ __host__ __device__ inline uint32_t floor_sum(uint32_t n, uint32_t m, uint32_t a
 }
 
 // Key blocks of a request's unit: those of its last token, one for a token that sees nothing.
-__device__ __forceinline__ int unit_blocks(const CacheRequest& q, int nt, int u) {
-  return max(1, (q.seq - q.n + static_cast<int>(min((u + 1) * static_cast<int64_t>(2 * nt), static_cast<int64_t>(q.n))) +
-                 kKB - 1) / kKB);
+// (In a window only what the unit sees of them.)
+template <bool kWindow>
+__device__ __forceinline__ int unit_blocks(const CacheAttnDev& a, const CacheRequest& q, int nt, int u) {
+  const int all = max(1, (q.seq - q.n + static_cast<int>(min((u + 1) * static_cast<int64_t>(2 * nt), static_cast<int64_t>(q.n))) +
+                          kKB - 1) / kKB);
+  return kWindow ? all - CacheSkip(a, q.seq - q.n + u * 2 * nt, kKB).skip : all;
 }
 __device__ __forceinline__ int units_of(const CacheAttnDev& a, const CacheRequest& q, int nt) {
   return q.rows(a) > a.few_rows ? (q.n + 2 * nt - 1) / (2 * nt) : 0;
@@ -157,9 +177,9 @@ __device__ __forceinline__ int units_of(const CacheAttnDev& a, const CacheReques
 
 // Behind the queries before (qn of them), a segment's, by one thread of the calling warp; false if the
 // wait gave up.
-template <int D>
-__device__ __noinline__ bool load_queries(const CUtensorMap* map, unsigned char* sQ, const Segment& g, int G, ChunkSync& sy,
-                                          int qn) {
+template <int D, bool kWindow>
+__device__ __noinline__ bool load_queries(const CUtensorMap* map, unsigned char* sQ, const Segment<kWindow>& g, int G,
+                                          ChunkSync<kWindow>& sy, int qn) {
   bool ok = true;
   if (tc::elect_one()) {
     ok = qn == 0 || cache_wait(&sy.q_empty, (qn - 1) & 1);
@@ -182,24 +202,32 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int blocks) {
 // last token sees x = past + rows (i + 1) keys, for which it has kUnitSteps + max(1, ceil(x / (128 * 2^step_shift))) of them. For
 // requests of more than kNearUnits units: 128 of them, added up one by one and passed one by one, took up to
 // 24000 cycles before a CTA's first product and take 9000 so; eight of them 2500 and 5300.
+// In a window (step_shift 0) less the blocks that it leaves out: floor((past + rows i - window + 1) / 128) less the
+// sinks' of unit i, where that is positive.
 constexpr int kNearUnits = 32;
-static __device__ __noinline__ int steps_before(int past, int rows, int step_shift, int u) {
+template <bool kWindow>
+static __device__ __noinline__ int steps_before(const CacheAttnDev& a, int past, int rows, int u) {
   const int blind = past >= 0 ? 0 : min(u, -past / rows);  // units that see nothing
-  const uint32_t keys = static_cast<uint32_t>(kKB) << step_shift;
+  const uint32_t keys = static_cast<uint32_t>(kKB) << a.step_shift;
   int sum = kUnitSteps * u + blind;
   if (u > blind) sum += floor_sum(u - blind, keys, rows, past + (blind + 1) * rows + keys - 1);
+  if (kWindow) {
+    const int64_t at = static_cast<int64_t>(past) - a.window + 1 - static_cast<int64_t>((a.sinks + kKB - 1) / kKB) * kKB;
+    const int64_t first = at >= 0 ? 0 : (-at + rows - 1) / rows;
+    if (first < u) sum -= floor_sum(u - static_cast<int>(first), kKB, rows, static_cast<uint32_t>(at + first * rows));
+  }
   return sum;
 }
 
 // ---------------------------------------------------------------- attention
 // mapQ: q {d, Hq, T}, box 64 x G x floor(128 / G); mapK, mapV: the cache as
 // {d, row of the page, head, page}, box of 64 elements and `box` rows.
-template <int D>
+template <int D, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK,
               const __grid_constant__ CUtensorMap mapV, CacheAttnDev a) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ ChunkSync sy;
+  __shared__ ChunkSync<kWindow> sy;
   unsigned char* smem =
       reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   constexpr uint32_t kTile = tile_bytes(D);
@@ -253,17 +281,19 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   auto steps = [&](const CacheRequest& q, int& most) {
     const int U = units_of(a, q, nt);
     if (U == 0) return 0;
-    int sum = steps_of(a, unit_blocks(q, nt, U - 1));  // the last unit may be short
-    most = max(most, sum);
+    int sum = steps_of(a, unit_blocks<kWindow>(a, q, nt, U - 1));  // the last unit may be short
+    // In a window an earlier unit may be longer: its first and last blocks end elsewhere, and the last one's tokens
+    // may be fewer.
+    most = max(most, sum + (kWindow && U > 1 ? 1 + (2 * nt + kKB - 1) / kKB : 0));
     if (U > kNearUnits) {
-      sum += steps_before(q.seq - q.n, 2 * nt, a.step_shift, U - 1);
+      sum += steps_before<kWindow>(a, q.seq - q.n, 2 * nt, U - 1);
     } else {
 #pragma unroll 1
-      for (int u = 0; u < U - 1; ++u) sum += steps_of(a, unit_blocks(q, nt, u));
+      for (int u = 0; u < U - 1; ++u) sum += steps_of(a, unit_blocks<kWindow>(a, q, nt, u));
     }
     return sum * a.Hkv;
   };
-  if (a.R > kNearRequests) sy.plan.form(a, steps);
+  if (a.R > kNearRequests) sy.plan.template form<kWindow>(a, steps);
 
   // The ring. K_j and V_j of a segment lie in stages 2 (j % 2) and 2 (j % 2) + 1. The MMA thread
   // releases V_j and K_{j + 1} together, behind the last product with either: kv_empty[j % 2], once
@@ -282,11 +312,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     int t = 0, t1 = 0, pre = 0;  // steps: next, the run's end, before unit u of request r
     int r = 0, u = 0;
     CacheRuns runs;
-    CacheLine line;
+    CacheLine<kWindow> line;
     CacheChunkSplit split{};
     split.c1 = -1;
     if (kv == 0) {
-      line = CacheLine(a, sy.plan, mine, mine_ok, steps);
+      line = CacheLine<kWindow>(a, sy.plan, mine, mine_ok, steps);
       runs = CacheRuns(line.total, line.most, kUnitSteps + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
@@ -300,18 +330,18 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
 #pragma unroll 1
           for (int n = U; n > 1;) {  // it is among units u .. u + n - 1
             const int each = (n + 31) / 32, at = lane * each;
-            const bool before = at < n && pre + steps_before(past, 2 * nt, a.step_shift, u + at) * a.Hkv <= t;
+            const bool before = at < n && pre + steps_before<kWindow>(a, past, 2 * nt, u + at) * a.Hkv <= t;
             const int on = (__popc(__ballot_sync(0xffffffffu, before)) - 1) * each;
             u += on;
             n = min(each, n - on);
           }
-          pre += steps_before(past, 2 * nt, a.step_shift, u) * a.Hkv;
+          pre += steps_before<kWindow>(a, past, 2 * nt, u) * a.Hkv;
         }
       }
     }
 #pragma unroll 1
     for (int sc = 0;; ++sc) {
-      Segment g{};
+      Segment<kWindow> g{};
       if (kv == 0) {
         g.head = -1;
         int end = t;
@@ -324,7 +354,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             const int U = units_of(a, q, nt);
 #pragma unroll 1
             for (; u < U; ++u) {
-              nb = unit_blocks(q, nt, u);
+              nb = unit_blocks<kWindow>(a, q, nt, u);
               len = steps_of(a, nb);
               if (t < pre + len * a.Hkv) break;
               pre += len * a.Hkv;
@@ -341,6 +371,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           g.seq = q.seq;
           g.nt = nt;
           g.unit = u;
+          if constexpr (kWindow) {
+            const CacheSkip skip(a, q.seq - q.n + u * 2 * nt, kKB);
+            g.sinks = skip.sinks;
+            g.skip = skip.skip;
+          }
           g.req = r;
           g.j0 = max(0, t - s - kUnitSteps) << a.step_shift;
           g.j1 = min(nb, (end - s - kUnitSteps) << a.step_shift);
@@ -368,18 +403,21 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       if (g.head < 0) break;
       const int32_t* row = a.table + g.req * a.table_stride;
       const int blocks = g.j1 - g.j0;
+      const int low = kWindow ? cache_low(a, g.seq - g.n + g.tok0(0)) : 0;
       // the first queries wait for nothing; later ones come behind the segment's first keys, which
       // need not wait for the last product with the queries before
       if (kv == 0 && sc == 0) {
-        ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
+        ok = load_queries<D, kWindow>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
         qn = ok ? 1 : 0;
       }
 #pragma unroll 1
       for (int j = 0; j < blocks && !cache_raised(abort_flag); ++j) {
-        const int i0 = (g.j0 + j) * per_block, sb = 2 * (j & 1) + kv;
-        if (j == 0 || (i0 & 31) == 0)
-          if (sy.window[kv].load(a, row, g.seq, i0 & ~31)) sy.bad_page = g.req;
-        const int keys = min(kKB, g.seq - (g.j0 + j) * kKB);  // none: an empty cache
+        const int block = g.block(g.j0 + j), i0 = block * per_block, sb = 2 * (j & 1) + kv;
+        bool jump = false;
+        if constexpr (kWindow) jump = g.j0 + j == g.sinks;
+        if (j == 0 || (i0 & 31) == 0 || jump)
+          if (sy.boxes[kv].template load<kWindow>(a, row, g.seq, i0 & ~31, low)) sy.bad_page = g.req;
+        const int keys = min(kKB, g.seq - block * kKB);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
         // the stage's last occupant, block j - 2: V_{j - 2} is released in step j - 2, K_{j - 2} in
         // step j - 3; before the first two keys, the last release of the segment before, before the
@@ -401,7 +439,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             unsigned char* dst = sKV + sb * kTile;
 #pragma unroll 1
             for (int b = 0; b < boxes; ++b, dst += a.box * 128) {
-              const int2 at = sy.window[kv].at[(i0 + b) & 31];
+              const int2 at = sy.boxes[kv].at[(i0 + b) & 31];
 #pragma unroll
               for (int p = 0; p < D / 64; ++p)
                 tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, &sy.kv_full[sb]);
@@ -411,7 +449,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         __syncwarp();
         if (j & 1) ++loads1; else ++loads0;
         if (kv == 0 && j == 0 && sc > 0) {
-          ok = load_queries<D>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
+          ok = load_queries<D, kWindow>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
           if (ok) qn = sc + 1;
         }
       }
@@ -467,11 +505,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       for (int sc = 0; !bad; ++sc) {
         wait(&sy.seg_full[sc & 1], (sc >> 1) & 1, false);
         if (bad) break;
-        const Segment g = sy.seg[sc & 1];
+        const Segment<kWindow> g = sy.seg[sc & 1];
         tc::mbar_arrive(&sy.seg_empty[sc & 1]);
         if (g.head < 0) break;
         const int n0 = g.blocks(0), n1 = g.blocks(1), nm = max(n0, n1);
-        const int last_steps = max(0, (min(kKB, g.seq - (g.j1 - 1) * kKB) + 15) >> 4);
+        const int last_steps = max(0, (min(kKB, g.seq - g.block(g.j1 - 1) * kKB) + 15) >> 4);
         wait(&sy.q_full, sc & 1, false);
         wait(&sy.kv_full[0], ph0, false);
         tc::fence_after_sync();
@@ -557,7 +595,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     for (int sc = 0;; ++sc) {
       ok = cache_wait_warp(&sy.seg_full[sc & 1], (sc >> 1) & 1);
       if (!ok) break;
-      const Segment g = sy.seg[sc & 1];
+      const Segment<kWindow> g = sy.seg[sc & 1];
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&sy.seg_empty[sc & 1]);
       if (g.head < 0) break;
@@ -567,6 +605,13 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // keys this row sees (all of them for a row that is not stored), and every row of the warp
       const int limit = live ? max(0, g.seq - g.n + tok + 1) : 0x7fffffff;
       const int all_see = __reduce_min_sync(0xffffffffu, limit);
+      // in a window: the first key behind the sinks that this row sees, every row of the warp, any row of the unit
+      int low = 0, all_low = 0, unit_low = 0;
+      if (kWindow) {
+        low = live ? cache_low(a, g.seq - g.n + tok) : 0;
+        all_low = __reduce_max_sync(0xffffffffu, low);
+        unit_low = cache_low(a, g.seq - g.n + g.tok0(0));
+      }
       // row reference (log2 units), sum of exp2(c2 s - m). The reference begins as the maximum of the
       // first half, which is in registers anyway (the whole block's, with the half's exponentials
       // taken twice, cost 1400 cycles a segment; beginning at 0, sharp queries moved it too often).
@@ -575,8 +620,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         ok = cache_wait_warp(&sy.s_full[slot], (done + j) & 1);
         if (!ok) break;
         tc::fence_after_sync();
-        const int key0 = (g.j0 + j) * kKB;
-        const bool masked = key0 + kKB > all_see;
+        const int key0 = g.block(g.j0 + j) * kKB;
+        const bool masked = key0 + kKB > all_see || (kWindow && key0 < all_low && key0 + kKB > a.sinks);
         const int seen = limit - key0;  // of the block's keys
         const int valid = g.seq - key0;
         if (masked && quad == 0 && valid < kKB && valid > 0) {
@@ -592,6 +637,20 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           for (int e = lane; e < dead * 8 * (D / 64); e += 32) {
             const int ac = e / (dead * 8), w = e - ac * dead * 8;
             *reinterpret_cast<uint4*>(v + ac * kPanel + valid * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          tc::fence_proxy_async();
+        }
+        if (kWindow && key0 < unit_low && key0 + kKB > a.sinks) {
+          // likewise the values before the unit's first window and behind the sinks, a quarter of them a warp
+          const int sb = 2 * (j & 1) + 1;
+          ok = cache_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
+          if (!ok) break;
+          unsigned char* v = sKV + sb * kTile;
+          const int from = max(0, a.sinks - key0), rows = min(kKB, unit_low - key0) - from;
+#pragma unroll 1
+          for (int e = quad * 32 + lane; e < rows * 8 * (D / 64); e += 32 * kSlotWarps) {
+            const int ac = e / (rows * 8), w = e - ac * rows * 8;
+            *reinterpret_cast<uint4*>(v + ac * kPanel + from * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           tc::fence_proxy_async();
         }
@@ -658,6 +717,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
               const int left = seen - at * 64;
 #pragma unroll
               for (int c = 0; c < 64; ++c) su[c] = c < left ? su[c] : 0xff800000u;
+              if (kWindow) {
+                const int below = low - key0 - at * 64, sinks = a.sinks - key0 - at * 64;
+#pragma unroll
+                for (int c = 0; c < 64; ++c) su[c] = c >= below || c < sinks ? su[c] : 0xff800000u;
+              }
             }
             if (mode != kPlain) {
               float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -867,25 +931,27 @@ __global__ void __launch_bounds__(kChunkRows) k_cache_join(CacheAttnDev a, int d
   if (blockIdx.y == 0 && a.lse != nullptr) a.lse[head * a.lse_stride + t] = (M + log2f(L)) * kLn2;
 }
 
-template <int D>
+template <int D, bool kWindow>
 cudaError_t launch(int grid, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CacheAttnDev& a,
                    cudaStream_t s) {
   static PerDevice attrs;
   cudaError_t e = once_per_device(attrs, [](int, int*) {
-    return cudaFuncSetAttribute(k_cache_chunk<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(k_cache_chunk<D, kWindow>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 static_cast<int>(chunk_smem_bytes(D)));
   });
   if (e != cudaSuccess) return e;
-  e = launch_kernel(k_cache_chunk<D>, dim3(grid), dim3(kThreads), chunk_smem_bytes(D), s, /*pdl=*/true, mq, mk, mv, a);
+  e = launch_kernel(k_cache_chunk<D, kWindow>, dim3(grid), dim3(kThreads), chunk_smem_bytes(D), s, /*pdl=*/true, mq, mk, mv, a);
   if (e != cudaSuccess) return e;
   return launch_kernel(k_cache_join, dim3(grid, D / 16), dim3(kChunkRows), 0, s, /*pdl=*/true, a, D);
 }
 
 }  // namespace
 
-cudaError_t launch_cache_chunk(int head_dim, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
+cudaError_t launch_cache_chunk(int head_dim, bool in_window, int grid, const CUtensorMap& mq, const CUtensorMap& mk,
                                const CUtensorMap& mv, const CacheAttnDev& a, cudaStream_t s) {
-  return head_dim == 128 ? launch<128>(grid, mq, mk, mv, a, s) : launch<64>(grid, mq, mk, mv, a, s);
+  if (in_window)
+    return head_dim == 128 ? launch<128, true>(grid, mq, mk, mv, a, s) : launch<64, true>(grid, mq, mk, mv, a, s);
+  return head_dim == 128 ? launch<128, false>(grid, mq, mk, mv, a, s) : launch<64, false>(grid, mq, mk, mv, a, s);
 }
 
 }  // namespace avtp
