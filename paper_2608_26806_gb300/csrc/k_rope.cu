@@ -4,67 +4,85 @@
 //   z_a = f (y_a cos t - y_b sin t),  z_b = f (y_b cos t + y_a sin t),  t = pos[plane_i] inv_freq_i
 // for the pairs (a, b) = (i, i + rot/2) or (2i, 2i + 1) of a head's first rot elements; the others are y.
 //
-// What bounds it: bytes. Each q, k and v row is read and written once, and a head's norm and rotation are
-// between. A head is D/16 lanes of 16 elements each, held as two pieces of V elements (or twice two of four) that
-// turn into one another: piece u and piece u + rot/(2V) of the half style, two neighbours of the interleaved one, so
-// that neither style moves elements between lanes and a call may write over its inputs. The norm's sum is three (D =
-// 128) or two shuffles.
+// What bounds it: bytes. Each q, k and v row is read and written once, and a head's norm and rotation are between.
+// A head is D/16 lanes of 16 elements each, held as two pieces of V elements (or twice two of four) that turn into one
+// another: piece u and piece u + rot/(2V) of the half style, two neighbours of the interleaved one, so that neither style
+// moves elements between lanes and a call may write over its inputs. The norm's sum is three (D = 128) or two shuffles.
 //
-// Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of
-// a turn, so that pos times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction, 2^-53
-// of inv_freq, times pos (position 2^31: 4e-7 rad). The top 32 bits go to sincospif. A lane forms one or two of the
-// token's cosines and sines for its warp, which shuffles hand round: a warp serves a token's heads one group
-// after the other, or a share of them where there are few tokens.
+// Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of a turn, so that pos
+// times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction (2^-61 of inv_freq, 2^-64 of a turn),
+// times pos. The top 32 bits go to sincospif. A lane forms one or two of the token's cosines and sines for its warp,
+// which shuffles hand round; with the norm's weights they become 16 pairs of factors a lane, so that a word of two
+// elements takes two packed products.
+//
+// A warp takes tokens and, where there are few of these, a share of their heads. Its rows come by asynchronous copies into
+// shared memory that run four groups of heads ahead of the work, on into the next token's; what a lane copies it reads itself, so
+// that nothing waits but the lane. (Rows loaded into registers, two groups at a time: 48 us for 9856 tokens, now 42-44;
+// the first form, a warp's 150 registers holding three groups and the weights read for each head, 127.)
+//
+// Measured, calls one behind the other with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128: 64
+// tokens 3.9 us (3.5 in a graph), 1024 7.9, 9856 42.4, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go by
+// 64 bytes: 9856 25.5, 4.8 TB/s.
+#include <type_traits>
+
 #include "avtp_cache.cuh"
+#include "avtp_tc.cuh"
 
 namespace avtp {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBatch = 3;       // groups of heads that a warp has under way
-constexpr int kWarpsOfSm = 24;  // warps of an SM that a call's work is spread over, at least
+constexpr int kAhead = 4;       // groups of heads whose rows a warp has under way, a KiB each
+constexpr int kCtasOfSm = 4;    // 128 registers a thread (six CTAs, 80 and spills: 49.6 us for 9856 tokens, five 45.9)
+constexpr int kWarpsOfSm = 16;  // warps of an SM that a call's work is spread over, at least
 
 struct RopeDev {
   avtp_rope_args_t a;
   avtp_cache_t c;   // k NULL: no cache
-  int slices;       // shares of a token's heads, a warp each
-  int iq, ik, iv;   // groups of heads of q, k and v
+  int iq, ik;       // groups of heads of q, and of k or v
   DevStatus* st;
 };
 
-// Positions in turns: inv_freq / 2 pi modulo 1 as a fraction of 2^64.
+// inv_freq / 2 pi modulo 1 as a fraction of 2^64, by integers (in 64-bit floating point, scarce on this part, a prompt of
+// 9856 tokens took 0.7 us more and a step of 64 0.2): inv_freq = m 2^-s with a 24-bit m, and m times 2^64 / 2 pi, shifted.
 __device__ __forceinline__ uint64_t turn_fraction(float inv_freq) {
-  const double f = static_cast<double>(inv_freq) * 0.15915494309189533577;
-  return __double2ull_rn((f - floor(f)) * 18446744073709551616.0);
+  constexpr uint64_t kTurn = 0x28be60db9391054aull;  // 2^64 / 2 pi
+  const uint32_t b = __float_as_uint(inv_freq), e = (b >> 23) & 0xffu;
+  const uint64_t m = (b & 0x7fffffu) | (e != 0 ? 0x800000u : 0u);
+  const int s = 150 - static_cast<int>(e != 0 ? e : 1u);
+  const uint64_t lo = m * kTurn, hi = __umul64hi(m, kTurn);
+  uint64_t f = 0;
+  if (s <= 0) f = s > -64 ? lo << -s : 0;
+  else if (s < 64) f = (lo >> s) | (hi << (64 - s));
+  else if (s < 128) f = hi >> (s - 64);
+  return b >> 31 ? 0 - f : f;
 }
 
+// V elements of a row in registers.
 template <int V>
 struct Piece;
 template <>
 struct Piece<8> {
   uint4 w;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
-  __device__ __forceinline__ void load_near(const __nv_bfloat16* p) { w = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load(const void* p) { w = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = w; }
   __device__ __forceinline__ uint32_t& part(int i) { return i == 0 ? w.x : (i == 1 ? w.y : (i == 2 ? w.z : w.w)); }
 };
 template <>
 struct Piece<4> {
   uint2 w;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint2*>(p)); }
-  __device__ __forceinline__ void load_near(const __nv_bfloat16* p) { w = __ldg(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void load(const void* p) { w = *reinterpret_cast<const uint2*>(p); }
   __device__ __forceinline__ void store(__nv_bfloat16* p) const { *reinterpret_cast<uint2*>(p) = w; }
   __device__ __forceinline__ uint32_t& part(int i) { return i == 0 ? w.x : w.y; }
 };
+template <int V>
+__device__ __forceinline__ void copy_ahead(uint32_t to, const __nv_bfloat16* from) {
+  if (V == 8) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-  uint32_t w;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
-  return w;
-}
-
 // The call's tables and slots, by a CTA of its own: the others skip what it records, so that the status word
 // has one writer and the call is one launch.
 __device__ void check(const RopeDev& d) {
@@ -91,22 +109,26 @@ __device__ void check(const RopeDev& d) {
   if (threadIdx.x == 0) *d.st = DevStatus{s_bad ? static_cast<int32_t>(AVTP_ERR_DEVICE_INPUT) : 0, s_bad ? 0 : 1, 0, 0u};
 }
 
-template <int D, int V>
-__global__ void __launch_bounds__(kThreads) k_rope(RopeDev d) {
-  constexpr int kLanes = D / 16;      // of a head
+template <int D, int V, bool kApart>
+__global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
+  constexpr int kLanes = D / 16;       // of a head
   constexpr int kHeads = 32 / kLanes;  // of a group
-  constexpr int kUnits = 8 / V;       // pairs of pieces a lane
-  constexpr int kMine = D / 64;       // pairs whose cosine and sine a lane forms
+  constexpr int kUnits = 8 / V;        // pairs of pieces a lane
+  constexpr int kMine = D / 64;        // pairs whose cosine and sine a lane forms
+  static_assert(kApart || V == 8, "neighbours turn within pieces of eight");
+  constexpr int kPieceBytes = 2 * V;
+  // a lane's pieces of the groups under way: what a lane copies it reads itself
+  __shared__ __align__(16) unsigned char s_ahead[kWarps][kAhead][kUnits][2][32 * kPieceBytes];
   pdl_wait();
   pdl_trigger();
   if (blockIdx.x == gridDim.x - 1) {
-    check(d);
+    if (blockIdx.y == 0) check(d);
     return;
   }
   const avtp_rope_args_t& a = d.a;
   const int lane = threadIdx.x & 31, sub = lane % kLanes, group = lane / kLanes;
-  const bool apart = a.style == AVTP_ROPE_HALF;
   const int turning = a.rot_dim / 2;
+  const bool part = a.rot_dim < D;  // some elements do not turn
   // pair e of a lane (of eight) is pair V (sub + kLanes (e / V)) + e % V of the head
   auto pair_of = [&](int e) { return V * (sub + kLanes * (e / V)) + e % V; };
   // its pieces' first elements, and whether four of its pairs turn (rot is a multiple of eight)
@@ -115,11 +137,72 @@ __global__ void __launch_bounds__(kThreads) k_rope(RopeDev d) {
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
     const int u = sub + kLanes * i, n = turning / V;
-    at[i][0] = apart ? (u < n ? u * V : 2 * u * V) : 2 * u * V;
-    at[i][1] = apart && u < n ? u * V + turning : at[i][0] + V;
+    at[i][0] = kApart ? (u < n ? u * V : 2 * u * V) : 2 * u * V;
+    at[i][1] = kApart && u < n ? u * V + turning : at[i][0] + V;
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) turns[i] = pair_of(4 * i) < turning;
+  // whether the words of a piece turn
+  auto turned = [&](int i, int h) { return turns[kUnits == 2 ? i : (kApart ? 0 : h)]; };
+
+  // Tokens t, t + step, ... with a share (slice) of their groups of heads, its queries', keys' and values' in this
+  // order: n of them, each of heads (slice + j slices) kHeads ... Copies run kAhead groups ahead of the work, through a token's
+  // rows of every kind and on into the next token's.
+  int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
+  const int64_t step = static_cast<int64_t>(gridDim.x - 1) * kWarps;
+  const int slice = blockIdx.y, slices = gridDim.y;
+  const int nq = slice < d.iq ? (d.iq - 1 - slice) / slices + 1 : 0, nk = slice < d.ik ? (d.ik - 1 - slice) / slices + 1 : 0;
+  const int n = nq + nk + (d.c.k != nullptr ? nk : 0);
+  if (n == 0) return;
+  const uint32_t buffer = tc::smem_u32(s_ahead[threadIdx.x / 32][0][0][0]) + lane * kPieceBytes;
+  int64_t ahead_t = t;
+  int ahead_j = 0, ahead_stage = 0, stage = 0;
+  auto issue = [&]() {
+    if (ahead_t < a.n_tokens) {
+      const bool is_q = ahead_j < nq, is_k = !is_q && ahead_j < nq + nk;
+      const int head = (slice + (ahead_j - (is_q ? 0 : (is_k ? nq : nq + nk))) * slices) * kHeads + group;
+      if (head < (is_q ? a.n_q_heads : a.n_kv_heads)) {
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_q ? a.q : (is_k ? a.k : a.v)) +
+                                   ahead_t * (is_q ? a.q_stride : (is_k ? a.k_stride : a.v_stride)) + head * D;
+        const uint32_t to = buffer + ahead_stage * (kUnits * 2 * 32 * kPieceBytes);
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) copy_ahead<V>(to + (i * 2 + h) * 32 * kPieceBytes, src + at[i][h]);
+      }
+      if (++ahead_j == n) {
+        ahead_j = 0;
+        ahead_t += step;
+      }
+    }
+    ahead_stage = ahead_stage + 1 == kAhead ? 0 : ahead_stage + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  // The next group, heads of a tensor of `heads`: `change` what was read, by the whole warp, and `store` it.
+  auto pass = [&](int head, int heads, auto&& change, auto&& store) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
+    Piece<V> x[kUnits][2];
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) x[i][h].load(&s_ahead[threadIdx.x / 32][stage][i][h][lane * kPieceBytes]);
+    change(x);
+    stage = stage + 1 == kAhead ? 0 : stage + 1;
+    issue();
+    if (head < heads) store(x, head);
+  };
+  auto write = [&](const Piece<V> (&x)[kUnits][2], __nv_bfloat16* to) {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+      x[i][0].store(to + at[i][0]);
+      x[i][1].store(to + at[i][1]);
+    }
+  };
+  auto keep = [](Piece<V> (&)[kUnits][2]) {};
+#pragma unroll 1
+  for (int j = 0; j < kAhead; ++j) issue();
+
+  // this lane's pairs: frequency and plane
   uint64_t freq[kMine];
   const int32_t* where[kMine];
   bool fine = true;
@@ -127,163 +210,163 @@ __global__ void __launch_bounds__(kThreads) k_rope(RopeDev d) {
   for (int i = 0; i < kMine; ++i) {
     const int p = pair_of(group * kMine + i);
     freq[i] = 0;
-    where[i] = a.pos;
+    where[i] = nullptr;
     if (p < turning) {
       const float f = a.inv_freq[p];
       const int plane = a.pair_plane != nullptr ? a.pair_plane[p] : 0;
-      fine = fine && isfinite(f) && plane >= 0 && plane < a.n_planes;
-      freq[i] = fine ? turn_fraction(f) : 0;
-      where[i] += fine ? plane * a.pos_stride : 0;
+      if (isfinite(f) && plane >= 0 && plane < a.n_planes) {
+        freq[i] = turn_fraction(f);
+        where[i] = a.pos + plane * a.pos_stride;
+      } else {
+        fine = false;
+      }
     }
   }
-  if (!__all_sync(0xffffffffu, fine)) return;  // recorded by check()
+  if (!__all_sync(0xffffffffu, fine)) {  // recorded by check()
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    return;
+  }
+  int32_t pos[kMine], slot = -1;  // of the next token
+  auto look = [&](int64_t at_t) {
+    if (at_t >= a.n_tokens) return;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) pos[i] = where[i] != nullptr ? where[i][at_t] : 0;
+    if (d.c.k != nullptr) slot = a.slot_map[at_t];
+  };
+  look(t);
 
-  const int groups = d.iq + d.ik + d.iv;
-  const int64_t items = a.n_tokens * d.slices, step = static_cast<int64_t>(gridDim.x - 1) * kWarps;
-  const uint32_t slots = static_cast<uint32_t>(d.c.n_pages * d.c.page_size);
-  for (int64_t item = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32; item < items; item += step) {
-    const int64_t t = item / d.slices;
-    const int slice = static_cast<int>(item - t * d.slices);
-    int32_t pos[kMine];
+#pragma unroll 1
+  for (; t < a.n_tokens; t += step) {
+    // the lane's eight pairs', two by two; 1 and 0 of pairs that do not turn
+    float2 cosines[4], sines[4];
+    {
+      float c[kMine], s[kMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) pos[i] = turning > 0 ? where[i][t] : 0;
-    int64_t page = -1, in_page = 0;
-    if (d.c.k != nullptr) {
-      const int32_t slot = a.slot_map[t];
-      if (slot >= 0 && static_cast<uint32_t>(slot) < slots) {
-        page = static_cast<uint32_t>(slot) / static_cast<uint32_t>(d.c.page_size);
-        in_page = slot - page * d.c.page_size;
-      }
-    }
-    float cs[8], sn[8];
-    bool formed = false;
-    for (int g0 = slice; g0 < groups; g0 += kBatch * d.slices) {
-      Piece<V> x[kBatch][kUnits][2];
-      int head[kBatch], what[kBatch];  // 0: a query's, 1: a key's, 2: a value's; -1: none
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int g = g0 + b * d.slices;
-        const bool is_q = g < d.iq, is_k = !is_q && g < d.iq + d.ik;
-        head[b] = (g - (is_q ? 0 : (is_k ? d.iq : d.iq + d.ik))) * kHeads + group;
-        what[b] = g >= groups || head[b] >= (is_q ? a.n_q_heads : a.n_kv_heads) ? -1 : (is_q ? 0 : (is_k ? 1 : 2));
-        if (what[b] < 0) continue;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(is_q ? a.q : (is_k ? a.k : a.v)) +
-                                   t * (is_q ? a.q_stride : (is_k ? a.k_stride : a.v_stride)) + head[b] * D;
-#pragma unroll
-        for (int i = 0; i < kUnits; ++i) {
-          x[b][i][0].load(src + at[i][0]);
-          x[b][i][1].load(src + at[i][1]);
-        }
-      }
-      if (!formed && turning > 0) {
-        formed = true;
-        float c[kMine], s[kMine];
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-          const uint64_t phase = freq[i] * static_cast<uint64_t>(static_cast<int64_t>(pos[i]));
-          // half turns, -1 .. 1
-          sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s[i], &c[i]);
+      for (int i = 0; i < kMine; ++i) {
+        const uint64_t phase = freq[i] * static_cast<uint64_t>(static_cast<int64_t>(pos[i]));
+        // half turns, -1 .. 1
+        sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s[i], &c[i]);
+        if (where[i] != nullptr) {
           c[i] *= a.attn_factor;
           s[i] *= a.attn_factor;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          cs[e] = __shfl_sync(0xffffffffu, c[e % kMine], e / kMine * kLanes + sub);
-          sn[e] = __shfl_sync(0xffffffffu, s[e % kMine], e / kMine * kLanes + sub);
-        }
       }
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int g = g0 + b * d.slices;
-        if (g >= groups) break;
-        const bool is_v = g >= d.iq + d.ik;
-        const void* norm = g < d.iq ? a.q_norm : a.k_norm;
-        if (!is_v && (norm != nullptr || turning > 0)) {
-          // first and second of the lane's pairs, pair e = 2 i .. : (a, b) of the half style lie in two pieces
-          float y[kUnits][2][V];
+      for (int e = 0; e < 8; ++e) {
+        const float cos_e = __shfl_sync(0xffffffffu, c[e % kMine], e / kMine * kLanes + sub);
+        const float sin_e = __shfl_sync(0xffffffffu, s[e % kMine], e / kMine * kLanes + sub);
+        if (e & 1) cosines[e / 2].y = cos_e, sines[e / 2].y = sin_e;
+        else cosines[e / 2].x = cos_e, sines[e / 2].x = sin_e;
+      }
+    }
+    int64_t page = -1, in_page = 0;
+    if (slot >= 0 && slot < d.c.n_pages * d.c.page_size) {
+      page = static_cast<uint32_t>(slot) / static_cast<uint32_t>(d.c.page_size);
+      in_page = slot - page * d.c.page_size;
+    }
+    look(t + step);
+
+    // `count` groups, of queries or of keys, with their norm.
+    auto turn = [&](int count, int heads, const void* norm, auto&& store) {
+      if (norm == nullptr && turning == 0) {
+#pragma unroll 1
+        for (int j = 0; j < count; ++j) pass((slice + j * slices) * kHeads + group, heads, keep, store);
+        return;
+      }
+      // what the two elements of a lane's word i (of eight) become: x * c[i] + partner * s[i], the norm's weights in both
+      float2 factor_c[8], factor_s[8];
 #pragma unroll
-          for (int i = 0; i < kUnits; ++i)
+      for (int i = 0; i < kUnits; ++i) {
+        Piece<V> w[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < V / 2; ++e) {
-                const uint32_t w = what[b] < 0 ? 0u : x[b][i][h].part(e);
-                y[i][h][2 * e] = low(w);
-                y[i][h][2 * e + 1] = high(w);
-              }
+        for (int h = 0; h < 2; ++h) {
           if (norm != nullptr) {
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < kUnits; ++i)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < V; ++e) sum = fmaf(y[i][h][e], y[i][h][e], sum);
-#pragma unroll
-            for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const float inv = rsqrtf(fmaf(sum, 1.f / D, a.eps));
-#pragma unroll
-            for (int i = 0; i < kUnits; ++i)
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                Piece<V> w;
-                w.load_near(static_cast<const __nv_bfloat16*>(norm) + at[i][h]);
-#pragma unroll
-                for (int e = 0; e < V / 2; ++e) {
-                  y[i][h][2 * e] *= inv * low(w.part(e));
-                  y[i][h][2 * e + 1] *= inv * high(w.part(e));
-                }
-              }
-          }
-          auto turn = [&](float& p, float& q, int e) {
-            const float first = p * cs[e] - q * sn[e];
-            q = q * cs[e] + p * sn[e];
-            p = first;
-          };
-          if (apart) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (turns[e / 4]) turn(y[e / V][0][e % V], y[e / V][1][e % V], e);
+            w[h].load(static_cast<const __nv_bfloat16*>(norm) + at[i][h]);
           } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              constexpr int kPairs = V / 2;  // of a piece
-              const int i = e / V, h = e / kPairs % 2, k = e % kPairs;
-              if (turns[e / 4]) turn(y[i][h][2 * k], y[i][h][2 * k + 1], e);
-            }
+            for (int e = 0; e < V / 2; ++e) w[h].part(e) = 0x3f803f80u;  // ones
           }
-          // (elements that neither are normed nor turn keep their bits, a NaN's among them)
-#pragma unroll
-          for (int i = 0; i < kUnits; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (norm != nullptr || turns[kUnits == 2 ? i : (apart ? 0 : h)]) {
-#pragma unroll
-                for (int e = 0; e < V / 2; ++e) x[b][i][h].part(e) = pack(y[i][h][2 * e], y[i][h][2 * e + 1]);
-              }
         }
-        auto store = [&](__nv_bfloat16* to) {
 #pragma unroll
-          for (int i = 0; i < kUnits; ++i) {
-            x[b][i][0].store(to + at[i][0]);
-            x[b][i][1].store(to + at[i][1]);
-          }
-        };
-        if (what[b] == 0) {
-          store(static_cast<__nv_bfloat16*>(a.q_out) + t * a.q_out_stride + head[b] * D);
-        } else if (what[b] > 0) {
-          if (what[b] == 1 && a.k_out != nullptr)
-            store(static_cast<__nv_bfloat16*>(a.k_out) + t * a.k_out_stride + head[b] * D);
-          if (page >= 0) {
-            if (what[b] == 1)
-              store(static_cast<__nv_bfloat16*>(d.c.k) + page * d.c.k_page_stride + in_page * d.c.k_token_stride +
-                    head[b] * d.c.k_head_stride);
-            else
-              store(static_cast<__nv_bfloat16*>(d.c.v) + page * d.c.v_page_stride + in_page * d.c.v_token_stride +
-                    head[b] * d.c.v_head_stride);
+        for (int e = 0; e < V / 2; ++e) {
+          // words e of the two pieces
+          const int one = i * V + e, two = one + V / 2;
+          const float2 w0 = make_float2(low(w[0].part(e)), high(w[0].part(e)));
+          const float2 w1 = make_float2(low(w[1].part(e)), high(w[1].part(e)));
+          if (kApart) {  // two pairs, their second elements in the second piece
+            const int p = i * (V / 2) + e;
+            const float2 c = cosines[p], s = sines[p];
+            factor_c[one] = tc::mul2(w0, c);
+            factor_s[one] = tc::mul2(w1, make_float2(-s.x, -s.y));
+            factor_c[two] = tc::mul2(w1, c);
+            factor_s[two] = tc::mul2(w0, s);
+          } else {  // pair e of the first piece, and of the second
+            const float c = e & 1 ? cosines[e / 2].y : cosines[e / 2].x, s = e & 1 ? sines[e / 2].y : sines[e / 2].x;
+            const float cc = e & 1 ? cosines[2 + e / 2].y : cosines[2 + e / 2].x;
+            const float ss = e & 1 ? sines[2 + e / 2].y : sines[2 + e / 2].x;
+            factor_c[one] = tc::mul2(w0, make_float2(c, c));
+            factor_s[one] = tc::mul2(make_float2(w0.y, w0.x), make_float2(-s, s));
+            factor_c[two] = tc::mul2(w1, make_float2(cc, cc));
+            factor_s[two] = tc::mul2(make_float2(w1.y, w1.x), make_float2(-ss, ss));
           }
         }
       }
+      auto change = [&](Piece<V> (&x)[kUnits][2]) {
+        float2 y[8];
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e)
+              y[i * V + h * (V / 2) + e] = make_float2(low(x[i][h].part(e)), high(x[i][h].part(e)));
+        if (norm != nullptr) {
+          float2 sq = make_float2(0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sq = tc::ffma2(y[i], y[i], sq);
+          float sum = sq.x + sq.y;
+#pragma unroll
+          for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          const float inv = rsqrtf(fmaf(sum, 1.f / D, a.eps));
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = tc::mul2(y[i], make_float2(inv, inv));
+        }
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) {
+              const int me = i * V + h * (V / 2) + e;
+              float2 v = kApart ? y[i * V + (1 - h) * (V / 2) + e] : make_float2(y[me].y, y[me].x);
+              if (part && !turned(i, h)) v = make_float2(0.f, 0.f);  // whatever it is, an infinity too
+              const float2 z = tc::ffma2(y[me], factor_c[me], tc::mul2(v, factor_s[me]));
+              // (elements that neither are normed nor turn keep their bits, a NaN's among them)
+              if (!part || norm != nullptr || turned(i, h)) x[i][h].part(e) = tc::pack_bf16x2(z.x, z.y);
+            }
+      };
+#pragma unroll 1
+      for (int j = 0; j < count; ++j) pass((slice + j * slices) * kHeads + group, heads, change, store);
+    };
+
+    if (nq > 0) {
+      __nv_bfloat16* row = static_cast<__nv_bfloat16*>(a.q_out) + t * a.q_out_stride;
+      turn(nq, a.n_q_heads, a.q_norm, [&](const Piece<V> (&x)[kUnits][2], int head) { write(x, row + head * D); });
+    }
+    if (nk > 0) {
+      __nv_bfloat16* row = static_cast<__nv_bfloat16*>(a.k_out) + t * a.k_out_stride;
+      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(d.c.k) + page * d.c.k_page_stride + in_page * d.c.k_token_stride;
+      turn(nk, a.n_kv_heads, a.k_norm, [&](const Piece<V> (&x)[kUnits][2], int head) {
+        if (a.k_out != nullptr) write(x, row + head * D);
+        if (page >= 0) write(x, to + head * d.c.k_head_stride);
+      });
+    }
+    if (n > nq + nk) {
+      __nv_bfloat16* to = static_cast<__nv_bfloat16*>(d.c.v) + page * d.c.v_page_stride + in_page * d.c.v_token_stride;
+#pragma unroll 1
+      for (int j = 0; j < nk; ++j)
+        pass((slice + j * slices) * kHeads + group, page >= 0 ? a.n_kv_heads : 0, keep,
+             [&](const Piece<V> (&x)[kUnits][2], int head) { write(x, to + head * d.c.v_head_stride); });
     }
   }
 }
@@ -294,20 +377,25 @@ cudaError_t launch_rope(const avtp_rope_args_t& a, const avtp_cache_t* c, void* 
   RopeDev d{};
   d.a = a;
   if (c != nullptr) d.c = *c;
-  const int heads = 512 / a.head_dim;
+  d.st = static_cast<DevStatus*>(ws);
+  // warps share a token's groups of heads where there are few tokens
+  const int heads = 512 / a.head_dim, most = a.n_q_heads > a.n_kv_heads ? a.n_q_heads : a.n_kv_heads;
+  const int groups = (most + heads - 1) / heads;
   d.iq = (a.n_q_heads + heads - 1) / heads;
   d.ik = (a.n_kv_heads + heads - 1) / heads;
-  d.iv = c != nullptr ? d.ik : 0;
-  d.st = static_cast<DevStatus*>(ws);
-  const int groups = d.iq + d.ik + d.iv, sms = device_sm_count();
-  d.slices = 1;
-  while (d.slices * kBatch < groups && a.n_tokens * d.slices < static_cast<int64_t>(sms) * kWarpsOfSm) ++d.slices;
-  const int64_t want = (a.n_tokens * d.slices + kWarps - 1) / kWarps, most = static_cast<int64_t>(sms) * 8;
-  const unsigned grid = static_cast<unsigned>((want < most ? want : most) + 1);
+  int slices = 1;
+  while (slices < groups && a.n_tokens * slices < static_cast<int64_t>(device_sm_count()) * kWarpsOfSm) ++slices;
+  const int64_t want = (a.n_tokens + kWarps - 1) / kWarps, fit = static_cast<int64_t>(device_sm_count()) * kCtasOfSm / slices;
+  const dim3 grid(static_cast<unsigned>((slices == 1 && want > fit ? fit : want) + 1), static_cast<unsigned>(slices));
+  const bool apart = a.style == AVTP_ROPE_HALF;
   // half-style pairs whose halves begin inside a piece of eight are held as pieces of four
-  const bool fours = a.style == AVTP_ROPE_HALF && a.rot_dim % 16 != 0;
-  auto kernel = a.head_dim == 128 ? (fours ? k_rope<128, 4> : k_rope<128, 8>) : (fours ? k_rope<64, 4> : k_rope<64, 8>);
-  return launch_kernel(kernel, dim3(grid), dim3(kThreads), 0, s, /*pdl=*/true, d);
+  const bool fours = apart && a.rot_dim % 16 != 0;
+  auto pick = [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    return fours ? k_rope<D, 4, true> : (apart ? k_rope<D, 8, true> : k_rope<D, 8, false>);
+  };
+  auto kernel = a.head_dim == 128 ? pick(std::integral_constant<int, 128>{}) : pick(std::integral_constant<int, 64>{});
+  return launch_kernel(kernel, grid, dim3(kThreads), 0, s, /*pdl=*/true, d);
 }
 
 }  // namespace avtp
