@@ -2,18 +2,22 @@
 // (avtp_cache_compact), to pages of their own or in place:
 //   row(dst_table[r], j) = row(block_table[r], keep_idx[keep_cu[r] + j] - base_r),  row(t, p) = page t[p / P], row p % P
 //
-// Copies: 4 * Hkv * d bytes read and written a token bound them. Between different pages every row goes by
-// itself: a warp finds the slots of 32 tokens, a lane each, and then moves them row by row, 16 bytes a lane.
+// Copies: 4 * Hkv * d bytes read and written a token bound them. Between different pages every row goes by itself: a
+// warp finds the slots of as many tokens as leave all warps in one wave, a lane each, and then moves them row by row, 16
+// bytes a lane. 64 requests of 1000 kept tokens, 8 KV heads, d = 128: 90 us, 5.8 TB/s; four of 2900 20.5 us, 4.6 TB/s, of
+// which the way to the first row (offsets, position, two tables) and the launch take 4.
 //
 // In place a row's destination may be another's source. Kept positions ascend and j <= keep_j - base, so that in their
 // order a row is read before anything is written over it: what is written for tokens [a, b) lies before b, what is
-// read for tokens from b on lies at b or behind. So a CTA takes a column of the request's rows (a slice of a head's keys or
-// values) through all its tokens, a tile at a time, with a barrier between a tile's loads and its stores; columns are
-// independent, and no CTA waits for another.
+// read for tokens from b on lies at b or behind. So a CTA takes columns of the request's rows (slices of a head's keys or
+// values) through all its tokens, a tile at a time, with a barrier between a tile's reads and its writes, and the
+// next tiles' copies under way; columns are independent, and no CTA waits for another. 64 requests of 1000 of 3000 tokens
+// 133 us, 3.95 TB/s; one of 3000 of 9000 22 us, where twelve tiles one behind the other take 11 and the look at the
+// positions 6 (to other pages 6.2).
 //
-// What the calls record is found by a CTA of its own (the last one), the only writer of the status word; the
-// others skip by the same rules. A request moved in place is checked as a whole by each of its CTAs before they move
-// anything.
+// What is wrong is recorded where it is met, in a status word that a kernel beside this one clears. (A CTA that looked
+// through all kept tokens instead took longer than the copies: 50 us for 11600 of them.) A request moved in place is checked
+// as a whole by each of its CTAs before they move anything.
 #include "avtp_cache.cuh"
 
 namespace avtp {
@@ -21,6 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
+constexpr int kWarpsOfSm = 24;  // that an SM holds of k_cache_compact (80 registers a thread)
 
 __device__ __forceinline__ void write_status(DevStatus* st, int bad, int detail) {
   *st = DevStatus{bad ? static_cast<int32_t>(AVTP_ERR_DEVICE_INPUT) : 0, bad ? 0 : 1, bad ? detail : 0, 0u};
@@ -99,20 +104,12 @@ struct CompactDev {
   int lanes;    // to other pages: lanes of a row (a power of two, at most 32); pieces and head_sh as in the cache's write
   int pieces;
   int head_sh;
-  int slice;    // in place: pieces of a head that a CTA takes; a power of two
-  int slices;   // of a request, CTAs: Hkv * 2 * (pieces of a head / slice)
+  int slice;    // in place: pieces of a column, a power of two
+  int columns;  // of a request: Hkv * 2 * (pieces of a head / slice)
+  int parts;    // CTAs of a request, an equal share of its columns each
+  int page_sh;  // log2 of the page size; -1: no power of two
   DevStatus* st;
 };
-
-// Offsets in order, by all threads of the CTA.
-__device__ bool offsets_fine(const avtp_cache_compact_args_t& a) {
-  bool bad = threadIdx.x == 0 && a.keep_cu[0] != 0;
-  for (int r = threadIdx.x; r < a.n_requests; r += kThreads) {
-    const int64_t lo = a.keep_cu[r], hi = a.keep_cu[r + 1];
-    bad = bad || lo < 0 || hi < lo || hi > a.n_kept;
-  }
-  return __syncthreads_or(bad) == 0;
-}
 
 // Slot of a request's row p; -1 where it lies outside the table or the pool, or (held) on a page let go of.
 __device__ __forceinline__ int64_t slot_of(const avtp_cache_t& c, const int32_t* row, int max_pages, int64_t p,
@@ -130,161 +127,241 @@ struct Move {
   int64_t from, to;  // slots; -1: not moved
   bool bad;
 };
-// Kept token i of request r, to other pages.
-__device__ __forceinline__ Move move_of(const CompactDev& d, int r, int64_t i) {
+// Kept token i of request r, whose first is token `first`, to other pages.
+__device__ __forceinline__ Move move_of(const CompactDev& d, int r, int64_t i, int64_t first) {
   const avtp_cache_compact_args_t& a = d.a;
   const int64_t p = static_cast<int64_t>(a.keep_idx[i]) - (a.base_cu != nullptr ? a.base_cu[r] : 0);
   Move m;
   m.from = p >= a.seq_len[r] ? -1 : slot_of(d.c, a.block_table + r * a.table_stride, a.max_pages, p, &d.held, held_len(d, r));
-  m.to = slot_of(d.c, a.dst_table + r * a.dst_stride, a.dst_max_pages, i - a.keep_cu[r], nullptr, 0);
+  m.to = slot_of(d.c, a.dst_table + r * a.dst_stride, a.dst_max_pages, i - first, nullptr, 0);
   m.bad = m.from < 0 || m.to < 0;
   if (m.bad) m.from = m.to = -1;
   return m;
 }
-// What kept token j of n in place has wrong: its position or its order, its pages, or a page that others hold.
-__device__ __forceinline__ bool bad_in_place(const CompactDev& d, int r, int64_t first, int64_t j) {
+// Kept tokens j0 + thread, + kThreads, ... below j1 of a request in place, four at a time: f(j, where from, where to), slots, to
+// -1 of one that stays. True if one is wrong: its position or its order, its pages, or a page that others hold.
+template <class F>
+__device__ bool look_in_place(const CompactDev& d, int r, int64_t first, int64_t j0, int64_t j1, F f) {
+  constexpr int N = 4;
   const avtp_cache_compact_args_t& a = d.a;
-  const int64_t base = a.base_cu != nullptr ? a.base_cu[r] : 0, p = a.keep_idx[first + j] - base;
-  if (p < j || p >= a.seq_len[r] || (j > 0 && p <= a.keep_idx[first + j - 1] - base)) return true;
+  const int64_t base = a.base_cu != nullptr ? a.base_cu[r] : 0;
+  const int32_t seq = a.seq_len[r], held = held_len(d, r);
   const int32_t* row = a.block_table + r * a.table_stride;
-  if (p == j) return false;
-  const int64_t to = slot_of(d.c, row, a.max_pages, j, &d.held, held_len(d, r));
-  if (to < 0 || slot_of(d.c, row, a.max_pages, p, &d.held, held_len(d, r)) < 0) return true;
-  return a.shared != nullptr && a.shared[to / d.c.page_size] > 0;
+  bool bad = false;
+  for (int64_t j = j0 + threadIdx.x; j < j1; j += N * kThreads) {
+    int64_t p[N], before[N], from[N], to[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t k = j + i * kThreads;
+      p[i] = k < j1 ? a.keep_idx[first + k] - base : k;
+      before[i] = k < j1 && k > 0 ? a.keep_idx[first + k - 1] - base : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t k = j + i * kThreads;
+      const bool wrong = k < j1 && (p[i] < k || p[i] >= seq || p[i] <= before[i]), moves = k < j1 && p[i] != k && !wrong;
+      to[i] = moves ? slot_of(d.c, row, a.max_pages, k, &d.held, held) : -1;
+      from[i] = moves ? slot_of(d.c, row, a.max_pages, p[i], &d.held, held) : -1;
+      bad = bad || wrong || (moves && (to[i] < 0 || from[i] < 0));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t k = j + i * kThreads;
+      if (a.shared != nullptr && to[i] >= 0 && a.shared[to[i] / d.c.page_size] > 0) bad = true;
+      if (k < j1) f(k, from[i], to[i]);
+    }
+  }
+  return bad;
 }
 
-// The CTA that records, and writes the new lengths.
-__device__ void record(const CompactDev& d, bool in_place) {
-  __shared__ int s_bad;
-  if (threadIdx.x == 0) s_bad = 0x7fffffff;
-  const avtp_cache_compact_args_t& a = d.a;
-  if (!offsets_fine(a)) {
-    if (threadIdx.x == 0) write_status(d.st, 1, -1);
-    return;
+constexpr int kStaged = 1024;  // requests whose offsets are kept in shared memory
+
+// keep_cu, from shared memory where it fits; NULL where it is refused. All threads of the CTA.
+__device__ const int32_t* offsets(const avtp_cache_compact_args_t& a, int32_t (&s_cu)[kStaged + 1]) {
+  const bool staged = a.n_requests <= kStaged;
+  bool bad = false;
+  for (int r = threadIdx.x; r <= a.n_requests; r += kThreads) {
+    const int64_t lo = r == 0 ? 0 : a.keep_cu[r - 1], hi = a.keep_cu[r];
+    bad = bad || hi < lo || hi > a.n_kept || (r == 0 && hi != 0);
+    if (staged) s_cu[r] = static_cast<int32_t>(hi);
   }
-  const int64_t n = a.keep_cu[a.n_requests];
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-    const int r = upper_index(a.keep_cu, a.n_requests, i);
-    if (in_place ? bad_in_place(d, r, a.keep_cu[r], i - a.keep_cu[r]) : move_of(d, r, i).bad) atomicMin(&s_bad, r);
-  }
-  if (a.len_out != nullptr)
-    for (int r = threadIdx.x; r < a.n_requests; r += kThreads) a.len_out[r] = a.keep_cu[r + 1] - a.keep_cu[r];
-  __syncthreads();
-  if (threadIdx.x == 0) write_status(d.st, s_bad != 0x7fffffff, s_bad);
+  if (__syncthreads_or(bad)) return nullptr;
+  return staged ? s_cu : a.keep_cu;
+}
+
+// The call's first CTA: the new lengths.
+__device__ void write_lengths(const avtp_cache_compact_args_t& a, const int32_t* cu) {
+  if (blockIdx.x != 0 || a.len_out == nullptr) return;
+  for (int r = threadIdx.x; r < a.n_requests; r += kThreads) a.len_out[r] = cu[r + 1] - cu[r];
 }
 
 __global__ void __launch_bounds__(kThreads) k_cache_compact(CompactDev d) {
-  pdl_wait();
+  __shared__ int32_t s_cu[kStaged + 1];
   pdl_trigger();
-  if (blockIdx.x == gridDim.x - 1) {
-    record(d, false);
-    return;
-  }
-  if (!offsets_fine(d.a)) return;
   const avtp_cache_compact_args_t& a = d.a;
-  const int lane = threadIdx.x & 31, sub = lane & (d.lanes - 1), rows = 32 / d.lanes;
-  const int64_t n = a.keep_cu[a.n_requests];
-  const int64_t warps = static_cast<int64_t>(gridDim.x - 1) * (kThreads / 32);
-  for (int64_t i0 = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32) * d.each; i0 < n;
-       i0 += warps * d.each) {
-    Move mine{-1, -1, false};
-    if (lane < d.each && i0 + lane < n) mine = move_of(d, upper_index(a.keep_cu, a.n_requests, i0 + lane), i0 + lane);
-    for (int k = 0; k < d.each; k += rows) {
-      const int64_t from = __shfl_sync(0xffffffffu, mine.from, k + lane / d.lanes);
-      const int64_t to = __shfl_sync(0xffffffffu, mine.to, k + lane / d.lanes);
-      if (from < 0) continue;
-      const uint32_t P = d.c.page_size;
-      const uint32_t fp = static_cast<uint32_t>(from) / P, tp = static_cast<uint32_t>(to) / P;
-      const int64_t fr = from - static_cast<int64_t>(fp) * P, tr = to - static_cast<int64_t>(tp) * P;
-      __nv_bfloat16* kp = static_cast<__nv_bfloat16*>(d.c.k);
-      __nv_bfloat16* vp = static_cast<__nv_bfloat16*>(d.c.v);
-      const __nv_bfloat16* ks = kp + fp * d.c.k_page_stride + fr * d.c.k_token_stride;
-      const __nv_bfloat16* vs = vp + fp * d.c.v_page_stride + fr * d.c.v_token_stride;
-      __nv_bfloat16* kd = kp + tp * d.c.k_page_stride + tr * d.c.k_token_stride;
-      __nv_bfloat16* vd = vp + tp * d.c.v_page_stride + tr * d.c.v_token_stride;
-      for (int c0 = sub; c0 < d.pieces; c0 += d.lanes * kUnroll) {
-        uint4 kx[kUnroll], vx[kUnroll];
+  const int32_t* cu = offsets(a, s_cu);
+  int bad = cu != nullptr ? -1 : 0x7fffffff;
+  if (cu != nullptr) {
+    write_lengths(a, cu);
+    const int lane = threadIdx.x & 31, sub = lane & (d.lanes - 1), rows = 32 / d.lanes;
+    const int64_t n = cu[a.n_requests];
+    const int64_t warps = static_cast<int64_t>(gridDim.x) * (kThreads / 32);
+    for (int64_t i0 = (static_cast<int64_t>(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32) * d.each; i0 < n;
+         i0 += warps * d.each) {
+      Move mine{-1, -1, false};
+      if (lane < d.each && i0 + lane < n) {
+        const int r = upper_index(cu, a.n_requests, i0 + lane);
+        mine = move_of(d, r, i0 + lane, cu[r]);
+        if (mine.bad) bad = r;
+      }
+      for (int k = 0; k < d.each; k += rows) {
+        const int64_t from = __shfl_sync(0xffffffffu, mine.from, k + lane / d.lanes);
+        const int64_t to = __shfl_sync(0xffffffffu, mine.to, k + lane / d.lanes);
+        if (from < 0) continue;
+        const uint32_t P = d.c.page_size;
+        const uint32_t fp = static_cast<uint32_t>(from) / P, tp = static_cast<uint32_t>(to) / P;
+        const int64_t fr = from - static_cast<int64_t>(fp) * P, tr = to - static_cast<int64_t>(tp) * P;
+        __nv_bfloat16* kp = static_cast<__nv_bfloat16*>(d.c.k);
+        __nv_bfloat16* vp = static_cast<__nv_bfloat16*>(d.c.v);
+        const __nv_bfloat16* ks = kp + fp * d.c.k_page_stride + fr * d.c.k_token_stride;
+        const __nv_bfloat16* vs = vp + fp * d.c.v_page_stride + fr * d.c.v_token_stride;
+        __nv_bfloat16* kd = kp + tp * d.c.k_page_stride + tr * d.c.k_token_stride;
+        __nv_bfloat16* vd = vp + tp * d.c.v_page_stride + tr * d.c.v_token_stride;
+        for (int c0 = sub; c0 < d.pieces; c0 += d.lanes * kUnroll) {
+          uint4 kx[kUnroll], vx[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int c = c0 + u * d.lanes;
-          if (c < d.pieces) {
-            const int64_t h = c >> d.head_sh;
-            const int off = (c & ((1 << d.head_sh) - 1)) * 8;
-            kx[u] = __ldcs(reinterpret_cast<const uint4*>(ks + h * d.c.k_head_stride + off));
-            vx[u] = __ldcs(reinterpret_cast<const uint4*>(vs + h * d.c.v_head_stride + off));
+          for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + u * d.lanes;
+            if (c < d.pieces) {
+              const int64_t h = c >> d.head_sh;
+              const int off = (c & ((1 << d.head_sh) - 1)) * 8;
+              kx[u] = __ldcs(reinterpret_cast<const uint4*>(ks + h * d.c.k_head_stride + off));
+              vx[u] = __ldcs(reinterpret_cast<const uint4*>(vs + h * d.c.v_head_stride + off));
+            }
           }
-        }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-          const int c = c0 + u * d.lanes;
-          if (c < d.pieces) {
-            const int64_t h = c >> d.head_sh;
-            const int off = (c & ((1 << d.head_sh) - 1)) * 8;
-            *reinterpret_cast<uint4*>(kd + h * d.c.k_head_stride + off) = kx[u];
-            *reinterpret_cast<uint4*>(vd + h * d.c.v_head_stride + off) = vx[u];
+          for (int u = 0; u < kUnroll; ++u) {
+            const int c = c0 + u * d.lanes;
+            if (c < d.pieces) {
+              const int64_t h = c >> d.head_sh;
+              const int off = (c & ((1 << d.head_sh) - 1)) * 8;
+              *reinterpret_cast<uint4*>(kd + h * d.c.k_head_stride + off) = kx[u];
+              *reinterpret_cast<uint4*>(vd + h * d.c.v_head_stride + off) = vx[u];
+            }
           }
         }
       }
     }
   }
+  pdl_wait();  // the status word is cleared by the kernel ahead
+  if (bad >= 0) record_error(d.st, AVTP_ERR_DEVICE_INPUT, bad);
 }
 
-__global__ void __launch_bounds__(kThreads) k_cache_compact_in_place(CompactDev d) {
-  pdl_wait();
+constexpr int kChunk = 4096;    // kept tokens whose slots are in shared memory
+constexpr int kRows = 4;        // rows of a thread, a tile
+constexpr int kTiles = 4;       // under way
+constexpr int kColumnCtas = 2;  // of an SM
+constexpr size_t kInPlaceSmem = kTiles * kRows * kThreads * 16 + 2 * kChunk * 4;
+
+__global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_place(CompactDev d) {
+  extern __shared__ uint4 s_ring[];  // [kTiles][kRows][kThreads]: what a thread copies it reads itself
+  __shared__ int32_t s_cu[kStaged + 1];
+  int32_t* s_from = reinterpret_cast<int32_t*>(s_ring + kTiles * kRows * kThreads);  // slots; to -1: stays
+  int32_t* s_to = s_from + kChunk;
   pdl_trigger();
-  if (blockIdx.x == gridDim.x - 1) {
-    record(d, true);
-    return;
-  }
-  if (!offsets_fine(d.a)) return;
   const avtp_cache_compact_args_t& a = d.a;
-  const int per_head = (1 << d.head_sh) / d.slice, sub = threadIdx.x & (d.slice - 1);
-  const int rows = kThreads / d.slice;  // at once
-  const int64_t items = static_cast<int64_t>(a.n_requests) * d.slices;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x - 1) {
-    const int r = static_cast<int>(item / d.slices);
-    int column = static_cast<int>(item - static_cast<int64_t>(r) * d.slices);
-    const int64_t first = a.keep_cu[r], n = a.keep_cu[r + 1] - first;
-    if (n == 0) continue;
-    bool bad = false;
-    for (int64_t j = threadIdx.x; j < n; j += kThreads) bad = bad || bad_in_place(d, r, first, j);
-    if (__syncthreads_or(bad)) continue;
-    const bool is_v = column >= d.c.n_kv_heads * per_head;
-    if (is_v) column -= d.c.n_kv_heads * per_head;
-    const int64_t page = is_v ? d.c.v_page_stride : d.c.k_page_stride;
-    const int64_t token = is_v ? d.c.v_token_stride : d.c.k_token_stride;
-    __nv_bfloat16* pool = static_cast<__nv_bfloat16*>(is_v ? d.c.v : d.c.k) +
-                          (column / per_head) * (is_v ? d.c.v_head_stride : d.c.k_head_stride) +
-                          ((column % per_head) * d.slice + sub) * 8;
-    const int32_t* row = a.block_table + r * a.table_stride;
-    const int64_t base = a.base_cu != nullptr ? a.base_cu[r] : 0;
+  const int32_t* cu = offsets(a, s_cu);
+  int wrong = cu != nullptr ? -1 : 0x7fffffff;
+  if (cu != nullptr) {
+    write_lengths(a, cu);
+    const int per_head = (1 << d.head_sh) / d.slice, sub = threadIdx.x & (d.slice - 1);
+    const int at_once = kThreads / d.slice, first_row = threadIdx.x / d.slice;
     const uint32_t P = d.c.page_size;
-    auto place = [&](int64_t p) {
-      const uint32_t column = static_cast<uint32_t>(p) / P;
-      return pool + row[column] * page + (p - static_cast<int64_t>(column) * P) * token;
-    };
-    constexpr int kRows = 8;  // of a thread, a tile
-    for (int64_t j0 = threadIdx.x / d.slice; j0 - threadIdx.x / d.slice < n; j0 += rows * kRows) {
-      uint4 x[kRows];
-      __nv_bfloat16* to[kRows];
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + threadIdx.x * 16;
+    const int64_t items = static_cast<int64_t>(a.n_requests) * d.parts;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+      const int r = static_cast<int>(item / d.parts), part = static_cast<int>(item - static_cast<int64_t>(r) * d.parts);
+      const int c0 = static_cast<int>(static_cast<int64_t>(part) * d.columns / d.parts);
+      const int c1 = static_cast<int>(static_cast<int64_t>(part + 1) * d.columns / d.parts);
+      const int64_t first = cu[r], n = cu[r + 1] - first;
+      if (n == 0) continue;
+      auto look = [&](int64_t j0) {  // tokens j0 .. j0 + kChunk - 1
+        return look_in_place(d, r, first, j0, min(n, j0 + kChunk), [&](int64_t j, int64_t from, int64_t to) {
+          s_from[j - j0] = static_cast<int32_t>(from);
+          s_to[j - j0] = static_cast<int32_t>(to);
+        });
+      };
+      bool bad = look(0);
+      if (n > kChunk) bad = look_in_place(d, r, first, kChunk, n, [](int64_t, int64_t, int64_t) {}) || bad;
+      if (__syncthreads_or(bad)) {
+        wrong = r;
+        __syncthreads();
+        continue;
+      }
+      for (int64_t j0 = 0; j0 < n; j0 += kChunk) {
+        if (j0 > 0) {
+          __syncthreads();
+          look(j0);
+          __syncthreads();
+        }
+        const int rows = static_cast<int>(min(n - j0, static_cast<int64_t>(kChunk)));
+        // Tiles, column by column. Copies run kTiles tiles ahead of the stores: a column's later rows lie behind all that
+        // its earlier ones are written over, and columns do not meet.
+        const int tiles = (rows + at_once * kRows - 1) / (at_once * kRows), all = tiles * (c1 - c0);
+        struct Place {
+          __nv_bfloat16* base;
+          int64_t page, token;
+          int row0;
+        };
+        auto tile_of = [&](int q) {
+          const int c = q / tiles, col = c0 + c;
+          const bool is_v = col >= d.c.n_kv_heads * per_head;
+          const int within = is_v ? col - d.c.n_kv_heads * per_head : col;
+          return Place{static_cast<__nv_bfloat16*>(is_v ? d.c.v : d.c.k) +
+                           (within / per_head) * (is_v ? d.c.v_head_stride : d.c.k_head_stride) +
+                           ((within % per_head) * d.slice + sub) * 8,
+                       is_v ? d.c.v_page_stride : d.c.k_page_stride, is_v ? d.c.v_token_stride : d.c.k_token_stride,
+                       (q - c * tiles) * at_once * kRows + first_row};
+        };
+        auto place = [&](const Place& t, int32_t slot) {
+          const uint32_t p = d.page_sh >= 0 ? static_cast<uint32_t>(slot) >> d.page_sh : static_cast<uint32_t>(slot) / P;
+          return t.base + p * t.page + (slot - p * P) * t.token;
+        };
+        auto issue = [&](int q) {
+          if (q < all) {
+            const Place t = tile_of(q);
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        const int64_t j = j0 + i * rows;
-        to[i] = nullptr;
-        if (j < n) {
-          const int64_t p = a.keep_idx[first + j] - base;
-          if (p != j) {
-            to[i] = place(j);
-            x[i] = *reinterpret_cast<const uint4*>(place(p));
+            for (int i = 0; i < kRows; ++i) {
+              const int j = t.row0 + i * at_once;
+              if (j < rows && s_to[j] >= 0)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring + (q % kTiles * kRows + i) * kThreads * 16),
+                             "l"(place(t, s_from[j]))
+                             : "memory");
+            }
           }
+          asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+#pragma unroll 1
+        for (int q = 0; q < kTiles; ++q) issue(q);
+#pragma unroll 1
+        for (int q = 0; q < all; ++q) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kTiles - 1) : "memory");
+          __syncthreads();  // the tile has been read
+          const Place t = tile_of(q);
+#pragma unroll
+          for (int i = 0; i < kRows; ++i) {
+            const int j = t.row0 + i * at_once;
+            if (j < rows && s_to[j] >= 0)
+              *reinterpret_cast<uint4*>(place(t, s_to[j])) = s_ring[(q % kTiles * kRows + i) * kThreads + threadIdx.x];
+          }
+          issue(q + kTiles);
         }
       }
       __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kRows; ++i)
-        if (to[i] != nullptr) *reinterpret_cast<uint4*>(to[i]) = x[i];
     }
   }
+  pdl_wait();  // the status word is cleared by the kernel ahead
+  if (wrong >= 0 && threadIdx.x == 0) record_error(d.st, AVTP_ERR_DEVICE_INPUT, wrong);
 }
 
 int head_shift(int d) { return d == 128 ? 4 : 3; }
@@ -320,18 +397,34 @@ cudaError_t launch_cache_compact(const avtp_cache_t& c, const avtp_cache_compact
   d.st = static_cast<DevStatus*>(ws);
   const int64_t sms = device_sm_count();
   d.held = CachePages::of(c.page_size, a.window, a.n_sinks);
+  const cudaError_t e = launch_cache_status(d.st, s);
+  if (e != cudaSuccess) return e;
   if (a.dst_table != nullptr) {
-    d.each = 32;  // fewer where warps would be missing
-    while (d.each > 32 / d.lanes && a.n_kept < d.each * 32 * sms) d.each /= 2;
+    d.each = 32;  // fewer where that leaves all warps in one wave
+    while (d.each > 32 / d.lanes && a.n_kept <= d.each / 2 * kWarpsOfSm * sms) d.each /= 2;
     const int64_t per_cta = d.each * (kThreads / 32), want = (a.n_kept + per_cta - 1) / per_cta, most = 8 * sms;
-    return launch_kernel(k_cache_compact, dim3(static_cast<unsigned>((want < most ? want : most) + 1)), dim3(kThreads), 0, s,
-                         /*pdl=*/true, d);
+    const unsigned grid = static_cast<unsigned>(want < 1 ? 1 : (want < most ? want : most));
+    return launch_kernel(k_cache_compact, dim3(grid), dim3(kThreads), 0, s, /*pdl=*/true, d);
   }
+  static PerDevice attrs;
+  const cudaError_t set = once_per_device(attrs, [](int, int*) {
+    return cudaFuncSetAttribute(k_cache_compact_in_place, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                static_cast<int>(kInPlaceSmem));
+  });
+  if (set != cudaSuccess) return set;
+  // Columns of a head's width, several a CTA where requests are many (they share the look at its tokens), or as
+  // narrow as 64 bytes where CTAs would be missing.
+  const int64_t most = kColumnCtas * sms, wanted = (most + a.n_requests - 1) / a.n_requests;
   d.slice = 1 << d.head_sh;
-  d.slices = 2 * c.n_kv_heads * ((1 << d.head_sh) / d.slice);
-  const int64_t want = static_cast<int64_t>(a.n_requests) * d.slices, most = 8 * sms;
-  return launch_kernel(k_cache_compact_in_place, dim3(static_cast<unsigned>((want < most ? want : most) + 1)),
-                       dim3(kThreads), 0, s, /*pdl=*/true, d);
+  while (d.slice > 4 && 2 * c.n_kv_heads * ((1 << d.head_sh) / d.slice) < wanted) d.slice /= 2;
+  d.columns = 2 * c.n_kv_heads * ((1 << d.head_sh) / d.slice);
+  d.parts = static_cast<int>(d.columns < wanted ? d.columns : wanted);
+  d.page_sh = -1;
+  if ((c.page_size & (c.page_size - 1)) == 0)
+    for (d.page_sh = 0; (1 << d.page_sh) < c.page_size;) ++d.page_sh;
+  const int64_t want = static_cast<int64_t>(a.n_requests) * d.parts;
+  return launch_kernel(k_cache_compact_in_place, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(kThreads),
+                       kInPlaceSmem, s, /*pdl=*/true, d);
 }
 
 }  // namespace avtp

@@ -7,12 +7,18 @@
 // A call's entries (a request's or child's pages of that kind, in order) are numbered through: a prefix sum over the
 // requests, then a binary search an entry.
 //
-// What bounds it: latency, three to five rounds of dependent loads, so that a call is one cluster of kCtas CTAs, whose
-// barriers (1 us less than a grid's each) part the rounds. Everything is checked before the first write.
+// What bounds it: latency, a chain of dependent loads a round. A call is one cluster of up to kMostCtas CTAs, each of
+// which forms the sums for itself, so that barriers part the rounds and nothing else does; a thread's first kKept pages
+// stay in its registers from round to round. Everything is checked before the first write. Calls one behind the other:
+// 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 5.7 us; the pages that 64
+// windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.9; eight children
+// of a prompt of 146 pages 7.2; 171 children of 64 (21000 entries) 10.6. (With eight CTAs 6.8, 19.9, 8.5 and 13.1; with entries looked
+// up again in every round, and the others' findings read from their shared memory, 11.7, 36.7, 11.2 and 18.8.)
 //
-// A page that several rows of a call let go of: every entry counts itself (rel) and the last one in order (last: a maximum)
-// stands for the page, so that neither the counts nor the list's order depend on who came first. Both arrays are
-// cleared where the call's entries point, not as a whole.
+// A page of several holders that rows of a call let go of: every entry counts itself (rel) and the last one in order
+// (last: a maximum) stands for the page, so that neither the counts nor the list's order depend on who came first. Both
+// arrays are cleared where the call's entries point, not as a whole. A page of one holder has one entry, which finds itself
+// in last.
 #include <cooperative_groups.h>
 
 #include "avtp_cache.cuh"
@@ -23,7 +29,9 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kThreads = 1024;
-constexpr int kCtas = 8;
+constexpr int kMostCtas = 16;  // of a cluster where the device has room for that many, else 8
+constexpr int64_t kEntriesOfCta = 1024;  // of the table, where fewer CTAs than kMostCtas do
+constexpr int kKept = 4;
 constexpr int kStaged = 2048;  // requests whose numbers are kept in shared memory
 
 // What a request or child brings: up to three ranges of table columns.
@@ -66,47 +74,74 @@ struct Pages : CachePages {
   }
 };
 
-// What a round of checks found, in a CTA's shared memory, read by all behind a barrier. A flag a round: one that
-// the next round could set while a slower CTA still reads it would part the CTAs, and the next barrier not end.
-constexpr int kRounds = 3;
-struct Verdict {
-  int err[kRounds], detail[kRounds];
-  __device__ __forceinline__ void fail(int round, int d) {
-    if (atomicExch(&err[round], 1) == 0) detail[round] = d;
+// What a CTA's checks found, and its pages for the list, for the others of the cluster: every CTA puts its note into all
+// the others' shared memory ahead of the barrier. (Reading theirs behind it took 4 us of 18 for sixteen.)
+struct Note {
+  int err, detail;
+  int64_t gives;
+  __device__ __forceinline__ void fail(int d) {
+    if (atomicExch(&err, 1) == 0) detail = d;
   }
 };
-// All threads of the cluster; true if none has failed in this round. Behind it everything written before it is seen.
-__device__ bool agree(cg::cluster_group& cluster, Verdict& mine, int round, int* detail) {
+// All threads of the cluster, once a call; true if none has failed. Behind it everything written before it is seen.
+__device__ bool agree(cg::cluster_group& cluster, Note& mine, Note (&notes)[kMostCtas], int* detail, int64_t* gives,
+                      int64_t* before) {
+  const int ctas = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+  const int lane = threadIdx.x & 31;
+  __syncthreads();
+  if (threadIdx.x < ctas) *cluster.map_shared_rank(&notes[rank], threadIdx.x) = mine;
   cluster.sync();
-  bool ok = true;
-  for (int c = 0; c < kCtas; ++c) {
-    const Verdict* v = cluster.map_shared_rank(&mine, c);
-    if (v->err[round]) {
-      if (ok) *detail = v->detail[round];
-      ok = false;
-    }
-  }
-  return ok;
+  Note n{0, -1, 0};
+  if (lane < ctas) n = notes[lane];
+  const unsigned bad = __ballot_sync(0xffffffffu, n.err != 0);
+  *detail = bad ? __shfl_sync(0xffffffffu, n.detail, __ffs(bad) - 1) : -1;
+  // a call's pages are a 32-bit number
+  *gives = __reduce_add_sync(0xffffffffu, static_cast<int>(n.gives));
+  *before = __reduce_add_sync(0xffffffffu, lane < rank ? static_cast<int>(n.gives) : 0);
+  return bad == 0;
 }
 
-// Inclusive sum over the CTA; total in *all. Two barriers.
-__device__ int64_t block_scan(int64_t x, int64_t* s_warp, int64_t* all) {
+// Inclusive sums of N numbers a thread over the CTA; totals in all. Two barriers.
+template <int N>
+__device__ void block_scan(int64_t (&x)[N], int64_t (&s_warp)[N][kThreads / 32], int64_t (&all)[N]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto warp_scan = [&](int64_t v) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += y;
+    }
+    return v;
+  };
+  static_assert(kThreads == 1024, "a warp's lane a warp");
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = warp_scan(x[i]);
+  __syncthreads();
+  if (lane == 31) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) s_warp[i][warp] = x[i];
   }
   __syncthreads();
-  if (lane == 31) s_warp[warp] = x;
-  __syncthreads();
-  int64_t before = 0, sum = 0;
-  for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += s_warp[w];
-    sum += s_warp[w];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t sums = warp_scan(s_warp[i][lane]);
+    all[i] = __shfl_sync(0xffffffffu, sums, 31);
+    const int64_t before = __shfl_sync(0xffffffffu, sums, warp == 0 ? 0 : warp - 1);
+    if (warp > 0) x[i] += before;
   }
-  *all = sum;
-  return before + x;
+}
+
+__device__ __forceinline__ int32_t clamped(int64_t x) { return static_cast<int32_t>(x < 0x7fffffff ? x : 0x7fffffff); }
+
+// Calls f(entry, its page, which of the thread's) for entries begin, begin + step, ... < end, with the first kKept pages
+// from registers.
+template <class P, class F>
+__device__ __forceinline__ void each_entry(int64_t begin, int64_t end, int64_t step, const int32_t (&kept)[kKept], P page_of,
+                                           F f) {
+#pragma unroll
+  for (int i = 0; i < kKept; ++i)
+    if (begin + i * step < end) f(begin + i * step, kept[i], i);
+  for (int64_t e = begin + kKept * step; e < end; e += step) f(e, page_of(e), kKept);
 }
 
 // ---------------------------------------------------------------- free
@@ -119,30 +154,32 @@ struct FreeDev {
   int32_t* last;   // [n_pages]: the last of them
 };
 
-__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
-  __shared__ Verdict s_v;
-  __shared__ int64_t s_warp[kThreads / 32], s_gives;
-  __shared__ int32_t s_first[kStaged + 1];
+__global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
+  __shared__ Note s_v, s_notes[kMostCtas];
+  __shared__ int64_t s_warp[1][kThreads / 32];
+  __shared__ int32_t s_first[kStaged + 1], s_seq[kStaged], s_now[kStaged], s_held[kStaged];
   pdl_wait();
   pdl_trigger();
   cg::cluster_group cluster = cg::this_cluster();
   const avtp_cache_free_args_t& a = d.a;
-  const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank());
+  const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks());
   const int R = a.n_requests;
   const Pages& pages = d.pages;
   const bool staged = R <= kStaged;
-  int32_t* first = staged ? s_first : d.first;
   const int64_t head = *a.free_head;
-  if (tid == 0) s_v = Verdict{{head < 0 || head > a.n_free ? 1 : 0, 0, 0}, {-1, -1, -1}};
+  if (tid == 0) s_v = Note{head < 0 || head > a.n_free ? 1 : 0, -1, 0};
   __syncthreads();
 
-  // lengths, and the entries before each request's (where they go to memory the first CTA writes them)
+  // lengths, and the entries before each request's; none of a request whose lengths are refused
   int64_t total = 0;
   for (int base = 0; base < R; base += kThreads) {
     const int r = base + tid;
     int64_t n = 0;
+    int32_t seq = 0, now = 0, held = 0;
     if (r < R) {
-      const int32_t seq = a.seq_len[r], now = a.new_len[r], held = a.window > 0 ? a.held_len[r] : 0;
+      seq = a.seq_len[r];
+      now = a.new_len[r];
+      held = a.window > 0 ? a.held_len[r] : 0;
       bool bad = seq < 0 || now < 0 || now > seq || held < 0 || held > seq ||
                  seq > static_cast<int64_t>(a.max_pages) * a.page_size;
       if (!bad && now > 0 && pages.left(now) < pages.left(held)) bad = true;  // it would need pages let go of
@@ -151,94 +188,120 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) k_cach
         const int32_t page = a.block_table[r * a.table_stride + now / a.page_size];
         bad = page < 0 || page >= a.n_pages || a.shared[page] > 0;
       }
-      if (bad) s_v.fail(0, r);
+      if (bad) s_v.fail(r);
       else n = pages.gone(seq, now, held).total();
     }
-    int64_t all;
-    const int64_t incl = block_scan(n, s_warp, &all);
-    const int64_t before = total + incl - n;
-    if (r < R && (staged || rank == 0)) first[r] = static_cast<int32_t>(before < 0x7fffffff ? before : 0x7fffffff);
-    total += all;
-  }
-  if (tid == 0 && (staged || rank == 0)) first[R] = static_cast<int32_t>(total < 0x7fffffff ? total : 0x7fffffff);
-  if (total > 0x7fffffff && tid == 0) s_v.fail(0, R);
-  int detail = -1;
-  bool ok = agree(cluster, s_v, 0, &detail);
-
-  // the CTA's entries, in order
-  const int64_t each = ((total + kCtas - 1) / kCtas + kThreads - 1) / kThreads * kThreads;
-  const int64_t e0 = each * rank, e1 = min(total, e0 + each);
-  auto page_of = [&](int64_t e) -> int32_t {
-    const int r = upper_index(first, R, e);
-    const Span s = pages.gone(a.seq_len[r], a.new_len[r], a.window > 0 ? a.held_len[r] : 0);
-    return a.block_table[r * a.table_stride + s.column(static_cast<int32_t>(e - first[r]))];
-  };
-  if (ok) {
-    for (int64_t e = e0 + tid; e < e1; e += kThreads) {
-      const int32_t page = page_of(e);
-      if (page < 0 || page >= a.n_pages) {
-        s_v.fail(1, upper_index(first, R, e));
-      } else if (a.shared != nullptr) {
-        d.rel[page] = 0;
-        d.last[page] = -1;
+    int64_t sum[1] = {n}, all[1];
+    block_scan(sum, s_warp, all);
+    if (r < R) {
+      const int32_t before = clamped(total + sum[0] - n);
+      if (staged) {
+        s_first[r] = before;
+        s_seq[r] = seq;
+        s_now[r] = now;
+        s_held[r] = held;
+      } else if (rank == 0) {
+        d.first[r] = before;
       }
     }
-    ok = agree(cluster, s_v, 1, &detail);
+    total += all[0];
   }
-  int64_t gives = total;  // pages that go to the list
-  if (ok && a.shared != nullptr) {
-    for (int64_t e = e0 + tid; e < e1; e += kThreads) {
-      const int32_t page = page_of(e);
+  if (tid == 0) {
+    if (staged) s_first[R] = clamped(total);
+    else if (rank == 0) d.first[R] = clamped(total);
+    if (total > 0x7fffffff) s_v.fail(R);
+  }
+  if (total > 0x7fffffff) total = 0;
+  if (staged) __syncthreads();
+  else cluster.sync();
+
+  // the CTA's entries, in order
+  const int64_t each = ((total + ctas - 1) / ctas + kThreads - 1) / kThreads * kThreads;
+  const int64_t e0 = each * rank, e1 = min(total, e0 + each), mine0 = e0 + tid;
+  const int32_t* first = staged ? s_first : d.first;
+  auto page_of = [&](int64_t e) -> int32_t {
+    const int r = upper_index(first, R, e);
+    const Span s = staged ? pages.gone(s_seq[r], s_now[r], s_held[r])
+                          : pages.gone(a.seq_len[r], a.new_len[r], a.window > 0 ? a.held_len[r] : 0);
+    return a.block_table[r * a.table_stride + s.column(static_cast<int32_t>(e - first[r]))];
+  };
+  int32_t kept[kKept];
+#pragma unroll
+  for (int i = 0; i < kKept; ++i) kept[i] = mine0 + i * kThreads < e1 ? page_of(mine0 + i * kThreads) : 0;
+  auto entries = [&](auto f) { each_entry(mine0, e1, kThreads, kept, page_of, f); };
+  auto in_pool = [&](int32_t page) { return page >= 0 && page < a.n_pages; };
+  int32_t others[kKept + 1] = {};  // the pages' holders beyond the first
+  auto others_of = [&](int32_t page, int i) { return i < kKept ? others[i] : a.shared[page]; };
+#pragma unroll
+  for (int i = 0; i < kKept; ++i)
+    others[i] = a.shared != nullptr && mine0 + i * kThreads < e1 && in_pool(kept[i]) ? a.shared[kept[i]] : 0;
+  entries([&](int64_t e, int32_t page, int i) {
+    if (!in_pool(page)) {
+      s_v.fail(upper_index(first, R, e));
+    } else if (a.shared != nullptr) {
+      const int32_t n = others_of(page, i);
+      if (n < 0) s_v.fail(upper_index(first, R, e));
+      if (n > 0) d.rel[page] = 0;
+      d.last[page] = n > 0 ? -1 : static_cast<int32_t>(e);
+    }
+  });
+  if (a.shared != nullptr) {
+    cluster.sync();
+    entries([&](int64_t e, int32_t page, int i) {
+      if (!in_pool(page) || others_of(page, i) <= 0) return;
       atomicAdd(d.rel + page, 1);
       atomicMax(d.last + page, static_cast<int32_t>(e));
-    }
+    });
     cluster.sync();
-    int64_t mine = 0;
-    for (int64_t e = e0 + tid; e < e1; e += kThreads) {
-      const int32_t page = page_of(e), holders = a.shared[page], let_go = __ldcg(d.rel + page);
-      if (holders < 0 || let_go > holders + 1) s_v.fail(2, upper_index(first, R, e));
-      mine += let_go == holders + 1 && __ldcg(d.last + page) == e ? 1 : 0;
-    }
-    int64_t all;
-    block_scan(mine, s_warp, &all);
-    if (tid == 0) s_gives = all;
-    ok = agree(cluster, s_v, 2, &detail);
-    gives = 0;
-    for (int c = 0; c < kCtas; ++c) gives += *cluster.map_shared_rank(&s_gives, c);
+    int64_t mine[1] = {0}, all[1];
+    entries([&](int64_t e, int32_t page, int i) {
+      if (!in_pool(page)) return;
+      const int32_t n = others_of(page, i), counted = __ldcg(d.rel + page), let_go = n > 0 ? counted : 1;
+      const bool stands = __ldcg(d.last + page) == e;
+      // more entries than holders; of one holder, one that finds another
+      if (let_go > n + 1 || (n <= 0 && !stands)) s_v.fail(upper_index(first, R, e));
+      mine[0] += let_go == n + 1 && stands ? 1 : 0;
+    });
+    block_scan(mine, s_warp, all);
+    if (tid == 0) s_v.gives = all[0];
   }
+  int detail;
+  int64_t gives, at;  // pages that go to the list, and those of the CTAs before
+  bool ok = agree(cluster, s_v, s_notes, &detail, &gives, &at);
+  if (a.shared == nullptr) gives = total;
   if (ok && gives > head) {
     ok = false;
     detail = R;
   }
-  if (ok) {
-    int64_t at = head - gives;
-    if (a.shared == nullptr) {
-      for (int64_t e = e0 + tid; e < e1; e += kThreads) a.free_pages[at + e] = page_of(e);
-    } else {
-      for (int c = 0; c < rank; ++c) at += *cluster.map_shared_rank(&s_gives, c);
-      // counts of pages are read by entries of other CTAs above, behind the barrier of agree()
-      for (int64_t b = e0; b < e1; b += kThreads) {
-        const int64_t e = b + tid;
-        int32_t page = 0, rest = 0;
-        bool stands = false;
-        if (e < e1) {
-          page = page_of(e);
-          stands = __ldcg(d.last + page) == e;
-          if (stands) rest = a.shared[page] - __ldcg(d.rel + page);
+  at += head - gives;
+  if (ok && a.shared == nullptr) {
+    entries([&](int64_t e, int32_t page, int) { a.free_pages[at + e] = page; });
+  } else if (ok) {
+    for (int64_t b = e0, i = 0; b < e1; b += kThreads, ++i) {
+      const int64_t e = b + tid;
+      int32_t page = 0, rest = 0;
+      bool stands = false;
+      if (e < e1) {
+        page = i == 0 ? kept[0] : (i == 1 ? kept[1] : (i == 2 ? kept[2] : (i == 3 ? kept[3] : page_of(e))));
+        stands = __ldcg(d.last + page) == e;
+        if (stands) {
+          const int32_t n = a.shared[page];
+          rest = n > 0 ? n - __ldcg(d.rel + page) : -1;
+          if (n > 0) a.shared[page] = max(rest, 0);
         }
-        const bool give = stands && rest < 0;
-        int64_t all;
-        const int64_t incl = block_scan(give ? 1 : 0, s_warp, &all);
-        if (give) a.free_pages[at + incl - 1] = page;
-        if (stands) a.shared[page] = max(rest, 0);
-        at += all;
       }
+      const bool give = stands && rest < 0;
+      int64_t sum[1] = {give ? 1 : 0}, all[1];
+      block_scan(sum, s_warp, all);
+      if (give) a.free_pages[at + sum[0] - 1] = page;
+      at += all[0];
     }
   }
-  cluster.sync();  // lengths may be written over from here on, and no CTA reads another's shared memory
+  // Behind agree() every CTA has its lengths; where they are not in shared memory it looks at them again above.
+  if (!staged) cluster.sync();
   if (ok) {
-    for (int r = rank * kThreads + tid; r < R; r += kCtas * kThreads) {
-      const int32_t now = a.new_len[r];
+    for (int r = rank * kThreads + tid; r < R; r += ctas * kThreads) {
+      const int32_t now = staged ? s_now[r] : a.new_len[r];
       a.seq_len_out[r] = now;
       if (a.window > 0) a.held_len_out[r] = now;
     }
@@ -256,134 +319,215 @@ struct ForkDev {
   DevStatus* st;
   int32_t* first;  // [C + 1] where C > kStaged: entries before a child's
   int32_t* fresh;  // [C] there: copied pages before a child's
-  int32_t* mark;   // [R]: how often a row is a child
+  int32_t* mark;   // [R]: which child a row is, of parents -1
 };
 
-__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
-  __shared__ Verdict s_v;
-  __shared__ int64_t s_warp[kThreads / 32];
-  __shared__ int32_t s_first[kStaged + 1], s_fresh[kStaged];
+__global__ void __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
+  __shared__ Note s_v, s_notes[kMostCtas];
+  __shared__ int64_t s_warp[2][kThreads / 32];
+  // a child's numbers: entries before its, its copied page (-1: none), parent, length, the parent's held_len
+  __shared__ int32_t s_first[kStaged + 1], s_fresh[kStaged], s_parent[kStaged], s_len[kStaged], s_held[kStaged];
   pdl_wait();
   pdl_trigger();
   cg::cluster_group cluster = cg::this_cluster();
   const avtp_cache_fork_args_t& a = d.a;
-  const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank());
+  const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks());
   const int C = a.n_children, P = a.page_size;
   const Pages& pages = d.pages;
   const bool staged = C <= kStaged;
-  int32_t* first = staged ? s_first : d.first;
-  int32_t* fresh = staged ? s_fresh : d.fresh;
   const int64_t head = a.free_head != nullptr ? *a.free_head : 0;
-  if (tid == 0) s_v = Verdict{{head < 0 || head > a.n_free ? 1 : 0, 0, 0}, {-1, -1, -1}};
+  if (tid == 0) s_v = Note{head < 0 || head > a.n_free ? 1 : 0, -1, 0};
   __syncthreads();
-  auto length = [&](int i, int p) { return a.fork_len != nullptr ? a.fork_len[i] : a.seq_len[p]; };
+  auto in_pool = [&](int32_t page) { return page >= 0 && page < a.n_pages; };
 
+  // lengths, the entries before each child's and the copied pages; none of a child that is refused
   int64_t total = 0, copies = 0;
   for (int base = 0; base < C; base += kThreads) {
     const int i = base + tid;
-    int64_t n = 0, tail = 0;
+    int64_t n = 0;
+    int tail = 0;
+    int32_t p = -1, len = 0, held = 0;
     if (i < C) {
-      const int32_t p = a.parent[i], c = a.child[i];
+      const int32_t c = a.child[i];
+      p = a.parent[i];
       bool bad = p < 0 || p >= a.n_requests || c < 0 || c >= a.n_requests;
       if (!bad) {
-        const int32_t seq = a.seq_len[p], len = length(i, p), held = a.window > 0 ? a.held_len[p] : 0;
+        const int32_t seq = a.seq_len[p];
+        len = a.fork_len != nullptr ? a.fork_len[i] : seq;
+        held = a.window > 0 ? a.held_len[p] : 0;
         bad = seq < 0 || len < 0 || len > seq || held < 0 || held > seq ||
               seq > static_cast<int64_t>(a.max_pages) * P || (len > 0 && pages.left(len) < pages.left(held));
-        if (!bad) {
-          n = pages.full(len, held).total();
-          tail = len % P != 0 ? 1 : 0;
-          if (rank == 0) d.mark[p] = d.mark[c] = 0;
-        }
+        if (rank == 0) d.mark[p] = -1;
       }
-      if (bad) s_v.fail(0, i);
+      if (bad) {
+        s_v.fail(i);
+        p = -1;
+      } else {
+        n = pages.full(len, held).total();
+        tail = len % P != 0 ? 1 : 0;
+      }
     }
-    int64_t all, all_tails;
-    const int64_t incl = block_scan(n, s_warp, &all), incl_tails = block_scan(tail, s_warp, &all_tails);
-    if (i < C && (staged || rank == 0)) {
-      const int64_t before = total + incl - n;
-      first[i] = static_cast<int32_t>(before < 0x7fffffff ? before : 0x7fffffff);
-      fresh[i] = static_cast<int32_t>(copies + incl_tails - tail);
+    int64_t sum[2] = {n, tail}, all[2];
+    block_scan(sum, s_warp, all);
+    if (i < C) {
+      const int32_t before = clamped(total + sum[0] - n), page = static_cast<int32_t>(copies + sum[1] - 1);
+      if (staged) {
+        s_first[i] = before;
+        s_fresh[i] = tail ? page : -1;
+        s_parent[i] = p;
+        s_len[i] = len;
+        s_held[i] = held;
+      } else if (rank == 0) {
+        d.first[i] = before;
+        d.fresh[i] = tail ? page : -1;
+      }
     }
-    total += all;
-    copies += all_tails;
+    total += all[0];
+    copies += all[1];
   }
   if (tid == 0) {
-    if (staged || rank == 0) first[C] = static_cast<int32_t>(total < 0x7fffffff ? total : 0x7fffffff);
-    if (total > 0x7fffffff || head + copies > a.n_free) s_v.fail(0, C);
+    if (staged) s_first[C] = clamped(total);
+    else if (rank == 0) d.first[C] = clamped(total);
+    if (total > 0x7fffffff || head + copies > a.n_free) s_v.fail(C);
   }
-  int detail = -1;
-  bool ok = agree(cluster, s_v, 0, &detail);
+  const bool countable = total <= 0x7fffffff && head >= 0 && head + copies <= a.n_free;
+  if (!countable) total = 0;
+  if (staged) __syncthreads();
+  else cluster.sync();
 
-  const int64_t step = static_cast<int64_t>(kCtas) * kThreads, at = rank * kThreads + tid;
-  auto entry = [&](int64_t e, int* i, int* column) {
-    *i = upper_index(first, C, e);
-    const int32_t p = a.parent[*i];
-    const Span s = pages.full(length(*i, p), a.window > 0 ? a.held_len[p] : 0);
-    *column = s.column(static_cast<int32_t>(e - first[*i]));
-    return a.block_table[p * a.table_stride + *column];
+  const int32_t* first = staged ? s_first : d.first;
+  struct Child {
+    int32_t parent, len, held, fresh;  // parent -1: refused
   };
-  if (ok) {
+  auto child_of = [&](int i) {
+    if (staged) return Child{s_parent[i], s_len[i], s_held[i], s_fresh[i]};
+    const int32_t p = a.parent[i];
+    if (p < 0 || p >= a.n_requests) return Child{-1, 0, 0, -1};
+    return Child{p, a.fork_len != nullptr ? a.fork_len[i] : a.seq_len[p], a.window > 0 ? a.held_len[p] : 0, d.fresh[i]};
+  };
+  // a child's copied page: the parent's last, and the list's
+  auto tail_of = [&](const Child& k, int32_t* from, int32_t* to) {
+    *from = *to = -1;
+    if (k.parent < 0 || k.fresh < 0) return false;
+    *from = a.block_table[k.parent * a.table_stride + k.len / P];
+    *to = a.free_pages[head + k.fresh];
+    return true;
+  };
+  const int64_t step = static_cast<int64_t>(ctas) * kThreads, at = rank * kThreads + tid;
+  auto page_of = [&](int64_t e) {
+    const int i = upper_index(first, C, e);
+    const Child k = child_of(i);
+    return a.block_table[k.parent * a.table_stride + pages.full(k.len, k.held).column(static_cast<int32_t>(e - first[i]))];
+  };
+  int32_t kept[kKept];
+#pragma unroll
+  for (int i = 0; i < kKept; ++i) kept[i] = at + i * step < total ? page_of(at + i * step) : 0;
+  auto entries = [&](auto f) { each_entry(at, total, step, kept, page_of, f); };
+  int32_t from0 = -1, to0 = -1;  // of the thread's first child
+  if (countable) {
     for (int64_t i = at; i < C; i += step) {
-      if (atomicAdd(d.mark + a.child[i], 1) != 0) s_v.fail(1, static_cast<int>(i));
-      const int32_t p = a.parent[i], len = length(static_cast<int>(i), p);
-      if (len % P != 0) {
-        const int32_t from = a.block_table[p * a.table_stride + len / P], to = a.free_pages[head + fresh[i]];
-        if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) s_v.fail(1, static_cast<int>(i));
-      }
+      int32_t from, to;
+      if (tail_of(child_of(static_cast<int>(i)), &from, &to) && (!in_pool(from) || !in_pool(to))) s_v.fail(static_cast<int>(i));
+      if (i == at) from0 = from, to0 = to;
     }
-    for (int64_t e = at; e < total; e += step) {
-      int i, column;
-      const int32_t page = entry(e, &i, &column);
-      if (page < 0 || page >= a.n_pages) s_v.fail(1, i);
-    }
-    ok = agree(cluster, s_v, 1, &detail);
   }
-  if (ok) {
-    for (int64_t i = at; i < C; i += step)
-      if (__ldcg(d.mark + a.parent[i]) != 0) s_v.fail(2, static_cast<int>(i));
-    ok = agree(cluster, s_v, 2, &detail);
+  // every child once, and none of them a parent: the first CTA's to see
+  if (rank == 0) {
+    __syncthreads();
+    auto rows_fine = [&](int i) {
+      const int32_t p = a.parent[i], c = a.child[i];
+      return p >= 0 && p < a.n_requests && c >= 0 && c < a.n_requests;
+    };
+    for (int i = tid; i < C; i += kThreads)
+      if (rows_fine(i)) d.mark[a.child[i]] = i;
+    __syncthreads();
+    for (int i = tid; i < C; i += kThreads)
+      if (rows_fine(i) && (d.mark[a.child[i]] != i || d.mark[a.parent[i]] != -1)) s_v.fail(i);
   }
+  entries([&](int64_t e, int32_t page, int) {
+    if (!in_pool(page)) s_v.fail(upper_index(first, C, e));
+  });
+  int detail;
+  int64_t none, before;
+  const bool ok = agree(cluster, s_v, s_notes, &detail, &none, &before);
   // parents' rows and lengths are read, children's written: no row is both
   if (ok) {
-    for (int64_t e = at; e < total; e += step) {
-      int i, column;
-      const int32_t page = entry(e, &i, &column);
+    entries([&](int64_t e, int32_t page, int) {
+      const int i = upper_index(first, C, e);
+      const Child k = child_of(i);
+      const int32_t column = pages.full(k.len, k.held).column(static_cast<int32_t>(e - first[i]));
       a.block_table[a.child[i] * a.table_stride + column] = page;
       atomicAdd(a.shared + page, 1);
-    }
+    });
     for (int64_t i = at; i < C; i += step) {
-      const int32_t p = a.parent[i], c = a.child[i], len = length(static_cast<int>(i), p);
-      int32_t from = -1, to = -1;
-      if (len % P != 0) {
-        from = a.block_table[p * a.table_stride + len / P];
-        to = a.free_pages[head + fresh[i]];
-        a.block_table[c * a.table_stride + len / P] = to;
-      }
+      const Child k = child_of(static_cast<int>(i));
+      const int32_t c = a.child[i];
+      int32_t from = from0, to = to0;
+      if (i != at) tail_of(k, &from, &to);
+      if (to >= 0) a.block_table[c * a.table_stride + k.len / P] = to;
       a.copy_src[i] = from;
       a.copy_dst[i] = to;
-      a.seq_len[c] = len;
-      if (a.window > 0) a.held_len[c] = len > 0 ? a.held_len[p] : 0;
+      a.seq_len[c] = k.len;
+      if (a.window > 0) a.held_len[c] = k.len > 0 ? k.held : 0;
     }
   }
-  cluster.sync();  // no CTA reads another's shared memory from here on, nor the list's head
   if (rank == 0 && tid == 0) {
     *d.st = DevStatus{ok ? 0 : static_cast<int32_t>(AVTP_ERR_DEVICE_INPUT), ok ? 1 : 0, detail, 0u};
     if (ok && a.free_head_out != nullptr) *a.free_head_out = static_cast<int32_t>(head + copies);
   }
 }
 
+// A cluster of as many CTAs as the table's entries give work.
+template <class Dev>
+cudaError_t launch(void (*kernel)(Dev), PerDevice& most, const Dev& d, int64_t entries, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  auto of = [&](int ctas) {
+    cfg.gridDim = dim3(ctas);
+    attr[0].val.clusterDim.x = ctas;
+  };
+  int room = 0;
+  const cudaError_t e = once_per_device(most, [&](int, int* value) {
+    *value = 8;
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (set != cudaSuccess) return set;
+    int clusters = 0;
+    of(kMostCtas);
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) == cudaSuccess && clusters > 0) *value = kMostCtas;
+    else cudaGetLastError();
+    return cudaSuccess;
+  }, &room);
+  if (e != cudaSuccess) return e;
+  int ctas = 1;
+  while (ctas < room && entries > ctas * kEntriesOfCta) ctas *= 2;
+  of(ctas);
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, d);
+}
+
 }  // namespace
 
 cudaError_t launch_cache_free(const avtp_cache_free_args_t& a, void* ws, const FreeWs& p, cudaStream_t s) {
-  FreeDev d{a, {CachePages::of(a.page_size, a.window, a.n_sinks)}, ws_at<DevStatus>(ws, p.status), ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.rel),
-            ws_at<int32_t>(ws, p.last)};
-  return launch_kernel(k_cache_free, dim3(kCtas), dim3(kThreads), 0, s, /*pdl=*/true, d);
+  const FreeDev d{a, {CachePages::of(a.page_size, a.window, a.n_sinks)}, ws_at<DevStatus>(ws, p.status),
+                  ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.rel), ws_at<int32_t>(ws, p.last)};
+  static PerDevice most;
+  return launch(k_cache_free, most, d, static_cast<int64_t>(a.n_requests) * a.max_pages, s);
 }
 
 cudaError_t launch_cache_fork(const avtp_cache_fork_args_t& a, void* ws, const ForkWs& p, cudaStream_t s) {
-  ForkDev d{a, {CachePages::of(a.page_size, a.window, a.n_sinks)}, ws_at<DevStatus>(ws, p.status), ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.fresh),
-            ws_at<int32_t>(ws, p.mark)};
-  return launch_kernel(k_cache_fork, dim3(kCtas), dim3(kThreads), 0, s, /*pdl=*/true, d);
+  const ForkDev d{a, {CachePages::of(a.page_size, a.window, a.n_sinks)}, ws_at<DevStatus>(ws, p.status),
+                  ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.fresh), ws_at<int32_t>(ws, p.mark)};
+  static PerDevice most;
+  return launch(k_cache_fork, most, d, static_cast<int64_t>(a.n_children) * a.max_pages, s);
 }
 
 }  // namespace avtp

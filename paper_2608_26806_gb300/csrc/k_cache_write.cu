@@ -92,6 +92,10 @@ __global__ void __launch_bounds__(kThreads) k_cache_write(WriteDev w) {
 
 }  // namespace
 
+cudaError_t launch_cache_status(DevStatus* st, cudaStream_t s) {
+  return launch_kernel(k_cache_write_reset, dim3(1), dim3(1), 0, s, /*pdl=*/true, st);
+}
+
 cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_args_t& a, void* ws, cudaStream_t s) {
   WriteDev w{};
   w.c = c;
@@ -120,7 +124,7 @@ cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_arg
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, k_cache_write<true>, w);
   }
-  const cudaError_t e = launch_kernel(k_cache_write_reset, dim3(1), dim3(1), 0, s, /*pdl=*/true, w.st);
+  const cudaError_t e = launch_cache_status(w.st, s);
   if (e != cudaSuccess) return e;
   return launch_kernel(k_cache_write<false>, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(kThreads), 0, s,
                        /*pdl=*/true, w);
