@@ -47,7 +47,11 @@
 //
 // In a window (kWindow, see avtp.h) a unit's blocks are those of the sinks and those from its first token's window on
 // (Segment::block gives a block's place among the request's); its last blocks are masked above and its first ones
-// below, and values that none of its rows sees are cleared as those behind the last key are.
+// below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that no row
+// of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in windows of 2048, 512 and 128 tokens:
+// 225, 122 and 73 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50 by the figures above: first blocks and last
+// ones are masked, and a unit's ends weigh more. (Masks by comparison, every half looked at, values cleared by the softmax
+// warps: 279, 157 and 103.)
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
@@ -71,7 +75,10 @@ constexpr int kStages = 4;      // key or value blocks in shared memory
 // A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first
 // softmax with nothing to overlap, its rows' way out): its steps on the line are its blocks and these.
 // (With three, 9856 tokens 488 us instead of 494, 512 behind 9300 63.6 instead of 62.8.)
-constexpr int kUnitSteps = 2;
+// In a window, whose first blocks are masked too, four (8192 tokens behind 2176, 32 query heads, 8 KV heads, window 512: 118.8 us
+// and 125.8 with two, 117.0 with six; 2048: 233.8, 240.5, 235.5).
+template <bool kWindow>
+constexpr int kUnitSteps = kWindow ? 4 : 2;
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSCol = 0;    // S (and P) of slot s at kSCol + 128 s
 constexpr uint32_t kOCol = 256;  // O of slot s at kOCol + 128 s
@@ -138,6 +145,7 @@ struct ChunkSync {
   uint64_t half_done[2];   // P V of a block's first half complete (when someone may wait for that)
   uint64_t o_done[2];      // P V of a slot's last block in the segment complete
   uint64_t drain;
+  uint64_t edge[2];        // in a window: values to be cleared in part have landed, block j even, odd
   Segment<kWindow> seg[2];
   CachePlan<kThreads> plan;
   CacheBoxes boxes[2];  // of the keys' warp, of the values'
@@ -194,12 +202,13 @@ __device__ __noinline__ bool load_queries(const CUtensorMap* map, unsigned char*
   return __all_sync(0xffffffffu, ok);
 }
 
+template <bool kWindow>
 __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int blocks) {
-  return kUnitSteps + ((blocks + (1 << a.step_shift) - 1) >> a.step_shift);
+  return kUnitSteps<kWindow> + ((blocks + (1 << a.step_shift) - 1) >> a.step_shift);
 }
 
 // Steps of the first u units of a request's head, the last of all not among them, in closed form: unit i's
-// last token sees x = past + rows (i + 1) keys, for which it has kUnitSteps + max(1, ceil(x / (128 * 2^step_shift))) of them. For
+// last token sees x = past + rows (i + 1) keys, for which it has kUnitSteps<kWindow> + max(1, ceil(x / (128 * 2^step_shift))) of them. For
 // requests of more than kNearUnits units: 128 of them, added up one by one and passed one by one, took up to
 // 24000 cycles before a CTA's first product and take 9000 so; eight of them 2500 and 5300.
 // In a window (step_shift 0) less the blocks that it leaves out: floor((past + rows i - window + 1) / 128) less the
@@ -209,7 +218,7 @@ template <bool kWindow>
 static __device__ __noinline__ int steps_before(const CacheAttnDev& a, int past, int rows, int u) {
   const int blind = past >= 0 ? 0 : min(u, -past / rows);  // units that see nothing
   const uint32_t keys = static_cast<uint32_t>(kKB) << a.step_shift;
-  int sum = kUnitSteps * u + blind;
+  int sum = kUnitSteps<kWindow> * u + blind;
   if (u > blind) sum += floor_sum(u - blind, keys, rows, past + (blind + 1) * rows + keys - 1);
   if (kWindow) {
     const int64_t at = static_cast<int64_t>(past) - a.window + 1 - static_cast<int64_t>((a.sinks + kKB - 1) / kKB) * kKB;
@@ -240,6 +249,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) tc::mbar_init(&sy.kv_full[s], 1);
     for (int s = 0; s < 2; ++s) {
+      tc::mbar_init(&sy.edge[s], 1);
       tc::mbar_init(&sy.kv_empty[s], 1);
       tc::mbar_init(&sy.half_done[s], 1);
       tc::mbar_init(&sy.o_done[s], 1);
@@ -281,7 +291,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
   auto steps = [&](const CacheRequest& q, int& most) {
     const int U = units_of(a, q, nt);
     if (U == 0) return 0;
-    int sum = steps_of(a, unit_blocks<kWindow>(a, q, nt, U - 1));  // the last unit may be short
+    int sum = steps_of<kWindow>(a, unit_blocks<kWindow>(a, q, nt, U - 1));  // the last unit may be short
     // In a window an earlier unit may be longer: its first and last blocks end elsewhere, and the last one's tokens
     // may be fewer.
     most = max(most, sum + (kWindow && U > 1 ? 1 + (2 * nt + kKB - 1) / kKB : 0));
@@ -289,7 +299,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       sum += steps_before<kWindow>(a, q.seq - q.n, 2 * nt, U - 1);
     } else {
 #pragma unroll 1
-      for (int u = 0; u < U - 1; ++u) sum += steps_of(a, unit_blocks<kWindow>(a, q, nt, u));
+      for (int u = 0; u < U - 1; ++u) sum += steps_of<kWindow>(a, unit_blocks<kWindow>(a, q, nt, u));
     }
     return sum * a.Hkv;
   };
@@ -308,6 +318,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     int outs0 = 0, outs1 = 0;    // of o_done[0] and [1]
     int loads0 = 0, loads1 = 0;  // into the even and the odd blocks' stage
     int qn = 0;                  // queries loaded
+    uint32_t edge_phase = 0;     // of sy.edge[0] and [1], a bit each
     bool ok = true;
     int t = 0, t1 = 0, pre = 0;  // steps: next, the run's end, before unit u of request r
     int r = 0, u = 0;
@@ -317,7 +328,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     split.c1 = -1;
     if (kv == 0) {
       line = CacheLine<kWindow>(a, sy.plan, mine, mine_ok, steps);
-      runs = CacheRuns(line.total, line.most, kUnitSteps + 1, cache_ctas(a, line.weights, false));
+      runs = CacheRuns(line.total, line.most, kUnitSteps<kWindow> + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
       if (t < t1) {
@@ -355,7 +366,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
 #pragma unroll 1
             for (; u < U; ++u) {
               nb = unit_blocks<kWindow>(a, q, nt, u);
-              len = steps_of(a, nb);
+              len = steps_of<kWindow>(a, nb);
               if (t < pre + len * a.Hkv) break;
               pre += len * a.Hkv;
             }
@@ -365,7 +376,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           const int s = pre + head * len;  // the unit's first step
           end = min(t1, s + len);
           // a run that ends in a unit's first steps leaves its blocks to the next
-          g.head = end > s + kUnitSteps ? head : -1;
+          g.head = end > s + kUnitSteps<kWindow> ? head : -1;
           g.row0 = q.row0;
           g.n = q.n;
           g.seq = q.seq;
@@ -377,10 +388,10 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             g.skip = skip.skip;
           }
           g.req = r;
-          g.j0 = max(0, t - s - kUnitSteps) << a.step_shift;
-          g.j1 = min(nb, (end - s - kUnitSteps) << a.step_shift);
+          g.j0 = max(0, t - s - kUnitSteps<kWindow>) << a.step_shift;
+          g.j1 = min(nb, (end - s - kUnitSteps<kWindow>) << a.step_shift);
           const int me = static_cast<int>(blockIdx.x);
-          const int c0 = g.j0 == 0 ? me : runs.run(s + kUnitSteps);
+          const int c0 = g.j0 == 0 ? me : runs.run(s + kUnitSteps<kWindow>);
           const int c1 = end == s + len ? me : runs.run(s + len - 1);
           g.place = c0 == c1 ? -1 : piece_place(me, g.j0 == 0);
           if (g.head >= 0 && c0 < c1 && c0 == me) split = CacheChunkSplit{g.row0, g.n, g.head, g.unit, c0, c1};
@@ -404,6 +415,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       const int32_t* row = a.table + g.req * a.table_stride;
       const int blocks = g.j1 - g.j0;
       const int low = kWindow ? cache_low(a, g.seq - g.n + g.tok0(0)) : 0;
+      uint32_t pending = 0;  // blocks to be cleared in part, even and odd
       // the first queries wait for nothing; later ones come behind the segment's first keys, which
       // need not wait for the last product with the queries before
       if (kv == 0 && sc == 0) {
@@ -417,6 +429,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         if constexpr (kWindow) jump = g.j0 + j == g.sinks;
         if (j == 0 || (i0 & 31) == 0 || jump)
           if (sy.boxes[kv].template load<kWindow>(a, row, g.seq, i0 & ~31, low)) sy.bad_page = g.req;
+        const bool edge = kWindow && kv == 1 && block * kKB < low && block * kKB + kKB > a.sinks;
         const int keys = min(kKB, g.seq - block * kKB);  // none: an empty cache
         const int boxes = keys <= 0 ? 0 : (keys + a.box - 1) / a.box;
         // the stage's last occupant, block j - 2: V_{j - 2} is released in step j - 2, K_{j - 2} in
@@ -435,18 +448,47 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           if (!fine) {
             *abort_flag = 1;
           } else {
-            tc::mbar_arrive_expect_tx(&sy.kv_full[sb], boxes * a.box * D * 2);
+            uint64_t* full = kWindow && edge ? &sy.edge[j & 1] : &sy.kv_full[sb];
+            tc::mbar_arrive_expect_tx(full, boxes * a.box * D * 2);
             unsigned char* dst = sKV + sb * kTile;
 #pragma unroll 1
             for (int b = 0; b < boxes; ++b, dst += a.box * 128) {
               const int2 at = sy.boxes[kv].at[(i0 + b) & 31];
 #pragma unroll
-              for (int p = 0; p < D / 64; ++p)
-                tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, &sy.kv_full[sb]);
+              for (int p = 0; p < D / 64; ++p) tma_load_4d(dst + p * kPanel, map, p * 64, at.y, g.head, at.x, full);
             }
           }
         }
         __syncwarp();
+        if constexpr (kWindow) {
+          // Values behind the sinks and before the unit's first window, which no row of it sees: cleared, so that P = 0 meets
+          // no infinity, before the others may use the stage. (A segment's first two blocks, which may both be such,
+          // land beside each other.)
+          if (edge) pending |= 1u << (j & 1);
+          if (pending != 0 && (j > 0 || blocks == 1)) {
+#pragma unroll 1
+            for (int i = max(0, j - 1); i <= j; ++i) {
+              if (!(pending >> (i & 1) & 1)) continue;
+              if (!cache_wait_warp(&sy.edge[i & 1], edge_phase >> (i & 1) & 1)) {
+                *abort_flag = 1;
+                cache_wait_warp(&sy.edge[i & 1], edge_phase >> (i & 1) & 1);  // once more, for copies still in flight
+                break;
+              }
+              edge_phase ^= 1u << (i & 1);
+              const int key0 = g.block(g.j0 + i) * kKB, from = max(0, a.sinks - key0), rows = min(kKB, low - key0) - from;
+              uint4* v = reinterpret_cast<uint4*>(sKV + (2 * (i & 1) + 1) * kTile + from * 128);
+#pragma unroll 4
+              for (int w = lane; w < rows * 8; w += 32)
+#pragma unroll
+                for (int p = 0; p < D / 64; ++p) v[p * (kPanel / 16) + w] = make_uint4(0u, 0u, 0u, 0u);
+              tc::fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) tc::mbar_arrive(&sy.kv_full[2 * (i & 1) + 1]);
+            }
+            pending = 0;
+            __syncwarp();
+          }
+        }
         if (j & 1) ++loads1; else ++loads0;
         if (kv == 0 && j == 0 && sc > 0) {
           ok = load_queries<D, kWindow>(&mapQ, sQ, sy.seg[sc & 1], a.G, sy, sc);
@@ -605,12 +647,15 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // keys this row sees (all of them for a row that is not stored), and every row of the warp
       const int limit = live ? max(0, g.seq - g.n + tok + 1) : 0x7fffffff;
       const int all_see = __reduce_min_sync(0xffffffffu, limit);
-      // in a window: the first key behind the sinks that this row sees, every row of the warp, any row of the unit
-      int low = 0, all_low = 0, unit_low = 0;
+      // in a window: the first key behind the sinks that this row sees, and every row of the warp
+      int low = 0, all_low = 0;
+      int any_see = 0, any_low = 0;  // keys that some stored row of the warp sees: below the one, from the other on
+      bool fresh = true;             // the segment's rows have no references yet
       if (kWindow) {
         low = live ? cache_low(a, g.seq - g.n + tok) : 0;
         all_low = __reduce_max_sync(0xffffffffu, low);
-        unit_low = cache_low(a, g.seq - g.n + g.tok0(0));
+        any_low = __reduce_min_sync(0xffffffffu, live ? low : 0x7fffffff);
+        any_see = __reduce_max_sync(0xffffffffu, live ? limit : 0);
       }
       // row reference (log2 units), sum of exp2(c2 s - m). The reference begins as the maximum of the
       // first half, which is in registers anyway (the whole block's, with the half's exponentials
@@ -637,20 +682,6 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           for (int e = lane; e < dead * 8 * (D / 64); e += 32) {
             const int ac = e / (dead * 8), w = e - ac * dead * 8;
             *reinterpret_cast<uint4*>(v + ac * kPanel + valid * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          tc::fence_proxy_async();
-        }
-        if (kWindow && key0 < unit_low && key0 + kKB > a.sinks) {
-          // likewise the values before the unit's first window and behind the sinks, a quarter of them a warp
-          const int sb = 2 * (j & 1) + 1;
-          ok = cache_wait_warp(&sy.kv_full[sb], ((j & 1 ? loads1 : loads0) + (j >> 1)) & 1);
-          if (!ok) break;
-          unsigned char* v = sKV + sb * kTile;
-          const int from = max(0, a.sinks - key0), rows = min(kKB, unit_low - key0) - from;
-#pragma unroll 1
-          for (int e = quad * 32 + lane; e < rows * 8 * (D / 64); e += 32 * kSlotWarps) {
-            const int ac = e / (rows * 8), w = e - ac * rows * 8;
-            *reinterpret_cast<uint4*>(v + ac * kPanel + from * 128 + w * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           tc::fence_proxy_async();
         }
@@ -685,7 +716,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         // Nearly every block: no mask, and a reference that stays. Its instructions lie one behind the
         // other; what the others need comes behind, once.
         int hf = 0;
-        if (!masked && j > 0) {
+        if (!masked && (kWindow ? !fresh : j > 0)) {
           tc::tmem_ld64_async(tS, su);
           tc::tmem_wait64(su);
           float sum = exps();
@@ -707,21 +738,39 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           // Once through the loop but for a reference to be found: the half's maximum as a segment's
           // first one (kFirst), the maximum of what is left of the block where a sum asks for it (kMove).
           enum { kPlain, kFirst, kMove };
-          int mode = hf == 0 && j == 0 ? kFirst : kPlain;
+          int mode = (kWindow ? fresh : hf == 0 && j == 0) ? kFirst : kPlain;
           int at = hf;  // the half in su
+          // most halves that a window's edge leaves in a block are out of the whole warp's sight
+          const int half0 = key0 + hf * 64;
+          const bool blind = kWindow && (half0 >= any_see || (half0 + 64 <= any_low && half0 >= a.sinks));
+          if (blind) {
+            sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) pk[c] = 0u;
+          } else {
+            fresh = false;
+          }
 #pragma unroll 1
-          for (;;) {
+          while (!blind) {
             tc::tmem_ld64_async(tS + at * 64, su);
             tc::tmem_wait64(su);
-            if (masked) {
+            if (kWindow) {
+              const int k0 = key0 + at * 64;
+              if (k0 + 64 > all_see || (k0 < all_low && k0 + 64 > a.sinks)) {
+                // the row's keys of the half, a bit each
+                auto below = [](int n) { return n <= 0 ? 0ull : (n >= 64 ? ~0ull : (1ull << n) - 1ull); };
+                const uint64_t sees = (below(limit - k0) & ~below(low - k0)) | (below(min(a.sinks, limit) - k0));
+                const uint32_t lo = static_cast<uint32_t>(sees), hi = static_cast<uint32_t>(sees >> 32);
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                  su[c] = lo & (1u << c) ? su[c] : 0xff800000u;
+                  su[32 + c] = hi & (1u << c) ? su[32 + c] : 0xff800000u;
+                }
+              }
+            } else if (masked) {
               const int left = seen - at * 64;
 #pragma unroll
               for (int c = 0; c < 64; ++c) su[c] = c < left ? su[c] : 0xff800000u;
-              if (kWindow) {
-                const int below = low - key0 - at * 64, sinks = a.sinks - key0 - at * 64;
-#pragma unroll
-                for (int c = 0; c < 64; ++c) su[c] = c >= below || c < sinks ? su[c] : 0xff800000u;
-              }
             }
             if (mode != kPlain) {
               float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
