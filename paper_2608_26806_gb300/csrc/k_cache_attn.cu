@@ -36,8 +36,10 @@
 // wait gives up records AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and
 // their values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 //
-// In a window (kWindow, see avtp.h) a row block's tiles are those of the sinks and those from its first token's window on;
-// the line of tiles is as long as what is seen. Keys that none of its rows sees are cleared like those behind the last.
+// In a window (kWindow, see avtp.h) a row block's tiles are those of the sinks and those from its first token's window
+// on; the line of tiles is as long as what is seen. Values that none of its rows sees are cleared like those behind the last
+// key. 256 requests of 200-8000 tokens, eight KV heads, in windows of 1024 and 4096 184 and 497 us, 5.9 and 6.3 TB/s; eight of 30-65
+// thousand in 4096 31 us, 4.4 TB/s, in which the figures of one request above weigh.
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -75,6 +77,11 @@ struct Segment {
 __host__ __device__ constexpr int tile_keys(int d) { return d == 128 ? 64 : 128; }
 __host__ __device__ constexpr uint32_t stage_bytes(int d) { return 2u * tile_keys(d) * d * 2; }
 constexpr int kStages = 5;
+// In a window, whose row blocks are short, one that a cut falls into costs more (a piece through L2, its count, the join:
+// about eight tiles' time) than a longer run, if that is not much longer. 61 requests of 200-8000 tokens, four KV heads, window
+// 128: 15.0 us, 17.3 without; 16 of 700-4000, five tokens of eight heads, window 512 16.2 and 20.4, 2048 36.6 and 36.7 (a
+// slack of eight tiles: 45.4); 24 of 4000 in 256 14.8 either way (15.6).
+constexpr int kWholeSlack = 4;
 // A warp's O on its way to the others: 16 rows of d floats, 8 floats of padding so that the eight
 // rows of an accumulator's column pair fall into different banks.
 __host__ __device__ constexpr int out_row(int d) { return d + 8; }
@@ -258,6 +265,25 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       runs = CacheRuns(line.total, line.most, 1, cache_ctas(a, line.weights, true));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
+      // In a window a row block goes whole to the run that most of it lies in where that makes the longest run, of blocks of
+      // equal length, kWholeSlack steps longer at most.
+      if (kWindow && (runs.each + line.most - 1) / line.most * line.most <= runs.each + kWholeSlack) {
+        auto whole = [&](int x) {
+          if (x >= line.total) return line.total;
+          int before;
+#pragma unroll 1
+          for (int q = line.find(a, sh.plan, x, &before);; ++q) {
+            const int len = steps_of(a, tiles_of<D, kWindow>(a, line.request(a, mine, q)));
+            if (x < before + len * a.Hkv) {
+              const int in = static_cast<int>(static_cast<uint32_t>(x - before) % static_cast<uint32_t>(len));
+              return 2 * in < len ? x - in : x - in + len;
+            }
+            before += len * a.Hkv;
+          }
+        };
+        t = whole(t);
+        t1 = whole(t1);
+      }
       if (t < t1) r = line.find(a, sh.plan, t, &pre);
     }
     int n = 0;
@@ -345,18 +371,11 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
     const uint32_t base = tc::smem_u32(smem);
     const float c2 = a.c2;
     int n = 0;
-    for (int sc = 0;; ++sc) {
-      if (!cache_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1)) *abort_flag = 1;
-      if (bar_consumers_any(*abort_flag != 0)) break;
-      const Segment g = sh.seg[sc & 1];
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(&sh.seg_empty[sc & 1]);
-      if (g.head < 0) break;
+    // Q as the A operand; keys visible to this lane's two rows, in a window the first ones behind the sinks too
+    uint32_t qa[D / 16][4];
+    int limit[2], low[2];
+    auto queries = [&](const Segment& g) {
       const int rows = g.n * a.G;
-      // Q as the A operand; keys visible to this lane's two rows
-      uint32_t qa[D / 16][4];
-      int limit[2];
-      int low[2];  // in a window, the first keys behind the sinks that they see
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int row = wm * 16 + gr + 8 * i;
@@ -375,6 +394,19 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
         if (row >= rows) limit[i] = g.seq;
         low[i] = cache_low(a, row >= rows ? g.seq - 1 : g.seq - g.n + tok);
       }
+    };
+    Segment g;
+    for (int sc = 0;; ++sc) {
+      if (!kWindow || sc == 0) {
+        if (!cache_wait_warp(&sh.seg_full[sc & 1], (sc >> 1) & 1)) *abort_flag = 1;
+        if (bar_consumers_any(*abort_flag != 0)) break;
+        g = sh.seg[sc & 1];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.seg_empty[sc & 1]);
+        if (g.head < 0) break;
+        queries(g);
+      }
+      const int rows = g.n * a.G;
       const CacheSkip skip(a, g.seq - g.n, kTile);
       const int first_low = cache_low(a, g.seq - g.n), last_low = cache_low(a, g.seq - 1);  // of the first token and the last
       const int all_see = g.seq - g.n + 1;  // keys that every row sees
@@ -561,6 +593,15 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           sh.w[warp][gr + 8 * i] = rs[2 * i];
         }
       }
+      // In a window, whose segments are short, the next one's queries come while this one's rows go out.
+      Segment next{};
+      if (kWindow) {
+        if (!cache_wait_warp(&sh.seg_full[(sc + 1) & 1], ((sc + 1) >> 1) & 1)) *abort_flag = 1;
+        next = sh.seg[(sc + 1) & 1];
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&sh.seg_empty[(sc + 1) & 1]);
+        if (next.head >= 0) queries(next);
+      }
       if (bar_consumers_any(*abort_flag != 0)) break;
       const int pieces = g.c1 - g.c0 + 1;
       constexpr int kLanes = D / 4;               // lanes of a row, four columns each
@@ -593,145 +634,152 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
           if (sub == 0) __stcg(a.part_ml + at, make_float4(M, L, W, 0.f));
         }
       }
-      if (pieces == 1) continue;
+      do {
+        if (pieces == 1) break;
 
-      // ---- a piece: the last of the block's to arrive joins them
-      bar_consumers();
-      if (tid == 0) {
-        pdl_wait();  // the counters are cleared by the kernel ahead
-        // behind this CTA's piece, ahead of its reads of the others' (0.4 us less than two fences)
-        int before;
-        asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(a.count + g.c0) : "memory");
-        sh.last = before == pieces - 1;
-      }
-      bar_consumers();
-      if (!sh.last) continue;
-      // Eight pieces of a row at a time or two of four rows, whichever takes fewer turns, each of which is one
-      // trip to L2; a row's reference moves between turns. (One request of 3425 tokens, 7 rows a head in 27
-      // pieces: 12.6 us the one way, 14.6 the other; 16 of 700-4000, 16 rows in 2 or 3: 39.5 and 37.9.) Beyond
-      // 16 pieces, join_many: the first 11.0 us so, five tokens of 32 heads 18.7 -> 16.5. (For the second, and
-      // for ten pieces a head, it would take 0.3 to 1.2 us more.)
-      auto join = [&](auto rows_at_once) {
-        constexpr int N = decltype(rows_at_once)::value, P = 8 / N;
-        for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
-          float M[N], L[N], W[N];
-          float4 v[N];
+        // ---- a piece: the last of the block's to arrive joins them
+        bar_consumers();
+        if (tid == 0) {
+          pdl_wait();  // the counters are cleared by the kernel ahead
+          // behind this CTA's piece, ahead of its reads of the others' (0.4 us less than two fences)
+          int before;
+          asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(a.count + g.c0) : "memory");
+          sh.last = before == pieces - 1;
+        }
+        bar_consumers();
+        if (!sh.last) break;
+        // Eight pieces of a row at a time or two of four rows, whichever takes fewer turns, each of which is one
+        // trip to L2; a row's reference moves between turns. (One request of 3425 tokens, 7 rows a head in 27
+        // pieces: 12.6 us the one way, 14.6 the other; 16 of 700-4000, 16 rows in 2 or 3: 39.5 and 37.9.) Beyond
+        // 16 pieces, join_many: the first 11.0 us so, five tokens of 32 heads 18.7 -> 16.5. (For the second, and
+        // for ten pieces a head, it would take 0.3 to 1.2 us more.)
+        auto join = [&](auto rows_at_once) {
+          constexpr int N = decltype(rows_at_once)::value, P = 8 / N;
+          for (int row0 = tid / kLanes; row0 < rows; row0 += kAtOnce * N) {
+            float M[N], L[N], W[N];
+            float4 v[N];
 #pragma unroll
-          for (int i = 0; i < N; ++i) {
-            M[i] = -INFINITY;
-            L[i] = W[i] = 0.f;
-            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          }
+            for (int i = 0; i < N; ++i) {
+              M[i] = -INFINITY;
+              L[i] = W[i] = 0.f;
+              v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
 #pragma unroll 1
-          for (int k0 = 0; k0 < pieces; k0 += P) {
-            float4 ml[N][P];
-            float4 x[N][P];
+            for (int k0 = 0; k0 < pieces; k0 += P) {
+              float4 ml[N][P];
+              float4 x[N][P];
 #pragma unroll
-            for (int k = 0; k < P; ++k) {
-              const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
+              for (int k = 0; k < P; ++k) {
+                const int64_t at = static_cast<int64_t>(piece_place(g.c0 + k0 + k, k0 + k == 0)) * kRows + row0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                  ml[i][k] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                  x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                  if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
+                    ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
+                    x[i][k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + i * kAtOnce) * D + col));
+                  }
+                }
+              }
 #pragma unroll
               for (int i = 0; i < N; ++i) {
-                ml[i][k] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-                x[i][k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (k0 + k < pieces && row0 + i * kAtOnce < rows) {
-                  ml[i][k] = __ldcg(a.part_ml + at + i * kAtOnce);
-                  x[i][k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + (at + i * kAtOnce) * D + col));
+                float mn = M[i];
+#pragma unroll
+                for (int k = 0; k < P; ++k) mn = fmaxf(mn, ml[i][k].x);
+                const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
+                M[i] = mn;
+                L[i] *= old;
+                W[i] *= old;
+                v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                  const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
+                  L[i] = fmaf(f, ml[i][k].y, L[i]);
+                  W[i] = fmaf(f, ml[i][k].z, W[i]);
+                  v[i].x = fmaf(f, x[i][k].x, v[i].x);
+                  v[i].y = fmaf(f, x[i][k].y, v[i].y);
+                  v[i].z = fmaf(f, x[i][k].z, v[i].z);
+                  v[i].w = fmaf(f, x[i][k].w, v[i].w);
                 }
               }
             }
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-              float mn = M[i];
+            for (int i = 0; i < N; ++i)
+              if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
+          }
+        };
+        // A row in many pieces: their references and sums lie with the row's lanes, one or two a lane, and the
+        // weights are formed once, while the first sixteen pieces' rows are on their way.
+        auto join_many = [&]() {
+          constexpr int P = 16, E = kCacheMaxPieces / kLanes;
+          auto place = [&](int piece, int row) {
+            return piece_place(g.c0 + piece, piece == 0) * static_cast<int64_t>(kRows) + row;
+          };
+          // the warp stays together: row0 of its first lanes
+#pragma unroll 1
+          for (int row0 = warp * 32 / kLanes; row0 < rows; row0 += kAtOnce) {
+            const int row = row0 + lane / kLanes;
+            const bool here = row < rows;
+            float4 ml[E];
+            float weight[E];
+            float M = -INFINITY, L = 0.f, W = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-              for (int k = 0; k < P; ++k) mn = fmaxf(mn, ml[i][k].x);
-              const float old = M[i] == -INFINITY ? 0.f : tc::ex2(M[i] - mn);
-              M[i] = mn;
-              L[i] *= old;
-              W[i] *= old;
-              v[i] = make_float4(v[i].x * old, v[i].y * old, v[i].z * old, v[i].w * old);
+            for (int e = 0; e < E; ++e) {
+              const int piece = sub + e * kLanes;
+              ml[e] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+              if (piece < pieces && here) ml[e] = __ldcg(a.part_ml + place(piece, row));
+            }
+#pragma unroll 1
+            for (int k0 = 0; k0 < pieces; k0 += P) {
+              float4 x[P];
 #pragma unroll
               for (int k = 0; k < P; ++k) {
-                const float f = ml[i][k].x == -INFINITY ? 0.f : tc::ex2(ml[i][k].x - mn);
-                L[i] = fmaf(f, ml[i][k].y, L[i]);
-                W[i] = fmaf(f, ml[i][k].z, W[i]);
-                v[i].x = fmaf(f, x[i][k].x, v[i].x);
-                v[i].y = fmaf(f, x[i][k].y, v[i].y);
-                v[i].z = fmaf(f, x[i][k].z, v[i].z);
-                v[i].w = fmaf(f, x[i][k].w, v[i].w);
+                x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k0 + k < pieces && here)
+                  x[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + place(k0 + k, row) * D + col));
+              }
+              if (k0 == 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) M = fmaxf(M, ml[e].x);
+#pragma unroll 1
+                for (int o = kLanes / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                  weight[e] = ml[e].x == -INFINITY ? 0.f : tc::ex2(ml[e].x - M);
+                  L = fmaf(weight[e], ml[e].y, L);
+                  W = fmaf(weight[e], ml[e].z, W);
+                }
+#pragma unroll 1
+                for (int o = kLanes / 2; o > 0; o >>= 1) {
+                  L += __shfl_xor_sync(0xffffffffu, L, o);
+                  W += __shfl_xor_sync(0xffffffffu, W, o);
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < P; ++k) {
+                const float mine = E == 2 && k0 + k >= kLanes ? weight[E - 1] : weight[0];
+                const float f = __shfl_sync(0xffffffffu, mine, k0 + k, kLanes);
+                v.x = fmaf(f, x[k].x, v.x);
+                v.y = fmaf(f, x[k].y, v.y);
+                v.z = fmaf(f, x[k].z, v.z);
+                v.w = fmaf(f, x[k].w, v.w);
               }
             }
+            if (here) store_row<D>(a, g, row, col, v, M, L, W);
           }
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (row0 + i * kAtOnce < rows) store_row<D>(a, g, row0 + i * kAtOnce, col, v[i], M[i], L[i], W[i]);
-        }
-      };
-      // A row in many pieces: their references and sums lie with the row's lanes, one or two a lane, and the
-      // weights are formed once, while the first sixteen pieces' rows are on their way.
-      auto join_many = [&]() {
-        constexpr int P = 16, E = kCacheMaxPieces / kLanes;
-        auto place = [&](int piece, int row) {
-          return piece_place(g.c0 + piece, piece == 0) * static_cast<int64_t>(kRows) + row;
         };
-        // the warp stays together: row0 of its first lanes
-#pragma unroll 1
-        for (int row0 = warp * 32 / kLanes; row0 < rows; row0 += kAtOnce) {
-          const int row = row0 + lane / kLanes;
-          const bool here = row < rows;
-          float4 ml[E];
-          float weight[E];
-          float M = -INFINITY, L = 0.f, W = 0.f;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int piece = sub + e * kLanes;
-            ml[e] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            if (piece < pieces && here) ml[e] = __ldcg(a.part_ml + place(piece, row));
-          }
-#pragma unroll 1
-          for (int k0 = 0; k0 < pieces; k0 += P) {
-            float4 x[P];
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-              x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (k0 + k < pieces && here)
-                x[k] = __ldcg(reinterpret_cast<const float4*>(a.part_o + place(k0 + k, row) * D + col));
-            }
-            if (k0 == 0) {
-#pragma unroll
-              for (int e = 0; e < E; ++e) M = fmaxf(M, ml[e].x);
-#pragma unroll 1
-              for (int o = kLanes / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-#pragma unroll
-              for (int e = 0; e < E; ++e) {
-                weight[e] = ml[e].x == -INFINITY ? 0.f : tc::ex2(ml[e].x - M);
-                L = fmaf(weight[e], ml[e].y, L);
-                W = fmaf(weight[e], ml[e].z, W);
-              }
-#pragma unroll 1
-              for (int o = kLanes / 2; o > 0; o >>= 1) {
-                L += __shfl_xor_sync(0xffffffffu, L, o);
-                W += __shfl_xor_sync(0xffffffffu, W, o);
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < P; ++k) {
-              const float mine = E == 2 && k0 + k >= kLanes ? weight[E - 1] : weight[0];
-              const float f = __shfl_sync(0xffffffffu, mine, k0 + k, kLanes);
-              v.x = fmaf(f, x[k].x, v.x);
-              v.y = fmaf(f, x[k].y, v.y);
-              v.z = fmaf(f, x[k].z, v.z);
-              v.w = fmaf(f, x[k].w, v.w);
-            }
-          }
-          if (here) store_row<D>(a, g, row, col, v, M, L, W);
-        }
-      };
-      const int turns = (rows + kAtOnce - 1) / kAtOnce;  // of one row a thread
-      const int few = (turns + 3) / 4 * ((pieces + 1) / 2);
-      if (pieces > 16 && turns * 2 < few) join_many();
-      else if (few < turns * ((pieces + 7) / 8)) join(std::integral_constant<int, 4>{});
-      else join(std::integral_constant<int, 1>{});
+        const int turns = (rows + kAtOnce - 1) / kAtOnce;  // of one row a thread
+        const int few = (turns + 3) / 4 * ((pieces + 1) / 2);
+        if (pieces > 16 && turns * 2 < few) join_many();
+        else if (few < turns * ((pieces + 7) / 8)) join(std::integral_constant<int, 4>{});
+        else join(std::integral_constant<int, 1>{});
+      } while (false);
+      if (kWindow) {
+        if (pieces == 1) bar_consumers();  // the shares have been read
+        g = next;
+        if (g.head < 0) break;
+      }
     }
   }
   pdl_wait();  // this grid's end implies the validation kernel's, which resets the status word

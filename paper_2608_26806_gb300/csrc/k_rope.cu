@@ -376,6 +376,7 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
 cudaError_t launch_rope(const avtp_rope_args_t& a, const avtp_cache_t* c, void* ws, cudaStream_t s) {
   RopeDev d{};
   d.a = a;
+  if (a.n_tokens == 0) d.a.rot_dim = 0;  // its tables may be missing
   if (c != nullptr) d.c = *c;
   d.st = static_cast<DevStatus*>(ws);
   // warps share a token's groups of heads where there are few tokens

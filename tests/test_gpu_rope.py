@@ -1,5 +1,7 @@
 """Rotary positions on the GPU against a plain 64-bit form: styles, parts of a head, planes, norms, the cache as
 destination, and the calls that could go wrong."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -263,6 +265,23 @@ def test_no_tokens():
     call = avtp.RopeCall(torch.empty(0, dtype=torch.int32, device="cuda"), torch.ones(32, device="cuda"), q=e(0, 4, 64),
                          k=e(0, 2, 64)).run()
     assert status(call) == avtp.OK and call.q_out.shape == (0, 4, 64)
+
+
+def test_no_tokens_and_no_tables():
+    """A call without tokens reads nothing, the frequencies among it."""
+    ws = avtp.new_workspace(256)
+    a = avtp._RopeArgs(0, 4, 2, 64, None, 256, None, 256, None, 128, None, 128, None, 128, None, 64, avtp.ROPE_HALF, None,
+                       None, 0, 1, None, 1.0, None, None, 1e-6)
+    assert avtp.load().avtp_rope(ctypes.byref(a), None, ws.data_ptr(), 256, None) == avtp.OK
+    assert avtp.read_device_status(ws) == avtp.OK
+
+
+def test_no_heads():
+    a = avtp._RopeArgs(5, 0, 0, 64, None, 0, None, 0, None, 0, None, 0, None, 0, None, 0, avtp.ROPE_HALF, None, None, 0, 1,
+                       None, 1.0, None, None, 1e-6)
+    ws = avtp.new_workspace(256)
+    assert avtp.load().avtp_rope(ctypes.byref(a), None, ws.data_ptr(), 256, None) == avtp.OK
+    assert avtp.read_device_status(ws) == avtp.OK
 
 
 def test_a_captured_call_replays_on_new_positions():
