@@ -87,6 +87,7 @@ FREE_CASES = {
     "rows_at_the_limit": ([5] * 2048, [0] * 2048, 4),
     "rows_past_the_limit": ([5] * 2049, [0] * 2049, 4),
     "long": ([200000, 3, 70000], [0, 3, 5], 16),
+    "more_than_registers_hold": ([1200000, 3, 40], [0, 3, 0], 16),
 }
 
 
@@ -143,6 +144,30 @@ def test_free_of_many_shared_pages_does_not_depend_on_who_comes_first():
     f = Freed([n] * R, [0 if r % 3 else n for r in range(R)], 16, seed=5)
     shared_rows(f, [(tuple(range(g, g + 10)), 50) for g in range(0, R, 10)])
     f.check(f.call().run())
+
+
+def test_free_of_more_shared_pages_than_registers_hold():
+    R, n = 1800, 1000
+    f = Freed([n] * R, [0 if r % 3 else n for r in range(R)], 16, seed=7)
+    shared_rows(f, [(tuple(range(g, g + 6)), 30) for g in range(0, R, 6)])
+    f.check(f.call().run())
+
+
+@pytest.mark.parametrize("R", [2048, 2049, 2500])
+def test_free_over_its_own_lengths_of_many_requests(R):
+    """Lengths, held lengths and the list's head advanced in place, from shared memory or not."""
+    rng = np.random.default_rng(R)
+    seq = rng.integers(0, 90, R)
+    held = np.maximum(seq - rng.integers(20, 60, R), 0)
+    new = np.where(rng.random(R) < 0.3, 0, seq)
+    f = Freed(seq, new, 4, window=9, sinks=5, held=held, seed=R)
+    f.call()  # for its tensors
+    d = f.dev
+    dev_held = i32(held)
+    c = avtp.CacheFreeCall(d["seq"], d["new"], d["table"], page_size=4, n_pages=f.n_pages, free_pages=d["free"],
+                           free_head=d["head"], window=9, sinks=5, held_len=dev_held, seq_len_out=d["seq"],
+                           held_len_out=dev_held, free_head_out=d["head"]).run()
+    f.check(c)
 
 
 def test_free_of_shared_pages_in_a_window():
@@ -274,6 +299,8 @@ FORKS = {
     "none": dict(seq=[10], parent=[], child=[], page=16),
     "many": dict(seq=[1000 + 13 * i for i in range(100)], parent=[i // 5 for i in range(500)],
                  child=[100 + (i * 7) % 500 for i in range(500)], page=16),
+    "more_than_registers_hold": dict(seq=[1600 + i for i in range(60)], parent=[i // 15 for i in range(900)],
+                                     child=[60 + (i * 7) % 900 for i in range(900)], page=16),
     "children_at_the_limit": dict(seq=[5], parent=[0] * 2048, child=list(range(1, 2049)), page=4),
     "children_past_the_limit": dict(seq=[5, 9], parent=[i % 2 for i in range(2100)], child=list(range(2, 2102)), page=4),
     "window": dict(seq=[500, 90, 33], parent=[0, 0, 1, 2], child=[3, 4, 5, 6], page=16, window=40, sinks=20,
@@ -407,6 +434,8 @@ COMPACTS = {
     "odd_page": ([100, 31], [61, 7], 7),
     "long": ([9000, 4000], [3000, 3999], 64),
     "many": ([100 + i for i in range(200)], [50 + i // 2 for i in range(200)], 16),
+    "chunks": ([20000, 50, 9000], [9001, 20, 4097], 64),
+    "requests_past_the_limit": ([20 + i % 9 for i in range(1100)], [7 + i % 5 for i in range(1100)], 4),
 }
 
 
@@ -426,6 +455,32 @@ def test_compact_of_any_order_of_pages(order, other, Hkv, d):
     c = Compacted([300, 77], [140, 50], 16, Hkv, d, order, other=other)
     call = c.call().run()
     assert status(call) == avtp.OK and c.same(c.want())
+
+
+@pytest.mark.parametrize("other", [True, False])
+def test_a_captured_compaction_replays_on_new_positions(other):
+    c = Compacted([300, 200], [100, 60], 16, other=other)
+    kept = avtp.CacheCompactCall(avtp.PagedCache(c.k, c.v), i32(c.cu), i32(c.idx), i32(c.seq), i32(c.table),
+                                 **(dict(dst_table=i32(c.to)) if other else {}))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept.run()
+    new = Compacted([300, 200], [100, 60], 16, other=other, seed=0)
+    for r, n in enumerate((100, 60)):  # other positions, the same numbers of them
+        new.idx[new.cu[r]:new.cu[r + 1]] = np.arange(n) * 2 + r + 1
+    kept._keep[1].copy_(i32(new.idx))
+    graph.replay()
+    torch.cuda.synchronize()
+    assert status(kept) == avtp.OK
+    c.idx = new.idx
+    assert c.same(c.want())
+
+
+@pytest.mark.parametrize("other", [True, False])
+def test_compact_of_nothing(other):
+    c = Compacted([30, 20], [0, 0], 16, other=other)
+    call = c.call().run()
+    assert status(call) == avtp.OK and c.same(c.before) and (call.len_out == 0).all()
 
 
 def test_compact_to_other_pages_takes_positions_in_any_order():
@@ -518,6 +573,32 @@ def test_compact_with_bad_offsets_writes_nothing(what, other):
         c.cu[2] = len(c.idx) + 1
     call = c.call().run()
     assert status(call) == avtp.ERR_DEVICE_INPUT and c.same(c.before) and (call.len_out == -1).all()
+
+
+def test_calls_on_another_stream():
+    """Buffers that a call makes come from the stream that it runs on."""
+    s = torch.cuda.Stream()
+    c = Compacted([300, 200], [100, 60], 16)
+    f = Forked([100, 50], [0, 1, 1], [2, 3, 4], 16)
+    f.call()
+    g = Freed([100, 50], [0, 50], 16)
+    g.call()
+    torch.cuda.synchronize()
+    kept = avtp.cache_compact(avtp.PagedCache(c.k, c.v), i32(c.cu), i32(c.idx), i32(c.seq), i32(c.table),
+                              dst_table=i32(c.to), stream=s)
+    d = f.dev
+    src, dst, head = avtp.cache_fork(d["parent"], d["child"], d["seq"], d["table"], page_size=16, n_pages=f.n_pages,
+                                     free_pages=d["free"], free_head=d["head"], shared=d["shared"], stream=s)
+    avtp.cache_copy(avtp.PagedCache(c.k, c.v), i32([0]), i32([-1]), stream=s)
+    e = g.dev
+    seq, ghead = avtp.cache_free(e["seq"], e["new"], e["table"], page_size=16, n_pages=g.n_pages, free_pages=e["free"],
+                                 free_head=e["head"], stream=s)
+    s.synchronize()
+    assert c.same(c.want()) and np.array_equal(ints(kept), np.diff(c.cu))
+    want = fork_plain(f.parent, f.child, f.seq, f.table, f.free, f.head, 16, f.shared)
+    assert np.array_equal(ints(d["table"]), want[0]) and np.array_equal(ints(src), want[4]) and int(head) == want[2]
+    free, h, _ = free_plain(g.seq, g.new, g.table, g.free, g.head, 16)
+    assert np.array_equal(ints(e["free"]), free) and int(ghead) == h and np.array_equal(ints(seq), g.new)
 
 
 def test_the_binding_refuses():
