@@ -463,15 +463,16 @@ AVTP_API avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_ca
                                         size_t workspace_bytes, avtp_stream_t stream);
 
 /* Rotary positions of a step's queries and keys, behind the norm of each head where the model has
- * one, with the keys and values to their slots of the cache. For token t and every head, x a row of q
- * or k:
+ * one, with the keys and values to their slots of the cache. For token t and every head, x a row of
+ * q or k:
  *   y = x * rsqrt(mean(x^2) + eps) * w         (w: q_norm or k_norm; NULL: y = x)
  *   (y_a, y_b) -> attn_factor * (y_a cos z - y_b sin z, y_b cos z + y_a sin z),
  *   z = pos[pair_plane[i]][t] * inv_freq[i]
- * for the pairs i < rot_dim / 2 of a head's first rot_dim elements, (a, b) = (i, i + rot_dim / 2) or
- * (2 i, 2 i + 1); the other elements stay y. In 32 bits, angles exact to 2^-53 * pos * inv_freq beside
- * that; rounded to bf16 once. Position ids of several planes (M-RoPE) are gathered by avtp_prune like
- * any others: pos may be its output planes. */
+ * for the pairs i < rot_dim / 2 of a head's first rot_dim elements, (a, b) = (i, i + rot_dim / 2)
+ * or (2 i, 2 i + 1); the other elements stay y. Computed in 32 bits but for the angles, which are
+ * exact to 2^-61 * pos * (1 + inv_freq) ahead of their sines, however far the position; rounded to
+ * bf16 once. Position ids of several planes (M-RoPE) are gathered by avtp_prune like any others:
+ * pos may be its output planes. */
 typedef enum {
   AVTP_ROPE_HALF = 0,        /* pairs (i, i + rot_dim / 2) */
   AVTP_ROPE_INTERLEAVED = 1  /* pairs (2 i, 2 i + 1)       */
@@ -507,20 +508,21 @@ typedef struct {
 } avtp_rope_args_t;
 
 /* cache: NULL, or where the keys and values go (n_kv_heads and head_dim as in args). A slot outside
- * [-1, n_pages * page_size) is skipped and recorded as AVTP_ERR_DEVICE_INPUT; a frequency that is not
- * finite or a plane outside [0, n_planes) is recorded too, and then nothing is written. workspace:
- * 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
+ * [-1, n_pages * page_size) is skipped and recorded as AVTP_ERR_DEVICE_INPUT; a frequency that is
+ * not finite or a plane outside [0, n_planes) is recorded too, and then nothing is written.
+ * workspace: 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_rope(const avtp_rope_args_t* args, const avtp_cache_t* cache, void* workspace,
                                  size_t workspace_bytes, avtp_stream_t stream);
 
-/* Frequencies for avtp_rope, with th_i = base^(-2 i / rot_dim) the unscaled ones, for contexts `factor` times as
- * long as the original_len positions that a model was trained on:
+/* Frequencies for avtp_rope, with th_i = base^(-2 i / rot_dim) the unscaled ones, for contexts
+ * `factor` times as long as the original_len positions that a model was trained on:
  *   NONE     th_i
  *   LINEAR   th_i / factor (positions interpolated)
- *   NTK      th_i with base * factor^(rot_dim / (rot_dim - 2)): the slowest pair as in LINEAR, the fastest kept
- *   YARN     (1 - g_i) th_i / factor + g_i th_i, g_i = clamp((r_i - slow) / (fast - slow), 0, 1) with r_i =
- *            original_len * th_i / (2 pi) turns of the pair over the original context, and an attn_factor of
- *            0.1 ln(factor) + 1 (arXiv 2309.00071) */
+ *   NTK      th_i with base * factor^(rot_dim / (rot_dim - 2)): the slowest pair as in LINEAR, the
+ *            fastest kept
+ *   YARN     (1 - g_i) th_i / factor + g_i th_i, g_i = clamp((r_i - slow) / (fast - slow), 0, 1) with
+ *            r_i = original_len * th_i / (2 pi) turns of the pair over the original context, and an
+ *            attn_factor of 0.1 ln(factor) + 1 (arXiv 2309.00071) */
 typedef enum {
   AVTP_ROPE_SCALE_NONE = 0,
   AVTP_ROPE_SCALE_LINEAR = 1,
@@ -537,7 +539,8 @@ typedef struct {
   double slow, fast;     /* 0 <= slow < fast, YARN; the paper uses 1 and 32       */
 } avtp_rope_freq_args_t;
 
-/* Host arrays: inv_freq [rot_dim / 2], rounded to fp32 once, and attn_factor [1] (1 but for YARN; NULL to skip). */
+/* Host arrays: inv_freq [rot_dim / 2], rounded to fp32 once, and attn_factor [1] (1 but for YARN;
+ * NULL to skip). */
 AVTP_API avtp_status_t avtp_rope_frequencies(const avtp_rope_freq_args_t* args, float* inv_freq, float* attn_factor);
 
 /* Causal attention of a step's new tokens over the cache, which holds their own keys and values
@@ -574,24 +577,24 @@ typedef struct {
 AVTP_API avtp_status_t avtp_cache_attention_workspace_size(const avtp_cache_t* cache,
                                                            const avtp_cache_attn_args_t* args, size_t* bytes);
 
-/* Products on bf16 operands with fp32 accumulation, softmax in fp32, P rounded to bf16 before
- * P V as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run. Two
- * kernels share the requests by their rows a KV head and the call's bounds, and divide O by the sum of
- * the rounded or of the exact weights: last bits may change with the batch that a request is in.
- * Offsets that decrease or pass n_tokens, a length that is negative or longer than max_pages
- * pages or 2^31 - 256 tokens, or more than max_new new tokens are recorded as
- * AVTP_ERR_DEVICE_INPUT, and then nothing is written; a page outside [0, n_pages) is recorded too,
- * is not read, and leaves its request's rows unspecified. Slots behind a request's last token may
- * hold anything; a value of a later new token that is not finite may reach the earlier tokens of its
- * chunk (0 * inf). With G query heads a KV head, (n_requests + n_tokens / (2 * (128 / G))) *
- * n_kv_heads above 2^27 returns AVTP_ERR_RANGE.
- * Asynchronous on `stream`. */
+/* Products on bf16 operands with fp32 accumulation, softmax in fp32, P rounded to bf16 before P V
+ * as in avtp_attn_forward; O is rounded to bf16 once. Results do not change from run to run. Two
+ * kernels share the requests by their rows a KV head and the call's bounds, and divide O by the sum
+ * of the rounded or of the exact weights: last bits may change with the batch that a request is in.
+ * Offsets that decrease or pass n_tokens, a length that is negative or longer than max_pages pages
+ * or 2^31 - 256 tokens, or more than max_new new tokens are recorded as AVTP_ERR_DEVICE_INPUT, and
+ * then nothing is written; a page outside [0, n_pages) is recorded too, is not read, and leaves its
+ * request's rows unspecified. Slots behind a request's last token may hold anything; a value of a
+ * later new token that is not finite may reach the earlier tokens of its chunk (0 * inf). With G
+ * query heads a KV head, (n_requests + n_tokens / (2 * (128 / G))) * n_kv_heads above 2^27 returns
+ * AVTP_ERR_RANGE. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                             void* workspace, size_t workspace_bytes, avtp_stream_t stream);
 
-/* avtp_cache_attention in a sliding window that keeps the first tokens in sight (sinks): the new token at place p =
- * seq_len[r] - n_r + i of its request sees the cached tokens u <= p with u > p - window or u < n_sinks, a window of
- * its own and `window` - 1 tokens before it. Work and bytes go by what is seen. */
+/* avtp_cache_attention in a sliding window that keeps the first tokens in sight (sinks): the new
+ * token at place p = seq_len[r] - n_r + i of its request sees the cached tokens u <= p with u > p -
+ * window or u < n_sinks, a window of its own and `window` - 1 tokens before it. Work and bytes go
+ * by what is seen. */
 typedef struct {
   int32_t window;    /* >= 1; one as long as the table's pages leaves nothing out */
   int32_t n_sinks;   /* >= 0                                                      */
@@ -601,32 +604,38 @@ AVTP_API avtp_status_t avtp_cache_window_attention_workspace_size(const avtp_cac
                                                                   const avtp_cache_attn_args_t* args,
                                                                   const avtp_cache_window_t* window, size_t* bytes);
 
-/* As avtp_cache_attention, with its results, errors and limits. Table entries of pages that no new token of their
- * request sees a row of are not read (avtp_cache_free gives those pages back). A value that is not finite may reach the
- * other tokens of its chunk only where one of these sees it (0 * inf). Tokens / (2 * (128 / G)) + n_requests blocks of rows, each of
- * (window + n_sinks) / 128 + 10 steps or so, times n_kv_heads, above 2^31 return AVTP_ERR_RANGE. Asynchronous on `stream`. */
+/* As avtp_cache_attention, with its results, errors and limits. Table entries of pages that no new
+ * token of their request sees a row of are not read (avtp_cache_free gives those pages back). A
+ * value that is not finite may reach the other tokens of its chunk only where one of these sees it
+ * (0 * inf). Tokens / (2 * (128 / G)) + n_requests blocks of rows, each of (window + n_sinks) / 128
+ * + 10 steps or so, times n_kv_heads, above 2^31 return AVTP_ERR_RANGE.
+ * Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_window_attention(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,
                                                    const avtp_cache_window_t* window, void* workspace,
                                                    size_t workspace_bytes, avtp_stream_t stream);
 
-/* Upkeep of the cache's pages: cached prompts pruned further, several requests on one prompt, pages given back.
+/* Upkeep of the cache's pages: cached prompts pruned further, several requests on one prompt, pages
+ * given back.
  *
- * Pages may have several holders. `shared` (device int32 [n_pages], zeros at first) is the number of a page's
- * holders beyond the first: avtp_cache_fork adds to it, avtp_cache_free takes from it, and a page that
- * avtp_cache_slots takes from the free list has one holder. Calls without `shared` treat every page as held once.
+ * Pages may have several holders. `shared` (device int32 [n_pages], zeros at first) is the number
+ * of a page's holders beyond the first: avtp_cache_fork adds to it, avtp_cache_free takes from it,
+ * and a page that avtp_cache_slots takes from the free list has one holder. Calls without `shared`
+ * treat every page as held once.
  *
- * Requests may let go of pages that a sliding window has left (see avtp_cache_window_attention): with `window` > 0 a
- * request that was `held_len` tokens long at its last such call holds the pages of its first n_sinks tokens, and
- * of those from held_len - window + 1 on, the first that the window of its next token needs. held_len (device
- * [R], zeros at first) goes with the lengths: avtp_cache_free writes it, avtp_cache_fork copies it. Table entries of
- * pages let go of stay as they were and are not read. window 0: every request holds all its pages. */
+ * Requests may let go of pages that a sliding window has left (see avtp_cache_window_attention):
+ * with `window` > 0 a request that was `held_len` tokens long at its last such call holds the pages
+ * of its first n_sinks tokens, and of those from held_len - window + 1 on, the first that the
+ * window of its next token needs. held_len (device [R], zeros at first) goes with the lengths:
+ * avtp_cache_free writes it, avtp_cache_fork copies it. Table entries of pages let go of stay as
+ * they were and are not read. window 0: every request holds all its pages. */
 
-/* The kept tokens of cached requests moved together, in one layer's cache: for j < n_r = keep_cu[r+1] -
- * keep_cu[r], the rows of token keep_idx[keep_cu[r] + j] - base of request r go to the place of its token j, in
- * the pages of dst_table, or without one in its own (then base + j <= keep_idx: a prune of the cache in place). base
- * is 0, or base_cu[r]: with avtp_prune's kept_idx, out_cu_seqlens and the batch's cu_seqlens the positions are used
- * where they were made. Whoever holds one table for several layers calls this for each, then, in place,
- * avtp_cache_free once with len_out. */
+/* The kept tokens of cached requests moved together, in one layer's cache: for j < n_r =
+ * keep_cu[r+1] - keep_cu[r], the rows of token keep_idx[keep_cu[r] + j] - base of request r go to
+ * the place of its token j, in the pages of dst_table, or without one in its own (then base + j <=
+ * keep_idx, ascending: a prune of the cache in place; to other pages they may come in any order,
+ * and twice). base is 0, or base_cu[r]: with avtp_prune's kept_idx, out_cu_seqlens and the batch's
+ * cu_seqlens the positions are used where they were made. Whoever holds one table for several
+ * layers calls this for each, then, in place, avtp_cache_free once with len_out. */
 typedef struct {
   int32_t n_requests;          /* R >= 1, at most 2^31 - 1025                                        */
   int64_t n_kept;              /* length of keep_idx, >= keep_cu[R] (host); < 2^31                   */
@@ -647,25 +656,28 @@ typedef struct {
   int32_t* len_out;            /* device [R] or NULL: n_r, written; not seq_len                      */
 } avtp_cache_compact_args_t;
 
-/* Offsets that decrease or pass n_kept are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. Recorded too:
- * - with dst_table, a position outside its request's tokens or on a page let go of, or a page outside [0, n_pages) or the
- *   table: that token is not moved;
- * - in place, the same, positions that do not ascend, or a row to be moved to a page let go of or with shared > 0 (others
- *   hold it): that request is left as it was.
+/* Offsets that decrease or pass n_kept are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is
+ * written. Recorded too:
+ * - with dst_table, a position outside its request's tokens or on a page let go of, or a page
+ *   outside [0, n_pages) or the table: that token is not moved;
+ * - in place, the same, positions that do not ascend, or a row to be moved to a page let go of or
+ *   with shared > 0 (others hold it): that request is left as it was.
  * workspace: 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,
                                           size_t workspace_bytes, avtp_stream_t stream);
 
-/* Whole pages of one layer's cache: for i < n with src[i] >= 0 and dst[i] >= 0, page src[i] to page dst[i] (a page that no
- * other pair names). A page outside [-1, n_pages) is skipped and recorded as AVTP_ERR_DEVICE_INPUT. workspace: 256-byte
- * aligned, at least 16 bytes. Asynchronous on `stream`. */
+/* Whole pages of one layer's cache: for i < n with src[i] >= 0 and dst[i] >= 0, page src[i] to page
+ * dst[i] (a page that no other pair names). A page outside [-1, n_pages) is skipped and recorded as
+ * AVTP_ERR_DEVICE_INPUT. workspace: 256-byte aligned, at least 16 bytes.
+ * Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_copy(const avtp_cache_t* cache, const int32_t* src, const int32_t* dst, int64_t n,
                                        void* workspace, size_t workspace_bytes, avtp_stream_t stream);
 
-/* Requests that go on from others' cached tokens: child i, row child[i] of the table, becomes the first
- * fork_len[i] tokens of row parent[i]. Their full pages get a holder more; a last one that is not full is copied, since
- * both will write to it: the child's table gets a page of the free list (from entry *free_head on, child by child),
- * and copy_src / copy_dst name the two for avtp_cache_copy, once a layer (-1 where nothing is to be copied). */
+/* Requests that go on from others' cached tokens: child i, row child[i] of the table, becomes the
+ * first fork_len[i] tokens of row parent[i]. Their full pages get a holder more; a last one that is
+ * not full is copied, since both will write to it: the child's table gets a page of the free list
+ * (from entry *free_head on, child by child), and copy_src / copy_dst name the two for
+ * avtp_cache_copy, once a layer (-1 where nothing is to be copied). */
 typedef struct {
   int32_t n_requests;          /* R >= 1: rows of the table; at most 2^31 - 1025                    */
   int32_t n_children;          /* >= 0, at most 2^31 - 1025                                         */
@@ -692,17 +704,19 @@ typedef struct {
 
 AVTP_API avtp_status_t avtp_cache_fork_workspace_size(const avtp_cache_fork_args_t* args, size_t* bytes);
 
-/* A row outside the table, a child given twice or that is a parent, a length that is negative, longer than the parent or
- * max_pages pages or, with a window, so short that it needs a page let go of, a page outside [0, n_pages), or a free list that runs out are
- * recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
+/* A row outside the table, a child given twice or that is a parent, a length that is negative,
+ * longer than the parent or max_pages pages or, with a window, so short that it needs a page let go
+ * of, a page outside [0, n_pages), or a free list that runs out are recorded as
+ * AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_fork(const avtp_cache_fork_args_t* args, void* workspace, size_t workspace_bytes,
                                        avtp_stream_t stream);
 
-/* Pages back to the free list: request r goes from seq_len[r] to new_len[r] tokens (0: it is done; fewer: drafted
- * tokens taken back, or a cache compacted in place; the same: only what the window has left) and lets go of the pages that
- * it needs no more. Those whose last holder lets go are put before entry *free_head of the free list, in the table's
- * order (row by row, a row's entries ascending; a page that several rows of the call let go of at the last of
- * them): results do not change from run to run. */
+/* Pages back to the free list: request r goes from seq_len[r] to new_len[r] tokens (0: it is done;
+ * fewer: drafted tokens taken back, or a cache compacted in place; the same: only what the window
+ * has left) and lets go of the pages that it needs no more. Those whose last holder lets go are put
+ * before entry *free_head of the free list, in the table's order (row by row, a row's entries
+ * ascending; a page that several rows of the call let go of at the last of them): results do not
+ * change from run to run. */
 typedef struct {
   int32_t n_requests;          /* R >= 1, at most 2^31 - 1025                                       */
   int32_t page_size;
@@ -726,10 +740,11 @@ typedef struct {
 
 AVTP_API avtp_status_t avtp_cache_free_workspace_size(const avtp_cache_free_args_t* args, size_t* bytes);
 
-/* Lengths out of range (as above; a held_len beyond seq_len), a page outside [0, n_pages), one that more rows let go of than hold
- * it, a new_len inside a page with shared > 0 (the request's next tokens would be written over the others'; whoever
- * wants that forks the request first), or a free list with too few entries before *free_head are recorded as
- * AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
+/* Lengths out of range (as above; a held_len beyond seq_len), a page outside [0, n_pages), one that
+ * more rows let go of than hold it, a new_len inside a page with shared > 0 (the request's next
+ * tokens would be written over the others'; whoever wants that forks the request first), or a free
+ * list with too few entries before *free_head are recorded as AVTP_ERR_DEVICE_INPUT, and then
+ * nothing is written. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_free(const avtp_cache_free_args_t* args, void* workspace, size_t workspace_bytes,
                                        avtp_stream_t stream);
 

@@ -17,8 +17,8 @@ struct SlotsWs {
 cudaError_t launch_cache_slots(const avtp_cache_slots_args_t& a, void* ws, const SlotsWs& p, cudaStream_t s);
 
 // ---------------------------------------------------------------- write
-// Clears a status word. The kernel behind it starts beside it, behind everything ahead of both, and waits for it (pdl_wait)
-// before it records.
+// Clears a status word. The kernel behind it starts beside it, behind everything ahead of both, and waits for it
+// (pdl_wait) before it records.
 cudaError_t launch_cache_status(DevStatus* st, cudaStream_t s);
 cudaError_t launch_cache_write(const avtp_cache_t& c, const avtp_cache_write_args_t& a, void* ws, cudaStream_t s);
 

@@ -306,7 +306,8 @@ avtp_status_t avtp_cache_attention(const avtp_cache_t* cache, const avtp_cache_a
   if (st != AVTP_OK) return st;
   const CacheAttnWs p = plan_cache_attention(*cache, *args);
   if ((st = check_ws(workspace, workspace_bytes, p.total)) != AVTP_OK) return st;
-  return from_cuda(launch_cache_attention(*cache, *args, avtp_cache_window_t{0, 0}, workspace, p, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_cache_attention(*cache, *args, avtp_cache_window_t{0, 0}, workspace, p,
+                                          reinterpret_cast<cudaStream_t>(stream)));
 }
 
 avtp_status_t avtp_cache_window_attention_workspace_size(const avtp_cache_t* cache, const avtp_cache_attn_args_t* args,

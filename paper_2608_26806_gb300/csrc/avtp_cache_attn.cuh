@@ -55,8 +55,8 @@ struct CacheRequest {
 
 // In a window, the first key behind the sinks that a token at place p sees (p negative: it sees nothing).
 __device__ __forceinline__ int cache_low(const CacheAttnDev& a, int p) { return p < a.window ? 0 : p - a.window + 1; }
-// The tiles between the sinks' and the first that a row block sees are left out: of those behind the sinks', tile j is
-// the request's tile j + skip.
+// The tiles between the sinks' and the first that a row block sees are left out: of those behind the sinks', tile j
+// is the request's tile j + skip.
 struct CacheSkip {
   int32_t sinks, skip;  // tiles
   // `first`: place of the row block's first new token
@@ -193,6 +193,7 @@ struct CacheLine {
   int most;   // steps of the longest row block (a row block's steps are one after the other on the line)
   int incl;   // up to kNearRequests requests: steps up to this lane's, its own included
   int2 weights;
+  bool fine;  // up to kNearRequests requests: validation refuses none
 
   CacheLine() = default;
   template <int NT, class F>
@@ -209,7 +210,8 @@ struct CacheLine {
       incl = lane < a.R && mine_ok ? steps(mine, longest) : 0;
       incl = a.R > 1 ? cache_scan(incl) : __shfl_sync(0xffffffffu, incl, 0);
       most = __reduce_max_sync(0xffffffffu, longest);
-      total = __all_sync(0xffffffffu, mine_ok || lane >= a.R) ? __shfl_sync(0xffffffffu, incl, 31) : 0;
+      fine = __all_sync(0xffffffffu, mine_ok || lane >= a.R);
+      total = fine ? __shfl_sync(0xffffffffu, incl, 31) : 0;
       weights = make_int2(0, 0);
       if (a.both) {
         const int2 w = lane < a.R && mine_ok ? cache_weights<kWindow>(a, mine) : make_int2(0, 0);
@@ -277,9 +279,9 @@ __device__ __forceinline__ int piece_place(int run, bool begins) { return 2 * ru
 // lane a box, and one thread issues their copies. Box i holds keys i * box ..
 struct CacheBoxes {
   int2 at[32];  // page, row of the page
-  // Boxes i0 .. i0 + 31 (i0 a multiple of 32) of a request of `seq` tokens; true if a page lies outside
-  // the pool: page 0 then stands in its place. In a window no page is looked up for boxes behind the sinks that end at
-  // or before key `low`, for it may have been let go of: their copies read behind the pool, and bring zeros.
+  // Boxes i0 .. i0 + 31 (i0 a multiple of 32) of a request of `seq` tokens; true if a page lies outside the pool:
+  // page 0 then stands in its place. In a window no page is looked up for boxes behind the sinks that end at or
+  // before key `low`, for it may have been let go of: their copies read behind the pool, and bring zeros.
   template <bool kWindow>
   __device__ __forceinline__ bool load(const CacheAttnDev& a, const int32_t* row, int seq, int i0, int low = 0) {
     const int lane = threadIdx.x & 31;

@@ -36,10 +36,10 @@
 // wait gives up records AVTP_ERR_TIMEOUT and leaves. Keys behind a request's last are masked by selection and
 // their values cleared in registers, so nothing there (an infinity, a NaN) reaches a row.
 //
-// In a window (kWindow, see avtp.h) a row block's tiles are those of the sinks and those from its first token's window
-// on; the line of tiles is as long as what is seen. Values that none of its rows sees are cleared like those behind the last
-// key. 256 requests of 200-8000 tokens, eight KV heads, in windows of 1024 and 4096 184 and 497 us, 5.9 and 6.3 TB/s; eight of 30-65
-// thousand in 4096 31 us, 4.4 TB/s, in which the figures of one request above weigh.
+// In a window (kWindow, see avtp.h) a row block's tiles are those of the sinks and those from its first token's
+// window on; the line of tiles is as long as what is seen. Values that none of its rows sees are cleared like those
+// behind the last key. 256 requests of 200-8000 tokens, eight KV heads, in windows of 1024 and 4096 184 and 497 us,
+// 5.9 and 6.3 TB/s; eight of 30-65 thousand in 4096 31 us, 4.4 TB/s, in which the figures of one request above weigh.
 #include <cudaTypedefs.h>
 
 #include <type_traits>
@@ -77,10 +77,10 @@ struct Segment {
 __host__ __device__ constexpr int tile_keys(int d) { return d == 128 ? 64 : 128; }
 __host__ __device__ constexpr uint32_t stage_bytes(int d) { return 2u * tile_keys(d) * d * 2; }
 constexpr int kStages = 5;
-// In a window, whose row blocks are short, one that a cut falls into costs more (a piece through L2, its count, the join:
-// about eight tiles' time) than a longer run, if that is not much longer. 61 requests of 200-8000 tokens, four KV heads, window
-// 128: 15.0 us, 17.3 without; 16 of 700-4000, five tokens of eight heads, window 512 16.2 and 20.4, 2048 36.6 and 36.7 (a
-// slack of eight tiles: 45.4); 24 of 4000 in 256 14.8 either way (15.6).
+// In a window, whose row blocks are short, one that a cut falls into costs more (a piece through L2, its count, the
+// join: about eight tiles' time) than a longer run, if that is not much longer. 61 requests of 200-8000 tokens, four
+// KV heads, window 128: 15.0 us, 17.3 without; 16 of 700-4000, five tokens of eight heads, window 512 16.2 and 20.4,
+// 2048 36.6 and 36.7 (a slack of eight tiles: 45.4); 24 of 4000 in 256 14.8 either way (15.6).
 constexpr int kWholeSlack = 4;
 // A warp's O on its way to the others: 16 rows of d floats, 8 floats of padding so that the eight
 // rows of an accumulator's column pair fall into different banks.
@@ -97,6 +97,7 @@ struct Shared {
   CacheBoxes boxes[2];  // of the keys' warp, of the values'
   float m[kWarps][16], l[kWarps][16], w[kWarps][16];  // reference, sum of P, of its rounded values
   int32_t last;
+  int refused;  // in a window: validation refuses a length
   int abort, bad_page;
 };
 constexpr size_t kMostShared = 227 * 1024;  // of a CTA
@@ -188,16 +189,35 @@ __device__ __forceinline__ void store_row(const CacheAttnDev& a, const Segment& 
 }
 
 // ---------------------------------------------------------------- attention
-// Tiles of a row block: one for an empty cache, whose rows are zeros; none for requests without new
-// tokens, or with more rows than this kernel takes.
+// Tiles of a row block: one for an empty cache, whose rows are zeros (none in a window); none for requests without
+// new tokens, or with more rows than this kernel takes.
 template <int D, bool kWindow>
 __device__ __forceinline__ int tiles_of(const CacheAttnDev& a, const CacheRequest& q) {
+  if (kWindow && q.seq == 0) return 0;  // see write_empty
   const int all = max(1, (q.seq - 1) / tile_keys(D) + 1);
   return q.n == 0 || q.rows(a) > a.few_rows ? 0 : all - (kWindow ? CacheSkip(a, q.seq - q.n, tile_keys(D)).skip : 0);
 }
 
 __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
   return (tiles + (1 << a.step_shift) - 1) >> a.step_shift;
+}
+
+// In a window, the rows of every gridDim-th request that has no cached tokens, by the computing warps: a captured batch's
+// padding. (As a tile and a segment a KV head of each on the line, three such requests of four KV heads behind 61 of
+// 200-8000 tokens in a window of 1024 took 9 us of 42, all in the last run.)
+template <int D>
+__device__ __noinline__ void write_empty(const CacheAttnDev& a) {
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    CacheRequest q;
+    if (!q.load(a, r) || q.seq > 0 || q.rows(a) > a.few_rows) continue;
+    const int heads = a.Hkv * a.G;
+    for (int i = threadIdx.x; i < q.n * heads * (D / 8); i += kConsumers) {
+      const int row = i / (D / 8), tok = row / heads, head = row - tok * heads, piece = i % (D / 8);
+      const int64_t t = static_cast<int64_t>(q.row0) + tok;
+      reinterpret_cast<uint4*>(a.o + t * a.o_stride + static_cast<int64_t>(head) * D)[piece] = make_uint4(0u, 0u, 0u, 0u);
+      if (piece == 0 && a.lse != nullptr) a.lse[head * a.lse_stride + t] = -INFINITY;
+    }
+  }
 }
 
 // A wait looks at one bit of a barrier's phase, so a warp may be at most one phase behind what it waits for.
@@ -265,8 +285,9 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       runs = CacheRuns(line.total, line.most, 1, cache_ctas(a, line.weights, true));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
-      // In a window a row block goes whole to the run that most of it lies in where that makes the longest run, of blocks of
-      // equal length, kWholeSlack steps longer at most.
+      if (kWindow && lane == 0) sh.refused = a.R > kNearRequests ? !sh.plan.ok : !line.fine;
+      // In a window a row block goes whole to the run that most of it lies in where that makes the longest run, of
+      // blocks of equal length, kWholeSlack steps longer at most.
       if (kWindow && (runs.each + line.most - 1) / line.most * line.most <= runs.each + kWholeSlack) {
         auto whole = [&](int x) {
           if (x >= line.total) return line.total;
@@ -784,6 +805,7 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
   }
   pdl_wait();  // this grid's end implies the validation kernel's, which resets the status word
   __syncthreads();
+  if (kWindow && warp < kWarps && !sh.refused && !sh.abort) write_empty<D>(a);
   if (tid == 0) {
     if (sh.abort) record_error(a.st, AVTP_ERR_TIMEOUT, static_cast<int32_t>(blockIdx.x));
     if (sh.bad_page >= 0) record_error(a.st, AVTP_ERR_DEVICE_INPUT, sh.bad_page);
@@ -863,8 +885,8 @@ int64_t most_keys(const avtp_cache_t& c, const avtp_cache_attn_args_t& a) {
 bool windowed(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w) {
   return w.window > 0 && w.window < most_keys(c, a);
 }
-// Steps of k_cache_chunk's line, at most, in a window: its sums of units' blocks in closed form want steps of one block,
-// so that this has to stay below 2^31.
+// Steps of k_cache_chunk's line, at most, in a window: its sums of units' blocks in closed form want steps of one
+// block, so that this has to stay below 2^31.
 double chunk_steps(const avtp_cache_t& c, const avtp_cache_attn_args_t& a, const avtp_cache_window_t& w) {
   const int G = a.n_q_heads / c.n_kv_heads;
   if (static_cast<int64_t>(a.max_new) * G <= kCacheFewRows) return 0.0;

@@ -47,11 +47,11 @@
 //
 // In a window (kWindow, see avtp.h) a unit's blocks are those of the sinks and those from its first token's window on
 // (Segment::block gives a block's place among the request's); its last blocks are masked above and its first ones
-// below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that no row
-// of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in windows of 2048, 512 and 128 tokens:
-// 225, 122 and 73 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50 by the figures above: first blocks and last
-// ones are masked, and a unit's ends weigh more. (Masks by comparison, every half looked at, values cleared by the softmax
-// warps: 279, 157 and 103.)
+// below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that
+// no row of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in windows of 2048, 512
+// and 128 tokens: 225, 122 and 73 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50 by the figures
+// above: first blocks and last ones are masked, and a unit's ends weigh more. (Masks by comparison, every half looked
+// at, values cleared by the softmax warps: 279, 157 and 103.)
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
@@ -72,11 +72,11 @@ constexpr int kValueWarp = kMmaWarp + 1;
 constexpr int kThreads = 32 * (kValueWarp + 1);
 static_assert(kSlotWarps * 32 == kQT, "a thread a row of a slot");
 constexpr int kStages = 4;      // key or value blocks in shared memory
-// A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first
-// softmax with nothing to overlap, its rows' way out): its steps on the line are its blocks and these.
-// (With three, 9856 tokens 488 us instead of 494, 512 behind 9300 63.6 instead of 62.8.)
-// In a window, whose first blocks are masked too, four (8192 tokens behind 2176, 32 query heads, 8 KV heads, window 512: 118.8 us
-// and 125.8 with two, 117.0 with six; 2048: 233.8, 240.5, 235.5).
+// A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first softmax with
+// nothing to overlap, its rows' way out): its steps on the line are its blocks and these. (With three, 9856 tokens
+// 488 us instead of 494, 512 behind 9300 63.6 instead of 62.8.) In a window, whose first blocks are masked too, four
+// (8192 tokens behind 2176, 32 query heads, 8 KV heads, window 512: 118.8 us and 125.8 with two, 117.0 with six;
+// 2048: 233.8, 240.5, 235.5).
 template <bool kWindow>
 constexpr int kUnitSteps = kWindow ? 4 : 2;
 constexpr uint32_t kTmemCols = 512;
@@ -207,12 +207,12 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int blocks) {
   return kUnitSteps<kWindow> + ((blocks + (1 << a.step_shift) - 1) >> a.step_shift);
 }
 
-// Steps of the first u units of a request's head, the last of all not among them, in closed form: unit i's
-// last token sees x = past + rows (i + 1) keys, for which it has kUnitSteps<kWindow> + max(1, ceil(x / (128 * 2^step_shift))) of them. For
-// requests of more than kNearUnits units: 128 of them, added up one by one and passed one by one, took up to
-// 24000 cycles before a CTA's first product and take 9000 so; eight of them 2500 and 5300.
-// In a window (step_shift 0) less the blocks that it leaves out: floor((past + rows i - window + 1) / 128) less the
-// sinks' of unit i, where that is positive.
+// Steps of the first u units of a request's head, the last of all not among them, in closed form: unit i's last token
+// sees x = past + rows (i + 1) keys, for which it has kUnitSteps<kWindow> + max(1, ceil(x / (128 * 2^step_shift))) of
+// them. For requests of more than kNearUnits units: 128 of them, added up one by one and passed one by one, took up
+// to 24000 cycles before a CTA's first product and take 9000 so; eight of them 2500 and 5300. In a window (step_shift
+// 0) less the blocks that it leaves out: floor((past + rows i - window + 1) / 128) less the sinks' of unit i, where
+// that is positive.
 constexpr int kNearUnits = 32;
 template <bool kWindow>
 static __device__ __noinline__ int steps_before(const CacheAttnDev& a, int past, int rows, int u) {
@@ -461,9 +461,9 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         }
         __syncwarp();
         if constexpr (kWindow) {
-          // Values behind the sinks and before the unit's first window, which no row of it sees: cleared, so that P = 0 meets
-          // no infinity, before the others may use the stage. (A segment's first two blocks, which may both be such,
-          // land beside each other.)
+          // Values behind the sinks and before the unit's first window, which no row of it sees: cleared, so that P =
+          // 0 meets no infinity, before the others may use the stage. (A segment's first two blocks, which may both
+          // be such, land beside each other.)
           if (edge) pending |= 1u << (j & 1);
           if (pending != 0 && (j > 0 || blocks == 1)) {
 #pragma unroll 1

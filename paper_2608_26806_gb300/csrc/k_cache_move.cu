@@ -3,21 +3,21 @@
 //   row(dst_table[r], j) = row(block_table[r], keep_idx[keep_cu[r] + j] - base_r),  row(t, p) = page t[p / P], row p % P
 //
 // Copies: 4 * Hkv * d bytes read and written a token bound them. Between different pages every row goes by itself: a
-// warp finds the slots of as many tokens as leave all warps in one wave, a lane each, and then moves them row by row, 16
-// bytes a lane. 64 requests of 1000 kept tokens, 8 KV heads, d = 128: 90 us, 5.8 TB/s; four of 2900 20.5 us, 4.6 TB/s, of
-// which the way to the first row (offsets, position, two tables) and the launch take 4.
+// warp finds the slots of as many tokens as leave all warps in one wave, a lane each, and then moves them row by row,
+// 16 bytes a lane. 64 requests of 1000 kept tokens, 8 KV heads, d = 128: 90 us, 5.8 TB/s; four of 2900 20.5 us, 4.6
+// TB/s, of which the way to the first row (offsets, position, two tables) and the launch take 4.
 //
-// In place a row's destination may be another's source. Kept positions ascend and j <= keep_j - base, so that in their
-// order a row is read before anything is written over it: what is written for tokens [a, b) lies before b, what is
-// read for tokens from b on lies at b or behind. So a CTA takes columns of the request's rows (slices of a head's keys or
-// values) through all its tokens, a tile at a time, with a barrier between a tile's reads and its writes, and the
-// next tiles' copies under way; columns are independent, and no CTA waits for another. 64 requests of 1000 of 3000 tokens
-// 133 us, 3.95 TB/s; one of 3000 of 9000 22 us, where twelve tiles one behind the other take 11 and the look at the
-// positions 6 (to other pages 6.2).
+// In place a row's destination may be another's source. Kept positions ascend and j <= keep_j - base, so that in
+// their order a row is read before anything is written over it: what is written for tokens [a, b) lies before b, what
+// is read for tokens from b on lies at b or behind. So a CTA takes columns of the request's rows (slices of a head's
+// keys or values) through all its tokens, a tile at a time, with a barrier between a tile's reads and its writes, and
+// the next tiles' copies under way; columns are independent, and no CTA waits for another. 64 requests of 1000 of
+// 3000 tokens 133 us, 3.95 TB/s; one of 3000 of 9000 22 us, where twelve tiles one behind the other take 11 and the
+// look at the positions 6 (to other pages 6.2).
 //
-// What is wrong is recorded where it is met, in a status word that a kernel beside this one clears. (A CTA that looked
-// through all kept tokens instead took longer than the copies: 50 us for 11600 of them.) A request moved in place is checked
-// as a whole by each of its CTAs before they move anything.
+// What is wrong is recorded where it is met, in a status word that a kernel beside this one clears. (A CTA that
+// looked through all kept tokens instead took longer than the copies: 50 us for 11600 of them.) A request moved in
+// place is checked as a whole by each of its CTAs before they move anything.
 #include "avtp_cache.cuh"
 
 namespace avtp {
@@ -138,8 +138,9 @@ __device__ __forceinline__ Move move_of(const CompactDev& d, int r, int64_t i, i
   if (m.bad) m.from = m.to = -1;
   return m;
 }
-// Kept tokens j0 + thread, + kThreads, ... below j1 of a request in place, four at a time: f(j, where from, where to), slots, to
-// -1 of one that stays. True if one is wrong: its position or its order, its pages, or a page that others hold.
+// Kept tokens j0 + thread, + kThreads, ... below j1 of a request in place, four at a time: f(j, where from, where
+// to), slots, to -1 of one that stays. True if one is wrong: its position or its order, its pages, or a page that
+// others hold.
 template <class F>
 __device__ bool look_in_place(const CompactDev& d, int r, int64_t first, int64_t j0, int64_t j1, F f) {
   constexpr int N = 4;
@@ -305,8 +306,8 @@ __global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_plac
           __syncthreads();
         }
         const int rows = static_cast<int>(min(n - j0, static_cast<int64_t>(kChunk)));
-        // Tiles, column by column. Copies run kTiles tiles ahead of the stores: a column's later rows lie behind all that
-        // its earlier ones are written over, and columns do not meet.
+        // Tiles, column by column. Copies run kTiles tiles ahead of the stores: a column's later rows lie behind all
+        // that its earlier ones are written over, and columns do not meet.
         const int tiles = (rows + at_once * kRows - 1) / (at_once * kRows), all = tiles * (c1 - c0);
         struct Place {
           __nv_bfloat16* base;

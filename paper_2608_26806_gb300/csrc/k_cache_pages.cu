@@ -8,17 +8,18 @@
 // requests, then a binary search an entry.
 //
 // What bounds it: latency, a chain of dependent loads a round. A call is one cluster of up to kMostCtas CTAs, each of
-// which forms the sums for itself, so that barriers part the rounds and nothing else does; a thread's first kKept pages
-// stay in its registers from round to round. Everything is checked before the first write. Calls one behind the other:
-// 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 5.7 us; the pages that 64
-// windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.9; eight children
-// of a prompt of 146 pages 7.2; 171 children of 64 (21000 entries) 10.6. (With eight CTAs 6.8, 19.9, 8.5 and 13.1; with entries looked
-// up again in every round, and the others' findings read from their shared memory, 11.7, 36.7, 11.2 and 18.8.)
+// which forms the sums for itself, so that barriers part the rounds and nothing else does; a thread's first kKept
+// pages stay in its registers from round to round. Everything is checked before the first write. Calls one behind the
+// other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 5.7 us; the pages that
+// 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.9; eight
+// children of a prompt of 146 pages 7.2; 171 children of 64 (21000 entries) 10.6. (With eight CTAs 6.8, 19.9, 8.5 and
+// 13.1; with entries looked up again in every round, and the others' findings read from their shared memory, 11.7,
+// 36.7, 11.2 and 18.8.)
 //
 // A page of several holders that rows of a call let go of: every entry counts itself (rel) and the last one in order
-// (last: a maximum) stands for the page, so that neither the counts nor the list's order depend on who came first. Both
-// arrays are cleared where the call's entries point, not as a whole. A page of one holder has one entry, which finds itself
-// in last.
+// (last: a maximum) stands for the page, so that neither the counts nor the list's order depend on who came first.
+// Both arrays are cleared where the call's entries point, not as a whole. A page of one holder has one entry, which
+// finds itself in last.
 #include <cooperative_groups.h>
 
 #include "avtp_cache.cuh"
@@ -74,8 +75,8 @@ struct Pages : CachePages {
   }
 };
 
-// What a CTA's checks found, and its pages for the list, for the others of the cluster: every CTA puts its note into all
-// the others' shared memory ahead of the barrier. (Reading theirs behind it took 4 us of 18 for sixteen.)
+// What a CTA's checks found, and its pages for the list, for the others of the cluster: every CTA puts its note into
+// all the others' shared memory ahead of the barrier. (Reading theirs behind it took 4 us of 18 for sixteen.)
 struct Note {
   int err, detail;
   int64_t gives;
@@ -133,8 +134,8 @@ __device__ void block_scan(int64_t (&x)[N], int64_t (&s_warp)[N][kThreads / 32],
 
 __device__ __forceinline__ int32_t clamped(int64_t x) { return static_cast<int32_t>(x < 0x7fffffff ? x : 0x7fffffff); }
 
-// Calls f(entry, its page, which of the thread's) for entries begin, begin + step, ... < end, with the first kKept pages
-// from registers.
+// Calls f(entry, its page, which of the thread's) for entries begin, begin + step, ... < end, with the first kKept
+// pages from registers.
 template <class P, class F>
 __device__ __forceinline__ void each_entry(int64_t begin, int64_t end, int64_t step, const int32_t (&kept)[kKept], P page_of,
                                            F f) {

@@ -4,25 +4,27 @@
 //   z_a = f (y_a cos t - y_b sin t),  z_b = f (y_b cos t + y_a sin t),  t = pos[plane_i] inv_freq_i
 // for the pairs (a, b) = (i, i + rot/2) or (2i, 2i + 1) of a head's first rot elements; the others are y.
 //
-// What bounds it: bytes. Each q, k and v row is read and written once, and a head's norm and rotation are between.
-// A head is D/16 lanes of 16 elements each, held as two pieces of V elements (or twice two of four) that turn into one
-// another: piece u and piece u + rot/(2V) of the half style, two neighbours of the interleaved one, so that neither style
-// moves elements between lanes and a call may write over its inputs. The norm's sum is three (D = 128) or two shuffles.
+// What bounds it: bytes. Each q, k and v row is read and written once, and a head's norm and rotation are between. A
+// head is D/16 lanes of 16 elements each, held as two pieces of V elements (or twice two of four) that turn into one
+// another: piece u and piece u + rot/(2V) of the half style, two neighbours of the interleaved one, so that neither
+// style moves elements between lanes and a call may write over its inputs. The norm's sum is three (D = 128) or two
+// shuffles.
 //
-// Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of a turn, so that pos
-// times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction (2^-61 of inv_freq, 2^-64 of a turn),
-// times pos. The top 32 bits go to sincospif. A lane forms one or two of the token's cosines and sines for its warp,
-// which shuffles hand round; with the norm's weights they become 16 pairs of factors a lane, so that a word of two
-// elements takes two packed products.
+// Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of a turn,
+// so that pos times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction (2^-61
+// of inv_freq, 2^-64 of a turn), times pos. The top 32 bits go to sincospif. A lane forms one or two of the token's
+// cosines and sines for its warp, which shuffles hand round; with the norm's weights they become 16 pairs of factors
+// a lane, so that a word of two elements takes two packed products.
 //
-// A warp takes tokens and, where there are few of these, a share of their heads. Its rows come by asynchronous copies into
-// shared memory that run four groups of heads ahead of the work, on into the next token's; what a lane copies it reads itself, so
-// that nothing waits but the lane. (Rows loaded into registers, two groups at a time: 48 us for 9856 tokens, now 42-44;
-// the first form, a warp's 150 registers holding three groups and the weights read for each head, 127.)
+// A warp takes tokens and, where there are few of these, a share of their heads. Its rows come by asynchronous copies
+// into shared memory that run four groups of heads ahead of the work, on into the next token's; what a lane copies it
+// reads itself, so that nothing waits but the lane. (Rows loaded into registers, two groups at a time: 48 us for 9856
+// tokens, now 42-44; the first form, a warp's 150 registers holding three groups and the weights read for each head,
+// 127.)
 //
-// Measured, calls one behind the other with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128: 64
-// tokens 3.9 us (3.5 in a graph), 1024 7.9, 9856 42.4, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go by
-// 64 bytes: 9856 25.5, 4.8 TB/s.
+// Measured, calls one behind the other with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128:
+// 64 tokens 3.9 us (3.5 in a graph), 1024 7.9, 9856 42.4, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go
+// by 64 bytes: 9856 25.5, 4.8 TB/s.
 #include <type_traits>
 
 #include "avtp_cache.cuh"
@@ -44,8 +46,9 @@ struct RopeDev {
   DevStatus* st;
 };
 
-// inv_freq / 2 pi modulo 1 as a fraction of 2^64, by integers (in 64-bit floating point, scarce on this part, a prompt of
-// 9856 tokens took 0.7 us more and a step of 64 0.2): inv_freq = m 2^-s with a 24-bit m, and m times 2^64 / 2 pi, shifted.
+// inv_freq / 2 pi modulo 1 as a fraction of 2^64, by integers (in 64-bit floating point, scarce on this part, a
+// prompt of 9856 tokens took 0.7 us more and a step of 64 0.2): inv_freq = m 2^-s with a 24-bit m, and m times 2^64 /
+// 2 pi, shifted.
 __device__ __forceinline__ uint64_t turn_fraction(float inv_freq) {
   constexpr uint64_t kTurn = 0x28be60db9391054aull;  // 2^64 / 2 pi
   const uint32_t b = __float_as_uint(inv_freq), e = (b >> 23) & 0xffu;
@@ -146,8 +149,8 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
   auto turned = [&](int i, int h) { return turns[kUnits == 2 ? i : (kApart ? 0 : h)]; };
 
   // Tokens t, t + step, ... with a share (slice) of their groups of heads, its queries', keys' and values' in this
-  // order: n of them, each of heads (slice + j slices) kHeads ... Copies run kAhead groups ahead of the work, through a token's
-  // rows of every kind and on into the next token's.
+  // order: n of them, each of heads (slice + j slices) kHeads ... Copies run kAhead groups ahead of the work, through
+  // a token's rows of every kind and on into the next token's.
   int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
   const int64_t step = static_cast<int64_t>(gridDim.x - 1) * kWarps;
   const int slice = blockIdx.y, slices = gridDim.y;
@@ -273,7 +276,8 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
         for (int j = 0; j < count; ++j) pass((slice + j * slices) * kHeads + group, heads, keep, store);
         return;
       }
-      // what the two elements of a lane's word i (of eight) become: x * c[i] + partner * s[i], the norm's weights in both
+      // what the two elements of a lane's word i (of eight) become: x * c[i] + partner * s[i], the norm's weights in
+      // both
       float2 factor_c[8], factor_s[8];
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {

@@ -164,6 +164,28 @@ def test_tokens_that_see_nothing(window, sinks):
     run(Windowed([(3, 10), (0, 5), (100, 200), (1, 1), (260, 300)], 8, 2, 128, 16, window, sinks))
 
 
+@pytest.mark.parametrize("idle", [1, 3, 40])
+@pytest.mark.parametrize("live", [0, 1, 50])
+def test_idle_requests_of_a_padded_batch(live, idle):
+    """Requests without cached tokens: rows of zeros, beside others or alone; rows behind the last stay."""
+    b = Windowed([(300 + 11 * i, 1) for i in range(live)] + [(0, 1 + i % 2) for i in range(idle)], 8, 2, 64, 16, 100, 4,
+                 tail=2)
+    o = torch.full((b.T, 8, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((8, b.T), 4.0, device="cuda")
+    run(b, o=o, lse=lse)
+    assert (o[-2:] == 3.0).all() and (lse[:, -2:] == 4.0).all()
+
+
+@pytest.mark.parametrize("R", [5, 40])
+def test_a_refused_call_with_idle_requests_writes_nothing(R):
+    b = Windowed([(300, 1)] * (R - 2) + [(0, 1), (0, 1)], 8, 2, 64, 16, 100, 4)
+    b.dev["seq"][1] = -1
+    o = torch.full((b.T, 8, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    lse = torch.full((8, b.T), 4.0, device="cuda")
+    c = b.call(o=o, lse=lse).run()
+    assert status(c) == avtp.ERR_DEVICE_INPUT and (o == 3.0).all() and (lse == 4.0).all()
+
+
 def test_long_requests_in_pieces():
     run(Windowed([(30000, 1)], 8, 2, 128, 64, 20000, 1000))
     run(Windowed([(9000, 200)], 4, 1, 64, 64, 5000, 500))

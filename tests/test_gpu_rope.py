@@ -33,7 +33,8 @@ def plain(x, pos, inv_freq, style, plane, factor, norm):
       2 units in the last place, three products: below 2^-20;
     - sine and cosine: half a turn in 24 bits (2^-25 of a half turn, 2^-23.3 rad), two units of sincospif (2^-23), the
       factor's product and the rotation's three (2^-22): below 2^-20 together;
-    - the angle: the frequency's fraction of a turn, off by 2^-53 relative twice, and 2^-32 of a turn: pos f 2^-52 + 2^-29.
+    - the angle: 2^-61 pos (1 + f) for its fraction of a turn, 2^-32 of a turn for the bits that are left, and what
+      64 bits leave here, 2^-53 of it: below pos f 2^-52 + 2^-29.
     """
     d = x.shape[-1]
     y = x.double()
