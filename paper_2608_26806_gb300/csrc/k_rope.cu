@@ -13,8 +13,8 @@
 // Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of a turn,
 // so that pos times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction (2^-61
 // of inv_freq, 2^-64 of a turn), times pos. The top 32 bits go to sincospif. A lane forms one or two of the token's
-// cosines and sines for its warp, which shuffles hand round; with the norm's weights they become 16 pairs of factors
-// a lane, so that a word of two elements takes two packed products.
+// cosines and sines for its warp; with the norm's weights they become 16 pairs of factors a lane, so that a word of two
+// elements takes two packed products.
 //
 // A warp takes tokens and, where there are few of these, a share of their heads. Its rows come by asynchronous copies
 // into shared memory that run four groups of heads ahead of the work, on into the next token's; what a lane copies it
@@ -22,9 +22,8 @@
 // tokens, now 42-44; the first form, a warp's 150 registers holding three groups and the weights read for each head,
 // 127.)
 //
-// Measured, calls one behind the other with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128:
-// 64 tokens 3.9 us (3.5 in a graph), 1024 7.9, 9856 42.4, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go
-// by 64 bytes: 9856 25.5, 4.8 TB/s.
+// Measured, in a graph, with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128: 64 tokens 3.6 us,
+// 1024 8.1, 9856 42.5, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go by 64 bytes: 9856 25.5, 4.8 TB/s.
 #include <type_traits>
 
 #include "avtp_cache.cuh"
@@ -35,8 +34,8 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kAhead = 4;       // groups of heads whose rows a warp has under way, a KiB each
-constexpr int kCtasOfSm = 4;    // 128 registers a thread (six CTAs, 80 and spills: 49.6 us for 9856 tokens, five 45.9)
+constexpr int kAhead = 4;       // groups of heads whose rows a warp has under way, a KiB each (three 43.2 us, six 42.5)
+constexpr int kCtasOfSm = 4;    // up to 128 registers a thread (9856 tokens 42.5 us; five CTAs, 96 and spills 44.6, six 48.3)
 constexpr int kWarpsOfSm = 16;  // warps of an SM that a call's work is spread over, at least
 
 struct RopeDev {
@@ -121,6 +120,7 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
   static_assert(kApart || V == 8, "neighbours turn within pieces of eight");
   constexpr int kPieceBytes = 2 * V;
   // a lane's pieces of the groups under way: what a lane copies it reads itself
+  __shared__ __align__(16) float s_turn[kWarps][2][D / 2];  // the token's cosines and sines, pair by pair
   __shared__ __align__(16) unsigned char s_ahead[kWarps][kAhead][kUnits][2][32 * kPieceBytes];
   pdl_wait();
   pdl_trigger();
@@ -240,28 +240,19 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
 
 #pragma unroll 1
   for (; t < a.n_tokens; t += step) {
-    // the lane's eight pairs', two by two; 1 and 0 of pairs that do not turn
-    float2 cosines[4], sines[4];
-    {
-      float c[kMine], s[kMine];
+    __syncwarp();  // the token before has been set up
 #pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        const uint64_t phase = freq[i] * static_cast<uint64_t>(static_cast<int64_t>(pos[i]));
-        // half turns, -1 .. 1
-        sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s[i], &c[i]);
-        if (where[i] != nullptr) {
-          c[i] *= a.attn_factor;
-          s[i] *= a.attn_factor;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float cos_e = __shfl_sync(0xffffffffu, c[e % kMine], e / kMine * kLanes + sub);
-        const float sin_e = __shfl_sync(0xffffffffu, s[e % kMine], e / kMine * kLanes + sub);
-        if (e & 1) cosines[e / 2].y = cos_e, sines[e / 2].y = sin_e;
-        else cosines[e / 2].x = cos_e, sines[e / 2].x = sin_e;
-      }
+    for (int i = 0; i < kMine; ++i) {
+      const uint64_t phase = freq[i] * static_cast<uint64_t>(static_cast<int64_t>(pos[i]));
+      float c, s;
+      // half turns, -1 .. 1
+      sincospif(static_cast<float>(static_cast<int32_t>(phase >> 32)) * 0x1p-31f, &s, &c);
+      // (1 and 0 of pairs that do not turn)
+      const int p = pair_of(group * kMine + i);
+      s_turn[threadIdx.x / 32][0][p] = where[i] != nullptr ? c * a.attn_factor : 1.f;
+      s_turn[threadIdx.x / 32][1][p] = where[i] != nullptr ? s * a.attn_factor : 0.f;
     }
+    __syncwarp();
     int64_t page = -1, in_page = 0;
     if (slot >= 0 && slot < d.c.n_pages * d.c.page_size) {
       page = static_cast<uint32_t>(slot) / static_cast<uint32_t>(d.c.page_size);
@@ -291,6 +282,17 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
             for (int e = 0; e < V / 2; ++e) w[h].part(e) = 0x3f803f80u;  // ones
           }
         }
+        // the unit's pairs, two by two
+        float2 cosines[V / 2], sines[V / 2];
+#pragma unroll
+        for (int e = 0; e < V / 2; e += 2) {
+          const float4 c = *reinterpret_cast<const float4*>(&s_turn[threadIdx.x / 32][0][pair_of(i * V + 2 * e)]);
+          const float4 s = *reinterpret_cast<const float4*>(&s_turn[threadIdx.x / 32][1][pair_of(i * V + 2 * e)]);
+          cosines[e] = make_float2(c.x, c.y);
+          cosines[e + 1] = make_float2(c.z, c.w);
+          sines[e] = make_float2(s.x, s.y);
+          sines[e + 1] = make_float2(s.z, s.w);
+        }
 #pragma unroll
         for (int e = 0; e < V / 2; ++e) {
           // words e of the two pieces
@@ -298,8 +300,7 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
           const float2 w0 = make_float2(low(w[0].part(e)), high(w[0].part(e)));
           const float2 w1 = make_float2(low(w[1].part(e)), high(w[1].part(e)));
           if (kApart) {  // two pairs, their second elements in the second piece
-            const int p = i * (V / 2) + e;
-            const float2 c = cosines[p], s = sines[p];
+            const float2 c = cosines[e], s = sines[e];
             factor_c[one] = tc::mul2(w0, c);
             factor_s[one] = tc::mul2(w1, make_float2(-s.x, -s.y));
             factor_c[two] = tc::mul2(w1, c);
