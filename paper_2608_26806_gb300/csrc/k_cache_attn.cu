@@ -617,11 +617,14 @@ k_cache_attn(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ C
       // In a window, whose segments are short, the next one's queries come while this one's rows go out.
       Segment next{};
       if (kWindow) {
-        if (!cache_wait_warp(&sh.seg_full[(sc + 1) & 1], ((sc + 1) >> 1) & 1)) *abort_flag = 1;
-        next = sh.seg[(sc + 1) & 1];
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&sh.seg_empty[(sc + 1) & 1]);
-        if (next.head >= 0) queries(next);
+        if (cache_wait_warp(&sh.seg_full[(sc + 1) & 1], ((sc + 1) >> 1) & 1)) {
+          next = sh.seg[(sc + 1) & 1];
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(&sh.seg_empty[(sc + 1) & 1]);
+          if (next.head >= 0) queries(next);
+        } else {
+          *abort_flag = 1;
+        }
       }
       if (bar_consumers_any(*abort_flag != 0)) break;
       const int pieces = g.c1 - g.c0 + 1;

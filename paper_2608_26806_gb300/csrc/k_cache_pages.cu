@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
   pdl_wait();
   pdl_trigger();
   cg::cluster_group cluster = cg::this_cluster();
+  cluster.barrier_arrive();  // every CTA has started before any other writes into its shared memory
   const avtp_cache_free_args_t& a = d.a;
   const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks());
   const int R = a.n_requests;
@@ -213,6 +214,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
     if (total > 0x7fffffff) s_v.fail(R);
   }
   if (total > 0x7fffffff) total = 0;
+  cluster.barrier_wait();
   if (staged) __syncthreads();
   else cluster.sync();
 
@@ -331,6 +333,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
   pdl_wait();
   pdl_trigger();
   cg::cluster_group cluster = cg::this_cluster();
+  cluster.barrier_arrive();  // every CTA has started before any other writes into its shared memory
   const avtp_cache_fork_args_t& a = d.a;
   const int tid = threadIdx.x, rank = static_cast<int>(cluster.block_rank()), ctas = static_cast<int>(cluster.num_blocks());
   const int C = a.n_children, P = a.page_size;
@@ -393,6 +396,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
   }
   const bool countable = total <= 0x7fffffff && head >= 0 && head + copies <= a.n_free;
   if (!countable) total = 0;
+  cluster.barrier_wait();
   if (staged) __syncthreads();
   else cluster.sync();
 
