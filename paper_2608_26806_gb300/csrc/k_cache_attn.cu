@@ -202,9 +202,9 @@ __device__ __forceinline__ int steps_of(const CacheAttnDev& a, int tiles) {
   return (tiles + (1 << a.step_shift) - 1) >> a.step_shift;
 }
 
-// In a window, the rows of every gridDim-th request that has no cached tokens, by the computing warps: a captured batch's
-// padding. (As a tile and a segment a KV head of each on the line, three such requests of four KV heads behind 61 of
-// 200-8000 tokens in a window of 1024 took 9 us of 42, all in the last run.)
+// In a window, the rows of every gridDim-th request that has no cached tokens, by the computing warps: a captured
+// batch's padding. (As a tile and a segment a KV head of each on the line, three such requests of four KV heads
+// behind 61 of 200-8000 tokens in a window of 1024 took 9 us of 42, all in the last run.)
 template <int D>
 __device__ __noinline__ void write_empty(const CacheAttnDev& a) {
   for (int r = blockIdx.x; r < a.R; r += gridDim.x) {

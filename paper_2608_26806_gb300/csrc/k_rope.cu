@@ -13,8 +13,8 @@
 // Angles: far positions leave a 32-bit product no fraction. inv_freq / 2 pi is held as a 64-bit fraction of a turn,
 // so that pos times it, modulo 2^64, is the angle modulo a turn in integers: its error is that of the fraction (2^-61
 // of inv_freq, 2^-64 of a turn), times pos. The top 32 bits go to sincospif. A lane forms one or two of the token's
-// cosines and sines for its warp; with the norm's weights they become 16 pairs of factors a lane, so that a word of two
-// elements takes two packed products.
+// cosines and sines for its warp; with the norm's weights they become 16 pairs of factors a lane, so that a word of
+// two elements takes two packed products.
 //
 // A warp takes tokens and, where there are few of these, a share of their heads. Its rows come by asynchronous copies
 // into shared memory that run four groups of heads ahead of the work, on into the next token's; what a lane copies it
@@ -22,8 +22,9 @@
 // tokens, now 42-44; the first form, a warp's 150 registers holding three groups and the weights read for each head,
 // 127.)
 //
-// Measured, in a graph, with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128: 64 tokens 3.6 us,
-// 1024 8.1, 9856 42.5, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go by 64 bytes: 9856 25.5, 4.8 TB/s.
+// Measured, in a graph, with norms and the cache as destination: 32 query heads, 8 KV heads, d = 128: 64 tokens 3.6
+// us, 1024 8.1, 9856 42.5, 20000 81.7, 6.0 TB/s; 16 and 16 heads of 64, whose rows go by 64 bytes: 9856 25.5, 4.8
+// TB/s.
 #include <type_traits>
 
 #include "avtp_cache.cuh"
@@ -36,12 +37,14 @@ constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int kAhead = 4;       // groups of heads whose rows a warp has under way, a KiB each (three 43.2 us, six 42.5)
 constexpr int kCtasOfSm = 4;    // up to 128 registers a thread (9856 tokens 42.5 us; five CTAs, 96 and spills 44.6, six 48.3)
+constexpr int64_t kCheckTokens = 4096;
 constexpr int kWarpsOfSm = 16;  // warps of an SM that a call's work is spread over, at least
 
 struct RopeDev {
   avtp_rope_args_t a;
   avtp_cache_t c;   // k NULL: no cache
   int iq, ik;       // groups of heads of q, and of k or v
+  int checked;      // a CTA of its own checks tables and slots
   DevStatus* st;
 };
 
@@ -85,8 +88,10 @@ __device__ __forceinline__ void copy_ahead(uint32_t to, const __nv_bfloat16* fro
 }
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// The call's tables and slots, by a CTA of its own: the others skip what it records, so that the status word
-// has one writer and the call is one launch.
+// The call's tables and slots, by a CTA of its own: the others skip what it records, so that the status word has one
+// writer and the call is one launch. Of more tokens than kCheckTokens, which one CTA would take longer to look
+// through than the others to rotate (a million tokens of 4 + 2 heads of 64: 1.37 ms instead of 0.86), the warps
+// record what they meet themselves, in a status word that a kernel ahead has cleared.
 __device__ void check(const RopeDev& d) {
   __shared__ int s_bad;
   if (threadIdx.x == 0) s_bad = 0;
@@ -98,12 +103,13 @@ __device__ void check(const RopeDev& d) {
   }
   if (d.c.k != nullptr) {
     const int64_t slots = d.c.n_pages * d.c.page_size;
-    for (int64_t t0 = threadIdx.x; t0 < d.a.n_tokens; t0 += 8 * kThreads) {
-      int32_t s[8];
+    constexpr int N = 16;
+    for (int64_t t0 = threadIdx.x; t0 < d.a.n_tokens; t0 += N * kThreads) {
+      int32_t s[N];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = t0 + i * kThreads < d.a.n_tokens ? d.a.slot_map[t0 + i * kThreads] : -1;
+      for (int i = 0; i < N; ++i) s[i] = t0 + i * kThreads < d.a.n_tokens ? d.a.slot_map[t0 + i * kThreads] : -1;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) bad = bad || s[i] < -1 || s[i] >= slots;
+      for (int i = 0; i < N; ++i) bad = bad || s[i] < -1 || s[i] >= slots;
     }
   }
   if (bad) s_bad = 1;
@@ -124,7 +130,8 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
   __shared__ __align__(16) unsigned char s_ahead[kWarps][kAhead][kUnits][2][32 * kPieceBytes];
   pdl_wait();
   pdl_trigger();
-  if (blockIdx.x == gridDim.x - 1) {
+  const int workers = static_cast<int>(gridDim.x) - d.checked;
+  if (static_cast<int>(blockIdx.x) == workers) {
     if (blockIdx.y == 0) check(d);
     return;
   }
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
   // order: n of them, each of heads (slice + j slices) kHeads ... Copies run kAhead groups ahead of the work, through
   // a token's rows of every kind and on into the next token's.
   int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
-  const int64_t step = static_cast<int64_t>(gridDim.x - 1) * kWarps;
+  const int64_t step = static_cast<int64_t>(workers) * kWarps;
   const int slice = blockIdx.y, slices = gridDim.y;
   const int nq = slice < d.iq ? (d.iq - 1 - slice) / slices + 1 : 0, nk = slice < d.ik ? (d.ik - 1 - slice) / slices + 1 : 0;
   const int n = nq + nk + (d.c.k != nullptr ? nk : 0);
@@ -225,8 +232,9 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
       }
     }
   }
-  if (!__all_sync(0xffffffffu, fine)) {  // recorded by check()
+  if (!__all_sync(0xffffffffu, fine)) {
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!d.checked && lane == 0) record_error(d.st, AVTP_ERR_DEVICE_INPUT, -1);
     return;
   }
   int32_t pos[kMine], slot = -1;  // of the next token
@@ -254,6 +262,8 @@ __global__ void __launch_bounds__(kThreads, kCtasOfSm) k_rope(RopeDev d) {
     }
     __syncwarp();
     int64_t page = -1, in_page = 0;
+    if (!d.checked && lane == 0 && (slot < -1 || slot >= d.c.n_pages * d.c.page_size))
+      record_error(d.st, AVTP_ERR_DEVICE_INPUT, static_cast<int32_t>(t));
     if (slot >= 0 && slot < d.c.n_pages * d.c.page_size) {
       page = static_cast<uint32_t>(slot) / static_cast<uint32_t>(d.c.page_size);
       in_page = slot - page * d.c.page_size;
@@ -392,7 +402,13 @@ cudaError_t launch_rope(const avtp_rope_args_t& a, const avtp_cache_t* c, void* 
   int slices = 1;
   while (slices < groups && a.n_tokens * slices < static_cast<int64_t>(device_sm_count()) * kWarpsOfSm) ++slices;
   const int64_t want = (a.n_tokens + kWarps - 1) / kWarps, fit = static_cast<int64_t>(device_sm_count()) * kCtasOfSm / slices;
-  const dim3 grid(static_cast<unsigned>((slices == 1 && want > fit ? fit : want) + 1), static_cast<unsigned>(slices));
+  d.checked = c == nullptr || a.n_tokens <= kCheckTokens ? 1 : 0;
+  if (!d.checked) {
+    const cudaError_t e = launch_cache_status(d.st, s);
+    if (e != cudaSuccess) return e;
+  }
+  const dim3 grid(static_cast<unsigned>((slices == 1 && want > fit ? fit : want) + d.checked),
+                  static_cast<unsigned>(slices));
   const bool apart = a.style == AVTP_ROPE_HALF;
   // half-style pairs whose halves begin inside a piece of eight are held as pieces of four
   const bool fours = apart && a.rot_dim % 16 != 0;

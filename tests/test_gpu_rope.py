@@ -260,6 +260,44 @@ def test_bad_tables_write_nothing(what):
     assert (q_out == 5.0).all() and torch.isnan(k).all() and torch.isnan(v).all()
 
 
+@pytest.mark.parametrize("T", [4096, 4097, 9000])
+def test_what_many_tokens_have_wrong_is_recorded(T):
+    """By one CTA up to 4096 tokens, by those that rotate beyond."""
+    page, Hkv, d = 16, 1, 64
+    x = make(T, 2, Hkv, d, d, planes=2, seed=T)
+    dev = {n: x[n].cuda() for n in ("pos", "inv", "q", "k", "v", "plane")}
+    n_pages = T // page + 2
+    slots = torch.arange(T).int()
+
+    def call(slots, **tables):
+        k, v = pool(n_pages, page, Hkv, d)
+        t = {**dev, **tables}
+        c = avtp.RopeCall(t["pos"], t["inv"], q=t["q"], k=t["k"], v=t["v"], pair_plane=t["plane"],
+                          cache=avtp.PagedCache(k, v), slot_map=slots.cuda(),
+                          q_out=torch.full((T, 2, d), 5.0, dtype=torch.bfloat16, device="cuda"))
+        return c.run(), k, v
+
+    c, k, v = call(slots)
+    assert status(c) == avtp.OK
+    want, tol = plain(x["k"], x["pos"], x["inv"], "half", x["plane"].long(), 1.0, None)
+    close(k.reshape(-1, Hkv, d)[:T], (want, tol))
+    bad = slots.clone()
+    bad[T - 1], bad[7] = n_pages * page, -2
+    c, k, v = call(bad)
+    assert status(c) == avtp.ERR_DEVICE_INPUT
+    good = torch.ones(n_pages * page, dtype=torch.bool)
+    good[[7, T - 1]] = False
+    good[T:] = False
+    at = torch.nonzero(good)[:, 0]
+    close(k.cpu().reshape(-1, Hkv, d)[at], (want[at], tol[at]))
+    assert torch.isnan(k.cpu().reshape(-1, Hkv, d)[~good]).all() and torch.isnan(v.cpu().reshape(-1, Hkv, d)[~good]).all()
+    inv = x["inv"].clone()
+    inv[30] = float("nan")
+    c, k, v = call(slots, inv=inv.cuda())
+    assert status(c) == avtp.ERR_DEVICE_INPUT
+    assert (c.q_out == 5.0).all() and torch.isnan(k).all() and torch.isnan(v).all()
+
+
 # ---------------------------------------------------------------- how programs call it
 def test_no_tokens():
     e = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
