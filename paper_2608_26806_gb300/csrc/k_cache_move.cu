@@ -39,8 +39,10 @@ struct CopyDev {
   int64_t pieces;      // 16-byte pieces of a page of K, or of V
   int head_sh;         // log2 of a head's pieces
   int k_rows, v_rows;  // a page's rows in memory order: by token (0) or by head (1)
+  int checked;         // the pairs are checked by a CTA of its own, the status word's only writer
   DevStatus* st;
 };
+constexpr int64_t kCheckPairs = 2048;  // beyond, a kernel ahead clears the word and the copying CTAs record
 
 // Offset of piece i of a page, its rows in memory order.
 __device__ __forceinline__ int64_t piece_offset(const CopyDev& d, int64_t i, int by_head, int64_t token_stride,
@@ -53,7 +55,8 @@ __device__ __forceinline__ int64_t piece_offset(const CopyDev& d, int64_t i, int
 __global__ void __launch_bounds__(kThreads) k_cache_copy(CopyDev d) {
   pdl_wait();
   pdl_trigger();
-  if (blockIdx.x == gridDim.x - 1) {
+  const int64_t workers = static_cast<int64_t>(gridDim.x) - d.checked;
+  if (blockIdx.x == workers) {
     __shared__ int s_bad;
     if (threadIdx.x == 0) s_bad = 0x7fffffff;
     __syncthreads();
@@ -68,12 +71,14 @@ __global__ void __launch_bounds__(kThreads) k_cache_copy(CopyDev d) {
   // a CTA's share: kThreads * kUnroll pieces of a page of K or V
   const int64_t chunks = (d.pieces + kThreads * kUnroll - 1) / (kThreads * kUnroll);
   const int64_t items = d.n * 2 * chunks;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x - 1) {
+  for (int64_t item = blockIdx.x; item < items; item += workers) {
     const int64_t pair = item / (2 * chunks);
     const int64_t rest = item - pair * 2 * chunks;
     const bool is_v = rest >= chunks;
     const int64_t i0 = (rest - (is_v ? chunks : 0)) * kThreads * kUnroll + threadIdx.x;
     const int32_t from = d.src[pair], to = d.dst[pair];
+    if (!d.checked && threadIdx.x == 0 && (from < -1 || from >= d.c.n_pages || to < -1 || to >= d.c.n_pages))
+      record_error(d.st, AVTP_ERR_DEVICE_INPUT, static_cast<int32_t>(pair));
     if (from < 0 || from >= d.c.n_pages || to < 0 || to >= d.c.n_pages) continue;
     __nv_bfloat16* pool = static_cast<__nv_bfloat16*>(is_v ? d.c.v : d.c.k);
     const int64_t page = is_v ? d.c.v_page_stride : d.c.k_page_stride;
@@ -383,8 +388,13 @@ cudaError_t launch_cache_copy(const avtp_cache_t& c, const int32_t* src, const i
   d.st = static_cast<DevStatus*>(ws);
   const int64_t want = n * 2 * ((d.pieces + kThreads * kUnroll - 1) / (kThreads * kUnroll));
   const int64_t most = 8 * static_cast<int64_t>(device_sm_count());
-  return launch_kernel(k_cache_copy, dim3(static_cast<unsigned>((want < most ? want : most) + 1)), dim3(kThreads), 0, s,
-                       /*pdl=*/true, d);
+  d.checked = n <= kCheckPairs ? 1 : 0;
+  if (!d.checked) {
+    const cudaError_t e = launch_cache_status(d.st, s);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_kernel(k_cache_copy, dim3(static_cast<unsigned>((want < most ? want : most) + d.checked)), dim3(kThreads), 0,
+                       s, /*pdl=*/true, d);
 }
 
 cudaError_t launch_cache_compact(const avtp_cache_t& c, const avtp_cache_compact_args_t& a, void* ws, cudaStream_t s) {

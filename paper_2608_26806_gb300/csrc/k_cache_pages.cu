@@ -12,7 +12,7 @@
 // pages stay in its registers from round to round. Everything is checked before the first write. Calls one behind the
 // other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 5.7 us; the pages that
 // 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.9; eight
-// children of a prompt of 146 pages 7.2; 171 children of 64 (21000 entries) 10.6. (With eight CTAs 6.8, 19.9, 8.5 and
+// children of a prompt of 146 pages 7.7; 171 children of 64 (21000 entries) 10.8. (With eight CTAs 6.8, 19.9, 8.5 and
 // 13.1; with entries looked up again in every round, and the others' findings read from their shared memory, 11.7,
 // 36.7, 11.2 and 18.8.)
 //

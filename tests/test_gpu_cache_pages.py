@@ -372,6 +372,26 @@ def test_copy_of_pages(order, page, Hkv, d):
     assert status(none) == avtp.OK and torch.equal(k, want[0])
 
 
+@pytest.mark.parametrize("n", [2048, 2049, 5000])
+def test_copy_of_many_pages(n):
+    """Pairs checked by one CTA, or by those that copy."""
+    g = torch.Generator().manual_seed(n)
+    k, v = (torch.randn(2 * n, 1, 1, 64, generator=g).bfloat16().cuda() for _ in range(2))
+    ids = torch.randperm(2 * n, generator=g)
+    src, dst = ids[:n].clone(), ids[n:].clone()
+    src[5] = -1
+    for bad in (False, True):
+        want = [t.clone() for t in (k, v)]
+        if bad:
+            src[n - 1], dst[3] = 2 * n, -2
+        ok = ((src >= 0) & (src < 2 * n) & (dst >= 0)).nonzero()[:, 0]
+        for t in want:
+            t[dst[ok].cuda()] = t[src[ok].cuda()]
+        call = avtp.CacheCopyCall(avtp.PagedCache(k, v), i32(src), i32(dst)).run()
+        assert status(call) == (avtp.ERR_DEVICE_INPUT if bad else avtp.OK)
+        assert torch.equal(k, want[0]) and torch.equal(v, want[1])
+
+
 # ---------------------------------------------------------------- compact
 class Compacted:
     def __init__(self, seq, keep, page, Hkv=2, d=64, order="token", seed=0, other=True, base=False):
