@@ -11,7 +11,7 @@
 // which forms the sums for itself, so that barriers part the rounds and nothing else does; a thread's first kKept
 // pages stay in its registers from round to round. Everything is checked before the first write. Calls one behind the
 // other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 5.7 us; the pages that
-// 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.9; eight
+// 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.1; eight
 // children of a prompt of 146 pages 7.7; 171 children of 64 (21000 entries) 10.8. (With eight CTAs 6.8, 19.9, 8.5 and
 // 13.1; with entries looked up again in every round, and the others' findings read from their shared memory, 11.7,
 // 36.7, 11.2 and 18.8.)
@@ -248,6 +248,15 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
       d.last[page] = n > 0 ? -1 : static_cast<int32_t>(e);
     }
   });
+  // What an entry leaves of its page's others, if it stands for the page: -1, it goes to the list. kNone: it does not.
+  constexpr int32_t kNone = -2, kWrong = -3;
+  auto rest_of = [&](int64_t e, int32_t page, int32_t n) {
+    const bool stands = __ldcg(d.last + page) == e;
+    if (n <= 0) return stands ? -1 : kWrong;
+    const int32_t let_go = __ldcg(d.rel + page);
+    return let_go > n + 1 ? kWrong : (stands ? n - let_go : kNone);
+  };
+  int32_t rest[kKept + 1] = {};
   if (a.shared != nullptr) {
     cluster.sync();
     entries([&](int64_t e, int32_t page, int i) {
@@ -259,11 +268,11 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
     int64_t mine[1] = {0}, all[1];
     entries([&](int64_t e, int32_t page, int i) {
       if (!in_pool(page)) return;
-      const int32_t n = others_of(page, i), counted = __ldcg(d.rel + page), let_go = n > 0 ? counted : 1;
-      const bool stands = __ldcg(d.last + page) == e;
+      const int32_t n = others_of(page, i), left = rest_of(e, page, n);
       // more entries than holders; of one holder, one that finds another
-      if (let_go > n + 1 || (n <= 0 && !stands)) s_v.fail(upper_index(first, R, e));
-      mine[0] += let_go == n + 1 && stands ? 1 : 0;
+      if (left == kWrong) s_v.fail(upper_index(first, R, e));
+      mine[0] += left == -1 ? 1 : 0;
+      if (i < kKept) rest[i] = left;
     });
     block_scan(mine, s_warp, all);
     if (tid == 0) s_v.gives = all[0];
@@ -282,18 +291,20 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
   } else if (ok) {
     for (int64_t b = e0, i = 0; b < e1; b += kThreads, ++i) {
       const int64_t e = b + tid;
-      int32_t page = 0, rest = 0;
-      bool stands = false;
+      int32_t page = 0, left = kNone, n = 0;
       if (e < e1) {
-        page = i == 0 ? kept[0] : (i == 1 ? kept[1] : (i == 2 ? kept[2] : (i == 3 ? kept[3] : page_of(e))));
-        stands = __ldcg(d.last + page) == e;
-        if (stands) {
-          const int32_t n = a.shared[page];
-          rest = n > 0 ? n - __ldcg(d.rel + page) : -1;
-          if (n > 0) a.shared[page] = max(rest, 0);
+        if (i < kKept) {
+#pragma unroll
+          for (int k = 0; k < kKept; ++k)
+            if (i == k) page = kept[k], left = rest[k], n = others[k];
+        } else {
+          page = page_of(e);
+          n = a.shared[page];
+          left = rest_of(e, page, n);
         }
       }
-      const bool give = stands && rest < 0;
+      const bool give = left == -1;
+      if (n > 0 && left >= -1) a.shared[page] = max(left, 0);
       int64_t sum[1] = {give ? 1 : 0}, all[1];
       block_scan(sum, s_warp, all);
       if (give) a.free_pages[at + sum[0] - 1] = page;
