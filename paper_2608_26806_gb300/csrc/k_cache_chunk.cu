@@ -48,10 +48,10 @@
 // In a window (kWindow, see avtp.h) a unit's blocks are those of the sinks and those from its first token's window on
 // (Segment::block gives a block's place among the request's); its last blocks are masked above and its first ones
 // below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that
-// no row of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in windows of 2048, 512
-// and 128 tokens: 225, 122 and 73 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50 by the figures
-// above: first blocks and last ones are masked, and a unit's ends weigh more. (Masks by comparison, every half looked
-// at, values cleared by the softmax warps: 279, 157 and 103.)
+// no row of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in
+// windows of 2048, 512 and 128 tokens: 225, 107 and 67 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50
+// by the figures above: first blocks and last ones are masked, and a unit's ends weigh more. (Masks by comparison, every
+// half looked at, values cleared by the softmax warps, runs cut evenly: 279, 157 and 103.)
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
@@ -75,8 +75,8 @@ constexpr int kStages = 4;      // key or value blocks in shared memory
 // A unit's beginning costs about as much as this many key blocks (its queries' arrival, the first softmax with
 // nothing to overlap, its rows' way out): its steps on the line are its blocks and these. (With three, 9856 tokens
 // 488 us instead of 494, 512 behind 9300 63.6 instead of 62.8.) In a window, whose first blocks are masked too, four
-// (8192 tokens behind 2176, 32 query heads, 8 KV heads, window 512: 118.8 us and 125.8 with two, 117.0 with six;
-// 2048: 233.8, 240.5, 235.5).
+// (32 query heads, 8 KV heads: 8192 tokens behind 2176, their units cut into even runs, window 512 118.8 us and 125.8
+// with two, 2048 233.8 and 240.5; 512 behind 9300, window 512, 27.0 and 29.1 with six).
 template <bool kWindow>
 constexpr int kUnitSteps = kWindow ? 4 : 2;
 constexpr uint32_t kTmemCols = 512;
@@ -326,11 +326,25 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
     CacheLine<kWindow> line;
     CacheChunkSplit split{};
     split.c1 = -1;
+    bool whole = false;  // see below
     if (kv == 0) {
       line = CacheLine<kWindow>(a, sy.plan, mine, mine_ok, steps);
       runs = CacheRuns(line.total, line.most, kUnitSteps<kWindow> + 1, cache_ctas(a, line.weights, false));
       t = runs.begin(blockIdx.x);
       t1 = runs.begin(blockIdx.x + 1);
+      // In a window units are short, and nearly all of one length. Where there are many a run, and their number comes
+      // out nearly even, a cut is moved to the nearer end of the unit that it falls into, and no unit is in pieces; a
+      // run gets a unit more than its share at worst, where first units are shorter. (That every run is longer than
+      // half a unit keeps the last cut before the last unit's middle.) 32 query heads, 8 KV heads, 8192 tokens behind
+      // 2176, 6.7 units a run: window 2048 236 -> 225 us, 512 131 -> 107, 128 73 -> 67; 16384 tokens, window 512, 242
+      // -> 198; four requests of 943 behind 5000, 80 query heads, 16 KV heads, window 2048, where one run in 152 gets
+      // a seventh unit, 293 -> 296. With four units a run: four of 2315 behind 5000, 20 and 4 heads, 200 -> 213.
+      if (kWindow && a.R <= kNearRequests) {
+        const uint32_t units = a.Hkv * __reduce_add_sync(0xffffffffu, lane < a.R && mine_ok ? units_of(a, mine, nt) : 0);
+        const int usual = line.most - (1 + (2 * nt + kKB - 1) / kKB);
+        whole = units >= 6u * runs.N && (units + runs.N - 1) / runs.N * runs.N - units <= units >> 4 &&
+                int64_t(usual) * units <= int64_t(line.total) + (line.total >> 4) && 2 * runs.each > line.most;
+      }
       if (t < t1) {
         r = line.find(a, sy.plan, t, &pre);
         // a request of many units: its last one that begins at or before step t, 32 tries at a time (the
@@ -359,6 +373,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
         if (t < t1) {
           CacheRequest q;
           int nb = 0, len = 0;  // key blocks and steps of the unit
+          int h = 0;            // of whole units: a cut at most h steps before a unit's end counts as that end
 #pragma unroll 1
           for (;; ++r, u = 0) {
             q = line.request(a, mine, r);
@@ -367,14 +382,19 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             for (; u < U; ++u) {
               nb = unit_blocks<kWindow>(a, q, nt, u);
               len = steps_of<kWindow>(a, nb);
-              if (t < pre + len * a.Hkv) break;
+              if (kWindow && whole) h = (len - 1) >> 1;
+              if (t + h < pre + len * a.Hkv) break;
               pre += len * a.Hkv;
             }
             if (u < U) break;
           }
-          const int head = static_cast<int>(static_cast<uint32_t>(t - pre) / static_cast<uint32_t>(len));
+          const int head = static_cast<int>(static_cast<uint32_t>(max(0, t + h - pre)) / static_cast<uint32_t>(len));
           const int s = pre + head * len;  // the unit's first step
           end = min(t1, s + len);
+          if (kWindow && whole) {  // the unit is the next run's if t1 is moved to its beginning, or lies before it
+            end = t1 + h < s + len ? s : s + len;
+            t = s;
+          }
           // a run that ends in a unit's first steps leaves its blocks to the next
           g.head = end > s + kUnitSteps<kWindow> ? head : -1;
           g.row0 = q.row0;

@@ -137,6 +137,18 @@ def test_chunks_of_many_units(shape, n, window, sinks):
     run(Windowed([(n + 500, n), (300, 40), (n, n)], *SHAPES[shape], 64, window, sinks))
 
 
+@pytest.mark.parametrize("requests,Hq,Hkv,d,window,sinks", [
+    ([(300 + 7 * i, 40) for i in range(32)], 32, 32, 64, 100, 4),
+    ([(200 + 31 * i, 70) for i in range(19)], 48, 48, 64, 129, 0),
+    ([(500, 90), (0, 60), (700, 0), (45, 50)] + [(1000 - 30 * i, 50 + 9 * i) for i in range(25)], 40, 40, 64, 64, 130),
+    ([(400, 45), (300, 1), (90, 2)] * 10, 96, 96, 64, 70, 7),
+    ([(300, 300), (1700, 1500)], 128, 16, 128, 100, 4),
+    ([(1925, 1824)], 128, 16, 128, 127, 0)])
+def test_as_many_chunks_as_fill_the_device_some_times(requests, Hq, Hkv, d, window, sinks):
+    """Six units and more for each SM, nearly all of one length, none of which is in pieces."""
+    run(Windowed(requests, Hq, Hkv, d, 32, window, sinks))
+
+
 @pytest.mark.parametrize("order", ["token", "head", "mixed", "padded", "shared"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_orders_of_pages(order, d):
