@@ -1,4 +1,7 @@
 """The upkeep of the cache's pages on the GPU against plain forms one page and one token at a time."""
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -726,3 +729,41 @@ def test_a_pruned_batch_goes_on_pruned_in_place():
         at = torch.from_numpy(ints(table)[r, p // page]).long().cuda(), torch.from_numpy(p % page).cuda()
         rows = torch.from_numpy(kept[kept_cu[r]:kept_cu[r + 1]]).cuda()
         assert torch.equal(cache.k[at], k[rows]) and torch.equal(cache.v[at], v[rows])
+
+
+def test_the_readme_example_of_positions_and_upkeep():
+    """The example run as it stands, behind slots for the step's tokens: two requests cut to their kept tokens, and two
+    rows more that go on from the first."""
+    with open(os.path.join(os.path.dirname(__file__), "..", "README.md"), encoding="utf-8") as f:
+        code = [c for c in re.findall(r"```python\n(.*?)```", f.read(), re.S) if "cache_fork" in c]
+    assert len(code) == 1
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def rand(*shape):
+        return torch.randn(*shape, device="cuda", generator=g).to(torch.bfloat16)
+
+    n_pages, lens, keep = 24, [300, 130, 0, 0], [np.arange(0, 300, 3), np.arange(7, 130)]
+    cache = avtp.PagedCache.new(n_pages, page_size=64, n_kv_heads=8, head_dim=128)
+    cache.k.normal_(generator=g)
+    cache.v.normal_(generator=g)
+    table = torch.full((4, 8), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(n_pages, device="cuda", generator=g).to(torch.int32)
+    cu = i32(np.concatenate([[0], np.cumsum(lens)]))
+    slots, seq_len, free_head = avtp.cache_slots(cu, sum(lens), page_size=64, n_pages=n_pages, block_table=table,
+                                                 free_pages=free)
+    T = sum(lens)
+    env = dict(avtp=avtp, torch=torch, cache=cache, slots=slots, n_pages=n_pages, table=table, free=free,
+               free_head=free_head, seq_len=seq_len, q_new=rand(T, 32, 128), k_new=rand(T, 8, 128),
+               v_new=rand(T, 8, 128), wq=rand(128), wk=rand(128), pos=i32(np.tile(np.arange(T), (3, 1))),
+               plane_of_pair=i32(np.arange(64) % 3), keep_cu=i32([0, 100, 223, 223, 223]),
+               keep_idx=i32(np.concatenate(keep)), parent=i32([0, 0]), child=i32([2, 3]),
+               shared=torch.zeros(n_pages, dtype=torch.int32, device="cuda"))
+    exec(compile(code[0], "README.md", "exec"), env)  # noqa: S102
+    assert torch.isfinite(env["q"].float()).all()
+    assert env["seq_len"].tolist() == [100, 123, 100, 100] and env["free_head"].tolist() == [2 + 2 + 2]
+    # what a row holds is the kept tokens' values as they came in, and a child's are its parent's
+    flat = table.long()
+    for r, want in ((0, keep[0]), (1, keep[1] + 300), (2, keep[0]), (3, keep[0])):
+        j = torch.arange(len(want), device="cuda")
+        assert torch.equal(cache.v[flat[r][j // 64], j % 64], env["v_new"][torch.as_tensor(want).cuda()])
+    assert torch.equal(flat[2, :1], flat[0, :1]) and len({int(flat[r, 1]) for r in (0, 2, 3)}) == 3
