@@ -48,8 +48,9 @@
 // In a window (kWindow, see avtp.h) a unit's blocks are those of the sinks and those from its first token's window on
 // (Segment::block gives a block's place among the request's); its last blocks are masked above and its first ones
 // below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that
-// no row of the unit sees are cleared by the warp that loads them. 8192 tokens behind 2176 in
-// windows of 2048, 512 and 128 tokens: 225, 107 and 67 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50
+// no row of the unit sees are cleared by the warp that loads them; a row takes its reference from the first half that
+// shows it a key, so that the weight of a token that sees itself alone is 1. 8192 tokens behind 2176 in
+// windows of 2048, 512 and 128 tokens: 225, 107 and 63 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50
 // by the figures above: first blocks and last ones are masked, and a unit's ends weigh more. (Masks by comparison, every
 // half looked at, values cleared by the softmax warps, runs cut evenly: 279, 157 and 103.)
 //
@@ -88,6 +89,8 @@ constexpr float kRescaleSum = 16384.f;
 constexpr float kRescaleTau = 8.f;
 // A row whose sum is below this has no reference yet, or one too far above its logits.
 constexpr float kLeastSum = 1.f / 1024.f;
+// Of a row that a window has shown no key yet: its sums are zeros until it finds its reference.
+constexpr float kNoReference = -1e30f;
 constexpr float kLn2 = 0.6931471805599453f;
 static_assert(kChunkRows == 2 * kQT, "two slots a unit");
 
@@ -670,7 +673,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // in a window: the first key behind the sinks that this row sees, and every row of the warp
       int low = 0, all_low = 0;
       int any_see = 0, any_low = 0;  // keys that some stored row of the warp sees: below the one, from the other on
-      bool fresh = true;             // the segment's rows have no references yet
+      bool fresh = true;             // some stored row of the warp has no reference yet
       if (kWindow) {
         low = live ? cache_low(a, g.seq - g.n + tok) : 0;
         all_low = __reduce_max_sync(0xffffffffu, low);
@@ -680,7 +683,7 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // row reference (log2 units), sum of exp2(c2 s - m). The reference begins as the maximum of the
       // first half, which is in registers anyway (the whole block's, with the half's exponentials
       // taken twice, cost 1400 cycles a segment; beginning at 0, sharp queries moved it too often).
-      float m = 0.f, l = 0.f;
+      float m = kWindow ? kNoReference : 0.f, l = 0.f;
       for (int j = 0; j < nblk; ++j) {
         ok = cache_wait_warp(&sy.s_full[slot], (done + j) & 1);
         if (!ok) break;
@@ -724,7 +727,9 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           return (acc0.x + acc0.y) + (acc1.x + acc1.y);
         };
         // values far above the reference or, as yet, all far below it, or a NaN
-        auto off = [&](float sum) { return __any_sync(0xffffffffu, live && (!(sum <= kRescaleSum) || l + sum < kLeastSum)); };
+        auto off = [&](float sum, bool has) {
+          return __any_sync(0xffffffffu, has && (!(sum <= kRescaleSum) || l + sum < kLeastSum));
+        };
         auto hand_over = [&](int hf, float sum) {
           l += sum;
           tc::tmem_st32(tS + hf * 32, pk);
@@ -740,13 +745,13 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
           tc::tmem_ld64_async(tS, su);
           tc::tmem_wait64(su);
           float sum = exps();
-          if (!off(sum)) {
+          if (!off(sum, live)) {
             hand_over(0, sum);
             hf = 1;
             tc::tmem_ld64_async(tS + 64, su);
             tc::tmem_wait64(su);
             sum = exps();
-            if (!off(sum)) {
+            if (!off(sum, live)) {
               hand_over(1, sum);
               hf = 2;
             }
@@ -767,8 +772,6 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
             sum = 0.f;
 #pragma unroll
             for (int c = 0; c < 32; ++c) pk[c] = 0u;
-          } else {
-            fresh = false;
           }
 #pragma unroll 1
           while (!blind) {
@@ -802,7 +805,11 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
               }
               mb = fmaxf(mb, fmaxf(tc::max3(t[0], t[1], t[2]), t[3]) * c2);  // stays -inf when nothing is visible
               if (mode == kFirst) {
-                m = mb == -INFINITY ? 0.f : mb;
+                if (kWindow) {  // a row that sees none of these keys goes on looking
+                  m = m == kNoReference && mb != -INFINITY ? mb : m;
+                } else {
+                  m = mb == -INFINITY ? 0.f : mb;
+                }
               } else if (at > hf) {
                 at = hf;
                 continue;
@@ -834,12 +841,13 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
               }
             }
             sum = exps();
-            if (mode == kMove || !off(sum)) break;
+            if (mode == kMove || !off(sum, live && (!kWindow || m != kNoReference))) break;
             mode = kMove;
             mb = -INFINITY;
             at = 1;
           }
           if (!ok) break;
+          if (kWindow && !blind) fresh = __any_sync(0xffffffffu, live && m == kNoReference);
           hand_over(hf, sum);
         }
         if (!ok) break;

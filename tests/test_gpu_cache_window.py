@@ -149,6 +149,18 @@ def test_as_many_chunks_as_fill_the_device_some_times(requests, Hq, Hkv, d, wind
     run(Windowed(requests, Hq, Hkv, d, 32, window, sinks))
 
 
+@pytest.mark.parametrize("shape,n", [("four", 700), ("seven", 401), ("plain", 600), ("twenty", 333), ("most", 130),
+                                     ("four", 1), ("seven", 3)])
+def test_a_window_of_one_token(shape, n):
+    """A token that sees itself alone: its weight is 1 against its own maximum, and its value comes back as it was."""
+    b = Windowed([(n + 77, n), (n, n)], *SHAPES[shape], 64, 1, 0)
+    c = run(b)
+    G, at = b.Hq // b.Hkv, 0
+    for r, (s, m) in enumerate(b.requests):
+        assert torch.equal(c.o[at:at + m].cpu(), b.rows[r][1][s - m:].repeat_interleave(G, 1).cpu())
+        at += m
+
+
 @pytest.mark.parametrize("order", ["token", "head", "mixed", "padded", "shared"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_orders_of_pages(order, d):
