@@ -625,9 +625,10 @@ AVTP_API avtp_status_t avtp_cache_window_attention(const avtp_cache_t* cache, co
  * Requests may let go of pages that a sliding window has left (see avtp_cache_window_attention):
  * with `window` > 0 a request that was `held_len` tokens long at its last such call holds the pages
  * of its first n_sinks tokens, and of those from held_len - window + 1 on, the first that the
- * window of its next token needs. held_len (device [R], zeros at first) goes with the lengths:
- * avtp_cache_free writes it, avtp_cache_fork copies it. Table entries of pages let go of stay as
- * they were and are not read. window 0: every request holds all its pages. */
+ * window of its next token needs. held_len (device [R], zeros at first) goes with the lengths, and
+ * is never longer than they are: avtp_cache_free writes it, and avtp_cache_fork gives a child its
+ * parent's, or its own length where that is less. Table entries of pages let go of stay as they were
+ * and are not read. window 0: every request holds all its pages. */
 
 /* The kept tokens of cached requests moved together, in one layer's cache: for j < n_r =
  * keep_cu[r+1] - keep_cu[r], the rows of token keep_idx[keep_cu[r] + j] - base of request r go to

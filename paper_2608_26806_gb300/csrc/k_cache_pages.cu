@@ -484,7 +484,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
       a.copy_src[i] = from;
       a.copy_dst[i] = to;
       a.seq_len[c] = k.len;
-      if (a.window > 0) a.held_len[c] = k.len > 0 ? k.held : 0;
+      if (a.window > 0) a.held_len[c] = min(k.held, k.len);  // of a prefix shorter than that: the same pages
     }
   }
   if (rank == 0 && tid == 0) {

@@ -11,6 +11,13 @@ def holds(j, n, held, page, window=0, sinks=0):
     return j < -(-n // page) and (j < -(-sinks // page) or j >= left(held, page, window))
 
 
+def needs_lost(n, held, page, window=0, sinks=0):
+    """Whether n tokens need a page that a request held at `held` tokens has let go of."""
+    many = max(n, held) + page
+    return any(holds(j, n, n, page, window, sinks) and not holds(j, many, held, page, window, sinks)
+               for j in range(-(-n // page)))
+
+
 def free_plain(seq, new, table, free, head, page, shared=None, window=0, sinks=0, held=None):
     """avtp_cache_free: (free, head, shared)."""
     free, gone = free.copy(), []
@@ -47,7 +54,7 @@ def fork_plain(parent, child, seq, table, free, head, page, shared, length=None,
             head += 1
         seq[c] = n
         if held is not None:
-            held[c] = held[p] if n else 0
+            held[c] = min(held[p], n)
     return table, seq, head, shared, src, dst, held
 
 

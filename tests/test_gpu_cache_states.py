@@ -1,0 +1,92 @@
+"""What one call of the cache's upkeep leaves is what the next one takes: lengths, held lengths and pages from call to
+call, on the GPU, against the plain forms one page and one token at a time."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_26806_gb300 import avtp
+from tests.gpu_util import ensure_built
+from tests.pages_util import fork_plain, free_plain, holds, needs_lost
+from tests.test_gpu_cache_pages import Forked, i32, ints, status
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA device")
+    ensure_built()
+
+
+# ---------------------------------------------------------------- forks of prefixes in a window
+class Books:
+    """A table's numbers on the device and in the plain forms, call after call."""
+
+    def __init__(self, f):
+        f.call()
+        self.f, self.d = f, f.dev
+        self.seq, self.table, self.free, self.shared, self.held = (
+            np.array(x) for x in (f.seq, f.table, f.free, f.shared, f.held))
+        self.head = f.head
+        self.more = dict(page_size=f.page, n_pages=f.n_pages, free_pages=self.d["free"], free_head=self.d["head"],
+                         shared=self.d["shared"], window=f.window, sinks=f.sinks, held_len=self.d["held"],
+                         free_head_out=self.d["head"])
+
+    def fork(self, parent, child, length=None):
+        f, d = self.f, self.d
+        c = avtp.CacheForkCall(i32(parent), i32(child), d["seq"], d["table"],
+                               fork_len=None if length is None else i32(length), **self.more).run()
+        self.table, self.seq, self.head, self.shared, src, dst, self.held = fork_plain(
+            parent, child, self.seq, self.table, self.free, self.head, f.page, self.shared, length, f.window, f.sinks,
+            self.held)
+        assert status(c) == avtp.OK
+        assert np.array_equal(ints(c.copy_src), src) and np.array_equal(ints(c.copy_dst), dst)
+        self.agree()
+
+    def go_on(self, new):
+        f, d = self.f, self.d
+        c = avtp.CacheFreeCall(d["seq"], i32(new), d["table"], seq_len_out=d["seq"], held_len_out=d["held"], **self.more).run()
+        self.free, self.head, self.shared = free_plain(self.seq, new, self.table, self.free, self.head, f.page, self.shared,
+                                                       f.window, f.sinks, self.held)
+        self.seq, self.held = np.array(new), np.array(new)
+        assert status(c) == avtp.OK
+        self.agree()
+
+    def agree(self):
+        d = self.d
+        for name in ("seq", "table", "shared", "held", "free"):
+            assert np.array_equal(ints(d[name]), getattr(self, name)), name
+        assert int(d["head"]) == self.head and (self.held <= self.seq).all()
+        holders = np.zeros(self.f.n_pages, dtype=np.int64)
+        for r, n in enumerate(self.seq):
+            for j in range(-(-int(n) // self.f.page)):
+                if holds(j, n, self.held[r], self.f.page, self.f.window, self.f.sinks):
+                    holders[self.table[r, j]] += 1
+        assert np.array_equal(np.maximum(holders - 1, 0), self.shared)
+
+
+PREFIXES = {  # parents' lengths, held lengths, the prefix of the first, window, sinks
+    "window_not_full": ([100, 50], [100, 50], 60, 1024, 0),
+    "one_token": ([100, 50], [100, 50], 1, 1024, 4),
+    "nothing": ([100, 50], [100, 50], 0, 1024, 4),
+    "within_a_page": ([100, 50], [100, 50], 99, 30, 0),
+    "behind_what_is_held": ([120, 50], [100, 50], 110, 30, 20),
+}
+
+
+@pytest.mark.parametrize("page", [1, 7, 16])
+@pytest.mark.parametrize("name", PREFIXES)
+def test_a_forked_prefix_goes_on_is_forked_and_ends(name, page):
+    seq, held, n, window, sinks = PREFIXES[name]
+    if needs_lost(n, held[0], page, window, sinks):
+        n = next(m for m in range(n, seq[0] + 1) if not needs_lost(m, held[0], page, window, sinks))
+    b = Books(Forked(seq, [], [], page, rows=5, window=window, sinks=sinks, held=held, spare=20))
+    b.fork([0], [2], [n])
+    b.go_on([seq[0], seq[1], n, 0, 0])  # a step of the batch with the child in it
+    b.fork([2], [3], [n])
+    b.fork([3], [4])                    # a child as a parent, ahead of any step
+    b.go_on([0, seq[1], n, 0, n])       # and its end
+    b.go_on([0, seq[1], 0, 0, n])
+    b.go_on([0, 0, 0, 0, 0])
+    assert (b.shared == 0).all()
