@@ -40,6 +40,11 @@ struct CachePages {
   __device__ __forceinline__ bool holds(int32_t column, int32_t held) const {
     return column < sinks || column >= left(held);
   }
+  // Whether n tokens need a page that a request held at `held` tokens has let go of. (Not those whose pages are all the
+  // sinks', nor where the sinks reach what is held.)
+  __device__ __forceinline__ bool lacks(int32_t n, int32_t held) const {
+    return max(sinks, left(n)) < min(left(held), up(n));
+  }
 };
 
 struct FreeWs {

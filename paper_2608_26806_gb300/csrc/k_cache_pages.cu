@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
       held = a.window > 0 ? a.held_len[r] : 0;
       bool bad = seq < 0 || now < 0 || now > seq || held < 0 || held > seq ||
                  seq > static_cast<int64_t>(a.max_pages) * a.page_size;
-      if (!bad && now > 0 && pages.left(now) < pages.left(held)) bad = true;  // it would need pages let go of
+      if (!bad && pages.lacks(now, held)) bad = true;
       // a new end inside a page that others hold
       if (!bad && a.shared != nullptr && now > 0 && now < seq && now % a.page_size != 0) {
         const int32_t page = a.block_table[r * a.table_stride + now / a.page_size];
@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_fork(ForkDev d) {
         len = a.fork_len != nullptr ? a.fork_len[i] : seq;
         held = a.window > 0 ? a.held_len[p] : 0;
         bad = seq < 0 || len < 0 || len > seq || held < 0 || held > seq ||
-              seq > static_cast<int64_t>(a.max_pages) * P || (len > 0 && pages.left(len) < pages.left(held));
+              seq > static_cast<int64_t>(a.max_pages) * P || pages.lacks(len, held);
         if (rank == 0) d.mark[p] = -1;
       }
       if (bad) {

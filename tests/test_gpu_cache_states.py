@@ -7,7 +7,7 @@ import torch
 from paper_2608_26806_gb300 import avtp
 from tests.gpu_util import ensure_built
 from tests.pages_util import fork_plain, free_plain, holds, needs_lost
-from tests.test_gpu_cache_pages import Forked, i32, ints, status
+from tests.test_gpu_cache_pages import Forked, Freed, i32, ints, refused, status
 
 pytestmark = pytest.mark.gpu
 
@@ -88,5 +88,45 @@ def test_a_forked_prefix_goes_on_is_forked_and_ends(name, page):
     b.fork([3], [4])                    # a child as a parent, ahead of any step
     b.go_on([0, seq[1], n, 0, n])       # and its end
     b.go_on([0, seq[1], 0, 0, n])
+    b.go_on([0, 0, 0, 0, 0])
+    assert (b.shared == 0).all()
+
+
+# ---------------------------------------------------------------- lengths whose pages are all held
+LENGTHS = [(40, 20), (40, 33), (9, 60), (1, 0), (1, 17), (30, 110), (200, 5)]  # window, sinks
+
+
+@pytest.mark.parametrize("page", [1, 7, 16])
+@pytest.mark.parametrize("window,sinks", LENGTHS)
+def test_free_takes_every_length_whose_pages_are_held(window, sinks, page):
+    seq, held = 110, 100
+    lost = [n for n in range(seq + 1) if needs_lost(n, held, page, window, sinks)]
+    fine = [n for n in range(seq + 1) if n not in lost]
+    f = Freed([seq] * len(fine), fine, page, window=window, sinks=sinks, held=[held] * len(fine))
+    f.check(f.call().run())
+    for n in lost[:1] + lost[-1:]:
+        refused(Freed([seq, 50], [n, 50], page, window=window, sinks=sinks, held=[held, 0]))
+
+
+@pytest.mark.parametrize("page", [1, 7, 16])
+@pytest.mark.parametrize("window,sinks", LENGTHS)
+def test_fork_takes_every_length_whose_pages_are_held(window, sinks, page):
+    seq, held = 110, 100
+    lost = [n for n in range(seq + 1) if needs_lost(n, held, page, window, sinks)]
+    fine = [n for n in range(seq + 1) if n not in lost]
+    at = dict(window=window, sinks=sinks, held=[held])
+    f = Forked([seq], [0] * len(fine), list(range(1, len(fine) + 1)), page, length=fine, **at)
+    f.check(f.call().run())
+    for n in lost[:1] + lost[-1:]:
+        c = Forked([seq], [0], [1], page, length=[n], **at).call().run()
+        assert status(c) == avtp.ERR_DEVICE_INPUT and int(c.free_head_out) == -1
+
+
+def test_a_prompt_kept_as_sinks_is_forked_and_a_request_cut_back_to_it():
+    b = Books(Forked([500, 300], [], [], 16, rows=5, window=64, sinks=40, held=[500, 300], spare=10))
+    b.fork([0, 1], [2, 3], [40, 48])
+    b.go_on([32, 300, 40, 48, 0])
+    b.fork([0], [4], [32])
+    b.go_on([0, 48, 40, 0, 32])
     b.go_on([0, 0, 0, 0, 0])
     assert (b.shared == 0).all()
