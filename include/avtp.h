@@ -654,7 +654,8 @@ typedef struct {
   int32_t window;              /* see above; 0: none                                                 */
   int32_t n_sinks;
   const int32_t* held_len;     /* device [R], with a window                                          */
-  int32_t* len_out;            /* device [R] or NULL: n_r, written; not seq_len                      */
+  int32_t* len_out;            /* device [R] or NULL: n_r, or in place seq_len[r] of a request left  */
+                               /* as it was; written; not seq_len                                   */
 } avtp_cache_compact_args_t;
 
 /* Offsets that decrease or pass n_kept are recorded as AVTP_ERR_DEVICE_INPUT, and then nothing is
@@ -662,7 +663,7 @@ typedef struct {
  * - with dst_table, a position outside its request's tokens or on a page let go of, or a page
  *   outside [0, n_pages) or the table: that token is not moved;
  * - in place, the same, positions that do not ascend, or a row to be moved to a page let go of or
- *   with shared > 0 (others hold it): that request is left as it was.
+ *   with shared > 0 (others hold it): that request is left as it was, and len_out says so.
  * workspace: 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,
                                           size_t workspace_bytes, avtp_stream_t stream);

@@ -1116,8 +1116,9 @@ class CacheCompactCall(_CacheCall):
     """A prepared avtp_cache_compact call: the kept tokens of cached requests moved together in one layer's cache, to
     the pages of ``dst_table`` (int32 [R, columns]) or, without one, in place. ``keep_idx`` (int32): request r's kept
     positions at ``keep_cu[r] .. keep_cu[r+1]``, less ``base_cu[r]`` where that is given (a prune's ``kept_idx``,
-    ``out_cu_seqlens`` and the batch's ``cu_seqlens``). ``len_out`` (int32 [R]) receives the kept tokens; the pages
-    behind them go back with :class:`CacheFreeCall`. ``shared``, ``window``, ``sinks`` and ``held_len``: as there."""
+    ``out_cu_seqlens`` and the batch's ``cu_seqlens``). ``len_out`` (int32 [R]) receives the kept tokens, or in place
+    the whole length of a request that is refused and left as it was; the pages behind them go back with
+    :class:`CacheFreeCall`. ``shared``, ``window``, ``sinks`` and ``held_len``: as there."""
 
     def __init__(self, cache: PagedCache, keep_cu: torch.Tensor, keep_idx: torch.Tensor, seq_len: torch.Tensor,
                  block_table: torch.Tensor, *, dst_table=None, base_cu=None, shared=None, window=0, sinks=0, held_len=None,
@@ -1150,7 +1151,7 @@ class CacheCompactCall(_CacheCall):
 
 def cache_compact(cache: PagedCache, keep_cu: torch.Tensor, keep_idx: torch.Tensor, seq_len: torch.Tensor,
                   block_table: torch.Tensor, *, stream=None, **more) -> torch.Tensor:
-    """avtp_cache_compact: kept tokens together; returns their counts (int32 [R]). See :class:`CacheCompactCall`."""
+    """avtp_cache_compact: kept tokens together; returns the new lengths (int32 [R]). See :class:`CacheCompactCall`."""
     with _on_stream(stream):
         return CacheCompactCall(cache, keep_cu, keep_idx, seq_len, block_table, **more).run().len_out
 

@@ -195,7 +195,7 @@ __device__ const int32_t* offsets(const avtp_cache_compact_args_t& a, int32_t (&
   return staged ? s_cu : a.keep_cu;
 }
 
-// The call's first CTA: the new lengths.
+// To other pages, by the call's first CTA: the new lengths.
 __device__ void write_lengths(const avtp_cache_compact_args_t& a, const int32_t* cu) {
   if (blockIdx.x != 0 || a.len_out == nullptr) return;
   for (int r = threadIdx.x; r < a.n_requests; r += kThreads) a.len_out[r] = cu[r + 1] - cu[r];
@@ -279,7 +279,6 @@ __global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_plac
   const int32_t* cu = offsets(a, s_cu);
   int wrong = cu != nullptr ? -1 : 0x7fffffff;
   if (cu != nullptr) {
-    write_lengths(a, cu);
     const int per_head = (1 << d.head_sh) / d.slice, sub = threadIdx.x & (d.slice - 1);
     const int at_once = kThreads / d.slice, first_row = threadIdx.x / d.slice;
     const uint32_t P = d.c.page_size;
@@ -290,7 +289,15 @@ __global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_plac
       const int c0 = static_cast<int>(static_cast<int64_t>(part) * d.columns / d.parts);
       const int c1 = static_cast<int>(static_cast<int64_t>(part + 1) * d.columns / d.parts);
       const int64_t first = cu[r], n = cu[r + 1] - first;
-      if (n == 0) continue;
+      // A request's new length, by the CTA of its first columns behind the look: of one that stays as it was its old
+      // one, so that whoever hands the lengths on gives none of its pages away.
+      auto write_length = [&](int32_t len) {
+        if (part == 0 && threadIdx.x == 0 && a.len_out != nullptr) a.len_out[r] = len;
+      };
+      if (n == 0) {
+        write_length(0);
+        continue;
+      }
       auto look = [&](int64_t j0) {  // tokens j0 .. j0 + kChunk - 1
         return look_in_place(d, r, first, j0, min(n, j0 + kChunk), [&](int64_t j, int64_t from, int64_t to) {
           s_from[j - j0] = static_cast<int32_t>(from);
@@ -301,9 +308,11 @@ __global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_plac
       if (n > kChunk) bad = look_in_place(d, r, first, kChunk, n, [](int64_t, int64_t, int64_t) {}) || bad;
       if (__syncthreads_or(bad)) {
         wrong = r;
+        write_length(a.seq_len[r]);
         __syncthreads();
         continue;
       }
+      write_length(static_cast<int32_t>(n));
       for (int64_t j0 = 0; j0 < n; j0 += kChunk) {
         if (j0 > 0) {
           __syncthreads();

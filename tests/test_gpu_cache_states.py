@@ -7,7 +7,7 @@ import torch
 from paper_2608_26806_gb300 import avtp
 from tests.gpu_util import ensure_built
 from tests.pages_util import fork_plain, free_plain, holds, needs_lost
-from tests.test_gpu_cache_pages import Forked, Freed, i32, ints, refused, status
+from tests.test_gpu_cache_pages import BAD_IN_PLACE, Compacted, Forked, Freed, i32, ints, refused, status
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,62 @@ def test_a_prompt_kept_as_sinks_is_forked_and_a_request_cut_back_to_it():
     b.go_on([0, 48, 40, 0, 32])
     b.go_on([0, 0, 0, 0, 0])
     assert (b.shared == 0).all()
+
+
+# ---------------------------------------------------------------- compaction in place, then the pages behind it
+def refused_ones(name):
+    """A request with a fault, one that is moved and one of which nothing is kept; and what the call is told more."""
+    keep = list(range(3, 90, 3)) + [99]
+    c, more = Compacted([100, 60, 40], [keep, 20, 0], 16, other=False), {}
+    if name in BAD_IN_PLACE:
+        BAD_IN_PLACE[name](c)
+    elif name == "shared":
+        shared = np.zeros(c.n_pages, dtype=np.int32)
+        shared[c.table[0, 1]] = 1
+        more = dict(shared=i32(shared))
+    elif name == "let_go":
+        c = Compacted([100, 60, 40], [list(range(1, 16)) + list(range(70, 80)), [1, 40], 0], 16, other=False)
+        more = dict(window=32, sinks=16, held_len=i32([100, 60, 40]))
+    return c, more
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("name", list(BAD_IN_PLACE) + ["shared", "let_go"])
+def test_a_request_that_is_not_moved_keeps_its_length_and_its_pages(name, captured):
+    """The lengths that a compaction gives go to the free without a look at the status between them."""
+    c, more = refused_ones(name)
+    kept = c.call(len_out=torch.full((3,), -7, dtype=torch.int32, device="cuda"), **more)
+    free = np.arange(-40, 0)
+    seq, lst, head = i32(c.seq), i32(free), i32([30])
+    given = avtp.CacheFreeCall(seq, kept.len_out, kept._keep[3], page_size=16, n_pages=c.n_pages, free_pages=lst,
+                               free_head=head, **{k: v for k, v in more.items() if k != "shared"})
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            kept.run()
+            given.run()
+        graph.replay()
+        torch.cuda.synchronize()
+    else:
+        kept.run()
+        given.run()
+    n = [100, int(c.cu[2] - c.cu[1]), 0]
+    assert status(kept) == avtp.ERR_DEVICE_INPUT and ints(kept.len_out).tolist() == n
+    want, h, _ = free_plain(c.seq, n, c.table, free, 30, 16, None, *(
+        (32, 16, [100, 60, 40]) if name == "let_go" else ()))
+    assert status(given) == avtp.OK and np.array_equal(ints(lst), want) and int(given.free_head_out) == h
+    assert c.same(c.want(rows=[1]))
+
+
+@pytest.mark.parametrize("R", [40, 400, 1100])
+def test_lengths_of_many_requests_of_which_some_are_not_moved(R):
+    rng = np.random.default_rng(R)
+    c = Compacted([20 + i % 9 for i in range(R)], [int(k) for k in rng.integers(0, 8, R)], 4, other=False, seed=R)
+    n = np.diff(c.cu)
+    wrong = [r for r in range(R) if n[r] > 1 and r % 3 == 0]
+    for r in wrong:
+        c.idx[c.cu[r + 1] - 1] = c.idx[c.cu[r]]
+    call = c.call().run()
+    want = np.where(np.isin(np.arange(R), wrong), c.seq, n)
+    assert status(call) == avtp.ERR_DEVICE_INPUT and np.array_equal(ints(call.len_out), want)
+    assert c.same(c.want(rows=[r for r in range(R) if r not in wrong]))
