@@ -167,8 +167,9 @@ __device__ bool look_in_place(const CompactDev& d, int r, int64_t first, int64_t
       const int64_t k = j + i * kThreads;
       const bool wrong = k < j1 && (p[i] < k || p[i] >= seq || p[i] <= before[i]), moves = k < j1 && p[i] != k && !wrong;
       to[i] = moves ? slot_of(d.c, row, a.max_pages, k, &d.held, held) : -1;
-      from[i] = moves ? slot_of(d.c, row, a.max_pages, p[i], &d.held, held) : -1;
-      bad = bad || wrong || (moves && (to[i] < 0 || from[i] < 0));
+      // (a token that stays has to lie on a page of the request's too)
+      from[i] = k < j1 && !wrong ? slot_of(d.c, row, a.max_pages, p[i], &d.held, held) : -1;
+      bad = bad || wrong || (k < j1 && from[i] < 0) || (moves && to[i] < 0);
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {

@@ -189,3 +189,21 @@ def test_lengths_of_many_requests_of_which_some_are_not_moved(R):
     want = np.where(np.isin(np.arange(R), wrong), c.seq, n)
     assert status(call) == avtp.ERR_DEVICE_INPUT and np.array_equal(ints(call.len_out), want)
     assert c.same(c.want(rows=[r for r in range(R) if r not in wrong]))
+
+
+# ---------------------------------------------------------------- tokens that stay where they are
+def test_kept_tokens_that_stay_are_looked_at_too():
+    """On a page let go of, or outside the pool, a token cannot be kept, moved or not."""
+    more = dict(window=32, sinks=16, held_len=i32([100, 60]))
+    c = Compacted([100, 60], [list(range(21)), [1, 40]], 16, other=False)
+    call = c.call(**more).run()
+    assert status(call) == avtp.ERR_DEVICE_INPUT and ints(call.len_out).tolist() == [100, 2] and c.same(c.want(rows=[1]))
+    c = Compacted([100, 60], [list(range(16)), [1, 40]], 16, other=False)
+    call = c.call(**more).run()
+    assert status(call) == avtp.OK and ints(call.len_out).tolist() == [16, 2] and c.same(c.want(rows=[1]))
+    for page in (-1, 10 ** 6):
+        c = Compacted([100, 60], [list(range(40)) + [60, 99], 20], 16, other=False)
+        c.table[0, 1] = page
+        call = c.call().run()
+        assert status(call) == avtp.ERR_DEVICE_INPUT and ints(call.len_out).tolist() == [100, 20]
+        assert c.same(c.want(rows=[1]))
