@@ -743,10 +743,10 @@ typedef struct {
 AVTP_API avtp_status_t avtp_cache_free_workspace_size(const avtp_cache_free_args_t* args, size_t* bytes);
 
 /* Lengths out of range (as above; a held_len beyond seq_len), a page outside [0, n_pages), one that
- * more rows let go of than hold it, a new_len inside a page with shared > 0 (the request's next
- * tokens would be written over the others'; whoever wants that forks the request first), or a free
- * list with too few entries before *free_head are recorded as AVTP_ERR_DEVICE_INPUT, and then
- * nothing is written. Asynchronous on `stream`. */
+ * is let go of more often than it is held (without shared: more than once), a new_len inside a page
+ * with shared > 0 (the request's next tokens would be written over the others'; whoever wants that
+ * forks the request first), or a free list with too few entries before *free_head are recorded as
+ * AVTP_ERR_DEVICE_INPUT, and then nothing is written. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_free(const avtp_cache_free_args_t* args, void* workspace, size_t workspace_bytes,
                                        avtp_stream_t stream);
 

@@ -208,11 +208,11 @@ avtp_status_t check_free(const avtp_cache_free_args_t* a) {
 
 FreeWs plan_free(const avtp_cache_free_args_t& a) {
   FreeWs p{};
-  const size_t R = static_cast<size_t>(a.n_requests), n = a.shared != nullptr ? static_cast<size_t>(a.n_pages) : 0;
+  const size_t R = static_cast<size_t>(a.n_requests), n = static_cast<size_t>(a.n_pages);
   p.status = 0;
   p.first = align_up(sizeof(DevStatus));
   p.rel = p.first + align_up((R + 1) * 4);
-  p.last = p.rel + align_up(n * 4);
+  p.last = p.rel + (a.shared != nullptr ? align_up(n * 4) : 0);
   p.total = p.last + align_up(n * 4);
   return p;
 }

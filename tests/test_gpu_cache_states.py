@@ -207,3 +207,49 @@ def test_kept_tokens_that_stay_are_looked_at_too():
         call = c.call().run()
         assert status(call) == avtp.ERR_DEVICE_INPUT and ints(call.len_out).tolist() == [100, 20]
         assert c.same(c.want(rows=[1]))
+
+
+# ---------------------------------------------------------------- pages that are let go of twice
+def twice(f, a, b):
+    f.table[b] = f.table[a]
+    return f
+
+
+REPEATED = {
+    "two_rows": lambda: twice(Freed([100, 90], [0, 0], 16), (0, 2), (1, 4)),
+    "one_row": lambda: twice(Freed([100, 90], [100, 0], 16), (1, 0), (1, 5)),
+    "behind_cuts": lambda: twice(Freed([100, 90], [30, 40], 16), (0, 3), (1, 3)),
+    "two_windows": lambda: twice(Freed([300, 290], [300, 290], 16, window=40, sinks=5, held=[200, 0]), (0, 10), (1, 4)),
+    "many_rows": lambda: twice(Freed([17] * 2500, [0] * 2500, 16), (0, 1), (2499, 0)),
+    "many_pages": lambda: twice(Freed([1200000, 40], [0, 0], 16), (0, 70000), (0, 3)),
+}
+
+
+@pytest.mark.parametrize("name", REPEATED)
+def test_without_counts_a_page_let_go_of_twice_is_refused(name):
+    refused(REPEATED[name]())
+
+
+def test_without_counts_a_page_that_another_row_keeps_is_let_go_of_once():
+    f = twice(Freed([100, 90], [0, 90], 16), (0, 2), (1, 4))
+    f.check(f.call().run())
+
+
+POOLS = [32 * 12288, 32 * 12288 + 1, 32 * 12288 * 16, 32 * 12288 * 16 + 1]
+
+
+@pytest.mark.parametrize("n_pages", POOLS)
+@pytest.mark.parametrize("case", [([100, 90, 5], [0, 40, 5]), ([9000] * 40, [0, 9000] * 20), ([17] * 2500, [0] * 2500)])
+def test_repeated_pages_of_large_pools(n_pages, case):
+    """Pages all over pools of as many pages as a cluster of one CTA, or of sixteen, has bits for, and of one more."""
+    f = Freed(*case, 16)
+    ids = np.sort(np.random.default_rng(n_pages).choice(n_pages, f.n_pages, replace=False))
+    ids[0], ids[-1] = 0, n_pages - 1
+    f.table[f.table >= 0] = ids[f.table[f.table >= 0]]
+    f.n_pages = n_pages
+    f.check(f.call().run())
+    last = -(-case[0][0] // 16) - 1
+    f.table[0, last] = f.table[0, 0]
+    refused(f)
+    f.table[0, last] = n_pages
+    refused(f)
