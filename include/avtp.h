@@ -662,8 +662,9 @@ typedef struct {
  * written. Recorded too:
  * - with dst_table, a position outside its request's tokens or on a page let go of, or a page
  *   outside [0, n_pages) or the table: that token is not moved;
- * - in place, the same, positions that do not ascend, or a row to be moved to a page let go of or
- *   with shared > 0 (others hold it): that request is left as it was, and len_out says so.
+ * - in place, the same, positions that do not ascend, a row to be moved to a page let go of or with
+ *   shared > 0 (others hold it), or fewer tokens than before that end inside a page with shared > 0
+ *   (see avtp_cache_free): that request is left as it was, and len_out says so.
  * workspace: 256-byte aligned, at least 16 bytes. Asynchronous on `stream`. */
 AVTP_API avtp_status_t avtp_cache_compact(const avtp_cache_t* cache, const avtp_cache_compact_args_t* args, void* workspace,
                                           size_t workspace_bytes, avtp_stream_t stream);

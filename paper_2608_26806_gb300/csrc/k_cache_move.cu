@@ -306,6 +306,11 @@ __global__ void __launch_bounds__(kThreads, kColumnCtas) k_cache_compact_in_plac
         });
       };
       bool bad = look(0);
+      // a new end inside a page that others hold: the request's next token would be written over theirs
+      if (a.shared != nullptr && threadIdx.x == 0 && n < a.seq_len[r] && n % P != 0 && n / P < a.max_pages) {
+        const int32_t page = a.block_table[r * a.table_stride + n / P];
+        bad = bad || (page >= 0 && page < d.c.n_pages && a.shared[page] > 0);
+      }
       if (n > kChunk) bad = look_in_place(d, r, first, kChunk, n, [](int64_t, int64_t, int64_t) {}) || bad;
       if (__syncthreads_or(bad)) {
         wrong = r;

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2608_26806_gb300 import avtp
+from tests.cache_util import pool
 from tests.gpu_util import ensure_built
 from tests.pages_util import fork_plain, free_plain, holds, needs_lost
 from tests.test_gpu_cache_pages import BAD_IN_PLACE, Compacted, Forked, Freed, i32, ints, refused, status
@@ -253,3 +254,133 @@ def test_repeated_pages_of_large_pools(n_pages, case):
     refused(f)
     f.table[0, last] = n_pages
     refused(f)
+
+
+# ---------------------------------------------------------------- kept tokens that end in a page of several holders
+@pytest.mark.parametrize("n,ok", [(40, False), (33, False), (47, False), (32, True), (48, True), (60, True), (100, True)])
+def test_kept_tokens_may_not_end_inside_a_page_that_others_hold(n, ok):
+    """A request's next token would be written over theirs; the free refuses such a length, with its whole batch."""
+    c = Compacted([100, 60], [list(range(n)), 20], 16, other=False)
+    shared = np.zeros(c.n_pages, dtype=np.int32)
+    shared[c.table[0, :3]] = 1
+    call = c.call(shared=i32(shared)).run()
+    want = [n if ok else 100, 20]
+    assert status(call) == (avtp.OK if ok else avtp.ERR_DEVICE_INPUT) and ints(call.len_out).tolist() == want
+    assert c.same(c.want(rows=[1]))
+    free = np.arange(-40, 0)
+    counts, lst = i32(shared), i32(free)
+    given = avtp.CacheFreeCall(i32(c.seq), call.len_out, i32(c.table), page_size=16, n_pages=c.n_pages, free_pages=lst,
+                               free_head=i32([30]), shared=counts).run()
+    f, h, s = free_plain(c.seq, want, c.table, free, 30, 16, shared)
+    assert status(given) == avtp.OK and np.array_equal(ints(lst), f) and int(given.free_head_out) == h
+    assert np.array_equal(ints(counts), s)
+
+
+# ---------------------------------------------------------------- together
+def may_stay(r, keep, seq, table, shared, held, page, window, sinks):
+    """Whether avtp_cache_compact moves these tokens together in place."""
+    def held_page(p):
+        return holds(p // page, seq[r], held[r], page, window, sinks)
+
+    n = len(keep)
+    if not all(held_page(p) for p in keep):
+        return False
+    if any(j != p and (not held_page(j) or shared[table[r, j // page]] > 0) for j, p in enumerate(keep)):
+        return False
+    return not (n < seq[r] and n % page and shared[table[r, n // page]] > 0)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 5), (40, 40), (500, 16), (9, 70)])
+@pytest.mark.parametrize("page", [4, 16])
+def test_a_run_with_prefixes_cuts_and_compactions(page, window, sinks):
+    """Steps of a serving program, every number on the device and no look at a status between the calls: new tokens, forks
+    of prefixes, selections in place (some of them refused), cuts and ends. The books agree with the plain forms', and
+    every token that is held is found where the table says."""
+    rng = np.random.default_rng(page + window + sinks)
+    R, most = 10, 300
+    columns = -(-(most + 40) // page)
+    n_pages = R * columns + 8
+    k, v = pool(n_pages, page, 1, 64, fill=0.0)
+    cache = avtp.PagedCache(k, v)
+    table = i32(np.full((R, columns), -1))
+    seq, held, head = i32(np.zeros(R)), i32(np.zeros(R)), i32([0])
+    free, shared = i32(rng.permutation(n_pages)), i32(np.zeros(n_pages))
+    more = dict(window=window, sinks=sinks, held_len=held) if window else {}
+    tokens, stamp, refusals = [[] for _ in range(R)], 0, 0
+
+    def books():
+        h = ints(held) if window else np.zeros(R, np.int64)
+        return ints(seq).copy(), ints(table).copy(), ints(free).copy(), int(head), ints(shared).copy(), h.copy()
+
+    for step in range(30):
+        lens = np.asarray([len(t) for t in tokens])
+        new = np.where((lens > 0) | (rng.random(R) < 0.4), rng.integers(0, 40, R), 0)
+        new = np.where(lens + new > most, 0, new)
+        cu = np.concatenate([[0], np.cumsum(new)])
+        slots = avtp.cache_slots(i32(cu), int(cu[-1]), page_size=page, n_pages=n_pages, block_table=table, free_pages=free,
+                                 free_head=head, past_len=seq, seq_len=seq, free_head_out=head)[0]
+        marks = (stamp + torch.arange(int(cu[-1])) % 250).float()
+        stamp = (stamp + 7) % 100
+        rows = (marks[:, None, None] * torch.ones(len(marks), 1, 64)).bfloat16().cuda()
+        avtp.cache_write(cache, slots, rows, rows)
+        flat = rows[:, 0, 0].float().cpu().tolist()
+        for r in range(R):
+            tokens[r] += flat[cu[r]:cu[r + 1]]
+        # forks, of prefixes in every second step
+        s, t, f, h, n_shared, hl = books()
+        empty, parents = [r for r in range(R) if s[r] == 0], [r for r in range(R) if s[r] > 0]
+        if empty and parents:
+            p = [int(rng.choice(parents)) for _ in empty]
+            n = [int(rng.choice([m for m in range(s[r] + 1) if not needs_lost(m, hl[r], page, window, sinks)])) for r in p]
+            n = n if step % 2 else None
+            src, dst, _ = avtp.cache_fork(i32(p), i32(empty), seq, table, page_size=page, n_pages=n_pages, free_pages=free,
+                                          free_head=head, shared=shared, free_head_out=head,
+                                          fork_len=None if n is None else i32(n), **more)
+            avtp.cache_copy(cache, src, dst)
+            want = fork_plain(p, empty, s, t, f, h, page, n_shared, n, window, sinks, hl if window else None)
+            got = books()
+            assert np.array_equal(got[1], want[0]) and np.array_equal(got[0], want[1]) and got[3] == want[2]
+            assert np.array_equal(got[4], want[3]) and (not window or np.array_equal(got[5], want[6]))
+            for i, (a, b) in enumerate(zip(p, empty)):
+                tokens[b] = tokens[a][:len(tokens[a]) if n is None else n[i]]
+        # selections in place, and what they leave goes back
+        s, t, f, h, n_shared, hl = books()
+        keep = []
+        for r in range(R):
+            mine = list(range(s[r]))
+            if s[r] and rng.random() < 0.3:
+                fixed = int(rng.integers(0, s[r] + 1)) if rng.random() < 0.7 else 0
+                mine = [j for j in mine if holds(j // page, s[r], hl[r], page, window, sinks) or rng.random() < 0.02]
+                mine = [j for i, j in enumerate(mine) if j == i and j < fixed or rng.random() < 0.5]
+            else:
+                mine = mine if all(holds(j // page, s[r], hl[r], page, window, sinks) for j in mine) else None
+            keep.append(mine)
+        lens = np.asarray([s[r] if keep[r] is None or not may_stay(r, keep[r], s, t, n_shared, hl, page, window, sinks)
+                           else len(keep[r]) for r in range(R)])
+        # (a row that has let go of pages and is to stay as it is names a token of such a page)
+        named = [list(range(s[r])) if keep[r] is None else keep[r] for r in range(R)]
+        kept = avtp.CacheCompactCall(cache, i32(np.cumsum([0] + [len(x) for x in named])),
+                                     i32(np.concatenate(named + [[0]])), seq, table, shared=shared, **more).run()
+        ends = rng.random(R) < 0.1
+        given = kept.len_out * i32(~ends)
+        avtp.CacheFreeCall(seq, given, table, page_size=page, n_pages=n_pages, free_pages=free, free_head=head,
+                           shared=shared, seq_len_out=seq, free_head_out=head,
+                           **(dict(more, held_len_out=held) if window else {})).run()
+        want_len = np.where(ends, 0, lens)
+        wf, wh, ws = free_plain(s, want_len, t, f, h, page, n_shared, window, sinks, hl if window else None)
+        got = books()
+        assert np.array_equal(ints(kept.len_out), lens)
+        assert np.array_equal(got[0], want_len) and np.array_equal(got[2], wf) and got[3] == wh
+        assert np.array_equal(got[4], ws) and (not window or np.array_equal(got[5], want_len))
+        for r in range(R):
+            if keep[r] is not None and lens[r] == len(keep[r]):
+                tokens[r] = [tokens[r][j] for j in keep[r]]
+            else:
+                refusals += 1
+            tokens[r] = tokens[r][:want_len[r]]
+        rows_now = k[:, :, 0, 0].float().cpu().numpy()
+        for r in range(R):
+            for j, x in enumerate(tokens[r]):
+                if holds(j // page, want_len[r], want_len[r], page, window, sinks):
+                    assert rows_now[got[1][r, j // page], j % page] == x
+    assert refusals > 0 or window == 0
