@@ -116,14 +116,21 @@ struct CompactDev {
   DevStatus* st;
 };
 
-// Slot of a request's row p; -1 where it lies outside the table or the pool, or (held) on a page let go of.
-__device__ __forceinline__ int64_t slot_of(const avtp_cache_t& c, const int32_t* row, int max_pages, int64_t p,
-                                           const CachePages* held, int32_t held_len) {
+// Table column of a request's row p; -1 where it lies outside the table, or (held) on a page let go of.
+__device__ __forceinline__ int32_t column_of(const avtp_cache_t& c, int max_pages, int64_t p, const CachePages* held,
+                                             int32_t held_len) {
   const int64_t column = static_cast<uint32_t>(p) / static_cast<uint32_t>(c.page_size);
   if (p < 0 || p > 0x7fffffff || column >= max_pages) return -1;
-  if (held != nullptr && !held->holds(static_cast<int32_t>(column), held_len)) return -1;
-  const int32_t page = row[column];
-  return page < 0 || page >= c.n_pages ? -1 : static_cast<int64_t>(page) * c.page_size + (p - column * c.page_size);
+  return held == nullptr || held->holds(static_cast<int32_t>(column), held_len) ? static_cast<int32_t>(column) : -1;
+}
+// Its slot, on that column's page; -1 where that lies outside the pool.
+__device__ __forceinline__ int64_t slot_on(const avtp_cache_t& c, int64_t p, int32_t column, int32_t page) {
+  return page < 0 || page >= c.n_pages ? -1 : static_cast<int64_t>(page) * c.page_size + (p - static_cast<int64_t>(column) * c.page_size);
+}
+__device__ __forceinline__ int64_t slot_of(const avtp_cache_t& c, const int32_t* row, int max_pages, int64_t p,
+                                           const CachePages* held, int32_t held_len) {
+  const int32_t column = column_of(c, max_pages, p, held, held_len);
+  return column < 0 ? -1 : slot_on(c, p, column, row[column]);
 }
 
 __device__ __forceinline__ int32_t held_len(const CompactDev& d, int r) { return d.a.window > 0 ? d.a.held_len[r] : 0; }
@@ -162,14 +169,25 @@ __device__ bool look_in_place(const CompactDev& d, int r, int64_t first, int64_t
       p[i] = k < j1 ? a.keep_idx[first + k] - base : k;
       before[i] = k < j1 && k > 0 ? a.keep_idx[first + k - 1] - base : -1;
     }
+    // all looks into the table go out ahead of the first use of one
+    int32_t c_to[N], c_from[N], p_to[N], p_from[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int64_t k = j + i * kThreads;
-      const bool wrong = k < j1 && (p[i] < k || p[i] >= seq || p[i] <= before[i]), moves = k < j1 && p[i] != k && !wrong;
-      to[i] = moves ? slot_of(d.c, row, a.max_pages, k, &d.held, held) : -1;
-      // (a token that stays has to lie on a page of the request's too)
-      from[i] = k < j1 && !wrong ? slot_of(d.c, row, a.max_pages, p[i], &d.held, held) : -1;
-      bad = bad || wrong || (k < j1 && from[i] < 0) || (moves && to[i] < 0);
+      const bool fine = k < j1 && p[i] >= k && p[i] < seq && p[i] > before[i];
+      bad = bad || (k < j1 && !fine);
+      c_to[i] = fine ? column_of(d.c, a.max_pages, k, &d.held, held) : -1;
+      c_from[i] = fine ? column_of(d.c, a.max_pages, p[i], &d.held, held) : -1;
+      p_to[i] = c_to[i] >= 0 ? row[c_to[i]] : -1;
+      p_from[i] = c_from[i] >= 0 ? row[c_from[i]] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int64_t k = j + i * kThreads;
+      to[i] = slot_on(d.c, k, c_to[i], p_to[i]);
+      from[i] = slot_on(d.c, p[i], c_from[i], p_from[i]);
+      bad = bad || (k < j1 && (to[i] < 0 || from[i] < 0));
+      if (p[i] == k) to[i] = -1;  // stays, on a page that has to be the request's too
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
