@@ -469,10 +469,10 @@ AVTP_API avtp_status_t avtp_cache_write(const avtp_cache_t* cache, const avtp_ca
  *   (y_a, y_b) -> attn_factor * (y_a cos z - y_b sin z, y_b cos z + y_a sin z),
  *   z = pos[pair_plane[i]][t] * inv_freq[i]
  * for the pairs i < rot_dim / 2 of a head's first rot_dim elements, (a, b) = (i, i + rot_dim / 2)
- * or (2 i, 2 i + 1); the other elements stay y. Computed in 32 bits but for the angles, which are
- * exact to 2^-61 * pos * (1 + inv_freq) ahead of their sines, however far the position; rounded to
- * bf16 once. Position ids of several planes (M-RoPE) are gathered by avtp_prune like any others:
- * pos may be its output planes. */
+ * or (2 i, 2 i + 1); the other elements stay y. Computed in 32 bits but for the angles: a 64-bit
+ * fraction of a turn, off by at most 2^-61 * pos * (1 + inv_freq) radians however far the position,
+ * rounded to 32 bits (about 2^-23 radians) ahead of its sine. Rounded to bf16 once. Position ids of
+ * several planes (M-RoPE) are gathered by avtp_prune like any others: pos may be its output planes. */
 typedef enum {
   AVTP_ROPE_HALF = 0,        /* pairs (i, i + rot_dim / 2) */
   AVTP_ROPE_INTERLEAVED = 1  /* pairs (2 i, 2 i + 1)       */
@@ -522,7 +522,9 @@ AVTP_API avtp_status_t avtp_rope(const avtp_rope_args_t* args, const avtp_cache_
  *            fastest kept
  *   YARN     (1 - g_i) th_i / factor + g_i th_i, g_i = clamp((r_i - slow) / (fast - slow), 0, 1) with
  *            r_i = original_len * th_i / (2 pi) turns of the pair over the original context, and an
- *            attn_factor of 0.1 ln(factor) + 1 (arXiv 2309.00071) */
+ *            attn_factor of 0.1 ln(factor) + 1 (arXiv 2309.00071). The ramp is over the turns, as
+ *            in the paper; a checkpoint that was run with a ramp over the pair's index, between
+ *            rounded bounds, wants that model's own frequencies, which differ by tens of percent. */
 typedef enum {
   AVTP_ROPE_SCALE_NONE = 0,
   AVTP_ROPE_SCALE_LINEAR = 1,

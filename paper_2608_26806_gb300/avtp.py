@@ -958,7 +958,8 @@ def cache_write(cache: PagedCache, slot_map: torch.Tensor, k: torch.Tensor, v: t
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: Optional[str] = None, *, factor: float = 1.0,
                      original_len: float = 0.0, slow: float = 1.0, fast: float = 32.0) -> Tuple[np.ndarray, float]:
     """avtp_rope_frequencies: (inv_freq fp32 [rot_dim / 2], attn_factor) on the host, for ``scaling`` None,
-    "linear", "ntk" or "yarn"."""
+    "linear", "ntk" or "yarn". The last ramps over the pairs' turns as its paper does: a checkpoint that was run with
+    a ramp over the pair's index wants its own array for :class:`RopeCall`."""
     if scaling not in _ROPE_SCALES:
         raise ValueError(f"rope_frequencies: scaling must be one of {list(_ROPE_SCALES)}")
     out = np.empty(max(int(rot_dim) // 2, 1), dtype=np.float32)

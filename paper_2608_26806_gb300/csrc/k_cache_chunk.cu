@@ -50,9 +50,10 @@
 // below. Halves of a block that an edge leaves out of a whole warp's sight get P = 0 without a look at S; values that
 // no row of the unit sees are cleared by the warp that loads them; a row takes its reference from the first half that
 // shows it a key, so that the weight of a token that sees itself alone is 1. 8192 tokens behind 2176 in
-// windows of 2048, 512 and 128 tokens: 225, 107 and 63 us, where 17.5, 5.5 and 2.5 blocks a unit would take 195, 80 and 50
-// by the figures above: first blocks and last ones are masked, and a unit's ends weigh more. (Masks by comparison, every
-// half looked at, values cleared by the softmax warps, runs cut evenly: 279, 157 and 103.)
+// windows of 2048, 512 and 128 tokens: 216, 100 and 62 us, 17, 5 and 2 blocks a unit; with 16 sinks, whose block is one
+// more, 221, 105 and 73. At the rate without a window (532 us for 49.5 blocks and two for a unit's ends) that would be
+// 196, 72 and 41, and 207, 83 and 52: first blocks and last ones are masked, and a unit's ends weigh more. (At first, with
+// masks by comparison, every half looked at, values cleared by the softmax warps and runs cut evenly: 279, 157 and 103.)
 //
 // Warps 0-3: softmax and output of slot 0, 4-7 of slot 1 (warp w owns rows 32 (w % 4) ..). Warp 8:
 // segments, queries and keys; warp 10: values. Warp 9: TMEM and the MMAs. Every wait is bounded; a
@@ -339,8 +340,8 @@ k_cache_chunk(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ 
       // out nearly even, a cut is moved to the nearer end of the unit that it falls into, and no unit is in pieces; a
       // run gets a unit more than its share at worst, where first units are shorter. (That every run is longer than
       // half a unit keeps the last cut before the last unit's middle.) 32 query heads, 8 KV heads, 8192 tokens behind
-      // 2176, 6.7 units a run: window 2048 236 -> 225 us, 512 131 -> 107, 128 73 -> 67; 16384 tokens, window 512, 242
-      // -> 198; four requests of 943 behind 5000, 80 query heads, 16 KV heads, window 2048, where one run in 152 gets
+      // 2176, 6.7 units a run: window 2048 224 -> 216 us, 512 118 -> 100, 128 68 -> 62; 16384 tokens, window 512, 212
+      // -> 176; four requests of 943 behind 5000, 80 query heads, 16 KV heads, window 2048, where one run in 152 gets
       // a seventh unit, 293 -> 296. With four units a run: four of 2315 behind 5000, 20 and 4 heads, 200 -> 213.
       if (kWindow && a.R <= kNearRequests) {
         const uint32_t units = a.Hkv * __reduce_add_sync(0xffffffffu, lane < a.R && mine_ok ? units_of(a, mine, nt) : 0);

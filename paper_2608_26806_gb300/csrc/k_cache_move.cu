@@ -12,8 +12,8 @@
 // is read for tokens from b on lies at b or behind. So a CTA takes columns of the request's rows (slices of a head's
 // keys or values) through all its tokens, a tile at a time, with a barrier between a tile's reads and its writes, and
 // the next tiles' copies under way; columns are independent, and no CTA waits for another. 64 requests of 1000 of
-// 3000 tokens 133 us, 3.95 TB/s; one of 3000 of 9000 22 us, where twelve tiles one behind the other take 11 and the
-// look at the positions 6 (to other pages 6.2).
+// 3000 tokens 133-143 us, 3.7-3.9 TB/s; four of 2900 of 8600 29.7; one of 3000 of 9000 23.4, where twelve tiles one
+// behind the other take 11 and the look at the positions 7 (to other pages 6.2).
 //
 // What is wrong is recorded where it is met, in a status word that a kernel beside this one clears. (A CTA that
 // looked through all kept tokens instead took longer than the copies: 50 us for 11600 of them.) A request moved in
