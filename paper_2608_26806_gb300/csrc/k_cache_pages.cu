@@ -10,7 +10,7 @@
 // What bounds it: latency, a chain of dependent loads a round. A call is one cluster of up to kMostCtas CTAs, each of
 // which forms the sums for itself, so that barriers part the rounds and nothing else does; a thread's first kKept
 // pages stay in its registers from round to round. Everything is checked before the first write. Calls one behind the
-// other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 8.1 us; the pages that
+// other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 7.0 us; the pages that
 // 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.2; eight
 // children of a prompt of 146 pages 7.7; 171 children of 64 (21000 entries) 10.9. (At 5.7, 13.1, 7.7 and 10.8, without a
 // look for repeated pages: with eight CTAs 6.8, 19.9, 8.5 and 13.1; with entries looked up again in every round, and
@@ -23,9 +23,10 @@
 //
 // Without counts every page has one entry. That is seen in a bit a page of the pool, spread over the shared memory of
 // the cluster and cleared ahead of the wait for the kernel before: an entry sets its page's and looks at what was
-// there, ahead of the barrier behind the checks. A pool of too many pages for that (kSeenWords) has last instead, a
-// barrier and a trip to L2 more. 32, 367, 4370 and 17380 pages in a graph: 4.6, 5.2, 6.4 and 8.7 us; with last 5.6,
-// 6.2, 6.7 and 8.7; without a look 4.3, 4.9, 5.5 and 6.7, and a page that two rows let go of twice in the list.
+// there, ahead of the barrier behind the checks. A word has as few pages as there is room for, since they wait for each
+// other (always 32: 17380 pages 8.7 us instead of 7.6). A pool of too many pages (kSeenWords) has last instead, a barrier
+// and a trip to L2 more. 32, 367, 4370 and 17380 pages in a graph: 4.5, 5.2, 5.8 and 7.6 us; with last 5.3, 6.2, 6.7 and
+// 8.7; without a look 4.3, 4.9, 5.5 and 6.7, and a page that two rows let go of twice in the list.
 #include <cooperative_groups.h>
 
 #include "avtp_cache.cuh"
@@ -169,13 +170,14 @@ struct FreeDev {
   int32_t* rel;    // [n_pages], with counts: entries of a page
   int32_t* last;   // [n_pages]: the last of them
   int seen;        // words of a CTA's share of the pages' bits; 0: last instead
+  int seen_sh;     // log2 of the pages of a word
 };
 
 __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
   __shared__ Note s_v, s_notes[kMostCtas];
   __shared__ int64_t s_warp[1][kThreads / 32];
   __shared__ int32_t s_first[kStaged + 1], s_seq[kStaged], s_now[kStaged], s_held[kStaged];
-  extern __shared__ uint32_t s_seen[];  // page p: bit p % 32 of word p / 32, the words dealt to the CTAs in turn
+  extern __shared__ uint32_t s_seen[];  // a bit a page, the words dealt to the CTAs in turn
   for (int i = threadIdx.x; i < d.seen; i += kThreads) s_seen[i] = 0u;
   pdl_wait();
   pdl_trigger();
@@ -236,7 +238,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
   if (staged) __syncthreads();
   else cluster.sync();
 
-  // the CTA's entries, in order (an equal share: in whole turns of its threads 4370 pages took 7.0 us, now 6.4)
+  // the CTA's entries, in order (an equal share: in whole turns of its threads 4370 pages took 7.0 us instead of 6.4)
   const int64_t each = ((total + ctas - 1) / ctas + 31) / 32 * 32;
   const int64_t e0 = each * rank, e1 = min(total, e0 + each), mine0 = e0 + tid;
   const int32_t* first = staged ? s_first : d.first;
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_free(FreeDev d) {
     if (!in_pool(page)) {
       s_v.fail(upper_index(first, R, e));
     } else if (d.seen > 0) {
-      const uint32_t word = static_cast<uint32_t>(page) >> 5, bit = 1u << (page & 31);
+      const uint32_t word = static_cast<uint32_t>(page) >> d.seen_sh, bit = 1u << (page - (word << d.seen_sh));
       if (set_bit(s_seen + word / ctas, word % ctas, bit) & bit) repeated = e;
     } else {
       const int32_t n = others_of(page, i);
@@ -567,10 +569,12 @@ cudaError_t launch(void (*kernel)(Dev), PerDevice& most, Dev d, int64_t entries,
 
 cudaError_t launch_cache_free(const avtp_cache_free_args_t& a, void* ws, const FreeWs& p, cudaStream_t s) {
   const FreeDev d{a, {CachePages::of(a.page_size, a.window, a.n_sinks)}, ws_at<DevStatus>(ws, p.status),
-                  ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.rel), ws_at<int32_t>(ws, p.last), 0};
+                  ws_at<int32_t>(ws, p.first), ws_at<int32_t>(ws, p.rel), ws_at<int32_t>(ws, p.last), 0, 0};
   static PerDevice most;
   auto shape = [](int ctas, FreeDev& f) -> size_t {
-    const int64_t words = ((f.a.n_pages + 31) / 32 + ctas - 1) / ctas;
+    const int64_t pages = (f.a.n_pages + ctas - 1) / ctas;
+    while (f.seen_sh < 5 && pages > kSeenWords << f.seen_sh) ++f.seen_sh;
+    const int64_t words = (((f.a.n_pages - 1) >> f.seen_sh) + ctas) / ctas;
     f.seen = f.a.shared == nullptr && words <= kSeenWords ? static_cast<int>(words) : 0;
     return f.seen * 4;
   };

@@ -236,14 +236,16 @@ def test_without_counts_a_page_that_another_row_keeps_is_let_go_of_once():
     f.check(f.call().run())
 
 
-POOLS = [32 * 12288, 32 * 12288 + 1, 32 * 12288 * 16, 32 * 12288 * 16 + 1]
+POOLS = [12288, 12289, 3 * 12288, 16 * 12288 + 1, 32 * 12288, 32 * 12288 + 1, 32 * 12288 * 16, 32 * 12288 * 16 + 1]
 
 
 @pytest.mark.parametrize("n_pages", POOLS)
 @pytest.mark.parametrize("case", [([100, 90, 5], [0, 40, 5]), ([9000] * 40, [0, 9000] * 20), ([17] * 2500, [0] * 2500)])
 def test_repeated_pages_of_large_pools(n_pages, case):
-    """Pages all over pools of as many pages as a cluster of one CTA, or of sixteen, has bits for, and of one more."""
+    """Pages all over pools of as many pages as a cluster of one CTA, or of sixteen, has words or bits for, and of one more.
+    (The second case has 22520 pages in use.)"""
     f = Freed(*case, 16)
+    n_pages = max(n_pages, f.n_pages)
     ids = np.sort(np.random.default_rng(n_pages).choice(n_pages, f.n_pages, replace=False))
     ids[0], ids[-1] = 0, n_pages - 1
     f.table[f.table >= 0] = ids[f.table[f.table >= 0]]
