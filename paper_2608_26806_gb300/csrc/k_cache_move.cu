@@ -125,7 +125,8 @@ __device__ __forceinline__ int32_t column_of(const avtp_cache_t& c, int max_page
 }
 // Its slot, on that column's page; -1 where that lies outside the pool.
 __device__ __forceinline__ int64_t slot_on(const avtp_cache_t& c, int64_t p, int32_t column, int32_t page) {
-  return page < 0 || page >= c.n_pages ? -1 : static_cast<int64_t>(page) * c.page_size + (p - static_cast<int64_t>(column) * c.page_size);
+  if (page < 0 || page >= c.n_pages) return -1;
+  return static_cast<int64_t>(page) * c.page_size + (p - static_cast<int64_t>(column) * c.page_size);
 }
 __device__ __forceinline__ int64_t slot_of(const avtp_cache_t& c, const int32_t* row, int max_pages, int64_t p,
                                            const CachePages* held, int32_t held_len) {

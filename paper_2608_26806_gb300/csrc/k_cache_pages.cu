@@ -12,9 +12,9 @@
 // pages stay in its registers from round to round. Everything is checked before the first write. Calls one behind the
 // other: 256 requests of 200-8000 tokens on pages of 16, of which 64 are done (14900 pages), 7.0 us; the pages that
 // 64 windowed requests have left, with counts (16000 pages, four rounds that touch them in no order), 13.2; eight
-// children of a prompt of 146 pages 7.7; 171 children of 64 (21000 entries) 10.9. (At 5.7, 13.1, 7.7 and 10.8, without a
-// look for repeated pages: with eight CTAs 6.8, 19.9, 8.5 and 13.1; with entries looked up again in every round, and
-// the others' findings read from their shared memory, 11.7, 36.7, 11.2 and 18.8.)
+// children of a prompt of 146 pages 7.7; 171 children of 64 (21000 entries) 10.9. (Before the look for repeated pages
+// these were 5.7, 13.1, 7.7 and 10.8; then, with eight CTAs, 6.8, 19.9, 8.5 and 13.1; with entries looked up again in
+// every round, and the others' findings read from their shared memory, 11.7, 36.7, 11.2 and 18.8.)
 //
 // A page of several holders that rows of a call let go of: every entry counts itself (rel) and the last one in order
 // (last: a maximum) stands for the page, so that neither the counts nor the list's order depend on who came first.

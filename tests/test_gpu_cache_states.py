@@ -47,7 +47,8 @@ class Books:
 
     def go_on(self, new):
         f, d = self.f, self.d
-        c = avtp.CacheFreeCall(d["seq"], i32(new), d["table"], seq_len_out=d["seq"], held_len_out=d["held"], **self.more).run()
+        c = avtp.CacheFreeCall(d["seq"], i32(new), d["table"], seq_len_out=d["seq"], held_len_out=d["held"],
+                               **self.more).run()
         self.free, self.head, self.shared = free_plain(self.seq, new, self.table, self.free, self.head, f.page, self.shared,
                                                        f.window, f.sinks, self.held)
         self.seq, self.held = np.array(new), np.array(new)
